@@ -369,6 +369,129 @@ int sva_scatter_tokens(const void* src, const int64_t src_stride[3], const int32
                        int32_t M, int32_t n_dst, int32_t d, int32_t elem_bytes, void* dst,
                        const int64_t dst_stride[3], int32_t* device_status, void* stream);
 
+/*
+ * Linear layers in 8-bit floating point, one scale per block of 128 (the paper's deployments run QKV, output and FFN projections in
+ * low-bit formats and fuse GEMM + GELU and GEMM + residual; it prints no formula).  As read here, every scalar step of the
+ * quantisers one fp32 operation rounded to nearest:
+ *   activations  x [M,K] bf16:  per token m and group g of 128 inputs (the last may be shorter)  s = amax / 448 (1 if amax = 0),
+ *                x8 = e4m3(x / s), round-to-nearest-even, saturating;   x_scale[g,m] = s
+ *   weights      w [N,K] bf16:  the same per tile of 128 outputs x 128 inputs;   w_scale[n/128,g] = s
+ *   product      y[m,n] = sum_g x_scale[g,m] * w_scale[n/128,g] * sum_{k in g} x8[m,k] w8[n,k]
+ *                out[m,n] = bf16(act(y + bias[n]) + residual[m,n])
+ * Sums are fp32 throughout (a group's products in the tensor core, the groups with their scales in registers), in a fixed order: results
+ * are deterministic.  Codes may come from elsewhere (a checkpoint with fp32 scales per 128 x 128 tile of the weights); a code
+ * that is NaN makes its outputs NaN.  act: SVA_ACT_GELU is the tanh form.
+ */
+typedef enum { SVA_ACT_NONE = 0, SVA_ACT_GELU = 1, SVA_ACT_SILU = 2 } sva_act_t;
+
+typedef struct {
+  int32_t M, N, K;           /* tokens, outputs, inputs; M may be 0 (nothing is done)                                     */
+  int32_t act;               /* sva_act_t                                                                                 */
+  int64_t x_stride;          /* elements between rows of x, w, out, residual: multiples of 8                              */
+  int64_t w_stride;
+  int64_t out_stride;
+  int64_t residual_stride;
+  int64_t x8_stride;         /* bytes between rows of codes: multiples of 16, at least K                                  */
+  int64_t w8_stride;
+  int64_t x_scale_stride;    /* floats between groups of x_scale [ceil(K/128)][M], at least M                             */
+  int64_t w_scale_stride;    /* floats between rows of w_scale [ceil(N/128)][ceil(K/128)], at least ceil(K/128)           */
+} sva_linear_t;
+
+/*
+ * The three calls.  Pointers to x, w, x8, w8, out and residual are 16-byte aligned, the fp32 ones 4-byte aligned; only the
+ * members of p that a call's tensors need are looked at.  The quantisers write whole 16-byte pieces: bytes of a row of codes from K up to
+ * the next multiple of 16 become 0.  bias ([N] fp32) and residual (bf16 [M,N], may be `out` itself) are optional.  The product sets
+ * SVA_DEV_TIMEOUT in device_status (optional) when a bounded pipeline wait runs out; it needs no workspace.
+ * Errors: INVALID_ARG (null, sizes < 1, strides too small, bad act), ALIGNMENT, UNSUPPORTED (more than 2^31 tiles).
+ */
+int sva_quantize_rows_fp8(const sva_linear_t* p, const void* x_bf16, void* x8, float* x_scale, void* stream);
+int sva_quantize_tiles_fp8(const sva_linear_t* p, const void* w_bf16, void* w8, float* w_scale, void* stream);
+int sva_linear_fp8(const sva_linear_t* p, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* out,
+                   const float* bias, const void* residual, int32_t* device_status, void* stream);
+
+/*
+ * Rotary positions as a call of its own (the fused prologue above takes whole heads in the interleaved layout, from a table).
+ * The rotary_dim first channels of every head are rotary_dim/2 pairs, (2j, 2j+1) in the interleaved layout, (j, j + rotary_dim/2) in the
+ * half layout; the others pass through.  Pair j of a token at position p turns by p * theta_j:
+ *     (a, b) -> factor * (a cos - b sin, b cos + a sin)          inverse: sin -> -sin, which is also the gradient's rotation
+ * in fp32, rounded once to bf16.  theta_j / 2 pi is given as a 64-bit fraction of a turn, steps[j] = round(theta_j / 2 pi * 2^64)
+ * (uint64, device): p * steps[j] modulo 2^64 is the phase without its whole turns, exact for every 32-bit position.
+ * Positions: int32, one array per axis; the first axis_pairs[0] pairs turn with axis 0, the next axis_pairs[1] with axis 1, the rest with axis 2
+ * (video: frame, row, column), so the axis_pairs sum to rotary_dim/2; (rotary_dim/2, 0, 0) is one axis.
+ */
+typedef enum { SVA_ROPE_INTERLEAVED = 0, SVA_ROPE_HALF = 1 } sva_rope_layout_t;
+typedef enum { SVA_ROPE_PLAIN = 0, SVA_ROPE_LINEAR = 1, SVA_ROPE_NTK = 2, SVA_ROPE_PARTS = 3 } sva_rope_scaling_t;
+
+typedef struct {
+  int32_t B, Hq, Hk, N, d;   /* Q [B,Hq,N,d], K [B,Hk,N,d]; d a multiple of 8 up to 256; N may be 0 (nothing is done)     */
+  int32_t rotary_dim;        /* even, 2 .. d                                                                              */
+  int32_t layout;            /* sva_rope_layout_t                                                                         */
+  int32_t axis_pairs[3];
+  int32_t inverse;
+  float factor;              /* on cos and sin; 1 but for some context extensions                                         */
+  int64_t q_stride[3];       /* element strides of b, h, n: multiples of 8                                                */
+  int64_t k_stride[3];
+  int64_t q_out_stride[3];
+  int64_t k_out_stride[3];
+  int64_t pos_stride[2];     /* elements between axes, and between batch items (0: shared) of positions                   */
+} sva_rope_t;
+
+/* q_out / k_out may be q / k themselves (same strides), otherwise they must not overlap them.  k and k_out may both be NULL.
+ * Errors: INVALID_ARG, ALIGNMENT (16 bytes; steps 8, positions 4), UNSUPPORTED (d). */
+int sva_rope(const sva_rope_t* p, const void* q, const void* k, const uint64_t* steps, const int32_t* positions, void* q_out,
+             void* k_out, void* stream);
+
+/*
+ * The steps of a frequency ladder, on the HOST (nothing is launched): for each axis of P = axis_pairs[a] pairs
+ *     theta_j = base^(-j/P), j < P,    changed for contexts longer than the trained one by `factor` >= 1:
+ *     SVA_ROPE_LINEAR  theta_j / factor
+ *     SVA_ROPE_NTK     base * factor^(P/(P-1)) instead of base (the slowest pair is slowed down by factor, the fastest stays)
+ *     SVA_ROPE_PARTS   r = trained_length * theta_j / 2 pi turns in the trained length, g = clamp((r - beta_slow)/(beta_fast - beta_slow), 0, 1):
+ *                      theta_j * ((1 - g)/factor + g), and *out_factor = 0.1 ln(factor) + 1 (1 for the other rules)
+ * steps: rotary_dim/2 entries.  Any other rule is the caller's: fill steps by the formula above.
+ */
+int sva_rope_steps(int32_t rotary_dim, const int32_t axis_pairs[3], double base, int32_t scaling, double factor, double trained_length,
+                   double beta_fast, double beta_slow, uint64_t* steps, float* out_factor);
+
+/*
+ * Quantised K/V cache: K and V of tokens that later calls attend to again -- the tokens that a pruned denoising call does not compute, the
+ * earlier chunks of a clip that is generated in chunks -- kept in 8 or 4 bits (the paper keeps features between steps and prunes
+ * tokens; it prints no format).  The cache is `pages` pages of `page` tokens; a token's slot is (page id) * page + place in the page.
+ * A row is one token of one head (d values).  Per row, every scalar step one fp32 operation rounded to nearest:
+ *   SVA_CACHE_E4M3  scale = amax / 448 (1 if amax = 0), code = e4m3(x / scale);                   x ~= bf16(value(code) * scale)
+ *   SVA_CACHE_FP4   scale = amax / (6 * 448) (1 if amax = 0), per 16 channels sf = e4m3((amax16 / 6) / scale),
+ *                   code = e2m1(x / (value(sf) * scale)) (0 where sf = 0);                        x ~= bf16(value(code) * value(sf) * scale)
+ * round-to-nearest-even and saturating.  Arrays (contiguous, device):
+ *   codes  [pages][H][page][d] bytes, or [pages][H][page][d/2], two codes per byte (even channel in the low half); 16-byte aligned
+ *   scale  [pages][H][page] fp32
+ *   sf     [pages][H][page][d/16] bytes (SVA_CACHE_FP4 only)
+ */
+typedef enum { SVA_CACHE_E4M3 = 0, SVA_CACHE_FP4 = 1 } sva_cache_format_t;
+
+typedef struct {
+  int32_t H, d;              /* d = 64 or 128                                                                             */
+  int32_t page, pages;       /* pages * page < 2^31                                                                       */
+  int32_t format;            /* sva_cache_format_t                                                                        */
+  void *k_codes, *v_codes;
+  float *k_scale, *v_scale;
+  void *k_sf, *v_sf;
+} sva_kv_cache_t;
+
+/*
+ * write : k, v [B,H,T,d] bf16 (element strides of b, h, n; multiples of 8, 16-byte aligned) into the slots [B,T] int32.  A negative slot
+ *         leaves its token out (padding); one beyond the cache is reported (SVA_DEV_BAD_INDEX) and left out.  Slots of a
+ *         call that are equal make its result order-dependent.
+ * read  : row n < min(N, lengths[b]) of k, v [B,H,N,d] comes from place n % page of page page_table[b][n / page] (int32, max_pages per
+ *         row, table_stride between rows); rows from lengths[b] on become zeros.  A page id outside [0, pages), or a page beyond max_pages, is
+ *         reported and its rows become zeros.
+ * T and N may be 0 (nothing is done).  Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (d, cache size).
+ */
+int sva_kv_cache_write(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t k_stride[3], const int64_t v_stride[3],
+                       int32_t B, int32_t T, const int32_t* slots, int32_t* device_status, void* stream);
+int sva_kv_cache_read(const sva_kv_cache_t* c, const int32_t* page_table, int64_t table_stride, int32_t max_pages, const int32_t* lengths,
+                      int32_t B, int32_t N, void* k, void* v, const int64_t k_stride[3], const int64_t v_stride[3],
+                      int32_t* device_status, void* stream);
+
 const char* sva_status_string(int status);
 
 #ifdef __cplusplus

@@ -32,7 +32,8 @@ void sva_debug_set_prof_buffer(void* buf);
  *   bit 7: test aid: the remainder call masks the kept blocks of a block-mean tile by looking them up in the CSR
  *          (the form that serves more than 1024 key blocks) even where the kept-block bit masks would serve;
  *   bit 8: test aid: the kernel of the first-order term's block covariances withholds a part of its V tile, and
- *   bit 9: the one that adds them up withholds every column tile of a CTA after its first, so that bounded waits run out.
+ *   bit 9: the one that adds them up withholds every column tile of a CTA after its first, so that bounded waits run out;
+ *   bit 10: test aid: the linear layer's kernels withhold the inputs after the first 128 of every tile, likewise.
  */
 void sva_debug_set_mode(int bits);
 

@@ -24,6 +24,8 @@ EXPORTS = [
     "sva_quantize_qk_fp8", "sva_status_string", "sva_block_select_noalloc", "sva_attn_workspace_bytes",
     "sva_attn_prepare_v", "sva_block_sparse_attn_fwd_prepared", "sva_gather_tokens", "sva_scatter_tokens",
     "sva_attn_one_call_workspace_bytes", "sva_quantize_qk_fp4", "sva_block_sparse_attn_fwd_fp4", "sva_attn_remainder_workspace_bytes", "sva_block_sparse_attn_remainder_fwd", "sva_smooth_workspace_bytes", "sva_quantize_qk_fp8_smooth_k", "sva_block_select_pooled", "sva_qk_norm_rope_pool", "sva_pool_qk",
+    "sva_quantize_rows_fp8", "sva_quantize_tiles_fp8", "sva_linear_fp8", "sva_rope", "sva_rope_steps", "sva_kv_cache_write",
+    "sva_kv_cache_read",
 ]
 DEBUG_EXPORTS = ["sva_debug_set_prof_buffer", "sva_debug_set_mode", "sva_debug_set_wait_limit"]
 NOALLOC_SCRATCH_BYTES = 16 << 20
@@ -40,6 +42,25 @@ class Problem(C.Structure):
 class Select(C.Structure):
     _fields_ = [("mode", C.c_int32), ("k", C.c_int32), ("mass", C.c_float),
                 ("win_t", C.c_int32), ("win_s", C.c_int32), ("blocks_per_frame", C.c_int32)]
+
+
+class Linear(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("act", C.c_int32),
+                ("x_stride", C.c_int64), ("w_stride", C.c_int64), ("out_stride", C.c_int64), ("residual_stride", C.c_int64),
+                ("x8_stride", C.c_int64), ("w8_stride", C.c_int64), ("x_scale_stride", C.c_int64), ("w_scale_stride", C.c_int64)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hk", C.c_int32), ("N", C.c_int32), ("d", C.c_int32),
+                ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("axis_pairs", C.c_int32 * 3), ("inverse", C.c_int32),
+                ("factor", C.c_float), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
+                ("q_out_stride", C.c_int64 * 3), ("k_out_stride", C.c_int64 * 3), ("pos_stride", C.c_int64 * 2)]
+
+
+class KvCache(C.Structure):
+    _fields_ = [("H", C.c_int32), ("d", C.c_int32), ("page", C.c_int32), ("pages", C.c_int32), ("format", C.c_int32),
+                ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_sf", C.c_void_p), ("v_sf", C.c_void_p)]
 
 
 class SvaError(RuntimeError):
@@ -108,6 +129,23 @@ def lib():
         L.sva_qk_norm_rope_pool.restype = C.c_int
         L.sva_qk_norm_rope_pool.argtypes = [C.POINTER(Problem), vp, vp, vp, vp, vp, vp, C.c_float, vp, vp, vp, vp, vp, vp,
                                             vp, vp, vp]
+        L.sva_quantize_rows_fp8.restype = C.c_int
+        L.sva_quantize_rows_fp8.argtypes = [C.POINTER(Linear), vp, vp, vp, vp]
+        L.sva_quantize_tiles_fp8.restype = C.c_int
+        L.sva_quantize_tiles_fp8.argtypes = [C.POINTER(Linear), vp, vp, vp, vp]
+        L.sva_linear_fp8.restype = C.c_int
+        L.sva_linear_fp8.argtypes = [C.POINTER(Linear), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.sva_rope.restype = C.c_int
+        L.sva_rope.argtypes = [C.POINTER(Rope), vp, vp, vp, vp, vp, vp, vp]
+        L.sva_rope_steps.restype = C.c_int
+        L.sva_rope_steps.argtypes = [C.c_int32, C.POINTER(C.c_int32), C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double,
+                                     C.c_double, C.POINTER(C.c_uint64), C.POINTER(C.c_float)]
+        i64p = C.POINTER(C.c_int64)
+        L.sva_kv_cache_write.restype = C.c_int
+        L.sva_kv_cache_write.argtypes = [C.POINTER(KvCache), vp, vp, i64p, i64p, C.c_int32, C.c_int32, vp, vp, vp]
+        L.sva_kv_cache_read.restype = C.c_int
+        L.sva_kv_cache_read.argtypes = [C.POINTER(KvCache), vp, C.c_int64, C.c_int32, vp, C.c_int32, C.c_int32, vp, vp, i64p, i64p,
+                                        vp, vp]
         # test and tuning aids (include/sva_debug.h): process-global settings
         L.sva_debug_set_prof_buffer.restype = None
         L.sva_debug_set_prof_buffer.argtypes = [vp]
@@ -364,3 +402,144 @@ def block_sparse_attn_fwd_fp4(p: Problem, q4, k4, q_sf, k_sf, q_g, k_g, v, row_p
 def attn_one_call_workspace_bytes(p: Problem) -> int:
     """Workspace the one-call attention entry points need (e4m3 Q/K: just the row counters and tile lists)."""
     return int(lib().sva_attn_one_call_workspace_bytes(C.byref(p)))
+
+
+ACTIVATIONS = {"none": 0, "gelu": 1, "silu": 2}
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+CACHE_FORMATS = {"e4m3": 0, "fp4": 1}
+
+
+def _row_stride(t, what):
+    assert t.dim() == 2 and t.stride(1) == 1, f"{what} is a matrix with contiguous rows"
+    return t.stride(0)
+
+
+def make_linear(x=None, x8=None, x_scale=None, w8=None, w_scale=None, out=None, act: str = "none", residual=None, w=None, K: int = 0) -> Linear:
+    """A linear layer y = x w^T: x [M,K] bf16, x8 [M,>=K] codes, x_scale [ceil(K/128),M] fp32, w [N,K] bf16, w8 [N,>=K] codes,
+    w_scale [ceil(N/128),ceil(K/128)] fp32, out and residual [M,N] bf16.  What a call does not use may be left out; K is taken from x or
+    w, or given."""
+    p = Linear()
+    rows = x if x is not None else x8
+    p.M = rows.shape[0] if rows is not None else 0
+    p.K = K or (x.shape[1] if x is not None else w.shape[1] if w is not None else 0)
+    cols = w8 if w8 is not None else w
+    p.N = cols.shape[0] if cols is not None else 0
+    p.act = ACTIVATIONS[act]
+    for name, t in (("x", x), ("w", w), ("out", out), ("residual", residual), ("x8", x8), ("w8", w8), ("x_scale", x_scale),
+                    ("w_scale", w_scale)):
+        if t is not None:
+            # a matrix of one row may carry any stride: its row's length, rounded up, will do
+            one = -(-t.shape[1] // 16) * 16
+            setattr(p, name + "_stride", _row_stride(t, name) if t.shape[0] > 1 else max(_row_stride(t, name), one))
+    for t, shape in ((x, (p.M, p.K)), (out, (p.M, p.N)), (residual, (p.M, p.N)), (w, (p.N, p.K))):
+        assert t is None or tuple(t.shape) == shape and t.dtype == torch.bfloat16, "bf16 matrices of matching sizes"
+    for t, n in ((x8, p.M), (w8, p.N)):
+        assert t is None or t.shape[0] == n and t.shape[1] >= p.K and t.element_size() == 1, "codes are bytes, a row for each row"
+    groups = -(-p.K // 128)
+    for t, shape in ((x_scale, (groups, p.M)), (w_scale, (-(-p.N // 128), groups))):
+        assert t is None or t.dtype == torch.float32 and t.shape[0] == shape[0] and t.shape[1] >= shape[1], "fp32 scales, one per block of 128"
+    return p
+
+
+def quantize_rows_fp8(p: Linear, x, x8, x_scale) -> None:
+    """Activations to e4m3 codes, a scale per token and 128 inputs."""
+    rc = lib().sva_quantize_rows_fp8(C.byref(p), _ptr(x), _ptr(x8), _ptr(x_scale), _stream())
+    if rc != SVA_OK:
+        raise SvaError(rc, "sva_quantize_rows_fp8")
+
+
+def quantize_tiles_fp8(p: Linear, w, w8, w_scale) -> None:
+    """Weights to e4m3 codes, a scale per tile of 128 x 128."""
+    rc = lib().sva_quantize_tiles_fp8(C.byref(p), _ptr(w), _ptr(w8), _ptr(w_scale), _stream())
+    if rc != SVA_OK:
+        raise SvaError(rc, "sva_quantize_tiles_fp8")
+
+
+def linear_fp8(p: Linear, x8, x_scale, w8, w_scale, out, bias=None, residual=None, status=None) -> None:
+    """out = bf16(act(x w^T + bias) + residual) from codes and scales."""
+    assert bias is None or bias.dtype == torch.float32 and bias.numel() == p.N and bias.is_contiguous(), "bias is [N] fp32"
+    rc = lib().sva_linear_fp8(C.byref(p), _ptr(x8), _ptr(x_scale), _ptr(w8), _ptr(w_scale), _ptr(out), _ptr(bias), _ptr(residual),
+                              _ptr(status), _stream())
+    if rc != SVA_OK:
+        raise SvaError(rc, "sva_linear_fp8")
+
+
+def rope_steps(rotary_dim: int, axis_pairs=None, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained_length: float = 1.0,
+               beta_fast: float = 32.0, beta_slow: float = 1.0, device=None):
+    """The frequency ladder of rope(): (steps, an int64 tensor of rotary_dim/2 fractions of a turn; the factor on cos and sin)."""
+    pairs = list(axis_pairs or [rotary_dim // 2])
+    steps, out = (C.c_uint64 * max(1, rotary_dim // 2))(), C.c_float()
+    rc = lib().sva_rope_steps(rotary_dim, (C.c_int32 * 3)(*(pairs + [0, 0])[:3]), base, ROPE_SCALINGS[scaling], factor, trained_length,
+                              beta_fast, beta_slow, steps, C.byref(out))
+    if rc != SVA_OK:
+        raise SvaError(rc, "sva_rope_steps")
+    return torch.tensor(list(steps), dtype=torch.int64, device=device), out.value
+
+
+def make_rope(q, k, q_out, k_out, positions, rotary_dim: int, layout: str = "interleaved", axis_pairs=None, factor: float = 1.0,
+              inverse: bool = False) -> Rope:
+    """q [B,Hq,N,d], k [B,Hk,N,d] (or None) and where they go; positions [axes, B or 1, N] int32."""
+    p = Rope()
+    p.B, p.Hq, p.N, p.d = q.shape
+    p.Hk = k.shape[1] if k is not None else 0
+    p.rotary_dim, p.layout, p.inverse, p.factor = rotary_dim, ROPE_LAYOUTS[layout], int(inverse), factor
+    pairs = list(axis_pairs or [rotary_dim // 2])
+    p.axis_pairs = (C.c_int32 * 3)(*(pairs + [0, 0])[:3])
+    assert len(pairs) <= 3 and positions.dtype == torch.int32 and positions.dim() == 3 and positions.shape[0] >= len(pairs) and \
+        positions.shape[1] in (1, p.B) and positions.shape[2] == p.N and (p.N <= 1 or positions.stride(2) == 1), "positions are [axes, B or 1, N] int32"
+    p.pos_stride = (C.c_int64 * 2)(positions.stride(0), positions.stride(1) if positions.shape[1] > 1 else 0)
+    p.q_stride, p.q_out_stride = _strides(q), _strides(q_out)
+    assert q_out.shape == q.shape and q.dtype == q_out.dtype == torch.bfloat16
+    if k is not None:
+        assert k.shape == (p.B, p.Hk, p.N, p.d) and k_out.shape == k.shape and k.dtype == k_out.dtype == torch.bfloat16
+        p.k_stride, p.k_out_stride = _strides(k), _strides(k_out)
+    return p
+
+
+def rope(p: Rope, q, k, steps, positions, q_out, k_out) -> None:
+    """Rotary positions of q and k (k None: q alone)."""
+    rc = lib().sva_rope(C.byref(p), _ptr(q), _ptr(k), _ptr(steps), _ptr(positions), _ptr(q_out), _ptr(k_out), _stream())
+    if rc != SVA_OK:
+        raise SvaError(rc, "sva_rope")
+
+
+def make_kv_cache(k, v, format: str = "e4m3") -> KvCache:
+    """A cache over its arrays: k and v are [codes, scale] (e4m3) or [codes, scale, sf] (fp4), codes [pages,H,page,d or d/2] bytes, scale
+    [pages,H,page] fp32, sf [pages,H,page,d/16] bytes, all contiguous.  The arrays are kept alive."""
+    c = KvCache()
+    c.format = CACHE_FORMATS[format]
+    c.pages, c.H, c.page, row = k[0].shape
+    c.d = row * 2 if format == "fp4" else row
+    shapes = [(c.pages, c.H, c.page, row), (c.pages, c.H, c.page), (c.pages, c.H, c.page, c.d // 16)]
+    for arrays in (k, v):
+        assert len(arrays) == (3 if format == "fp4" else 2)
+        for t, shape, size in zip(arrays, shapes, (1, 4, 1)):
+            assert tuple(t.shape) == shape and t.is_contiguous() and t.element_size() == size, "contiguous arrays of the cache's sizes"
+    c.k_codes, c.v_codes, c.k_scale, c.v_scale = _ptr(k[0]), _ptr(v[0]), _ptr(k[1]), _ptr(v[1])
+    if format == "fp4":
+        c.k_sf, c.v_sf = _ptr(k[2]), _ptr(v[2])
+    c.arrays = (tuple(k), tuple(v))
+    return c
+
+
+def kv_cache_write(c: KvCache, k, v, slots, status=None) -> None:
+    """k, v [B,H,T,d] bf16 into the slots [B,T] int32 (negative: left out)."""
+    Bq, H, T, d = k.shape
+    assert H == c.H and d == c.d and v.shape == k.shape and k.dtype == v.dtype == torch.bfloat16
+    assert slots.shape == (Bq, T) and slots.dtype == torch.int32 and slots.is_contiguous(), "slots are [B,T] int32"
+    rc = lib().sva_kv_cache_write(C.byref(c), _ptr(k), _ptr(v), _strides(k), _strides(v), Bq, T, _ptr(slots), _ptr(status), _stream())
+    if rc != SVA_OK:
+        raise SvaError(rc, "sva_kv_cache_write")
+
+
+def kv_cache_read(c: KvCache, page_table, lengths, k, v, status=None) -> None:
+    """Each sequence's first rows, from its pages, into k, v [B,H,N,d] bf16; rows from lengths[b] on become zeros."""
+    Bq, H, N, d = k.shape
+    assert H == c.H and d == c.d and v.shape == k.shape and k.dtype == v.dtype == torch.bfloat16
+    assert page_table.shape[0] == Bq and page_table.dtype == torch.int32 and page_table.stride(1) == 1, "page_table is [B,pages] int32"
+    assert lengths.shape == (Bq,) and lengths.dtype == torch.int32 and lengths.is_contiguous(), "lengths is [B] int32"
+    rc = lib().sva_kv_cache_read(C.byref(c), _ptr(page_table), page_table.stride(0), page_table.shape[1], _ptr(lengths), Bq, N, _ptr(k),
+                                 _ptr(v), _strides(k), _strides(v), _ptr(status), _stream())
+    if rc != SVA_OK:
+        raise SvaError(rc, "sva_kv_cache_read")

@@ -1,4 +1,6 @@
 // C ABI entry points: host-side validation, then the kernel launchers.
+#include <cmath>
+
 #include "common.cuh"
 
 namespace sva {
@@ -9,6 +11,8 @@ void route_set_debug_mode(int v);
 void rem_set_debug_mode(int v);
 int ts_set_wait_limit(long long cycles);
 int rem_set_wait_limit(long long cycles);
+void lin_set_debug_mode(int v);
+int lin_set_wait_limit(long long cycles);
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -374,6 +378,144 @@ int sva_scatter_tokens(const void* src, const int64_t src_stride[3], const int32
                            device_status, (cudaStream_t)stream);
 }
 
+// Rows of the linear calls: 16-byte aligned base, a stride of whole 16-byte pieces that holds a row.
+static int check_rows(const void* ptr, int64_t stride, int64_t row, int elem_bytes) {
+  if (!ptr || stride < row) return SVA_ERR_INVALID_ARG;
+  if (!aligned16(ptr) || stride * elem_bytes % 16 != 0) return SVA_ERR_ALIGNMENT;
+  return SVA_OK;
+}
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static int check_floats(const void* ptr, int64_t stride, int64_t row) {
+  if (!ptr || stride < row) return SVA_ERR_INVALID_ARG;
+  return aligned4(ptr) ? SVA_OK : SVA_ERR_ALIGNMENT;
+}
+// (sizes whose tiles of 128 can be counted, and whose last tile's end can be formed, in 32 bits)
+static constexpr int32_t LINEAR_MAX = 0x7fffffff - 1024;
+
+int sva_quantize_rows_fp8(const sva_linear_t* p, const void* x_bf16, void* x8, float* x_scale, void* stream) {
+  if (!p || p->M < 0 || p->K < 1) return SVA_ERR_INVALID_ARG;
+  if (p->M > LINEAR_MAX || p->K > LINEAR_MAX) return SVA_ERR_UNSUPPORTED;
+  if (p->M == 0) return SVA_OK;
+  int rc = check_rows(x_bf16, p->x_stride, p->K, 2);
+  if (!rc) rc = check_rows(x8, p->x8_stride, p->K, 1);
+  if (!rc) rc = check_floats(x_scale, p->x_scale_stride, p->M);
+  return rc ? rc : launch_quantize_rows(p, x_bf16, x8, x_scale, (cudaStream_t)stream);
+}
+
+int sva_quantize_tiles_fp8(const sva_linear_t* p, const void* w_bf16, void* w8, float* w_scale, void* stream) {
+  if (!p || p->N < 1 || p->K < 1) return SVA_ERR_INVALID_ARG;
+  if (p->N > LINEAR_MAX || p->K > LINEAR_MAX) return SVA_ERR_UNSUPPORTED;
+  int rc = check_rows(w_bf16, p->w_stride, p->K, 2);
+  if (!rc) rc = check_rows(w8, p->w8_stride, p->K, 1);
+  if (!rc) rc = check_floats(w_scale, p->w_scale_stride, (p->K + 127) / 128);
+  return rc ? rc : launch_quantize_tiles(p, w_bf16, w8, w_scale, (cudaStream_t)stream);
+}
+
+int sva_linear_fp8(const sva_linear_t* p, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* out,
+                   const float* bias, const void* residual, int32_t* device_status, void* stream) {
+  if (!p || p->M < 0 || p->N < 1 || p->K < 1) return SVA_ERR_INVALID_ARG;
+  if (p->act < SVA_ACT_NONE || p->act > SVA_ACT_SILU) return SVA_ERR_INVALID_ARG;
+  if (p->M > LINEAR_MAX || p->N > LINEAR_MAX || p->K > LINEAR_MAX) return SVA_ERR_UNSUPPORTED;
+  if (p->M == 0) return SVA_OK;
+  int rc = check_rows(x8, p->x8_stride, p->K, 1);
+  if (!rc) rc = check_rows(w8, p->w8_stride, p->K, 1);
+  if (!rc) rc = check_rows(out, p->out_stride, p->N, 2);
+  if (!rc && residual) rc = check_rows(residual, p->residual_stride, p->N, 2);
+  if (!rc) rc = check_floats(x_scale, p->x_scale_stride, p->M);
+  if (!rc) rc = check_floats(w_scale, p->w_scale_stride, (p->K + 127) / 128);
+  if (!rc && !aligned4(bias)) rc = SVA_ERR_ALIGNMENT;
+  return rc ? rc : launch_linear(p, x8, x_scale, w8, w_scale, out, bias, residual, device_status, (cudaStream_t)stream);
+}
+
+int sva_rope(const sva_rope_t* p, const void* q, const void* k, const uint64_t* steps, const int32_t* positions, void* q_out, void* k_out,
+             void* stream) {
+  if (!p || p->B < 1 || p->Hq < 1 || p->N < 0 || p->d < 1 || (!k) != (!k_out) || (k && p->Hk < 1)) return SVA_ERR_INVALID_ARG;
+  if (p->rotary_dim < 2 || p->rotary_dim % 2 != 0 || p->rotary_dim > p->d) return SVA_ERR_INVALID_ARG;
+  if (p->layout != SVA_ROPE_INTERLEAVED && p->layout != SVA_ROPE_HALF) return SVA_ERR_INVALID_ARG;
+  for (int a = 0; a < 3; ++a)
+    if (p->axis_pairs[a] < 0 || p->axis_pairs[a] > p->rotary_dim / 2) return SVA_ERR_INVALID_ARG;
+  if (p->axis_pairs[0] + p->axis_pairs[1] + p->axis_pairs[2] != p->rotary_dim / 2) return SVA_ERR_INVALID_ARG;
+  if (p->d % 8 != 0 || p->d > 256) return SVA_ERR_UNSUPPORTED;
+  if (p->pos_stride[0] < 0 || p->pos_stride[1] < 0) return SVA_ERR_INVALID_ARG;
+  if (p->N == 0) return SVA_OK;
+  if (!q || !q_out || !steps || !positions) return SVA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(q_out) || !aligned16(k) || !aligned16(k_out) || !aligned4(positions) ||
+      (reinterpret_cast<uintptr_t>(steps) & 7u) != 0)
+    return SVA_ERR_ALIGNMENT;
+  int rc = check_strides(p->q_stride, 8);
+  if (!rc) rc = check_strides(p->q_out_stride, 8);
+  if (!rc && k) rc = check_strides(p->k_stride, 8);
+  if (!rc && k) rc = check_strides(p->k_out_stride, 8);
+  return rc ? rc : launch_rope(p, q, k, steps, positions, q_out, k_out, (cudaStream_t)stream);
+}
+
+int sva_rope_steps(int32_t rotary_dim, const int32_t axis_pairs[3], double base, int32_t scaling, double factor, double trained_length,
+                   double beta_fast, double beta_slow, uint64_t* steps, float* out_factor) {
+  if (!axis_pairs || !steps || !out_factor || rotary_dim < 2 || rotary_dim % 2 != 0) return SVA_ERR_INVALID_ARG;
+  if (scaling < SVA_ROPE_PLAIN || scaling > SVA_ROPE_PARTS) return SVA_ERR_INVALID_ARG;
+  if (!(base >= 1.0) || !std::isfinite(base) || !(factor >= 1.0) || !std::isfinite(factor)) return SVA_ERR_INVALID_ARG;
+  if (scaling == SVA_ROPE_PARTS && !(trained_length > 0.0 && beta_slow >= 0.0 && beta_fast > beta_slow)) return SVA_ERR_INVALID_ARG;
+  int64_t total = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (axis_pairs[a] < 0) return SVA_ERR_INVALID_ARG;
+    total += axis_pairs[a];
+  }
+  if (total != rotary_dim / 2) return SVA_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925;
+  int at = 0;
+  for (int a = 0; a < 3; ++a) {
+    const int P = axis_pairs[a];
+    const double b = scaling == SVA_ROPE_NTK && P > 1 ? base * std::pow(factor, (double)P / (P - 1)) : base;
+    for (int j = 0; j < P; ++j, ++at) {
+      double theta = std::pow(b, -(double)j / P);
+      if (scaling == SVA_ROPE_LINEAR) theta /= factor;
+      if (scaling == SVA_ROPE_PARTS) {
+        double g = (trained_length * theta / two_pi - beta_slow) / (beta_fast - beta_slow);
+        g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
+        theta *= (1.0 - g) / factor + g;
+      }
+      steps[at] = (uint64_t)std::nearbyint(theta / two_pi * 18446744073709551616.0);      // (theta <= 1: below 2^62)
+    }
+  }
+  *out_factor = scaling == SVA_ROPE_PARTS ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return SVA_OK;
+}
+
+static int validate_cache(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t ks[3], const int64_t vs[3], int B, int T) {
+  if (!c || !ks || !vs || B < 1 || T < 0 || c->H < 1 || c->d < 1 || c->page < 1 || c->pages < 1) return SVA_ERR_INVALID_ARG;
+  if (c->format != SVA_CACHE_E4M3 && c->format != SVA_CACHE_FP4) return SVA_ERR_INVALID_ARG;
+  if (c->d != 64 && c->d != 128) return SVA_ERR_UNSUPPORTED;
+  if ((long long)c->page * c->pages > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return SVA_ERR_INVALID_ARG;
+  if (c->format == SVA_CACHE_FP4 && (!c->k_sf || !c->v_sf)) return SVA_ERR_INVALID_ARG;
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned4(c->k_scale) || !aligned4(c->v_scale)) return SVA_ERR_ALIGNMENT;
+  if (T == 0) return SVA_OK;
+  if (!k || !v) return SVA_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v)) return SVA_ERR_ALIGNMENT;
+  const int rc = check_strides(ks, 8);
+  return rc ? rc : check_strides(vs, 8);
+}
+
+int sva_kv_cache_write(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t k_stride[3], const int64_t v_stride[3],
+                       int32_t B, int32_t T, const int32_t* slots, int32_t* device_status, void* stream) {
+  const int rc = validate_cache(c, k, v, k_stride, v_stride, B, T);
+  if (rc || T == 0) return rc;
+  if (!slots) return SVA_ERR_INVALID_ARG;
+  if (!aligned4(slots)) return SVA_ERR_ALIGNMENT;
+  return launch_cache_write(c, k, v, k_stride, v_stride, B, T, slots, device_status, (cudaStream_t)stream);
+}
+
+int sva_kv_cache_read(const sva_kv_cache_t* c, const int32_t* page_table, int64_t table_stride, int32_t max_pages, const int32_t* lengths,
+                      int32_t B, int32_t N, void* k, void* v, const int64_t k_stride[3], const int64_t v_stride[3],
+                      int32_t* device_status, void* stream) {
+  const int rc = validate_cache(c, k, v, k_stride, v_stride, B, N);
+  if (rc || N == 0) return rc;
+  if (!page_table || !lengths || max_pages < 1 || table_stride < (B > 1 ? max_pages : 0)) return SVA_ERR_INVALID_ARG;
+  if (!aligned4(page_table) || !aligned4(lengths)) return SVA_ERR_ALIGNMENT;
+  return launch_cache_read(c, page_table, table_stride, max_pages, lengths, B, N, k, v, k_stride, v_stride, device_status,
+                           (cudaStream_t)stream);
+}
+
 const char* sva_status_string(int status) {
   switch (status) {
     case SVA_OK: return "ok";
@@ -392,13 +534,15 @@ const char* sva_status_string(int status) {
 void sva_debug_set_prof_buffer(void* p) { ts_set_prof_buffer(p); }
 /* bit 4 (test aid) withholds a row's K tiles after the first so that a bounded wait runs out; bit 5 (measurement aid) has the one-call
    forms read a transposed copy of V; bit 6 (test aid) has routing ask for clusters that no device holds; bit 7 (test aid) has the
-   remainder look kept blocks up in the CSR; bits 8 and 9 (test aids) withhold loads of the first-order term's kernels */
+   remainder look kept blocks up in the CSR; bits 8 and 9 (test aids) withhold loads of the first-order term's kernels; bit 10 (test aid) those of the
+   linear layer's kernels */
 void sva_debug_set_mode(int v) {
   ts_set_debug_mode(v);
   route_set_debug_mode(v);
   rem_set_debug_mode(v);
+  lin_set_debug_mode(v);
 }
 /* test aid: cycles a device-side wait may last before the CTA gives up (<= 0 restores the default) */
-int sva_debug_set_wait_limit(long long cycles) { return ts_set_wait_limit(cycles) | rem_set_wait_limit(cycles); }
+int sva_debug_set_wait_limit(long long cycles) { return ts_set_wait_limit(cycles) | rem_set_wait_limit(cycles) | lin_set_wait_limit(cycles); }
 
 }  // extern "C"

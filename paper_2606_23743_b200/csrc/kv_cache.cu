@@ -1,0 +1,236 @@
+// Quantised K/V cache: rows of K and V (one token of one head, d values) as e4m3 codes with an fp32 scale, or as 4-bit codes with an e4m3
+// scale per 16 channels and an fp32 scale, in pages of `page` tokens, [pages][H][page][...].  A token has a slot
+// (page id * page + place in the page); writing quantises into slots, reading collects a sequence's pages into the [B,H,N,d] tensors that the
+// attention calls take.
+//
+// Both are HBM-bound streaming passes.  d/16 lanes own a row, 16 channels each (one 4-bit scale block), so that a row's maximum is
+// a few shuffles; a thread looks its token's slot up once and then has CACHE_HEADS heads' rows in flight.
+#include <cuda_fp4.h>
+
+#include "common.cuh"
+
+namespace sva {
+
+static constexpr int CACHE_THREADS = 256;
+static constexpr int CACHE_HEADS = 4;                     // rows in flight per thread
+
+struct CacheArrays {                                      // one of K, V
+  uint8_t* codes;
+  float* scale;
+  uint8_t* sf;
+};
+
+struct CacheParams {
+  CacheArrays k, v;
+  uint8_t *xk, *xv;                                       // bf16 tensors, read or written
+  Strides sk, sv;
+  const int32_t *slots, *table, *lengths;
+  long long table_stride, tokens;                         // tokens: B * T, or B * N
+  long long slot_count;
+  int H, T, page, pages, max_pages, head_groups;
+  int32_t* status;
+};
+
+__device__ __noinline__ float cache_div_slow(float a, float b) { return __fdiv_rn(a, b); }
+
+// row of (page, head, place) among all rows
+__device__ __forceinline__ long long cache_row(const CacheParams& prm, long long page, int h, int place) {
+  return (page * prm.H + h) * prm.page + place;
+}
+
+// the largest magnitude of 16 bf16 values, as fp32
+__device__ __forceinline__ float cache_amax(const uint4& a, const uint4& b) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  uint32_t m = 0u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(w[e] & 0x7fff7fffu));
+  return __uint_as_float(max(m << 16, m & 0xffff0000u));
+}
+
+template <int LANES, bool FP4>
+__global__ void __launch_bounds__(CACHE_THREADS)
+cache_write_kernel(const CacheParams prm) {
+  const int zero = grid_dep_wait();
+  const int which = blockIdx.x & 1, group = (int)((blockIdx.x >> 1) % prm.head_groups);
+  const long long t = (long long)((blockIdx.x >> 1) / prm.head_groups) * (CACHE_THREADS / LANES) + threadIdx.x / LANES + zero;
+  const int lane = threadIdx.x % LANES;
+  const CacheArrays out = which ? prm.v : prm.k;
+  const Strides s = which ? prm.sv : prm.sk;
+  // (all lanes of a row share its token; the shuffles below are taken by every thread)
+  long long slot = -1;
+  if (t < prm.tokens) slot = __ldg(prm.slots + t);
+  if (slot >= prm.slot_count) {
+    if (lane == 0 && group == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
+    slot = -1;
+  }
+  const bool there = slot >= 0;
+  const long long b = there ? t / prm.T : 0, n = there ? t - b * prm.T : 0;
+  const long long page = there ? slot / prm.page : 0;
+  const int place = there ? (int)(slot - page * prm.page) : 0;
+  const int h0 = group * CACHE_HEADS;
+  const uint8_t* src = (which ? prm.xv : prm.xk) + 2 * (b * s.b + n * s.n + lane * 16);
+  uint4 in[CACHE_HEADS][2];
+#pragma unroll
+  for (int i = 0; i < CACHE_HEADS; ++i) {
+    in[i][0] = in[i][1] = make_uint4(0u, 0u, 0u, 0u);
+    if (there && h0 + i < prm.H) {
+      const uint4* row = reinterpret_cast<const uint4*>(src + 2 * (h0 + i) * s.h);
+      in[i][0] = __ldg(row);
+      in[i][1] = __ldg(row + 1);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < CACHE_HEADS; ++i) {
+    const float own = cache_amax(in[i][0], in[i][1]);
+    float amax = own;
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if (!there || h0 + i >= prm.H) continue;
+    const long long row = cache_row(prm, page, h0 + i, place);
+    const uint32_t w[8] = {in[i][0].x, in[i][0].y, in[i][0].z, in[i][0].w, in[i][1].x, in[i][1].y, in[i][1].z, in[i][1].w};
+    const float scale = amax == 0.f ? 1.0f : __fdiv_rn(amax, FP4 ? 2688.0f : 448.0f);
+    if (lane == 0) out.scale[row] = scale;
+    if (!FP4) {
+      uint32_t c[4];
+      if (div_fast_ok(scale)) {
+        const float rcp = __frcp_rn(scale);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          c[e] = __byte_perm(e4m3x2(div_fast(bf16lo(w[2 * e]), scale, rcp), div_fast(bf16hi(w[2 * e]), scale, rcp)),
+                             e4m3x2(div_fast(bf16lo(w[2 * e + 1]), scale, rcp), div_fast(bf16hi(w[2 * e + 1]), scale, rcp)), 0x5410);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          c[e] = __byte_perm(e4m3x2(cache_div_slow(bf16lo(w[2 * e]), scale), cache_div_slow(bf16hi(w[2 * e]), scale)),
+                             e4m3x2(cache_div_slow(bf16lo(w[2 * e + 1]), scale), cache_div_slow(bf16hi(w[2 * e + 1]), scale)), 0x5410);
+      }
+      *reinterpret_cast<uint4*>(out.codes + (row * LANES + lane) * 16) = make_uint4(c[0], c[1], c[2], c[3]);
+    } else {
+      const uint32_t sf = (uint32_t)__nv_cvt_float_to_fp8(__fdiv_rn(__fdiv_rn(own, 6.0f), scale), __NV_SATFINITE, __NV_E4M3);
+      const float unit = __fmul_rn(e4m3_to_float(sf), scale);
+      uint32_t c[2] = {0u, 0u};
+      if (unit > 0.f) {
+        const bool fast = div_fast_ok(unit);
+        const float rcp = __frcp_rn(unit);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float lo = bf16lo(w[e]), hi = bf16hi(w[e]);
+          const float2 y = fast ? make_float2(div_fast(lo, unit, rcp), div_fast(hi, unit, rcp))
+                                : make_float2(cache_div_slow(lo, unit), cache_div_slow(hi, unit));
+          c[e >> 2] |= ((uint32_t)__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest) & 0xffu) << (8 * (e & 3));
+        }
+      }
+      out.sf[row * LANES + lane] = unit > 0.f ? (uint8_t)sf : (uint8_t)0;
+      *reinterpret_cast<uint2*>(out.codes + (row * LANES + lane) * 8) = make_uint2(c[0], c[1]);
+    }
+  }
+}
+
+template <int LANES, bool FP4>
+__global__ void __launch_bounds__(CACHE_THREADS)
+cache_read_kernel(const CacheParams prm) {
+  const int zero = grid_dep_wait();
+  const int which = blockIdx.x & 1, group = (int)((blockIdx.x >> 1) % prm.head_groups);
+  const long long t = (long long)((blockIdx.x >> 1) / prm.head_groups) * (CACHE_THREADS / LANES) + threadIdx.x / LANES + zero;
+  const int lane = threadIdx.x % LANES;
+  if (t >= prm.tokens) return;
+  const CacheArrays in = which ? prm.v : prm.k;
+  const Strides s = which ? prm.sv : prm.sk;
+  const long long b = t / prm.T;
+  const int n = (int)(t - b * prm.T), at = n / prm.page;
+  bool there = n < __ldg(prm.lengths + b);
+  long long page = 0;
+  if (there) {
+    page = at < prm.max_pages ? __ldg(prm.table + b * prm.table_stride + at) : -1;
+    if (page < 0 || page >= prm.pages) {
+      if (lane == 0 && group == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
+      there = false;
+    }
+  }
+  const int place = n - at * prm.page, h0 = group * CACHE_HEADS;
+  uint8_t* dst = (which ? prm.xv : prm.xk) + 2 * (b * s.b + (long long)n * s.n + lane * 16);
+  uint4 codes[CACHE_HEADS];
+  float scale[CACHE_HEADS];
+  uint32_t sf[CACHE_HEADS];
+#pragma unroll
+  for (int i = 0; i < CACHE_HEADS; ++i) {
+    codes[i] = make_uint4(0u, 0u, 0u, 0u);
+    scale[i] = 0.f;
+    sf[i] = 0u;
+    if (there && h0 + i < prm.H) {
+      const long long row = cache_row(prm, page, h0 + i, place);
+      scale[i] = __ldg(in.scale + row);
+      if (FP4) {
+        const uint2 c = __ldg(reinterpret_cast<const uint2*>(in.codes + (row * LANES + lane) * 8));
+        codes[i].x = c.x; codes[i].y = c.y;
+        sf[i] = __ldg(in.sf + row * LANES + lane);
+      } else {
+        codes[i] = __ldg(reinterpret_cast<const uint4*>(in.codes + (row * LANES + lane) * 16));
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < CACHE_HEADS; ++i) {
+    if (h0 + i >= prm.H) continue;
+    uint32_t o[8];
+    const uint32_t w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+    const float unit = FP4 ? e4m3_to_float(sf[i]) : 1.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float2 x;
+      if (FP4) {
+        const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(w[e >> 2] >> (8 * (e & 3)) & 0xffu), __NV_E2M1);
+        x = __half22float2(__half2(h));
+        x.x *= unit; x.y *= unit;                           // exact: 2 by 4 significant bits
+      } else {
+        x = e4m3x2_to_float2(w[e >> 1] >> (16 * (e & 1)) & 0xffffu);
+      }
+      const __nv_bfloat162 v = __floats2bfloat162_rn(__fmul_rn(x.x, scale[i]), __fmul_rn(x.y, scale[i]));
+      o[e] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    uint4* row = reinterpret_cast<uint4*>(dst + 2 * (h0 + i) * s.h);
+    row[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    row[1] = make_uint4(o[4], o[5], o[6], o[7]);
+  }
+}
+
+static int launch_cache(bool write, CacheParams& prm, const sva_kv_cache_t* c, cudaStream_t st) {
+  prm.k = CacheArrays{(uint8_t*)c->k_codes, c->k_scale, (uint8_t*)c->k_sf};
+  prm.v = CacheArrays{(uint8_t*)c->v_codes, c->v_scale, (uint8_t*)c->v_sf};
+  prm.H = c->H; prm.page = c->page; prm.pages = c->pages;
+  prm.head_groups = (c->H + CACHE_HEADS - 1) / CACHE_HEADS;
+  const int lanes = c->d / 16;
+  const long long ctas = (prm.tokens + CACHE_THREADS / lanes - 1) / (CACHE_THREADS / lanes) * prm.head_groups * 2;
+  if (ctas > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  const bool fp4 = c->format == SVA_CACHE_FP4;
+  auto kern = write ? (lanes == 8 ? (fp4 ? cache_write_kernel<8, true> : cache_write_kernel<8, false>)
+                                  : (fp4 ? cache_write_kernel<4, true> : cache_write_kernel<4, false>))
+                    : (lanes == 8 ? (fp4 ? cache_read_kernel<8, true> : cache_read_kernel<8, false>)
+                                  : (fp4 ? cache_read_kernel<4, true> : cache_read_kernel<4, false>));
+  return launch_dep(kern, dim3((unsigned)ctas), CACHE_THREADS, 0, st, prm);
+}
+
+int launch_cache_write(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t ks[3], const int64_t vs[3], int B, int T,
+                       const int32_t* slots, int32_t* status, cudaStream_t st) {
+  CacheParams prm = {};
+  prm.xk = (uint8_t*)k; prm.xv = (uint8_t*)v;
+  prm.sk = make_strides(ks); prm.sv = make_strides(vs);
+  prm.slots = slots;
+  prm.tokens = (long long)B * T; prm.T = T;
+  prm.slot_count = (long long)c->pages * c->page;
+  prm.status = status;
+  return launch_cache(true, prm, c, st);
+}
+
+int launch_cache_read(const sva_kv_cache_t* c, const int32_t* table, int64_t table_stride, int max_pages, const int32_t* lengths, int B, int N,
+                      void* k, void* v, const int64_t ks[3], const int64_t vs[3], int32_t* status, cudaStream_t st) {
+  CacheParams prm = {};
+  prm.xk = (uint8_t*)k; prm.xv = (uint8_t*)v;
+  prm.sk = make_strides(ks); prm.sv = make_strides(vs);
+  prm.table = table; prm.table_stride = table_stride; prm.max_pages = max_pages; prm.lengths = lengths;
+  prm.tokens = (long long)B * N; prm.T = N;
+  prm.status = status;
+  return launch_cache(false, prm, c, st);
+}
+
+}  // namespace sva
