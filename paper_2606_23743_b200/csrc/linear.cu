@@ -120,18 +120,21 @@ struct LinearParams {
   const float *xs, *ws, *bias;
   const __nv_bfloat16* residual;
   __nv_bfloat16* out;
-  long long xs_stride, ws_stride, out_stride, res_stride;
-  int M, N, K, Kb, act, debug;
+  long long xs_stride, ws_stride, out_stride;
+  int M, N, Kb, debug;
   int32_t* status;
 };
 
-__device__ __forceinline__ float lin_act(float y, int act) {
-  if (act == SVA_ACT_GELU) {                              // 0.5 y (1 + tanh u) = y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3)
-    const float u = 0.7978845608028654f * (y + 0.044715f * y * y * y);
-    return __fdividef(y, 1.f + __expf(fminf(-2.f * u, 80.f)));
-  }
-  if (act == SVA_ACT_SILU) return __fdividef(y, 1.f + __expf(fminf(-y, 80.f)));
-  return y;
+// GELU (tanh form) 0.5 y (1 + tanh u) = y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3); SiLU y / (1 + exp(-y)).  The exponent is
+// formed in base 2 and kept below 2^126, where its reciprocal is still a normal number.
+template <int ACT>
+__device__ __forceinline__ float lin_act(float y) {
+  if (ACT == SVA_ACT_NONE) return y;
+  constexpr float LOG2E = 1.4426950408889634f, C = -2.f * 0.7978845608028654f * LOG2E;
+  const float z = ACT == SVA_ACT_GELU ? y * fmaf(C * 0.044715f, y * y, C) : -LOG2E * y;
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(fminf(z, 126.f))));
+  return y * r;
 }
 
 __device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -159,203 +162,270 @@ __device__ __forceinline__ void lin_tile(int i, int mt, int nt, int& m, int& n) 
   n = r / rows;
 }
 
-// One persistent CTA per SM, output tiles of 128 tokens x BN weights rows.  x and w tiles of 128 inputs come through a ring by TMA; the tensor cores
-// multiply a group of 128 inputs into one of 512/BN accumulators in tensor memory; eight warps take each group's product out, times its
-// two scales, and add it up in registers, fp32 throughout.
-// Warps 0-7: a thread owns one token and BN/2 columns.  Warp 8 loads, warp 9 issues the MMAs.
+// Persistent CTAs, one per SM.  x and w tiles of 128 inputs come through a ring by TMA; the tensor cores multiply a group of 128 inputs
+// into one of the accumulators in tensor memory; eight warps take each group's product out, times its two scales, and add it up in
+// registers, fp32 throughout.
+//   PAIR   two CTAs make a tile of 256 tokens x 256 weights rows: each stages its 128 tokens and half of the weights rows, the first issues
+//          the MMAs of both (cta_group::2): 32 KB from the L2 per CTA and group where a CTA by itself would need 48 KB for its
+//          128 x 256; what bounds that is the way from the L2.
+//   else   a CTA makes 128 x 128: problems that are too small to fill the device with pairs.
+// Warps 0-7: a thread owns one token and half of the tile's columns.  Warp 8 loads, warp 9 issues the MMAs.
 namespace lin {
-constexpr int THREADS = 320;
-constexpr uint32_t A_BYTES = 128 * 128;
-template <int BN> struct Shape {
-  static constexpr uint32_t STAGE = A_BYTES + BN * 128;
-  static constexpr int STAGES = BN == 256 ? 4 : 6, BUFS = 512 / BN, COLS = BN / 2;
-  static constexpr uint32_t OUT = STAGES * STAGE, OUT_BYTES = 128 * 128;       // two staging tiles, 128 tokens x 64 columns
-  static constexpr int SMEM = 1024 + OUT + 2 * OUT_BYTES;
+constexpr int THREADS = 384;                              // (warps 10 and 11 only complete a warpgroup)
+constexpr int SUM_REGS = 232, HELPER_REGS = 40;
+static_assert(256 * SUM_REGS + 128 * HELPER_REGS <= THREADS * 168, "setmaxnreg draws on the registers of the launch");
+constexpr uint32_t A_BYTES = 128 * 128, STAGE = 2 * A_BYTES;
+constexpr uint32_t OUT_BYTES = 128 * 128;                 // staging tile, 128 tokens x 64 columns of bf16
+template <bool PAIR> struct Shape {                       // (227 KB: the staging tiles of all columns, the rest is ring)
+  static constexpr int OUTS = PAIR ? 4 : 2, STAGES = PAIR ? 5 : 6;
+  static constexpr uint32_t OUT = STAGES * STAGE;
+  static constexpr int SMEM = 1024 + OUT + OUTS * OUT_BYTES;
 };
 }
 
-template <int BN>
+template <bool PAIR, int ACT>
 __global__ void __launch_bounds__(lin::THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_o,
-              const LinearParams prm) {
-  using S = lin::Shape<BN>;
-  constexpr int STAGES = S::STAGES, BUFS = S::BUFS, COLS = S::COLS;
+              const __grid_constant__ CUtensorMap tm_r, const LinearParams prm) {
+  using namespace lin;
+  using S = Shape<PAIR>;
+  constexpr int STAGES = S::STAGES;
+  constexpr int BM = PAIR ? 256 : 128, BN = PAIR ? 256 : 128, BUFS = 512 / BN, COLS = BN / 2;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS];
+  __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS + 2];
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
   const uint32_t sbase = smem_u32(smem);
-  const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_free = bar_acc + 8 * BUFS;
+  const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_free = bar_acc + 8 * BUFS,
+                 bar_res = bar_free + 8 * BUFS;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int mt = (prm.M + 127) / 128, nt = (prm.N + BN - 1) / BN, tiles = mt * nt, Kb = prm.Kb;
+  const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, first = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
+  const int step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+  const int mt = (prm.M + BM - 1) / BM, nt = (prm.N + BN - 1) / BN, tiles = mt * nt, Kb = prm.Kb;
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
-    for (int i = 0; i < BUFS; ++i) { mbar_init(bar_acc + 8 * i, 1); mbar_init(bar_free + 8 * i, 8); }
+    for (int i = 0; i < BUFS; ++i) { mbar_init(bar_acc + 8 * i, 1); mbar_init(bar_free + 8 * i, PAIR ? 16 : 8); }
+    for (int i = 0; i < 2; ++i) mbar_init(bar_res + 8 * i, 1);
     abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     prefetch_tmap(&tm_x);
     prefetch_tmap(&tm_w);
     prefetch_tmap(&tm_o);
+    if (prm.residual) prefetch_tmap(&tm_r);
   }
   if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(512u) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(512u) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   tc_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync_all();                           // the other CTA's barriers are there
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
   const int zero = grid_dep_wait();
 
-  if (warp == 8) {
-    // ---- loads
-    bool ok = true;
-    int st = 0;
-    uint32_t ph = 0;
-    for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-      int m, n;
-      lin_tile(i, mt, nt, m, n);
-      for (int g = 0; g < Kb; ++g) {
-        ok = lin_wait(bar_empty + 8 * st, ph ^ 1u, abort_flag);
-        if (!ok) break;
-        if ((prm.debug & 1024) && g > 0) break;                                // test aid: the ring runs dry
-        if (lane == 0) {
-          const uint32_t dst = sbase + st * S::STAGE, bar = bar_full + 8 * st;
-          mbar_expect_tx(bar, S::STAGE);
-          tma_load_2d(dst, &tm_x, bar, g * 128, m * 128);
-          tma_load_2d(dst + lin::A_BYTES, &tm_w, bar, g * 128, n * BN);
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(HELPER_REGS));
+    if (warp == 8) {
+      // ---- loads; in a pair, the first CTA's barrier waits for the bytes of both
+      const uint32_t bar_lead = PAIR ? mapa(bar_full, 0) : bar_full;
+      bool ok = true;
+      int st = 0;
+      uint32_t ph = 0;
+      for (int i = first; i < tiles && ok; i += step) {
+        int m, n;
+        lin_tile(i, mt, nt, m, n);
+        const int m0 = m * BM + rank * 128, n0 = n * BN + rank * 128;
+        for (int g = 0; g < Kb; ++g) {
+          ok = lin_wait(bar_empty + 8 * st, ph ^ 1u, abort_flag);
+          if (!ok) break;
+          if ((prm.debug & 1024) && g > 0) break;                              // test aid: the ring runs dry
+          if (lane == 0) {
+            const uint32_t dst = sbase + st * STAGE;
+            if (PAIR) {
+              if (rank == 0) mbar_expect_tx(bar_full + 8 * st, 2 * STAGE);
+              tma_load_2d_pair(dst, &tm_x, bar_lead + 8 * st, g * 128, m0);
+              tma_load_2d_pair(dst + A_BYTES, &tm_w, bar_lead + 8 * st, g * 128, n0);
+            } else {
+              mbar_expect_tx(bar_full + 8 * st, STAGE);
+              tma_load_2d(dst, &tm_x, bar_full + 8 * st, g * 128, m0);
+              tma_load_2d(dst + A_BYTES, &tm_w, bar_full + 8 * st, g * 128, n0);
+            }
+          }
+          __syncwarp();
+          if (++st == STAGES) { st = 0; ph ^= 1u; }
         }
-        __syncwarp();
+      }
+      // in a pair, the MMAs' arrivals from the first CTA are all here before this one may go
+      for (int s = 0; PAIR && ok && s < STAGES; ++s) {
+        ok = lin_wait(bar_empty + 8 * st, ph ^ 1u, abort_flag);
         if (++st == STAGES) { st = 0; ph ^= 1u; }
       }
-    }
-  } else if (warp == 9) {
-    // ---- MMAs
-    constexpr uint32_t IDESC = instr_desc(128, BN, 0, false);
-    const uint32_t el = elect_one();
-    const uint64_t ad0 = smem_desc(sbase, 16, 1024), bd0 = smem_desc(sbase + lin::A_BYTES, 16, 1024);
-    bool ok = true;
-    int st = 0, buf = 0;
-    uint32_t ph = 0, bph = 0;
-    for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-      for (int g = 0; g < Kb; ++g) {
-        ok = lin_wait(bar_free + 8 * buf, bph ^ 1u, abort_flag) && lin_wait(bar_full + 8 * st, ph, abort_flag);
-        if (!ok) break;
-        tc_fence_after();
-        const uint64_t ad = ad0 + (uint64_t)(st * (S::STAGE >> 4)), bd = bd0 + (uint64_t)(st * (S::STAGE >> 4));
+    } else if (warp == 9 && rank == 0) {
+      // ---- MMAs
+      constexpr uint32_t IDESC = instr_desc(BM, BN, 0, false);
+      const uint32_t el = elect_one();
+      const uint64_t ad0 = smem_desc(sbase, 16, 1024), bd0 = smem_desc(sbase + A_BYTES, 16, 1024);
+      bool ok = true;
+      int st = 0, buf = 0;
+      uint32_t ph = 0, bph = 0;
+      for (int i = first; i < tiles && ok; i += step) {
+        for (int g = 0; g < Kb; ++g) {
+          ok = lin_wait(bar_free + 8 * buf, bph ^ 1u, abort_flag) && lin_wait(bar_full + 8 * st, ph, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t ad = ad0 + (uint64_t)(st * (STAGE >> 4)), bd = bd0 + (uint64_t)(st * (STAGE >> 4));
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) tc_mma_ss_f8(tmem + buf * BN, ad + 2 * kk, bd + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
-        tc_commit(bar_empty + 8 * st, el);
-        tc_commit(bar_acc + 8 * buf, el);
-        if (++st == STAGES) { st = 0; ph ^= 1u; }
-        if (++buf == BUFS) { buf = 0; bph ^= 1u; }
+          for (int kk = 0; kk < 4; ++kk) {
+            if (PAIR) tc_mma_ss_f8_pair(tmem + buf * BN, ad + 2 * kk, bd + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
+            else tc_mma_ss_f8(tmem + buf * BN, ad + 2 * kk, bd + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
+          }
+          if (PAIR) {
+            tc_commit_pair(bar_empty + 8 * st, el);
+            tc_commit_pair(bar_acc + 8 * buf, el);
+          } else {
+            tc_commit(bar_empty + 8 * st, el);
+            tc_commit(bar_acc + 8 * buf, el);
+          }
+          if (++st == STAGES) { st = 0; ph ^= 1u; }
+          if (++buf == BUFS) { buf = 0; bph ^= 1u; }
+        }
       }
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SUM_REGS));
     // ---- sums and epilogue
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * COLS;
     const bool leader = (threadIdx.x & 127) == 0;
-    uint8_t* stage = smem + S::OUT + wg * S::OUT_BYTES;
+    uint8_t* stage = smem + S::OUT + wg * (COLS / 64) * OUT_BYTES;
+    const uint32_t free_lead = PAIR ? mapa(bar_free, 0) : bar_free, res = bar_res + 8 * wg;
     bool ok = true;
     int buf = 0;
-    uint32_t bph = 0;
-    for (int i = blockIdx.x; i < tiles; i += gridDim.x) {
+    uint32_t bph = 0, rph = 0;
+    // scales of two groups at hand, those of the next two (of the next tile's first two, towards a tile's end) on their way
+    // (rows and columns that do not exist hold zeros: any scale will do)
+    const float *xs, *ws;
+    int m0, n0;
+    auto place = [&](int i) {
       int m, n;
       lin_tile(i, mt, nt, m, n);
-      const int tok = m * 128 + row, n0 = n * BN + wg * COLS;
-      // (rows and columns that do not exist hold zeros: any scale will do)
-      const float* xs = prm.xs + min(tok, prm.M - 1) + zero;
-      const float* ws = prm.ws + min(n0 / 128, (prm.N - 1) / 128) * prm.ws_stride + zero;
-      uint64_t acc[COLS / 2];
+      m0 = m * BM + rank * 128;
+      n0 = n * BN + wg * COLS;
+      xs = prm.xs + min(m0 + row, prm.M - 1) + zero;
+      ws = prm.ws + min(n0 / 128, (prm.N - 1) / 128) * prm.ws_stride + zero;
+    };
+    float x0, x1, w0, w1;
+    auto fetch = [&](int g) {
+      const int ga = min(g, Kb - 1), gb = min(g + 1, Kb - 1);
+      x0 = __ldg(xs + ga * prm.xs_stride); w0 = __ldg(ws + ga);
+      x1 = __ldg(xs + gb * prm.xs_stride); w1 = __ldg(ws + gb);
+    };
+    place(first);
+    fetch(0);
+    for (int i = first; i < tiles; i += step) {
+      const int m1 = m0, n1 = n0;                            // this tile's place (m0, n0 move on to the next before its epilogue)
+      if (leader) {
+        bulk_wait_read0();                                   // the staging tiles' last stores have been read
+        if (prm.residual) {                                  // what the result is added to comes to where it will be staged
+          mbar_expect_tx(res, COLS / 64 * OUT_BYTES);
 #pragma unroll
-      for (int c = 0; c < COLS / 2; ++c) acc[c] = 0ull;
-      float next[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) next[j] = j < Kb ? __ldg(xs + j * prm.xs_stride) * __ldg(ws + j) : 0.f;
-      for (int g0 = 0; g0 < Kb && ok; g0 += 4) {
-        float cur[4], nx[4], nw[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          cur[j] = next[j];
-          const int g = min(g0 + 4 + j, Kb - 1);
-          nx[j] = __ldg(xs + g * prm.xs_stride);
-          nw[j] = __ldg(ws + g);
+          for (int h = 0; h < COLS / 64; ++h) tma_load_2d(smem_u32(stage) + h * OUT_BYTES, &tm_r, res, n1 + h * 64, m1);
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (g0 + j >= Kb) break;
-          ok = lin_wait(bar_acc + 8 * buf, bph, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t s2 = pack2(cur[j], cur[j]);
-          uint32_t v[2][16];
-          tmem_ld16(taddr + buf * BN, v[0]);
-#pragma unroll
-          for (int c = 0; c < COLS / 16; ++c) {
-            tc_wait_ld16(v[c & 1]);
-            if (c + 1 < COLS / 16) tmem_ld16(taddr + buf * BN + (c + 1) * 16, v[(c + 1) & 1]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              acc[c * 8 + e] = fma2(pack2(__uint_as_float(v[c & 1][2 * e]), __uint_as_float(v[c & 1][2 * e + 1])), s2, acc[c * 8 + e]);
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar_free + 8 * buf);
-          if (++buf == BUFS) { buf = 0; bph ^= 1u; }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) next[j] = nx[j] * nw[j];
       }
-      ok = lin_group_all(ok, 1 + wg);                        // (the four warps go on together or not at all: there are barriers below)
-      if (!ok) break;
+      float acc[COLS];
 #pragma unroll
-      for (int half = 0; half < COLS / 64; ++half) {
-        if (leader) bulk_wait_read0();                       // the staging tile's last store has been read
-        lin_group_all(true, 1 + wg);
-        const int c0 = n0 + half * 64;
+      for (int c = 0; c < COLS; ++c) acc[c] = 0.f;
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll 1
+      for (int g = 0; g < Kb; ++g) {
+        if (!(g & 1)) {
+          s0 = x0 * w0;
+          s1 = x1 * w1;
+          fetch(g + 2);
+        }
+        const float s = g & 1 ? s1 : s0;
+        ok = lin_wait(bar_acc + 8 * buf, bph, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t v[2][32];
+        tmem_ld32(taddr + buf * BN, v[0]);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {                        // 8 columns at a time
-          const int c = c0 + q * 8;
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) unpack2(acc[half * 32 + q * 4 + e], y[2 * e], y[2 * e + 1]);
-          if (prm.bias) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] += c + e < prm.N ? __ldg(prm.bias + c + e) : 0.f;
-          }
-          if (prm.act) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = lin_act(y[e], prm.act);
-          }
-          if (prm.residual && tok < prm.M && c < prm.N) {
-            const __nv_bfloat16* r = prm.residual + (long long)tok * prm.res_stride + c;
-            if (c + 8 <= prm.N) {
-              const uint4 u = __ldg(reinterpret_cast<const uint4*>(r));
-              const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) { y[2 * e] += bf16lo(w[e]); y[2 * e + 1] += bf16hi(w[e]); }
-            } else {
-              for (int e = 0; e < 8; ++e)
-                if (c + e < prm.N) y[e] += __bfloat162float(r[e]);
+        for (int c = 0; c < COLS / 32; ++c) {
+          tc_wait_ld32(v[c & 1]);
+          if (c + 1 < COLS / 32) {
+            tmem_ld32(taddr + buf * BN + (c + 1) * 32, v[(c + 1) & 1]);
+          } else {                                           // all of it is in registers
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+              if (PAIR) mbar_arrive_cluster(free_lead + 8 * buf);
+              else mbar_arrive(bar_free + 8 * buf);
             }
           }
-          if (c < prm.N && c + 8 > prm.N && tok < prm.M) {   // columns behind the last whole 16 bytes, which the tile store would overrun
-            for (int e = 0; e < 7; ++e)
-              if (c + e < prm.N) prm.out[(long long)tok * prm.out_stride + c + e] = __float2bfloat16_rn(y[e]);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[c * 32 + e] = fmaf(__uint_as_float(v[c & 1][e]), s, acc[c * 32 + e]);
+        }
+        if (++buf == BUFS) { buf = 0; bph ^= 1u; }
+      }
+      if (i + step < tiles) {
+        place(i + step);
+        fetch(0);
+      }
+      if (prm.residual) {
+        ok = ok && lin_wait(res, rph, abort_flag);
+        rph ^= 1u;
+      }
+      ok = lin_group_all(ok, 1 + wg);                        // (the four warps go on together or not at all: there is a barrier below)
+      if (!ok) break;
+      const int tok = m1 + row;
+#pragma unroll
+      for (int q = 0; q < COLS / 8; ++q) {                   // 8 columns at a time
+        const int c = n1 + q * 8;
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = acc[q * 8 + e];
+        if (prm.bias) {
+          if (c + 8 <= prm.N) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] += __ldg(prm.bias + c + e);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (c + e < prm.N) y[e] += __ldg(prm.bias + c + e);
           }
-          *reinterpret_cast<uint4*>(stage + row * 128 + ((q ^ (row & 7)) << 4)) =
-              make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
         }
-        fence_async_smem();
-        lin_group_all(true, 1 + wg);
-        if (leader && c0 < (prm.N & ~7)) {
-          tma_store_2d(&tm_o, smem_u32(stage), c0, m * 128);
-          bulk_commit();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = lin_act<ACT>(y[e]);
+        uint4* to = reinterpret_cast<uint4*>(stage + (q >> 3) * OUT_BYTES + row * 128 + (((q & 7) ^ (row & 7)) << 4));
+        if (prm.residual) {
+          const uint4 u = *to;
+          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { y[2 * e] += bf16lo(w[e]); y[2 * e + 1] += bf16hi(w[e]); }
         }
+        if (c < prm.N && c + 8 > prm.N && tok < prm.M) {     // columns behind the last whole 16 bytes, which the tile store would overrun
+#pragma unroll
+          for (int e = 0; e < 7; ++e)
+            if (c + e < prm.N) prm.out[(long long)tok * prm.out_stride + c + e] = __float2bfloat16_rn(y[e]);
+        }
+        *to = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+      }
+      fence_async_smem();
+      lin_group_all(true, 1 + wg);
+      if (leader && m1 < prm.M) {
+#pragma unroll
+        for (int h = 0; h < COLS / 64; ++h)
+          if (n1 + h * 64 < (prm.N & ~7)) tma_store_2d(&tm_o, smem_u32(stage) + h * OUT_BYTES, n1 + h * 64, m1);
+        bulk_commit();
       }
     }
     if (leader) bulk_wait0();
@@ -364,10 +434,12 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   if (*abort_flag) lin_settle();
   tc_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync_all();                           // nothing arrives at a CTA that has gone
   if (threadIdx.x == 0 && *abort_flag && prm.status) atomicOr(prm.status, SVA_DEV_TIMEOUT);
   if (warp == 9) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
 }
 
@@ -434,21 +506,32 @@ int launch_quantize_tiles(const sva_linear_t* p, const void* w, void* w8, float*
                     (long long)p->w8_stride, w_scale, (long long)p->w_scale_stride);
 }
 
-template <int BN>
-static int launch_linear_bn(const sva_linear_t* p, const void* x8, const void* w8, void* out, const LinearParams& prm, int sms, cudaStream_t st) {
-  using S = lin::Shape<BN>;
+template <bool PAIR, int ACT>
+static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void* w8, void* out, const LinearParams& prm, int sms,
+                               cudaStream_t st) {
   static DeviceOnce once;
-  auto kern = linear_kernel<BN>;
-  int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) == cudaSuccess; });
+  auto kern = linear_kernel<PAIR, ACT>;
+  constexpr int SIDE = PAIR ? 256 : 128, CTAS = PAIR ? 2 : 1, SMEM = lin::Shape<PAIR>::SMEM;
+  int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) == cudaSuccess; });
   if (rc) return rc;
-  CUtensorMap tx, tw, to;
+  CUtensorMap tx, tw, to, tr;
   if ((rc = lin_map(&tx, x8, p->K, p->M, p->x8_stride, 1, 128))) return rc;
-  if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, BN))) return rc;
+  if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, 128))) return rc;
   // (a tile store writes whole 16-byte pieces, also beyond an inner extent that ends within one: it gets the whole pieces only)
   if ((rc = lin_map(&to, out, p->N < 8 ? 8 : p->N & ~7, p->M, 2 * p->out_stride, 2, 128))) return rc;
-  const long long tiles = (long long)((p->M + 127) / 128) * ((p->N + BN - 1) / BN);
+  tr = to;
+  if (prm.residual && (rc = lin_map(&tr, prm.residual, p->N, p->M, 2 * p->residual_stride, 2, 128))) return rc;
+  const long long tiles = (long long)((p->M + SIDE - 1) / SIDE) * ((p->N + SIDE - 1) / SIDE);
   if (tiles > 0x7fffffffLL - sms) return SVA_ERR_UNSUPPORTED;
-  return launch_dep(kern, dim3((unsigned)(tiles < sms ? tiles : sms)), lin::THREADS, S::SMEM, st, tx, tw, to, prm);
+  const long long most = sms / CTAS;
+  return launch_dep_cluster(CTAS, kern, dim3((unsigned)(CTAS * (tiles < most ? tiles : most))), lin::THREADS, SMEM, st, tx, tw, to, tr, prm);
+}
+
+template <bool PAIR>
+static int launch_linear_act(const sva_linear_t* p, const void* x8, const void* w8, void* out, const LinearParams& prm, int sms, cudaStream_t st) {
+  return p->act == SVA_ACT_GELU ? launch_linear_tiles<PAIR, SVA_ACT_GELU>(p, x8, w8, out, prm, sms, st)
+       : p->act == SVA_ACT_SILU ? launch_linear_tiles<PAIR, SVA_ACT_SILU>(p, x8, w8, out, prm, sms, st)
+                                : launch_linear_tiles<PAIR, SVA_ACT_NONE>(p, x8, w8, out, prm, sms, st);
 }
 
 int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* out,
@@ -458,12 +541,12 @@ int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, c
   LinearParams prm;
   prm.xs = x_scale; prm.ws = w_scale; prm.bias = bias;
   prm.residual = (const __nv_bfloat16*)residual; prm.out = (__nv_bfloat16*)out;
-  prm.xs_stride = p->x_scale_stride; prm.ws_stride = p->w_scale_stride; prm.out_stride = p->out_stride; prm.res_stride = p->residual_stride;
-  prm.M = p->M; prm.N = p->N; prm.K = p->K; prm.Kb = (p->K + 127) / 128; prm.act = p->act;
+  prm.xs_stride = p->x_scale_stride; prm.ws_stride = p->w_scale_stride; prm.out_stride = p->out_stride;
+  prm.M = p->M; prm.N = p->N; prm.Kb = (p->K + 127) / 128;
   prm.debug = g_debug_lin;
   prm.status = status;
-  const long long wide = (long long)((p->M + 127) / 128) * ((p->N + 255) / 256);
-  return wide >= sms ? launch_linear_bn<256>(p, x8, w8, out, prm, sms, st) : launch_linear_bn<128>(p, x8, w8, out, prm, sms, st);
+  const long long pairs = (long long)((p->M + 255) / 256) * ((p->N + 255) / 256);
+  return pairs >= sms / 2 ? launch_linear_act<true>(p, x8, w8, out, prm, sms, st) : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
 }
 
 }  // namespace sva

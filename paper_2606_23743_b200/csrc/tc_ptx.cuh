@@ -82,6 +82,35 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
 }
+// ---- pairs of CTAs (a cluster of two): the first issues the MMAs of both, each stages its own rows of A and half of B
+__device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {       // the same place in another CTA's shared memory
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t mapped) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// own shared memory, completion on a barrier of either CTA of the pair (mapa)
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t mapped_bar, int c0, int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(mapped_bar) : "memory");
+}
+// arrives on the barrier at this place in both CTAs
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar, uint32_t elected) {
+  asm volatile("{\n.reg .pred q;\n.reg .b16 m;\nsetp.ne.b32 q, %1, 0;\nmov.b16 m, 3;\n"
+               "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n}"
+               ::"r"(bar), "r"(elected) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ss_f8_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t elected) {
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
+               "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(elected) : "memory");
+}
 // shared -> global tile store (bulk group); the source must have been made visible to the async proxy
 __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
   asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
@@ -123,8 +152,8 @@ __device__ __forceinline__ void tc_wait_ld64(uint32_t* v) {
                : SVA_T8(v, 0), SVA_T8(v, 8), SVA_T8(v, 16), SVA_T8(v, 24), SVA_T8(v, 32), SVA_T8(v, 40), SVA_T8(v, 48), SVA_T8(v, 56)
                ::"memory");
 }
-__device__ __forceinline__ void tc_wait_ld16(uint32_t* v) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" : SVA_T8(v, 0), SVA_T8(v, 8)::"memory");
+__device__ __forceinline__ void tc_wait_ld32(uint32_t* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : SVA_T8(v, 0), SVA_T8(v, 8), SVA_T8(v, 16), SVA_T8(v, 24)::"memory");
 }
 #undef SVA_T8
 // The MMA warp runs its loop with all lanes (so addresses and descriptors stay warp-uniform)
