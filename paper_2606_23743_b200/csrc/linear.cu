@@ -4,6 +4,8 @@
 //     y[m,n] = sum_g sx[g,m] sw[n/128,g] sum_{k in group g} x8[m,k] w8[n,k],   out = bf16(act(y + bias[n]) + residual[m,n])
 //   quantize_rows_kernel, quantize_tiles_kernel   the codes (HBM-bound passes)
 //   linear_kernel                                 the product
+#include <type_traits>
+
 #include "tc_ptx.cuh"
 
 namespace sva {
@@ -141,13 +143,6 @@ __device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, volatile
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));      // (a warp gives up together)
 }
 
-// A barrier of the four warps of one epilogue group (id 1 or 2), and whether all of them may go on.
-__device__ __forceinline__ bool lin_group_all(bool ok, int id) {
-  uint32_t r;
-  asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbarrier.cta.red.and.pred q, %2, 128, p;\nselp.u32 %0, 1, 0, q;\n}"
-               : "=r"(r) : "r"((uint32_t)ok), "r"(id) : "memory");
-  return r != 0u;
-}
 // A wait has run out: copies and MMAs still in flight get time to land before shared memory and TMEM go away.
 static __device__ __noinline__ void lin_settle() {
   const long long t0 = clock64();
@@ -163,51 +158,59 @@ __device__ __forceinline__ void lin_tile(int i, int mt, int nt, int& m, int& n) 
 }
 
 // Persistent CTAs, one per SM.  x and w tiles of 128 inputs come through a ring by TMA; the tensor cores multiply a group of 128 inputs
-// into one of the accumulators in tensor memory; eight warps take each group's product out, times its two scales, and add it up in
+// into one of the accumulators in tensor memory; the sum warps take each group's product out, times its two scales, and add it up in
 // registers, fp32 throughout.
 //   PAIR   two CTAs make a tile of 256 tokens x 256 weights rows: each stages its 128 tokens and half of the weights rows, the first issues
-//          the MMAs of both (cta_group::2): 32 KB from the L2 per CTA and group where a CTA by itself would need 48 KB for its
-//          128 x 256; what bounds that is the way from the L2.
-//   else   a CTA makes 128 x 128: problems that are too small to fill the device with pairs.
-// Warps 0-7: a thread owns one token and half of the tile's columns.  Warp 8 loads, warp 9 issues the MMAs.
+//          the MMAs of both (cta_group::2): 32 KB from the L2 per CTA and group where a CTA by itself would need 48 KB for its 128 x 256
+//   else   a CTA makes 128 x 128: problems that are too small to fill the device with pairs
+// Warps: four per 64 columns sum, a thread owning one token's 64 (sixteen warps in a pair's CTA: with eight, 128 columns each,
+// a warp's way through a group -- wait, read, multiply-add -- took 870 cycles, the MMAs 512); then one that loads, one that issues the MMAs, one that
+// brings the scales, one that sees to the staging tiles.
 namespace lin {
-constexpr int THREADS = 384;                              // (warps 10 and 11 only complete a warpgroup)
-constexpr int SUM_REGS = 232, HELPER_REGS = 40;
-static_assert(256 * SUM_REGS + 128 * HELPER_REGS <= THREADS * 168, "setmaxnreg draws on the registers of the launch");
 constexpr uint32_t A_BYTES = 128 * 128, STAGE = 2 * A_BYTES;
 constexpr uint32_t OUT_BYTES = 128 * 128;                 // staging tile, 128 tokens x 64 columns of bf16
 template <bool PAIR> struct Shape {                       // (227 KB: the staging tiles of all columns, the rest is ring)
-  static constexpr int OUTS = PAIR ? 4 : 2, STAGES = PAIR ? 5 : 6;
+  static constexpr int SIDE = PAIR ? 256 : 128, BUFS = 512 / SIDE, COLS = SIDE / 2, SUM_WARPS = 8;      // columns of a sum warp,
+  static constexpr int UNITS = COLS / 64;                 // which it takes 64 at a time: a unit of the accumulator has barriers of its own
+  static constexpr int THREADS = 32 * (SUM_WARPS + 4), SLOTS = 2 * BUFS, SLOT = SIDE;      // scale slots, floats of one
+  static constexpr int STAGES = PAIR ? 4 : 5;
   static constexpr uint32_t OUT = STAGES * STAGE;
-  static constexpr int SMEM = 1024 + OUT + OUTS * OUT_BYTES;
+  static constexpr int SMEM = 1024 + OUT + SIDE / 64 * OUT_BYTES;
+  // registers of a thread that sums and of the others; the launch has 168 for each
+  static constexpr int SUM_REGS = 216, HELPER_REGS = 72;
+  static_assert(32 * SUM_WARPS * SUM_REGS + 128 * HELPER_REGS <= THREADS * 168, "setmaxnreg draws on the registers of the launch");
 };
 }
 
 template <bool PAIR, int ACT>
-__global__ void __launch_bounds__(lin::THREADS, 1)
+__global__ void __launch_bounds__(lin::Shape<PAIR>::THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_o,
               const __grid_constant__ CUtensorMap tm_r, const LinearParams prm) {
   using namespace lin;
   using S = Shape<PAIR>;
-  constexpr int STAGES = S::STAGES;
-  constexpr int BM = PAIR ? 256 : 128, BN = PAIR ? 256 : 128, BUFS = 512 / BN, COLS = BN / 2;
+  constexpr int STAGES = S::STAGES, SIDE = S::SIDE, BUFS = S::BUFS, SLOTS = S::SLOTS, SLOT = S::SLOT, COLS = S::COLS, UNITS = S::UNITS, LOADER = S::SUM_WARPS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS + 2];
+  __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS * UNITS + 4];
+  __shared__ __align__(16) float bias_s[2][COLS];
+  __shared__ float scale_s[SLOTS][SLOT];                   // x_scale * w_scale of a group: [weights block of 128][token]
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
   const uint32_t sbase = smem_u32(smem);
-  const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_free = bar_acc + 8 * BUFS,
-                 bar_res = bar_free + 8 * BUFS;
+  const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_free = bar_acc + 8 * BUFS * UNITS,
+                 bar_ready = bar_free + 8 * BUFS * UNITS, bar_staged = bar_ready + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, first = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
   const int step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
-  const int mt = (prm.M + BM - 1) / BM, nt = (prm.N + BN - 1) / BN, tiles = mt * nt, Kb = prm.Kb;
+  const int mt = (prm.M + SIDE - 1) / SIDE, nt = (prm.N + SIDE - 1) / SIDE, tiles = mt * nt, Kb = prm.Kb;
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
-    for (int i = 0; i < BUFS; ++i) { mbar_init(bar_acc + 8 * i, 1); mbar_init(bar_free + 8 * i, PAIR ? 16 : 8); }
-    for (int i = 0; i < 2; ++i) mbar_init(bar_res + 8 * i, 1);
+    for (int i = 0; i < BUFS * UNITS; ++i) {              // (the first unit of an accumulator waits for the scales too)
+      mbar_init(bar_acc + 8 * i, i % UNITS == 0 ? 2 : 1);
+      mbar_init(bar_free + 8 * i, PAIR ? 2 * S::SUM_WARPS : S::SUM_WARPS);
+    }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar_ready + 8 * i, 1); mbar_init(bar_staged + 8 * i, 4); }
     abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -216,7 +219,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     prefetch_tmap(&tm_o);
     if (prm.residual) prefetch_tmap(&tm_r);
   }
-  if (warp == 9) {
+  if (warp == LOADER + 1) {
     if (PAIR) {
       asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(512u) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -232,9 +235,9 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   const uint32_t tmem = tmem_base_s;
   const int zero = grid_dep_wait();
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(HELPER_REGS));
-    if (warp == 8) {
+  if (warp >= LOADER) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::HELPER_REGS));
+    if (warp == LOADER) {
       // ---- loads; in a pair, the first CTA's barrier waits for the bytes of both
       const uint32_t bar_lead = PAIR ? mapa(bar_full, 0) : bar_full;
       bool ok = true;
@@ -243,7 +246,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       for (int i = first; i < tiles && ok; i += step) {
         int m, n;
         lin_tile(i, mt, nt, m, n);
-        const int m0 = m * BM + rank * 128, n0 = n * BN + rank * 128;
+        const int m0 = m * SIDE + rank * 128, n0 = n * SIDE + rank * 128;
         for (int g = 0; g < Kb; ++g) {
           ok = lin_wait(bar_empty + 8 * st, ph ^ 1u, abort_flag);
           if (!ok) break;
@@ -269,166 +272,228 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         ok = lin_wait(bar_empty + 8 * st, ph ^ 1u, abort_flag);
         if (++st == STAGES) { st = 0; ph ^= 1u; }
       }
-    } else if (warp == 9 && rank == 0) {
+    } else if (warp == LOADER + 1 && rank == 0) {
       // ---- MMAs
-      constexpr uint32_t IDESC = instr_desc(BM, BN, 0, false);
+      // A unit is 128 columns of the accumulator: 128 weights rows, in a pair 64 of each CTA's 128 (so a sum warp's columns, 64 of each
+      // unit, are 128 that follow one another).
+      constexpr uint32_t IDESC = instr_desc(SIDE, 128, 0, false);
       const uint32_t el = elect_one();
       const uint64_t ad0 = smem_desc(sbase, 16, 1024), bd0 = smem_desc(sbase + A_BYTES, 16, 1024);
       bool ok = true;
       int st = 0, buf = 0;
       uint32_t ph = 0, bph = 0;
       for (int i = first; i < tiles && ok; i += step) {
-        for (int g = 0; g < Kb; ++g) {
-          ok = lin_wait(bar_free + 8 * buf, bph ^ 1u, abort_flag) && lin_wait(bar_full + 8 * st, ph, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
+        for (int g = 0; g < Kb && ok; ++g) {
+          ok = lin_wait(bar_full + 8 * st, ph, abort_flag);
           const uint64_t ad = ad0 + (uint64_t)(st * (STAGE >> 4)), bd = bd0 + (uint64_t)(st * (STAGE >> 4));
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            if (PAIR) tc_mma_ss_f8_pair(tmem + buf * BN, ad + 2 * kk, bd + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
-            else tc_mma_ss_f8(tmem + buf * BN, ad + 2 * kk, bd + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
+          for (int u = 0; u < UNITS; ++u) {
+            const int at = buf * UNITS + u;
+            ok = ok && lin_wait(bar_free + 8 * at, bph ^ 1u, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              const uint64_t bu = bd + u * (64 * 128 >> 4) + 2 * kk;
+              if (PAIR) tc_mma_ss_f8_pair(tmem + at * 128, ad + 2 * kk, bu, IDESC, kk > 0 ? 1u : 0u, el);
+              else tc_mma_ss_f8(tmem + at * 128, ad + 2 * kk, bu, IDESC, kk > 0 ? 1u : 0u, el);
+            }
+            if (PAIR) tc_commit_pair(bar_acc + 8 * at, el); else tc_commit(bar_acc + 8 * at, el);
           }
-          if (PAIR) {
-            tc_commit_pair(bar_empty + 8 * st, el);
-            tc_commit_pair(bar_acc + 8 * buf, el);
-          } else {
-            tc_commit(bar_empty + 8 * st, el);
-            tc_commit(bar_acc + 8 * buf, el);
-          }
+          if (!ok) break;
+          if (PAIR) tc_commit_pair(bar_empty + 8 * st, el); else tc_commit(bar_empty + 8 * st, el);
           if (++st == STAGES) { st = 0; ph ^= 1u; }
           if (++buf == BUFS) { buf = 0; bph ^= 1u; }
         }
       }
-    }
-  } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SUM_REGS));
-    // ---- sums and epilogue
-    const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * COLS;
-    const bool leader = (threadIdx.x & 127) == 0;
-    uint8_t* stage = smem + S::OUT + wg * (COLS / 64) * OUT_BYTES;
-    const uint32_t free_lead = PAIR ? mapa(bar_free, 0) : bar_free, res = bar_res + 8 * wg;
-    bool ok = true;
-    int buf = 0;
-    uint32_t bph = 0, rph = 0;
-    // scales of two groups at hand, those of the next two (of the next tile's first two, towards a tile's end) on their way
-    // (rows and columns that do not exist hold zeros: any scale will do)
-    const float *xs, *ws;
-    int m0, n0;
-    auto place = [&](int i) {
-      int m, n;
-      lin_tile(i, mt, nt, m, n);
-      m0 = m * BM + rank * 128;
-      n0 = n * BN + wg * COLS;
-      xs = prm.xs + min(m0 + row, prm.M - 1) + zero;
-      ws = prm.ws + min(n0 / 128, (prm.N - 1) / 128) * prm.ws_stride + zero;
-    };
-    float x0, x1, w0, w1;
-    auto fetch = [&](int g) {
-      const int ga = min(g, Kb - 1), gb = min(g + 1, Kb - 1);
-      x0 = __ldg(xs + ga * prm.xs_stride); w0 = __ldg(ws + ga);
-      x1 = __ldg(xs + gb * prm.xs_stride); w1 = __ldg(ws + gb);
-    };
-    place(first);
-    fetch(0);
-    for (int i = first; i < tiles; i += step) {
-      const int m1 = m0, n1 = n0;                            // this tile's place (m0, n0 move on to the next before its epilogue)
-      if (leader) {
-        bulk_wait_read0();                                   // the staging tiles' last stores have been read
-        if (prm.residual) {                                  // what the result is added to comes to where it will be staged
-          mbar_expect_tx(res, COLS / 64 * OUT_BYTES);
+    } else if (warp == LOADER + 2) {
+      // ---- scales: a lane has four tokens'; two groups' values are on their way while two are handed over
+      // A slot is free when the accumulator of BUFS groups ago is full: its MMAs began when the sum warps had given back the one of 2 BUFS
+      // groups ago, whose scales were in the slot.
+      constexpr int BLOCKS = SIDE / 128;
+      int i = first, g = 0, c = 0;                           // next group to fetch, groups handed over
+      const float *xs[4], *ws[BLOCKS];
+      auto place = [&]() {
+        int m, n;
+        lin_tile(i, mt, nt, m, n);
+        // (rows and columns that do not exist hold zeros: any scale will do)
 #pragma unroll
-          for (int h = 0; h < COLS / 64; ++h) tma_load_2d(smem_u32(stage) + h * OUT_BYTES, &tm_r, res, n1 + h * 64, m1);
+        for (int j = 0; j < 4; ++j) xs[j] = prm.xs + min(m * SIDE + rank * 128 + 32 * j + lane, prm.M - 1) + zero;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) ws[b] = prm.ws + min(n * BLOCKS + b, (prm.N - 1) / 128) * prm.ws_stride + zero;
+      };
+      if (i < tiles) place();
+      struct Two { float x[2][4], w[2][BLOCKS]; int n; };
+      auto fetch = [&](Two& t) {
+        t.n = 0;
+        if (i >= tiles) return;
+        t.n = min(2, Kb - g);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int at = min(g + q, Kb - 1);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t.x[q][j] = __ldg(xs[j] + at * prm.xs_stride);
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b) t.w[q][b] = __ldg(ws[b] + at);
         }
+        g += 2;
+        if (g >= Kb) {
+          g = 0;
+          i += step;
+          if (i < tiles) place();
+        }
+      };
+      auto hand_over = [&](const Two& t) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          if (q >= t.n) break;
+          if (c >= BUFS && !lin_wait(bar_acc + 8 * UNITS * (c % BUFS), (uint32_t)(c / BUFS - 1) & 1u, abort_flag)) return false;
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) scale_s[c % SLOTS][b * 128 + 32 * j + lane] = t.x[q][j] * t.w[q][b];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_acc + 8 * UNITS * (c % BUFS));
+          ++c;
+        }
+        return true;
+      };
+      Two a, b;
+      fetch(a);
+      while (a.n) {
+        fetch(b);
+        if (!hand_over(a) || !b.n) break;
+        fetch(a);
+        if (!hand_over(b)) break;
       }
-      float acc[COLS];
-#pragma unroll
-      for (int c = 0; c < COLS; ++c) acc[c] = 0.f;
-      float s0 = 0.f, s1 = 0.f;
-#pragma unroll 1
-      for (int g = 0; g < Kb; ++g) {
-        if (!(g & 1)) {
-          s0 = x0 * w0;
-          s1 = x1 * w1;
-          fetch(g + 2);
-        }
-        const float s = g & 1 ? s1 : s0;
-        ok = lin_wait(bar_acc + 8 * buf, bph, abort_flag);
-        if (!ok) break;
-        tc_fence_after();
-        uint32_t v[2][32];
-        tmem_ld32(taddr + buf * BN, v[0]);
-#pragma unroll
-        for (int c = 0; c < COLS / 32; ++c) {
-          tc_wait_ld32(v[c & 1]);
-          if (c + 1 < COLS / 32) {
-            tmem_ld32(taddr + buf * BN + (c + 1) * 32, v[(c + 1) & 1]);
-          } else {                                           // all of it is in registers
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-              if (PAIR) mbar_arrive_cluster(free_lead + 8 * buf);
-              else mbar_arrive(bar_free + 8 * buf);
+    } else if (warp == LOADER + 3) {
+      // ---- staging tiles: the bias of their columns, what the result is added to, the stores
+      bool ok = true;
+      uint32_t ph = 0;
+      for (int i = first; i < tiles && ok; i += step) {
+        int m, n;
+        lin_tile(i, mt, nt, m, n);
+        const int m0 = m * SIDE + rank * 128;
+        for (int h = 0; h < 2; ++h) {
+          const int n0 = n * SIDE + h * COLS;
+          for (int c = lane; c < COLS; c += 32) bias_s[h][c] = prm.bias && n0 + c < prm.N ? __ldg(prm.bias + n0 + c) : 0.f;
+          __syncwarp();
+          if (lane == 0) {
+            if (prm.residual) {                              // comes to where the result will be staged
+              mbar_expect_tx(bar_ready + 8 * h, COLS / 64 * OUT_BYTES);
+              for (int j = 0; j < COLS / 64; ++j)
+                tma_load_2d(sbase + S::OUT + (h * (COLS / 64) + j) * OUT_BYTES, &tm_r, bar_ready + 8 * h, n0 + j * 64, m0);
+            } else {
+              mbar_arrive(bar_ready + 8 * h);
             }
           }
-#pragma unroll
-          for (int e = 0; e < 32; ++e) acc[c * 32 + e] = fmaf(__uint_as_float(v[c & 1][e]), s, acc[c * 32 + e]);
         }
-        if (++buf == BUFS) { buf = 0; bph ^= 1u; }
-      }
-      if (i + step < tiles) {
-        place(i + step);
-        fetch(0);
-      }
-      if (prm.residual) {
-        ok = ok && lin_wait(res, rph, abort_flag);
-        rph ^= 1u;
-      }
-      ok = lin_group_all(ok, 1 + wg);                        // (the four warps go on together or not at all: there is a barrier below)
-      if (!ok) break;
-      const int tok = m1 + row;
-#pragma unroll
-      for (int q = 0; q < COLS / 8; ++q) {                   // 8 columns at a time
-        const int c = n1 + q * 8;
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = acc[q * 8 + e];
-        if (prm.bias) {
-          if (c + 8 <= prm.N) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] += __ldg(prm.bias + c + e);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (c + e < prm.N) y[e] += __ldg(prm.bias + c + e);
+        for (int h = 0; h < 2 && ok; ++h) {
+          const int n0 = n * SIDE + h * COLS;
+          ok = lin_wait(bar_staged + 8 * h, ph, abort_flag);
+          if (ok && lane == 0 && m0 < prm.M) {
+            for (int j = 0; j < COLS / 64; ++j)
+              if (n0 + j * 64 < (prm.N & ~7)) tma_store_2d(&tm_o, sbase + S::OUT + (h * (COLS / 64) + j) * OUT_BYTES, n0 + j * 64, m0);
+            bulk_commit();
           }
         }
+        ph ^= 1u;
+        if (lane == 0) bulk_wait_read0();                    // the staging tiles have been read
+        __syncwarp();
+      }
+      if (lane == 0) bulk_wait0();
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SUM_REGS));
+    // ---- sums and epilogue
+    const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * 64;
+    const float* scale = &scale_s[0][wg * (SLOT - 128) + row];
+    uint8_t* stage = smem + S::OUT + wg * (COLS / 64) * OUT_BYTES;
+    const uint32_t free_lead = PAIR ? mapa(bar_free, 0) : bar_free;
+    bool ok = true;
+    int buf = 0, slot = 0;
+    uint32_t bph = 0, rph = 0;
+    // A unit's 64 columns come out at once, are given back, and are added up; whether the next unit is there is asked before the sums and used
+    // after them.  What this is about: the tensor cores are done with a group in some 560 cycles, their end is seen 360 later, and the next
+    // MMAs on a unit begin 150 after it was given back, so with two accumulators a unit must not be held for long (128 columns, 32
+    // at a time between the sums: 600 cycles), and each wait whose answer is used at once costs a sum warp 100 to 250.  8 192 x 4 096 x 4 096,
+    // cycles per group: sums between the reads of 128 columns 873, units 838, the early question 780.
+    const uint32_t first_lane = lane == 0;
+    uint32_t there = 0u;
+    for (int i = first; i < tiles; i += step) {
+      uint64_t acc[COLS / 2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = lin_act<ACT>(y[e]);
-        uint4* to = reinterpret_cast<uint4*>(stage + (q >> 3) * OUT_BYTES + row * 128 + (((q & 7) ^ (row & 7)) << 4));
-        if (prm.residual) {
-          const uint4 u = *to;
-          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      for (int c = 0; c < COLS / 2; ++c) acc[c] = 0ull;
+#pragma unroll 1
+      for (int g = 0; g < Kb; ++g) {
+        float s = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { y[2 * e] += bf16lo(w[e]); y[2 * e + 1] += bf16hi(w[e]); }
+        for (int u = 0; u < UNITS; ++u) {
+          const int at = buf * UNITS + u;
+          if (!__all_sync(0xffffffffu, there)) ok = lin_wait(bar_acc + 8 * at, bph, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          uint32_t v[64];
+          tmem_ld32(taddr + at * 128, v);
+          tmem_ld32(taddr + at * 128 + 32, v + 32);
+          if (u == 0) s = scale[slot * SLOT];
+          tc_wait_ld64(v);
+          tc_fence_before();
+          if (PAIR) mbar_arrive_cluster_if(free_lead + 8 * at, first_lane);
+          else mbar_arrive_if(bar_free + 8 * at, first_lane);
+          const bool wraps = u + 1 == UNITS && buf + 1 == BUFS;
+          there = mbar_test(bar_acc + (wraps ? 0 : 8 * (at + 1)), wraps ? bph ^ 1u : bph);
+          const uint64_t s2 = pack2(s, s);
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            acc[u * 32 + e] = fma2(pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), s2, acc[u * 32 + e]);
         }
-        if (c < prm.N && c + 8 > prm.N && tok < prm.M) {     // columns behind the last whole 16 bytes, which the tile store would overrun
+        if (!ok) break;
+        if (++buf == BUFS) { buf = 0; bph ^= 1u; }
+        if (++slot == SLOTS) slot = 0;
+      }
+      int m, n;
+      lin_tile(i, mt, nt, m, n);
+      const int m1 = m * SIDE + rank * 128, n1 = n * SIDE + wg * COLS;
+      ok = ok && lin_wait(bar_ready + 8 * wg, rph, abort_flag);
+      if (!ok) break;
+      rph ^= 1u;
+      // (two straight pieces of code without a branch: 16 times 8 columns with the optional parts in their midst ran at the pace of
+      // instruction fetches, 4 000 cycles per tile)
+      auto finish = [&](auto res_tag) {
+        constexpr bool RES = decltype(res_tag)::value;
 #pragma unroll
-          for (int e = 0; e < 7; ++e)
-            if (c + e < prm.N) prm.out[(long long)tok * prm.out_stride + c + e] = __float2bfloat16_rn(y[e]);
+        for (int q = 0; q < COLS / 8; ++q) {                 // 8 columns at a time
+          const float4 b0 = *reinterpret_cast<const float4*>(&bias_s[wg][q * 8]), b1 = *reinterpret_cast<const float4*>(&bias_s[wg][q * 8 + 4]);
+          const float b[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
+          uint4* to = reinterpret_cast<uint4*>(stage + (q >> 3) * OUT_BYTES + row * 128 + (((q & 7) ^ (row & 7)) << 4));
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) unpack2(acc[q * 4 + e], y[2 * e], y[2 * e + 1]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = lin_act<ACT>(y[e] + b[e]);
+          if (RES) {
+            const uint4 u = *to;
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { y[2 * e] += bf16lo(w[e]); y[2 * e + 1] += bf16hi(w[e]); }
+          }
+          *to = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
         }
-        *to = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+      };
+      if (prm.residual) finish(std::true_type{}); else finish(std::false_type{});
+      // columns behind the last whole 16 bytes, which the tile store would overrun: a thread its row's
+      const int last = (prm.N & ~7) - n1;
+      if ((prm.N & 7) && last >= 0 && last < COLS && m1 + row < prm.M) {
+        const __nv_bfloat16* from =
+            reinterpret_cast<const __nv_bfloat16*>(stage + (last >> 6) * OUT_BYTES + row * 128 + ((((last >> 3) & 7) ^ (row & 7)) << 4));
+        for (int e = 0; e < (prm.N & 7); ++e) prm.out[(long long)(m1 + row) * prm.out_stride + n1 + last + e] = from[e];
       }
       fence_async_smem();
-      lin_group_all(true, 1 + wg);
-      if (leader && m1 < prm.M) {
-#pragma unroll
-        for (int h = 0; h < COLS / 64; ++h)
-          if (n1 + h * 64 < (prm.N & ~7)) tma_store_2d(&tm_o, smem_u32(stage) + h * OUT_BYTES, n1 + h * 64, m1);
-        bulk_commit();
-      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_staged + 8 * wg);
     }
-    if (leader) bulk_wait0();
   }
   __syncthreads();
   if (*abort_flag) lin_settle();
@@ -436,7 +501,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   __syncthreads();
   if (PAIR) cluster_sync_all();                           // nothing arrives at a CTA that has gone
   if (threadIdx.x == 0 && *abort_flag && prm.status) atomicOr(prm.status, SVA_DEV_TIMEOUT);
-  if (warp == 9) {
+  if (warp == LOADER + 1) {
     tc_fence_after();
     if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
@@ -511,7 +576,8 @@ static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void
                                cudaStream_t st) {
   static DeviceOnce once;
   auto kern = linear_kernel<PAIR, ACT>;
-  constexpr int SIDE = PAIR ? 256 : 128, CTAS = PAIR ? 2 : 1, SMEM = lin::Shape<PAIR>::SMEM;
+  using S = lin::Shape<PAIR>;
+  constexpr int SIDE = S::SIDE, CTAS = PAIR ? 2 : 1, SMEM = S::SMEM;
   int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) == cudaSuccess; });
   if (rc) return rc;
   CUtensorMap tx, tw, to, tr;
@@ -524,7 +590,7 @@ static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void
   const long long tiles = (long long)((p->M + SIDE - 1) / SIDE) * ((p->N + SIDE - 1) / SIDE);
   if (tiles > 0x7fffffffLL - sms) return SVA_ERR_UNSUPPORTED;
   const long long most = sms / CTAS;
-  return launch_dep_cluster(CTAS, kern, dim3((unsigned)(CTAS * (tiles < most ? tiles : most))), lin::THREADS, SMEM, st, tx, tw, to, tr, prm);
+  return launch_dep_cluster(CTAS, kern, dim3((unsigned)(CTAS * (tiles < most ? tiles : most))), S::THREADS, SMEM, st, tx, tw, to, tr, prm);
 }
 
 template <bool PAIR>
