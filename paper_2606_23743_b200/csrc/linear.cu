@@ -122,7 +122,7 @@ struct LinearParams {
   const float *xs, *ws, *bias;
   const __nv_bfloat16* residual;
   __nv_bfloat16* out;
-  long long xs_stride, ws_stride, out_stride;
+  long long xs_stride, ws_stride, out_stride, res_stride;
   int M, N, Kb, debug;
   int32_t* status;
 };
@@ -508,6 +508,171 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   }
 }
 
+// ------------------------------------------------------------------ few tokens
+// Up to 64 tokens (conditioning vectors, a decoded token, a short prompt): the weights are the work, read once.  The weights rows are the
+// M of the MMA and the tokens its N, so that a CTA takes 128 rows and no MMA row is empty; a cluster of CTAs splits the inputs of its 128 rows
+// between them, so that small layers fill the device too, and joins the sums through distributed shared memory in the order of its CTAs
+// (no workspace, no atomics: results repeat).  Several CTAs share an SM: what has to be in flight for the HBM is spread over all of them.
+// Warps 0-3: a thread sums one weights row for T tokens.  Warp 4 loads, warp 5 issues the MMAs.
+namespace few {
+constexpr int THREADS = 192, STAGES = 4, BUFS = 4;
+template <int T> struct Shape {
+  static constexpr uint32_t STAGE = 128 * 128 + T * 128, COLUMNS = BUFS * T;      // (T columns per accumulator: 64 .. 256 in all)
+  static constexpr int SMEM = 1024 + STAGES * STAGE, PER_SM = T == 16 ? 3 : 2;
+  static_assert(T * 128 * 4 <= STAGES * STAGE, "the ring takes the sums that are exchanged");
+};
+}
+
+template <int T>
+__global__ void __launch_bounds__(few::THREADS, few::Shape<T>::PER_SM)
+linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const LinearParams prm, int split, int act) {
+  using namespace few;
+  using S = Shape<T>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS];
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int abort_s;
+  volatile int* abort_flag = &abort_s;
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_free = bar_acc + 8 * BUFS;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x % split, J = blockIdx.x / split, t0 = blockIdx.y * T;
+  const int per = (prm.Kb + split - 1) / split, ga = min(rank * per, prm.Kb), gb = min(ga + per, prm.Kb);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+    for (int i = 0; i < BUFS; ++i) { mbar_init(bar_acc + 8 * i, 1); mbar_init(bar_free + 8 * i, 4); }
+    abort_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    prefetch_tmap(&tm_x);
+    // the weights can be on their way to the L2 while the kernel before this one (the quantiser of the tokens) still runs
+    for (int g = ga; g < min(gb, ga + STAGES); ++g) tma_prefetch_2d(&tm_w, g * 128, J * 128);
+  }
+  if (warp == 5) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(S::COLUMNS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s;
+  const int zero = grid_dep_wait();
+  float acc[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) acc[t] = 0.f;
+  bool ok = true;
+  if (warp == 4) {
+    for (int g = ga; g < gb; ++g) {
+      const int st = (g - ga) % STAGES;
+      ok = lin_wait(bar_empty + 8 * st, (uint32_t)((g - ga) / STAGES + 1) & 1u, abort_flag);
+      if (!ok) break;
+      if ((prm.debug & 1024) && g > ga) break;                                 // test aid: the ring runs dry
+      if (lane == 0) {
+        mbar_expect_tx(bar_full + 8 * st, S::STAGE);
+        tma_load_2d(sbase + st * S::STAGE, &tm_w, bar_full + 8 * st, g * 128, J * 128);
+        tma_load_2d(sbase + st * S::STAGE + 128 * 128, &tm_x, bar_full + 8 * st, g * 128, t0);
+      }
+      __syncwarp();
+    }
+  } else if (warp == 5) {
+    constexpr uint32_t IDESC = instr_desc(128, T, 0, false);
+    const uint32_t el = elect_one();
+    const uint64_t ad0 = smem_desc(sbase, 16, 1024), bd0 = smem_desc(sbase + 128 * 128, 16, 1024);
+    for (int g = ga; g < gb; ++g) {
+      const int i = g - ga, st = i % STAGES, buf = i % BUFS;
+      ok = lin_wait(bar_free + 8 * buf, (uint32_t)(i / BUFS + 1) & 1u, abort_flag) &&
+           lin_wait(bar_full + 8 * st, (uint32_t)(i / STAGES) & 1u, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      const uint64_t ad = ad0 + (uint64_t)(st * (S::STAGE >> 4)), bd = bd0 + (uint64_t)(st * (S::STAGE >> 4));
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) tc_mma_ss_f8(tmem + buf * T, ad + 2 * kk, bd + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
+      tc_commit(bar_empty + 8 * st, el);
+      tc_commit(bar_acc + 8 * buf, el);
+    }
+  } else {
+    const uint32_t taddr = tmem + ((uint32_t)(warp * 32) << 16);
+    // a lane has a token's scale (tokens that do not exist hold zeros: any scale will do), times the weights'
+    constexpr int PER = T > 32 ? 2 : 1;
+    const float* xs[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) xs[j] = prm.xs + min(t0 + (lane + 32 * j) % T, prm.M - 1) + zero;
+    const float* ws = prm.ws + J * prm.ws_stride + zero;
+    float nx[PER], nw = 0.f;
+    auto fetch = [&](int g) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) nx[j] = __ldg(xs[j] + g * prm.xs_stride);
+      nw = __ldg(ws + g);
+    };
+    if (ga < gb) fetch(ga);
+    for (int g = ga; g < gb; ++g) {
+      const int i = g - ga, buf = i % BUFS;
+      float s[PER];
+#pragma unroll
+      for (int j = 0; j < PER; ++j) s[j] = nx[j] * nw;
+      if (g + 1 < gb) fetch(g + 1);
+      ok = lin_wait(bar_acc + 8 * buf, (uint32_t)(i / BUFS) & 1u, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < T / 16; ++c) {
+        uint32_t v[16];
+        tmem_ld16(taddr + buf * T + c * 16, v);
+        tc_wait_ld16(v);
+        if (c + 1 == T / 16) {
+          tc_fence_before();
+          mbar_arrive_if(bar_free + 8 * buf, lane == 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          acc[c * 16 + e] = fmaf(__uint_as_float(v[e]), __shfl_sync(0xffffffffu, s[c * 16 / 32], (c * 16 + e) & 31), acc[c * 16 + e]);
+      }
+    }
+  }
+  // ---- join: each CTA of the cluster finishes T / split tokens
+  const int n = J * 128 + (int)threadIdx.x;
+  auto finish = [&](float y, int t) {
+    if (t >= prm.M || n >= prm.N) return;
+    if (prm.bias) y += __ldg(prm.bias + n);
+    y = act == SVA_ACT_GELU ? lin_act<SVA_ACT_GELU>(y) : act == SVA_ACT_SILU ? lin_act<SVA_ACT_SILU>(y) : y;
+    if (prm.residual) y += __bfloat162float(prm.residual[(long long)t * prm.res_stride + n]);
+    prm.out[(long long)t * prm.out_stride + n] = __float2bfloat16_rn(y);
+  };
+  if (split == 1) {
+    if (warp < 4 && ok) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) finish(acc[t], t0 + t);
+    }
+  } else {
+    float* mine = reinterpret_cast<float*>(smem);                              // (the MMAs that read the ring are done: their sums are here)
+    if (warp < 4 && ok) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) mine[t * 128 + threadIdx.x] = acc[t];
+    }
+    __syncwarp();
+    cluster_sync_all();
+    if (warp < 4 && ok) {
+      for (int t = rank * (T / split); t < (rank + 1) * (T / split); ++t) {
+        if (t0 + t >= prm.M) break;
+        float y = 0.f;
+        for (int q = 0; q < split; ++q) y += ld_cluster_f32(mapa(sbase + (uint32_t)(t * 128 + threadIdx.x) * 4u, q));
+        finish(y, t0 + t);
+      }
+    }
+    __syncwarp();
+    cluster_sync_all();                                                         // nobody's sums go before they were read
+  }
+  if (*abort_flag) lin_settle();
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag && prm.status) atomicOr(prm.status, SVA_DEV_TIMEOUT);
+  if (warp == 5) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::COLUMNS) : "memory");
+  }
+}
+
 // ------------------------------------------------------------------ host side
 typedef CUresult (*lin_encode_fn_t)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                     const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -600,6 +765,24 @@ static int launch_linear_act(const sva_linear_t* p, const void* x8, const void* 
                                 : launch_linear_tiles<PAIR, SVA_ACT_NONE>(p, x8, w8, out, prm, sms, st);
 }
 
+template <int T>
+static int launch_linear_few(const sva_linear_t* p, const void* x8, const void* w8, const LinearParams& prm, int sms, cudaStream_t st) {
+  using S = few::Shape<T>;
+  static DeviceOnce once;
+  auto kern = linear_few_kernel<T>;
+  int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) == cudaSuccess; });
+  if (rc) return rc;
+  CUtensorMap tx, tw;
+  if ((rc = lin_map(&tx, x8, p->K, p->M, p->x8_stride, 1, T))) return rc;
+  if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, 128))) return rc;
+  const long long rows = (p->N + 127) / 128, tokens = (p->M + T - 1) / T;
+  // The inputs are split while all CTAs still run at once: the HBM then has the most in flight, and all end together.
+  int split = 1;
+  while (split < 8 && 2 * split <= prm.Kb && rows * tokens * split * 2 <= (long long)sms * S::PER_SM) split *= 2;
+  if (rows * split > 0x7fffffffLL || tokens > 65535) return SVA_ERR_UNSUPPORTED;
+  return launch_dep_cluster(split, kern, dim3((unsigned)(rows * split), (unsigned)tokens), few::THREADS, S::SMEM, st, tx, tw, prm, split, p->act);
+}
+
 int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* out,
                   const float* bias, const void* residual, int32_t* status, cudaStream_t st) {
   int sms = 0, rc = lin_sms(&sms);
@@ -607,10 +790,13 @@ int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, c
   LinearParams prm;
   prm.xs = x_scale; prm.ws = w_scale; prm.bias = bias;
   prm.residual = (const __nv_bfloat16*)residual; prm.out = (__nv_bfloat16*)out;
-  prm.xs_stride = p->x_scale_stride; prm.ws_stride = p->w_scale_stride; prm.out_stride = p->out_stride;
+  prm.xs_stride = p->x_scale_stride; prm.ws_stride = p->w_scale_stride; prm.out_stride = p->out_stride; prm.res_stride = p->residual_stride;
   prm.M = p->M; prm.N = p->N; prm.Kb = (p->K + 127) / 128;
   prm.debug = g_debug_lin;
   prm.status = status;
+  if (p->M <= 16) return launch_linear_few<16>(p, x8, w8, prm, sms, st);
+  if (p->M <= 32) return launch_linear_few<32>(p, x8, w8, prm, sms, st);
+  if (p->M <= 64) return launch_linear_few<64>(p, x8, w8, prm, sms, st);
   const long long pairs = (long long)((p->M + 255) / 256) * ((p->N + 255) / 256);
   return pairs >= sms / 2 ? launch_linear_act<true>(p, x8, w8, out, prm, sms, st) : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
 }

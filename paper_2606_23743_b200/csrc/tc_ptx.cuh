@@ -104,6 +104,11 @@ __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {       /
 __device__ __forceinline__ void mbar_arrive_cluster_if(uint32_t mapped, uint32_t elected) {
   asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q mbarrier.arrive.shared::cluster.b64 _, [%0];\n}" ::"r"(mapped), "r"(elected) : "memory");
 }
+__device__ __forceinline__ float ld_cluster_f32(uint32_t mapped) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(mapped) : "memory");
+  return v;
+}
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -147,6 +152,9 @@ __device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int c0, 
   asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %2, %3, %4}];"
                ::"l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
+__device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* map, int c0, int c1) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(c0), "r"(c1) : "memory");
+}
 __device__ __forceinline__ void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait0() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -165,8 +173,8 @@ __device__ __forceinline__ void tc_wait_ld64(uint32_t* v) {
                : SVA_T8(v, 0), SVA_T8(v, 8), SVA_T8(v, 16), SVA_T8(v, 24), SVA_T8(v, 32), SVA_T8(v, 40), SVA_T8(v, 48), SVA_T8(v, 56)
                ::"memory");
 }
-__device__ __forceinline__ void tc_wait_ld32(uint32_t* v) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" : SVA_T8(v, 0), SVA_T8(v, 8), SVA_T8(v, 16), SVA_T8(v, 24)::"memory");
+__device__ __forceinline__ void tc_wait_ld16(uint32_t* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : SVA_T8(v, 0), SVA_T8(v, 8)::"memory");
 }
 #undef SVA_T8
 // The MMA warp runs its loop with all lanes (so addresses and descriptors stay warp-uniform)
