@@ -179,9 +179,13 @@ def _stream():
     return _raw_stream(torch.cuda.current_device())
 
 
+_Strides = C.c_int64 * 3
+
+
 def _strides(t):
-    assert t.dim() == 4 and t.stride(3) == 1, "tensors are [B,H,N,d] with d contiguous"
-    return (C.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
+    s = t.stride()
+    assert len(s) == 4 and s[3] == 1, "tensors are [B,H,N,d] with d contiguous"
+    return _Strides(s[0], s[1], s[2])
 
 
 def make_problem(q, k, v, o, N: int, block: int, scale: float = 0.0, fp8: bool = False) -> Problem:
@@ -458,7 +462,7 @@ def quantize_tiles_fp8(p: Linear, w, w8, w_scale) -> None:
 
 def linear_fp8(p: Linear, x8, x_scale, w8, w_scale, out, bias=None, residual=None, status=None) -> None:
     """out = bf16(act(x w^T + bias) + residual) from codes and scales."""
-    assert bias is None or bias.dtype == torch.float32 and bias.numel() == p.N and bias.is_contiguous(), "bias is [N] fp32"
+    assert bias is None or bias.dtype is torch.float32 and bias.numel() == p.N and bias.stride(-1) == 1, "bias is [N] fp32"
     rc = lib().sva_linear_fp8(C.byref(p), _ptr(x8), _ptr(x_scale), _ptr(w8), _ptr(w_scale), _ptr(out), _ptr(bias), _ptr(residual),
                               _ptr(status), _stream())
     if rc != SVA_OK:
@@ -525,9 +529,9 @@ def make_kv_cache(k, v, format: str = "e4m3") -> KvCache:
 
 def kv_cache_write(c: KvCache, k, v, slots, status=None) -> None:
     """k, v [B,H,T,d] bf16 into the slots [B,T] int32 (negative: left out)."""
-    Bq, H, T, d = k.shape
-    assert H == c.H and d == c.d and v.shape == k.shape and k.dtype == v.dtype == torch.bfloat16
-    assert slots.shape == (Bq, T) and slots.dtype == torch.int32 and slots.is_contiguous(), "slots are [B,T] int32"
+    shape = Bq, H, T, d = k.shape
+    assert H == c.H and d == c.d and v.shape == shape and k.dtype is torch.bfloat16 and v.dtype is torch.bfloat16, "k, v are [B,H,T,d] bf16"
+    assert slots.shape == (Bq, T) and slots.dtype is torch.int32 and slots.is_contiguous(), "slots are [B,T] int32"
     rc = lib().sva_kv_cache_write(C.byref(c), _ptr(k), _ptr(v), _strides(k), _strides(v), Bq, T, _ptr(slots), _ptr(status), _stream())
     if rc != SVA_OK:
         raise SvaError(rc, "sva_kv_cache_write")

@@ -27,7 +27,7 @@ struct CacheParams {
   const int32_t *slots, *table, *lengths;
   long long table_stride, tokens;                         // tokens: B * T, or B * N
   long long slot_count;
-  int H, T, page, pages, max_pages, head_groups;
+  int H, T, page, pages, max_pages, chunk, chunks;        // chunk: heads per CTA, chunks: CTAs per token tile and tensor
   int32_t* status;
 };
 
@@ -51,8 +51,8 @@ template <int LANES, bool FP4>
 __global__ void __launch_bounds__(CACHE_THREADS)
 cache_write_kernel(const CacheParams prm) {
   const int zero = grid_dep_wait();
-  const int which = blockIdx.x & 1, group = (int)((blockIdx.x >> 1) % prm.head_groups);
-  const long long t = (long long)((blockIdx.x >> 1) / prm.head_groups) * (CACHE_THREADS / LANES) + threadIdx.x / LANES + zero;
+  const int which = blockIdx.x & 1, part = (int)((blockIdx.x >> 1) % prm.chunks);
+  const long long t = (long long)((blockIdx.x >> 1) / prm.chunks) * (CACHE_THREADS / LANES) + threadIdx.x / LANES + zero;
   const int lane = threadIdx.x % LANES;
   const CacheArrays out = which ? prm.v : prm.k;
   const Strides s = which ? prm.sv : prm.sk;
@@ -60,68 +60,84 @@ cache_write_kernel(const CacheParams prm) {
   long long slot = -1;
   if (t < prm.tokens) slot = __ldg(prm.slots + t);
   if (slot >= prm.slot_count) {
-    if (lane == 0 && group == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
+    if (lane == 0 && part == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
     slot = -1;
   }
   const bool there = slot >= 0;
   const long long b = there ? t / prm.T : 0, n = there ? t - b * prm.T : 0;
   const long long page = there ? slot / prm.page : 0;
   const int place = there ? (int)(slot - page * prm.page) : 0;
-  const int h0 = group * CACHE_HEADS;
+  const int hb = part * prm.chunk, he = min(hb + prm.chunk, prm.H);
   const uint8_t* src = (which ? prm.xv : prm.xk) + 2 * (b * s.b + n * s.n + lane * 16);
-  uint4 in[CACHE_HEADS][2];
+  for (int h0 = hb; h0 < he; h0 += CACHE_HEADS) {
+    uint4 in[CACHE_HEADS][2];
 #pragma unroll
-  for (int i = 0; i < CACHE_HEADS; ++i) {
-    in[i][0] = in[i][1] = make_uint4(0u, 0u, 0u, 0u);
-    if (there && h0 + i < prm.H) {
-      const uint4* row = reinterpret_cast<const uint4*>(src + 2 * (h0 + i) * s.h);
-      in[i][0] = __ldg(row);
-      in[i][1] = __ldg(row + 1);
+    for (int i = 0; i < CACHE_HEADS; ++i) {
+      in[i][0] = in[i][1] = make_uint4(0u, 0u, 0u, 0u);
+      if (there && h0 + i < he) {
+        const uint4* row = reinterpret_cast<const uint4*>(src + 2 * (h0 + i) * s.h);
+        in[i][0] = __ldg(row);
+        in[i][1] = __ldg(row + 1);
+      }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < CACHE_HEADS; ++i) {
-    const float own = cache_amax(in[i][0], in[i][1]);
-    float amax = own;
+    for (int i = 0; i < CACHE_HEADS; ++i) {
+      const float own = cache_amax(in[i][0], in[i][1]);
+      float amax = own;
 #pragma unroll
-    for (int o = LANES / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    if (!there || h0 + i >= prm.H) continue;
-    const long long row = cache_row(prm, page, h0 + i, place);
-    const uint32_t w[8] = {in[i][0].x, in[i][0].y, in[i][0].z, in[i][0].w, in[i][1].x, in[i][1].y, in[i][1].z, in[i][1].w};
-    const float scale = amax == 0.f ? 1.0f : __fdiv_rn(amax, FP4 ? 2688.0f : 448.0f);
-    if (lane == 0) out.scale[row] = scale;
-    if (!FP4) {
-      uint32_t c[4];
-      if (div_fast_ok(scale)) {
-        const float rcp = __frcp_rn(scale);
+      for (int o = LANES / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+      if (!there || h0 + i >= he) continue;
+      const long long row = cache_row(prm, page, h0 + i, place);
+      const uint32_t w[8] = {in[i][0].x, in[i][0].y, in[i][0].z, in[i][0].w, in[i][1].x, in[i][1].y, in[i][1].z, in[i][1].w};
+      const float scale = amax == 0.f ? 1.0f : __fdiv_rn(amax, FP4 ? 2688.0f : 448.0f);
+      if (lane == 0) out.scale[row] = scale;
+      if (!FP4) {
+        uint32_t c[4];
+        if (div_fast_ok(scale)) {
+          const float rcp = __frcp_rn(scale);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          c[e] = __byte_perm(e4m3x2(div_fast(bf16lo(w[2 * e]), scale, rcp), div_fast(bf16hi(w[2 * e]), scale, rcp)),
-                             e4m3x2(div_fast(bf16lo(w[2 * e + 1]), scale, rcp), div_fast(bf16hi(w[2 * e + 1]), scale, rcp)), 0x5410);
-      } else {
+          for (int e = 0; e < 4; ++e)
+            c[e] = __byte_perm(e4m3x2(div_fast(bf16lo(w[2 * e]), scale, rcp), div_fast(bf16hi(w[2 * e]), scale, rcp)),
+                               e4m3x2(div_fast(bf16lo(w[2 * e + 1]), scale, rcp), div_fast(bf16hi(w[2 * e + 1]), scale, rcp)), 0x5410);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          c[e] = __byte_perm(e4m3x2(cache_div_slow(bf16lo(w[2 * e]), scale), cache_div_slow(bf16hi(w[2 * e]), scale)),
-                             e4m3x2(cache_div_slow(bf16lo(w[2 * e + 1]), scale), cache_div_slow(bf16hi(w[2 * e + 1]), scale)), 0x5410);
-      }
-      *reinterpret_cast<uint4*>(out.codes + (row * LANES + lane) * 16) = make_uint4(c[0], c[1], c[2], c[3]);
-    } else {
-      const uint32_t sf = (uint32_t)__nv_cvt_float_to_fp8(__fdiv_rn(__fdiv_rn(own, 6.0f), scale), __NV_SATFINITE, __NV_E4M3);
-      const float unit = __fmul_rn(e4m3_to_float(sf), scale);
-      uint32_t c[2] = {0u, 0u};
-      if (unit > 0.f) {
-        const bool fast = div_fast_ok(unit);
-        const float rcp = __frcp_rn(unit);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float lo = bf16lo(w[e]), hi = bf16hi(w[e]);
-          const float2 y = fast ? make_float2(div_fast(lo, unit, rcp), div_fast(hi, unit, rcp))
-                                : make_float2(cache_div_slow(lo, unit), cache_div_slow(hi, unit));
-          c[e >> 2] |= ((uint32_t)__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest) & 0xffu) << (8 * (e & 3));
+          for (int e = 0; e < 4; ++e)
+            c[e] = __byte_perm(e4m3x2(cache_div_slow(bf16lo(w[2 * e]), scale), cache_div_slow(bf16hi(w[2 * e]), scale)),
+                               e4m3x2(cache_div_slow(bf16lo(w[2 * e + 1]), scale), cache_div_slow(bf16hi(w[2 * e + 1]), scale)), 0x5410);
         }
+        *reinterpret_cast<uint4*>(out.codes + (row * LANES + lane) * 16) = make_uint4(c[0], c[1], c[2], c[3]);
+      } else {
+        // (own / 6) / scale, both quotients rounded: from reciprocals where that gives the rounded quotient (div_fast)
+        const bool quick = div_fast_ok(scale) && (own == 0.f || own >= 8.077935669463161e-28f);      // 2^-90
+        const float in6 = quick ? div_fast(own, 6.0f, 0.16666667163372039795f) : cache_div_slow(own, 6.0f);
+        const uint32_t sf = (uint32_t)__nv_cvt_float_to_fp8(quick ? div_fast(in6, scale, __frcp_rn(scale)) : cache_div_slow(in6, scale),
+                                                            __NV_SATFINITE, __NV_E4M3);
+        const float unit = __fmul_rn(e4m3_to_float(sf), scale);
+        uint32_t c[2] = {0u, 0u};
+        if (unit > 0.f) {
+          if (div_fast_ok(unit)) {                            // the same two values at a time
+            const float rcp = __frcp_rn(unit);
+            const uint64_t u2 = pack2(unit, unit), r2 = pack2(rcp, rcp), nr2 = pack2(-rcp, -rcp), nz = pack2(-0.f, -0.f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t neg = w[e] ^ 0x80008000u;
+              const uint64_t q0 = fma2(pack2(bf16lo(w[e]), bf16hi(w[e])), r2, nz);
+              const uint64_t res = fma2(q0, u2, pack2(bf16lo(neg), bf16hi(neg)));
+              float2 y;
+              unpack2(fma2(res, nr2, q0), y.x, y.y);
+              c[e >> 2] |= ((uint32_t)__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest) & 0xffu) << (8 * (e & 3));
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float2 y = make_float2(cache_div_slow(bf16lo(w[e]), unit), cache_div_slow(bf16hi(w[e]), unit));
+              c[e >> 2] |= ((uint32_t)__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest) & 0xffu) << (8 * (e & 3));
+            }
+          }
+        }
+        out.sf[row * LANES + lane] = unit > 0.f ? (uint8_t)sf : (uint8_t)0;
+        *reinterpret_cast<uint2*>(out.codes + (row * LANES + lane) * 8) = make_uint2(c[0], c[1]);
       }
-      out.sf[row * LANES + lane] = unit > 0.f ? (uint8_t)sf : (uint8_t)0;
-      *reinterpret_cast<uint2*>(out.codes + (row * LANES + lane) * 8) = make_uint2(c[0], c[1]);
     }
   }
 }
@@ -130,8 +146,8 @@ template <int LANES, bool FP4>
 __global__ void __launch_bounds__(CACHE_THREADS)
 cache_read_kernel(const CacheParams prm) {
   const int zero = grid_dep_wait();
-  const int which = blockIdx.x & 1, group = (int)((blockIdx.x >> 1) % prm.head_groups);
-  const long long t = (long long)((blockIdx.x >> 1) / prm.head_groups) * (CACHE_THREADS / LANES) + threadIdx.x / LANES + zero;
+  const int which = blockIdx.x & 1, part = (int)((blockIdx.x >> 1) % prm.chunks);
+  const long long t = (long long)((blockIdx.x >> 1) / prm.chunks) * (CACHE_THREADS / LANES) + threadIdx.x / LANES + zero;
   const int lane = threadIdx.x % LANES;
   if (t >= prm.tokens) return;
   const CacheArrays in = which ? prm.v : prm.k;
@@ -143,54 +159,56 @@ cache_read_kernel(const CacheParams prm) {
   if (there) {
     page = at < prm.max_pages ? __ldg(prm.table + b * prm.table_stride + at) : -1;
     if (page < 0 || page >= prm.pages) {
-      if (lane == 0 && group == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
+      if (lane == 0 && part == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
       there = false;
     }
   }
-  const int place = n - at * prm.page, h0 = group * CACHE_HEADS;
+  const int place = n - at * prm.page, hb = part * prm.chunk, he = min(hb + prm.chunk, prm.H);
   uint8_t* dst = (which ? prm.xv : prm.xk) + 2 * (b * s.b + (long long)n * s.n + lane * 16);
-  uint4 codes[CACHE_HEADS];
-  float scale[CACHE_HEADS];
-  uint32_t sf[CACHE_HEADS];
+  for (int h0 = hb; h0 < he; h0 += CACHE_HEADS) {
+    uint4 codes[CACHE_HEADS];
+    float scale[CACHE_HEADS];
+    uint32_t sf[CACHE_HEADS];
 #pragma unroll
-  for (int i = 0; i < CACHE_HEADS; ++i) {
-    codes[i] = make_uint4(0u, 0u, 0u, 0u);
-    scale[i] = 0.f;
-    sf[i] = 0u;
-    if (there && h0 + i < prm.H) {
-      const long long row = cache_row(prm, page, h0 + i, place);
-      scale[i] = __ldg(in.scale + row);
-      if (FP4) {
-        const uint2 c = __ldg(reinterpret_cast<const uint2*>(in.codes + (row * LANES + lane) * 8));
-        codes[i].x = c.x; codes[i].y = c.y;
-        sf[i] = __ldg(in.sf + row * LANES + lane);
-      } else {
-        codes[i] = __ldg(reinterpret_cast<const uint4*>(in.codes + (row * LANES + lane) * 16));
+    for (int i = 0; i < CACHE_HEADS; ++i) {
+      codes[i] = make_uint4(0u, 0u, 0u, 0u);
+      scale[i] = 0.f;
+      sf[i] = 0u;
+      if (there && h0 + i < he) {
+        const long long row = cache_row(prm, page, h0 + i, place);
+        scale[i] = __ldg(in.scale + row);
+        if (FP4) {
+          const uint2 c = __ldg(reinterpret_cast<const uint2*>(in.codes + (row * LANES + lane) * 8));
+          codes[i].x = c.x; codes[i].y = c.y;
+          sf[i] = __ldg(in.sf + row * LANES + lane);
+        } else {
+          codes[i] = __ldg(reinterpret_cast<const uint4*>(in.codes + (row * LANES + lane) * 16));
+        }
       }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < CACHE_HEADS; ++i) {
-    if (h0 + i >= prm.H) continue;
-    uint32_t o[8];
-    const uint32_t w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
-    const float unit = FP4 ? e4m3_to_float(sf[i]) : 1.f;
+    for (int i = 0; i < CACHE_HEADS; ++i) {
+      if (h0 + i >= he) continue;
+      uint32_t o[8];
+      const uint32_t w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+      const float unit = FP4 ? e4m3_to_float(sf[i]) : 1.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float2 x;
-      if (FP4) {
-        const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(w[e >> 2] >> (8 * (e & 3)) & 0xffu), __NV_E2M1);
-        x = __half22float2(__half2(h));
-        x.x *= unit; x.y *= unit;                           // exact: 2 by 4 significant bits
-      } else {
-        x = e4m3x2_to_float2(w[e >> 1] >> (16 * (e & 1)) & 0xffffu);
+      for (int e = 0; e < 8; ++e) {
+        float2 x;
+        if (FP4) {
+          const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(w[e >> 2] >> (8 * (e & 3)) & 0xffu), __NV_E2M1);
+          x = __half22float2(__half2(h));
+          x.x *= unit; x.y *= unit;                         // exact: 2 by 4 significant bits
+        } else {
+          x = e4m3x2_to_float2(w[e >> 1] >> (16 * (e & 1)) & 0xffffu);
+        }
+        const __nv_bfloat162 v = __floats2bfloat162_rn(__fmul_rn(x.x, scale[i]), __fmul_rn(x.y, scale[i]));
+        o[e] = *reinterpret_cast<const uint32_t*>(&v);
       }
-      const __nv_bfloat162 v = __floats2bfloat162_rn(__fmul_rn(x.x, scale[i]), __fmul_rn(x.y, scale[i]));
-      o[e] = *reinterpret_cast<const uint32_t*>(&v);
+      uint4* row = reinterpret_cast<uint4*>(dst + 2 * (h0 + i) * s.h);
+      row[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      row[1] = make_uint4(o[4], o[5], o[6], o[7]);
     }
-    uint4* row = reinterpret_cast<uint4*>(dst + 2 * (h0 + i) * s.h);
-    row[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    row[1] = make_uint4(o[4], o[5], o[6], o[7]);
   }
 }
 
@@ -198,9 +216,14 @@ static int launch_cache(bool write, CacheParams& prm, const sva_kv_cache_t* c, c
   prm.k = CacheArrays{(uint8_t*)c->k_codes, c->k_scale, (uint8_t*)c->k_sf};
   prm.v = CacheArrays{(uint8_t*)c->v_codes, c->v_scale, (uint8_t*)c->v_sf};
   prm.H = c->H; prm.page = c->page; prm.pages = c->pages;
-  prm.head_groups = (c->H + CACHE_HEADS - 1) / CACHE_HEADS;
   const int lanes = c->d / 16;
-  const long long ctas = (prm.tokens + CACHE_THREADS / lanes - 1) / (CACHE_THREADS / lanes) * prm.head_groups * 2;
+  const long long tiles = (prm.tokens + CACHE_THREADS / lanes - 1) / (CACHE_THREADS / lanes);
+  // Heads per CTA: eight, whose second half's loads find the slots and the table at hand, where the grid comes to sixteen CTAs per SM all the
+  // same.  2 x 47 616 tokens x 32 heads, e4m3, written / read, us: four heads 396 / 427, eight 361 / 391, sixteen 350 / 397.
+  prm.chunk = 2 * CACHE_HEADS;
+  if (2 * tiles * ((c->H + prm.chunk - 1) / prm.chunk) < 148 * 16) prm.chunk = CACHE_HEADS;
+  prm.chunks = (c->H + prm.chunk - 1) / prm.chunk;
+  const long long ctas = 2 * tiles * prm.chunks;
   if (ctas > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
   const bool fp4 = c->format == SVA_CACHE_FP4;
   auto kern = write ? (lanes == 8 ? (fp4 ? cache_write_kernel<8, true> : cache_write_kernel<8, false>)

@@ -64,94 +64,94 @@ __device__ __forceinline__ uint4 rope_store8(const float (&x)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// FORM 0: interleaved, a thread owns 8 channels (4 pairs).
-// FORM 1: half layout whose halves are whole 16-byte vectors: a thread owns vector u of both halves (8 pairs), or a vector behind them.
-// FORM 2: half layout otherwise: a thread owns 8 channels, whose partners lie at no fixed place of a vector: they come through shared memory,
-//         from the lanes of the same token (one warp), all of which have read a row before any of them writes it -- so in place is safe.
+// A thread owns 8 channels (a 16-byte vector), the lanes of a token lie in one warp.
+// FORM 0: interleaved, 4 pairs.
+// FORM 1: half layout whose halves are whole vectors: 8 pairs, whose other halves a lane of the same token holds: they come by shuffles.
+// FORM 2: half layout otherwise: the partners lie at no fixed place of a vector: they come through shared memory.
+// In forms 1 and 2 all lanes of a token have read a row before any of them writes it, so in place is safe.
 template <int FORM>
-__global__ void __launch_bounds__(ROPE_THREADS)
+__global__ void __launch_bounds__(ROPE_THREADS, FORM == 2 ? 3 : 4)
 rope_kernel(const RopeParams prm, int lanes) {
-  constexpr int V = FORM == 1 ? 2 : 1;                    // 16-byte vectors per thread and head
   __shared__ __align__(16) uint8_t stage[FORM == 2 ? ROPE_HEADS * ROPE_THREADS * 16 : 16];
   const int zero = grid_dep_wait();
   const int tile_chunk = blockIdx.x % prm.chunks;
   const long long tile = blockIdx.x / prm.chunks;
-  const int u = threadIdx.x % lanes;
+  const int u = threadIdx.x % lanes, c0 = u * 8;
   const long long t = tile * (ROPE_THREADS / lanes) + threadIdx.x / lanes + zero;
-  const int units = FORM == 1 ? prm.d / 8 - prm.half / 8 : prm.d / 8;
-  const bool mine = t < prm.tokens && u < units;
+  const bool mine = t < prm.tokens && c0 < prm.d;
   const long long b = mine ? t / prm.N : 0, n = mine ? t - b * prm.N : 0;
   const bool is_k = tile_chunk >= prm.q_chunks;
   const int h0 = (is_k ? tile_chunk - prm.q_chunks : tile_chunk) * prm.chunk, h1 = min(h0 + prm.chunk, is_k ? prm.Hk : prm.Hq);
   const Strides si = is_k ? prm.sk : prm.sq, so = is_k ? prm.sko : prm.sqo;
-  // channels of the first and the second vector
-  const bool paired = FORM == 1 && u * 8 < prm.half;
-  const int c0 = FORM == 1 ? (paired ? u * 8 : prm.half + u * 8) : u * 8;
-  const int c1 = FORM == 1 ? prm.half + u * 8 : 0;
-  const uint8_t* src = (is_k ? prm.k : prm.q) + 2 * (b * si.b + n * si.n);
-  uint8_t* dst = (is_k ? prm.ko : prm.qo) + 2 * (b * so.b + n * so.n);
+  const uint8_t* src = (is_k ? prm.k : prm.q) + 2 * (b * si.b + n * si.n + c0);
+  uint8_t* dst = (is_k ? prm.ko : prm.qo) + 2 * (b * so.b + n * so.n + c0);
 
-  uint4 in[ROPE_HEADS][V];
+  uint4 in[ROPE_HEADS];
   auto load = [&](int h) {
 #pragma unroll
     for (int i = 0; i < ROPE_HEADS; ++i) {
-      if (!mine || h + i >= h1) continue;
-      const uint8_t* row = src + 2 * (h + i) * si.h;
-      in[i][0] = *reinterpret_cast<const uint4*>(row + 2 * c0);
-      if (V == 2 && paired) in[i][V - 1] = *reinterpret_cast<const uint4*>(row + 2 * c1);
+      in[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (mine && h + i < h1) in[i] = *reinterpret_cast<const uint4*>(src + 2 * (h + i) * si.h);
     }
   };
   load(h0);
-  Turn turn[8];                                           // FORM 0: 4 pairs, 1: 8 pairs, 2: one per channel
+  Turn turn[FORM == 0 ? 4 : 8];                           // one per pair, or one per channel
   const int32_t* pos = prm.pos + b * prm.pos_batch + n;
 #pragma unroll
   for (int e = 0; e < (FORM == 0 ? 4 : 8); ++e) {
     const int c = c0 + e;
-    if (FORM == 0) turn[e] = mine ? rope_turn(prm, pos, c0 / 2 + e) : Turn{1.f, 0.f};
-    if (FORM == 1) turn[e] = mine && paired ? rope_turn(prm, pos, c) : Turn{1.f, 0.f};
-    if (FORM == 2) {
+    if (FORM == 0) {
+      turn[e] = mine ? rope_turn(prm, pos, c0 / 2 + e) : Turn{1.f, 0.f};
+    } else {
       turn[e] = mine && c < 2 * prm.half ? rope_turn(prm, pos, c < prm.half ? c : c - prm.half) : Turn{1.f, 0.f};
       if (c < prm.half) turn[e].s = -turn[e].s;           // first of a pair: a c - b s; second: b c + a s
     }
   }
+  const int words = prm.half - c0 / 2;                    // 4-byte words of the vector that are rotated, if fewer than 4
+  // the lane that has the other halves (form 1)
+  const int other = c0 < prm.half ? u + prm.half / 8 : c0 < 2 * prm.half ? u - prm.half / 8 : u;
+  const int from = (threadIdx.x & 31) - u + other;
   for (int h = h0; h < h1; h += ROPE_HEADS) {
     if (h > h0) load(h);
     if (FORM == 2) {
 #pragma unroll
-      for (int i = 0; i < ROPE_HEADS; ++i)
-        if (mine && h + i < h1) *reinterpret_cast<uint4*>(stage + (i * ROPE_THREADS + threadIdx.x) * 16) = in[i][0];
+      for (int i = 0; i < ROPE_HEADS; ++i) *reinterpret_cast<uint4*>(stage + (i * ROPE_THREADS + threadIdx.x) * 16) = in[i];
       __syncwarp();
     }
 #pragma unroll
     for (int i = 0; i < ROPE_HEADS; ++i) {
-      if (!mine || h + i >= h1) continue;
-      uint8_t* row = dst + 2 * (h + i) * so.h;
       float x[8];
-      rope_load8(in[i][0], x);
+      rope_load8(in[i], x);
       if (FORM == 0) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) rope_pair(x[2 * e], x[2 * e + 1], turn[e]);
       } else if (FORM == 1) {
-        if (paired) {
-          float y[8];
-          rope_load8(in[i][V - 1], y);
+        uint4 w;
+        w.x = __shfl_sync(0xffffffffu, in[i].x, from);
+        w.y = __shfl_sync(0xffffffffu, in[i].y, from);
+        w.z = __shfl_sync(0xffffffffu, in[i].z, from);
+        w.w = __shfl_sync(0xffffffffu, in[i].w, from);
+        float y[8];
+        rope_load8(w, y);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) rope_pair(x[e], y[e], turn[e]);
-          *reinterpret_cast<uint4*>(row + 2 * c1) = rope_store8(y);
-        }
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * turn[e].c + y[e] * turn[e].s;
       } else {
         // the token's row begins at its first lane's vector
         const __nv_bfloat16* held = reinterpret_cast<const __nv_bfloat16*>(stage + (i * ROPE_THREADS + threadIdx.x - u) * 16);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int c = c0 + e;
-          if (c < 2 * prm.half) {
-            const float other = __bfloat162float(held[c < prm.half ? c + prm.half : c - prm.half]);
-            x[e] = x[e] * turn[e].c + other * turn[e].s;
-          }
+          if (c < 2 * prm.half) x[e] = x[e] * turn[e].c + __bfloat162float(held[c < prm.half ? c + prm.half : c - prm.half]) * turn[e].s;
         }
       }
-      *reinterpret_cast<uint4*>(row + 2 * c0) = rope_store8(x);
+      uint4 o = rope_store8(x);
+      if (words < 4) {                                     // what is not rotated keeps its bits
+        if (words < 1) o.x = in[i].x;
+        if (words < 2) o.y = in[i].y;
+        if (words < 3) o.z = in[i].z;
+        o.w = in[i].w;
+      }
+      if (mine && h + i < h1) *reinterpret_cast<uint4*>(dst + 2 * (h + i) * so.h) = o;
     }
     if (FORM == 2) __syncwarp();
   }
@@ -174,14 +174,15 @@ int launch_rope(const sva_rope_t* p, const void* q, const void* k, const void* s
   prm.sin_factor = p->inverse ? -p->factor : p->factor;
 
   const int form = p->layout == SVA_ROPE_INTERLEAVED ? 0 : prm.half % 8 == 0 ? 1 : 2;
-  const int units = form == 1 ? prm.d / 8 - prm.half / 8 : prm.d / 8;
   int lanes = 1;
-  while (lanes < units) lanes *= 2;
+  while (lanes < prm.d / 8) lanes *= 2;
   const long long tiles = (prm.tokens + ROPE_THREADS / lanes - 1) / (ROPE_THREADS / lanes);
-  // Heads per CTA: all of them share the phases, but the grid should fill the device.
+  // Heads per CTA: they share the phases, but the grid should come to eight CTAs per SM; fewer than a thread has in flight gain nothing.
+  // 2 x 8 191 tokens, 32 + 8 heads: up to 32 heads 56.8 us, up to 16 53.4, but 8 192 tokens x 16 + 16 heads then 28.6 instead of 23.8;
+  // 1 024 tokens x 8 + 8: one head per CTA 10.7, four 4.6.
   prm.chunk = 8 * ROPE_HEADS;
   auto ctas = [&](int chunk) { return tiles * ((prm.Hq + chunk - 1) / chunk + (prm.Hk + chunk - 1) / chunk); };
-  while (prm.chunk > 1 && ctas(prm.chunk) < 148 * 6) prm.chunk /= 2;
+  while (prm.chunk > ROPE_HEADS && ctas(prm.chunk) < 148 * 8) prm.chunk /= 2;
   prm.q_chunks = (prm.Hq + prm.chunk - 1) / prm.chunk;
   prm.chunks = prm.q_chunks + (prm.Hk + prm.chunk - 1) / prm.chunk;
   if (tiles * prm.chunks > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;

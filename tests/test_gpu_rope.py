@@ -90,6 +90,21 @@ def test_rotation(case, inverse):
     assert torch.equal(q2, qo)
 
 
+@pytest.mark.parametrize("layout,R", [("half", 64), ("half", 20), ("interleaved", 64), ("interleaved", 74)])
+def test_what_is_not_rotated_keeps_its_bits(layout, R):
+    """Infinities, NaN and negative zeros behind the rotated channels, and an infinity among them that stays with its pair."""
+    q = torch.randn(1, 3, 10, 128, device="cuda").to(torch.bfloat16)
+    q[..., R::3], q[..., R + 1::3] = float("inf"), -0.0
+    q[0, 0, 0, 100], q[0, 1, 4, 0] = float("nan"), float("inf")
+    positions = torch.arange(1, 11, dtype=torch.int32, device="cuda")[None, None]
+    steps, _ = B.rope_steps(R, device="cuda")
+    out = torch.empty_like(q)
+    B.rope(B.make_rope(q, None, out, None, positions, R, layout), q, None, steps, positions, out, None)
+    assert torch.equal(out[..., R:].contiguous().view(torch.int16), q[..., R:].contiguous().view(torch.int16))
+    bad = ~torch.isfinite(out[..., :R])
+    assert int(bad.sum()) == 2 and bad[0, 1, 4, 0] and bad[0, 1, 4, R // 2 if layout == "half" else 1]
+
+
 def test_negative_positions():
     rng = np.random.default_rng(1)
     q = _tensor(rng, (1, 2, 9, 64), False)
