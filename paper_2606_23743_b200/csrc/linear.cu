@@ -517,8 +517,10 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 namespace few {
 constexpr int THREADS = 192, STAGES = 4, BUFS = 4;
 template <int T> struct Shape {
+  // CTAs per SM; groups whose scales are fetched together (four, for 16 tokens, would not leave room for a third CTA)
+  static constexpr int PER_SM = T == 16 ? 3 : 2, AHEAD = T == 16 ? 2 : 4;
   static constexpr uint32_t STAGE = 128 * 128 + T * 128, COLUMNS = BUFS * T;      // (T columns per accumulator: 64 .. 256 in all)
-  static constexpr int SMEM = 1024 + STAGES * STAGE, PER_SM = T == 16 ? 3 : 2;
+  static constexpr int SMEM = 1024 + STAGES * STAGE;
   static_assert(T * 128 * 4 <= STAGES * STAGE, "the ring takes the sums that are exchanged");
 };
 }
@@ -528,9 +530,11 @@ __global__ void __launch_bounds__(few::THREADS, few::Shape<T>::PER_SM)
 linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const LinearParams prm, int split, int act) {
   using namespace few;
   using S = Shape<T>;
+  constexpr int AHEAD = S::AHEAD;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS];
+  __shared__ __align__(16) float scale_s[2][4][AHEAD][T];  // a warp's own copy of some groups' scales, to be read four at a time
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
@@ -599,19 +603,32 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
 #pragma unroll
     for (int j = 0; j < PER; ++j) xs[j] = prm.xs + min(t0 + (lane + 32 * j) % T, prm.M - 1) + zero;
     const float* ws = prm.ws + J * prm.ws_stride + zero;
-    float nx[PER], nw = 0.f;
+    // The scales of AHEAD groups at a time, fetched while those before them are used (one group ahead, a fetch of 800 cycles was what a group took).
+    float nx[AHEAD][PER], nw[AHEAD];
     auto fetch = [&](int g) {
 #pragma unroll
-      for (int j = 0; j < PER; ++j) nx[j] = __ldg(xs[j] + g * prm.xs_stride);
-      nw = __ldg(ws + g);
+      for (int q = 0; q < AHEAD; ++q) {
+        const int at = min(g + q, gb - 1);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) nx[q][j] = __ldg(xs[j] + at * prm.xs_stride);
+        nw[q] = __ldg(ws + at);
+      }
     };
     if (ga < gb) fetch(ga);
+#pragma unroll 1
     for (int g = ga; g < gb; ++g) {
       const int i = g - ga, buf = i % BUFS;
-      float s[PER];
+      float (*block)[T] = scale_s[i / AHEAD & 1][warp];     // (the other one may still be read by a lane that is behind)
+      if (i % AHEAD == 0) {
 #pragma unroll
-      for (int j = 0; j < PER; ++j) s[j] = nx[j] * nw;
-      if (g + 1 < gb) fetch(g + 1);
+        for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+          for (int j = 0; j < PER; ++j)
+            if (lane < T) block[q][lane + 32 * j] = nx[q][j] * nw[q];
+        if (g + AHEAD < gb) fetch(g + AHEAD);
+        __syncwarp();
+      }
+      const float* s = block[i % AHEAD];
       ok = lin_wait(bar_acc + 8 * buf, (uint32_t)(i / BUFS) & 1u, abort_flag);
       if (!ok) break;
       tc_fence_after();
@@ -625,8 +642,13 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
           mbar_arrive_if(bar_free + 8 * buf, lane == 0);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          acc[c * 16 + e] = fmaf(__uint_as_float(v[e]), __shfl_sync(0xffffffffu, s[c * 16 / 32], (c * 16 + e) & 31), acc[c * 16 + e]);
+        for (int e = 0; e < 16; e += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(s + c * 16 + e);
+          acc[c * 16 + e] = fmaf(__uint_as_float(v[e]), f.x, acc[c * 16 + e]);
+          acc[c * 16 + e + 1] = fmaf(__uint_as_float(v[e + 1]), f.y, acc[c * 16 + e + 1]);
+          acc[c * 16 + e + 2] = fmaf(__uint_as_float(v[e + 2]), f.z, acc[c * 16 + e + 2]);
+          acc[c * 16 + e + 3] = fmaf(__uint_as_float(v[e + 3]), f.w, acc[c * 16 + e + 3]);
+        }
       }
     }
   }
