@@ -127,16 +127,30 @@ struct LinearParams {
   int32_t* status;
 };
 
-// GELU (tanh form) 0.5 y (1 + tanh u) = y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3); SiLU y / (1 + exp(-y)).  The exponent is
-// formed in base 2 and kept below 2^126, where its reciprocal is still a normal number.
+// GELU (tanh form) 0.5 y (1 + tanh u) = y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3); SiLU y / (1 + exp(-y)).
+// The denominator, with the exponent formed in base 2 and kept below 2^60: far outside of what a bf16 result can show, and the product of
+// two denominators has a reciprocal that is a normal number.
+template <int ACT>
+__device__ __forceinline__ float lin_denominator(float y) {
+  constexpr float LOG2E = 1.4426950408889634f, C = -2.f * 0.7978845608028654f * LOG2E;
+  return 1.f + ex2(fminf(ACT == SVA_ACT_GELU ? y * fmaf(C * 0.044715f, y * y, C) : -LOG2E * y, 60.f));
+}
+__device__ __forceinline__ float lin_rcp(float d) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+  return r;
+}
 template <int ACT>
 __device__ __forceinline__ float lin_act(float y) {
-  if (ACT == SVA_ACT_NONE) return y;
-  constexpr float LOG2E = 1.4426950408889634f, C = -2.f * 0.7978845608028654f * LOG2E;
-  const float z = ACT == SVA_ACT_GELU ? y * fmaf(C * 0.044715f, y * y, C) : -LOG2E * y;
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(fminf(z, 126.f))));
-  return y * r;
+  return ACT == SVA_ACT_NONE ? y : y * lin_rcp(lin_denominator<ACT>(y));
+}
+// two at a time, one reciprocal for both: exponentials and reciprocals leave the SM at 16 a cycle, 4 096 cycles for two of each of 256 x 128 values
+template <int ACT>
+__device__ __forceinline__ void lin_act2(float& a, float& b) {
+  if (ACT == SVA_ACT_NONE) return;
+  const float da = lin_denominator<ACT>(a), db = lin_denominator<ACT>(b), r = lin_rcp(da * db);
+  a *= r * db;
+  b *= r * da;
 }
 
 __device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -171,9 +185,9 @@ constexpr uint32_t A_BYTES = 128 * 128, STAGE = 2 * A_BYTES;
 constexpr uint32_t OUT_BYTES = 128 * 128;                 // staging tile, 128 tokens x 64 columns of bf16
 template <bool PAIR> struct Shape {                       // (227 KB: the staging tiles of all columns, the rest is ring)
   static constexpr int SIDE = PAIR ? 256 : 128, BUFS = 512 / SIDE, COLS = SIDE / 2, SUM_WARPS = 8;      // columns of a sum warp,
-  static constexpr int UNITS = COLS / 64;                 // which it takes 64 at a time: a unit of the accumulator has barriers of its own
+  static constexpr int UNITS = SIDE / 128;                // an accumulator is one or two units of 128 columns with barriers of their own
   static constexpr int THREADS = 32 * (SUM_WARPS + 4), SLOTS = 2 * BUFS, SLOT = SIDE;      // scale slots, floats of one
-  static constexpr int STAGES = PAIR ? 4 : 5;
+  static constexpr int STAGES = PAIR ? 4 : 5, AHEAD = PAIR ? 2 : 4;      // (a group of a single CTA takes a third of a pair's)
   static constexpr uint32_t OUT = STAGES * STAGE;
   static constexpr int SMEM = 1024 + OUT + SIDE / 64 * OUT_BYTES;
   // registers of a thread that sums and of the others; the launch has 168 for each
@@ -206,9 +220,9 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   const int mt = (prm.M + SIDE - 1) / SIDE, nt = (prm.N + SIDE - 1) / SIDE, tiles = mt * nt, Kb = prm.Kb;
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
-    for (int i = 0; i < BUFS * UNITS; ++i) {              // (the first unit of an accumulator waits for the scales too)
-      mbar_init(bar_acc + 8 * i, i % UNITS == 0 ? 2 : 1);
-      mbar_init(bar_free + 8 * i, PAIR ? 2 * S::SUM_WARPS : S::SUM_WARPS);
+    for (int i = 0; i < BUFS * UNITS; ++i) {              // full: by the MMAs and the scales; free: by eight warps, a pair's four in each CTA
+      mbar_init(bar_acc + 8 * i, 2);
+      mbar_init(bar_free + 8 * i, 8);
     }
     for (int i = 0; i < 2; ++i) { mbar_init(bar_ready + 8 * i, 1); mbar_init(bar_staged + 8 * i, 4); }
     abort_s = 0;
@@ -246,7 +260,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       for (int i = first; i < tiles && ok; i += step) {
         int m, n;
         lin_tile(i, mt, nt, m, n);
-        const int m0 = m * SIDE + rank * 128, n0 = n * SIDE + rank * 128;
+        const int m0 = m * SIDE + rank * 128, n0 = n * SIDE + rank * 64;
         for (int g = 0; g < Kb; ++g) {
           ok = lin_wait(bar_empty + 8 * st, ph ^ 1u, abort_flag);
           if (!ok) break;
@@ -256,7 +270,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             if (PAIR) {
               if (rank == 0) mbar_expect_tx(bar_full + 8 * st, 2 * STAGE);
               tma_load_2d_pair(dst, &tm_x, bar_lead + 8 * st, g * 128, m0);
-              tma_load_2d_pair(dst + A_BYTES, &tm_w, bar_lead + 8 * st, g * 128, n0);
+              tma_load_2d_pair(dst + A_BYTES, &tm_w, bar_lead + 8 * st, g * 128, n0);               // this CTA's half of unit 0,
+              tma_load_2d_pair(dst + A_BYTES + 64 * 128, &tm_w, bar_lead + 8 * st, g * 128, n0 + 128);       // of unit 1
             } else {
               mbar_expect_tx(bar_full + 8 * st, STAGE);
               tma_load_2d(dst, &tm_x, bar_full + 8 * st, g * 128, m0);
@@ -274,8 +289,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       }
     } else if (warp == LOADER + 1 && rank == 0) {
       // ---- MMAs
-      // A unit is 128 columns of the accumulator: 128 weights rows, in a pair 64 of each CTA's 128 (so a sum warp's columns, 64 of each
-      // unit, are 128 that follow one another).
+      // A unit is 128 columns of the accumulator: 128 weights rows, in a pair 64 staged by each CTA.
       constexpr uint32_t IDESC = instr_desc(SIDE, 128, 0, false);
       const uint32_t el = elect_one();
       const uint64_t ad0 = smem_desc(sbase, 16, 1024), bd0 = smem_desc(sbase + A_BYTES, 16, 1024);
@@ -307,10 +321,10 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         }
       }
     } else if (warp == LOADER + 2) {
-      // ---- scales: a lane has four tokens'; two groups' values are on their way while two are handed over
+      // ---- scales: a lane has four tokens'; AHEAD groups' values are on their way while as many are handed over
       // A slot is free when the accumulator of BUFS groups ago is full: its MMAs began when the sum warps had given back the one of 2 BUFS
       // groups ago, whose scales were in the slot.
-      constexpr int BLOCKS = SIDE / 128;
+      constexpr int BLOCKS = SIDE / 128, AHEAD = S::AHEAD;
       int i = first, g = 0, c = 0;                           // next group to fetch, groups handed over
       const float *xs[4], *ws[BLOCKS];
       auto place = [&]() {
@@ -323,42 +337,46 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         for (int b = 0; b < BLOCKS; ++b) ws[b] = prm.ws + min(n * BLOCKS + b, (prm.N - 1) / 128) * prm.ws_stride + zero;
       };
       if (i < tiles) place();
-      struct Two { float x[2][4], w[2][BLOCKS]; int n; };
-      auto fetch = [&](Two& t) {
+      struct Some { float x[AHEAD][4], w[AHEAD][BLOCKS]; int n; };
+      auto fetch = [&](Some& t) {
         t.n = 0;
         if (i >= tiles) return;
-        t.n = min(2, Kb - g);
+        t.n = min(AHEAD, Kb - g);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < AHEAD; ++q) {
           const int at = min(g + q, Kb - 1);
 #pragma unroll
           for (int j = 0; j < 4; ++j) t.x[q][j] = __ldg(xs[j] + at * prm.xs_stride);
 #pragma unroll
           for (int b = 0; b < BLOCKS; ++b) t.w[q][b] = __ldg(ws[b] + at);
         }
-        g += 2;
+        g += AHEAD;
         if (g >= Kb) {
           g = 0;
           i += step;
           if (i < tiles) place();
         }
       };
-      auto hand_over = [&](const Two& t) {
+      auto hand_over = [&](const Some& t) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < AHEAD; ++q) {
           if (q >= t.n) break;
-          if (c >= BUFS && !lin_wait(bar_acc + 8 * UNITS * (c % BUFS), (uint32_t)(c / BUFS - 1) & 1u, abort_flag)) return false;
+          if (c >= BUFS) {
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u)
+              if (!lin_wait(bar_acc + 8 * (UNITS * (c % BUFS) + u), (uint32_t)(c / BUFS - 1) & 1u, abort_flag)) return false;
+          }
 #pragma unroll
           for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int j = 0; j < 4; ++j) scale_s[c % SLOTS][b * 128 + 32 * j + lane] = t.x[q][j] * t.w[q][b];
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_acc + 8 * UNITS * (c % BUFS));
+          if (lane < UNITS) mbar_arrive(bar_acc + 8 * (UNITS * (c % BUFS) + lane));
           ++c;
         }
         return true;
       };
-      Two a, b;
+      Some a, b;
       fetch(a);
       while (a.n) {
         fetch(b);
@@ -407,18 +425,20 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SUM_REGS));
     // ---- sums and epilogue
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * 64;
+    // (a pair's CTA: each group of four warps has a unit of its own, the other's half a group's time later; else half of the unit)
+    const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * COLS;
     const float* scale = &scale_s[0][wg * (SLOT - 128) + row];
     uint8_t* stage = smem + S::OUT + wg * (COLS / 64) * OUT_BYTES;
     const uint32_t free_lead = PAIR ? mapa(bar_free, 0) : bar_free;
     bool ok = true;
     int buf = 0, slot = 0;
     uint32_t bph = 0, rph = 0;
-    // A unit's 64 columns come out at once, are given back, and are added up; whether the next unit is there is asked before the sums and used
-    // after them.  What this is about: the tensor cores are done with a group in some 560 cycles, their end is seen 360 later, and the next
-    // MMAs on a unit begin 150 after it was given back, so with two accumulators a unit must not be held for long (128 columns, 32
-    // at a time between the sums: 600 cycles), and each wait whose answer is used at once costs a sum warp 100 to 250.  8 192 x 4 096 x 4 096,
-    // cycles per group: sums between the reads of 128 columns 873, units 838, the early question 780.
+    // 64 columns come out at once and are added up; whether the next group's are there is asked before the last sums and used after them
+    // (a wait whose answer is used at once costs a sum warp 100 to 250 cycles even where there is nothing to wait for).
+    // 8 192 x 4 096 x 4 096, cycles per group of a pair: MMAs and loads alone 560 (MMAs of 256 columns) to 660 (of 128), with the accumulator
+    // read 650, with the sums 768.  What is left is not a wait: warps that multiply and add without having anything to do with
+    // the product slow the MMAs down as much (660 -> 890).  128 columns read between sums 32 at a time, no units: 870; sixteen sum
+    // warps of 64 columns: 1 000.
     const uint32_t first_lane = lane == 0;
     uint32_t there = 0u;
     for (int i = first; i < tiles; i += step) {
@@ -427,29 +447,31 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       for (int c = 0; c < COLS / 2; ++c) acc[c] = 0ull;
 #pragma unroll 1
       for (int g = 0; g < Kb; ++g) {
+        const int at = PAIR ? buf * UNITS + wg : buf;
+        if (!__all_sync(0xffffffffu, there)) ok = lin_wait(bar_acc + 8 * at, bph, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
         float s = 0.f;
+        uint64_t s2 = 0ull;
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          const int at = buf * UNITS + u;
-          if (!__all_sync(0xffffffffu, there)) ok = lin_wait(bar_acc + 8 * at, bph, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
+        for (int u = 0; u < COLS / 64; ++u) {
           uint32_t v[64];
-          tmem_ld32(taddr + at * 128, v);
-          tmem_ld32(taddr + at * 128 + 32, v + 32);
+          tmem_ld32(taddr + buf * SIDE + u * 64, v);
+          tmem_ld32(taddr + buf * SIDE + u * 64 + 32, v + 32);
           if (u == 0) s = scale[slot * SLOT];
           tc_wait_ld64(v);
-          tc_fence_before();
-          if (PAIR) mbar_arrive_cluster_if(free_lead + 8 * at, first_lane);
-          else mbar_arrive_if(bar_free + 8 * at, first_lane);
-          const bool wraps = u + 1 == UNITS && buf + 1 == BUFS;
-          there = mbar_test(bar_acc + (wraps ? 0 : 8 * (at + 1)), wraps ? bph ^ 1u : bph);
-          const uint64_t s2 = pack2(s, s);
+          if (u + 1 == COLS / 64) {
+            tc_fence_before();
+            if (PAIR) mbar_arrive_cluster_if(free_lead + 8 * at, first_lane);
+            else mbar_arrive_if(bar_free + 8 * at, first_lane);
+            const bool wraps = buf + 1 == BUFS;
+            there = mbar_test(bar_acc + 8 * (wraps ? at - buf * UNITS : at + UNITS), wraps ? bph ^ 1u : bph);
+          }
+          if (u == 0) s2 = pack2(s, s);
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             acc[u * 32 + e] = fma2(pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), s2, acc[u * 32 + e]);
         }
-        if (!ok) break;
         if (++buf == BUFS) { buf = 0; bph ^= 1u; }
         if (++slot == SLOTS) slot = 0;
       }
@@ -472,7 +494,9 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 #pragma unroll
           for (int e = 0; e < 4; ++e) unpack2(acc[q * 4 + e], y[2 * e], y[2 * e + 1]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = lin_act<ACT>(y[e] + b[e]);
+          for (int e = 0; e < 8; ++e) y[e] += b[e];
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) lin_act2<ACT>(y[e], y[e + 1]);
           if (RES) {
             const uint4 u = *to;
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -769,7 +793,7 @@ static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void
   if (rc) return rc;
   CUtensorMap tx, tw, to, tr;
   if ((rc = lin_map(&tx, x8, p->K, p->M, p->x8_stride, 1, 128))) return rc;
-  if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, 128))) return rc;
+  if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, PAIR ? 64 : 128))) return rc;
   // (a tile store writes whole 16-byte pieces, also beyond an inner extent that ends within one: it gets the whole pieces only)
   if ((rc = lin_map(&to, out, p->N < 8 ? 8 : p->N & ~7, p->M, 2 * p->out_stride, 2, 128))) return rc;
   tr = to;
