@@ -28,7 +28,8 @@ void sva_debug_set_prof_buffer(void* buf);
  *   bit 5: measurement aid: the one-call forms (but the 4-bit one) read a transposed copy of V that they make first, as the two-step form
  *          does, instead of V where it lies; they then need sva_attn_workspace_bytes() (the remainder: its own query, asked meanwhile);
  *   bit 6: test aid: the one-launch routing of small problems asks for clusters of 32 CTAs, which no device holds, so that the
- *          call goes the way it goes in a partition of the device that is too small for its clusters;
+ *          call goes the way it goes in a partition of the device that is too small for its clusters; the linear layer's kernels work
+ *          without theirs, likewise;
  *   bit 7: test aid: the remainder call masks the kept blocks of a block-mean tile by looking them up in the CSR
  *          (the form that serves more than 1024 key blocks) even where the kept-block bit masks would serve;
  *   bit 8: test aid: the kernel of the first-order term's block covariances withholds a part of its V tile, and

@@ -433,9 +433,9 @@ def make_linear(x=None, x8=None, x_scale=None, w8=None, w_scale=None, out=None, 
     for name, t in (("x", x), ("w", w), ("out", out), ("residual", residual), ("x8", x8), ("w8", w8), ("x_scale", x_scale),
                     ("w_scale", w_scale)):
         if t is not None:
-            # a matrix of one row may carry any stride: its row's length, rounded up, will do
-            one = -(-t.shape[1] // 16) * 16
-            setattr(p, name + "_stride", _row_stride(t, name) if t.shape[0] > 1 else max(_row_stride(t, name), one))
+            # (a matrix of one row may carry any stride: its row's length, rounded up, will do)
+            stride = _row_stride(t, name)
+            setattr(p, name + "_stride", stride if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16)
     for t, shape in ((x, (p.M, p.K)), (out, (p.M, p.N)), (residual, (p.M, p.N)), (w, (p.N, p.K))):
         assert t is None or tuple(t.shape) == shape and t.dtype == torch.bfloat16, "bf16 matrices of matching sizes"
     for t, n in ((x8, p.M), (w8, p.N)):

@@ -565,7 +565,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
   const uint32_t sbase = smem_u32(smem);
   const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_free = bar_acc + 8 * BUFS;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = blockIdx.x % split, J = blockIdx.x / split, t0 = blockIdx.y * T;
+  const int rank = blockIdx.x % split, J = blockIdx.x / split;
   const int per = (prm.Kb + split - 1) / split, ga = min(rank * per, prm.Kb), gb = min(ga + per, prm.Kb);
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
@@ -599,7 +599,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
       if (lane == 0) {
         mbar_expect_tx(bar_full + 8 * st, S::STAGE);
         tma_load_2d(sbase + st * S::STAGE, &tm_w, bar_full + 8 * st, g * 128, J * 128);
-        tma_load_2d(sbase + st * S::STAGE + 128 * 128, &tm_x, bar_full + 8 * st, g * 128, t0);
+        tma_load_2d(sbase + st * S::STAGE + 128 * 128, &tm_x, bar_full + 8 * st, g * 128, 0);
       }
       __syncwarp();
     }
@@ -625,7 +625,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     constexpr int PER = T > 32 ? 2 : 1;
     const float* xs[PER];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) xs[j] = prm.xs + min(t0 + (lane + 32 * j) % T, prm.M - 1) + zero;
+    for (int j = 0; j < PER; ++j) xs[j] = prm.xs + min((lane + 32 * j) % T, prm.M - 1) + zero;
     const float* ws = prm.ws + J * prm.ws_stride + zero;
     // The scales of AHEAD groups at a time, fetched while those before them are used (one group ahead, a fetch of 800 cycles was what a group took).
     float nx[AHEAD][PER], nw[AHEAD];
@@ -688,7 +688,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
   if (split == 1) {
     if (warp < 4 && ok) {
 #pragma unroll
-      for (int t = 0; t < T; ++t) finish(acc[t], t0 + t);
+      for (int t = 0; t < T; ++t) finish(acc[t], t);
     }
   } else {
     float* mine = reinterpret_cast<float*>(smem);                              // (the MMAs that read the ring are done: their sums are here)
@@ -700,10 +700,10 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     cluster_sync_all();
     if (warp < 4 && ok) {
       for (int t = rank * (T / split); t < (rank + 1) * (T / split); ++t) {
-        if (t0 + t >= prm.M) break;
+        if (t >= prm.M) break;
         float y = 0.f;
         for (int q = 0; q < split; ++q) y += ld_cluster_f32(mapa(sbase + (uint32_t)(t * 128 + threadIdx.x) * 4u, q));
-        finish(y, t0 + t);
+        finish(y, t);
       }
     }
     __syncwarp();
@@ -782,15 +782,44 @@ int launch_quantize_tiles(const sva_linear_t* p, const void* w, void* w8, float*
                     (long long)p->w8_stride, w_scale, (long long)p->w_scale_stride);
 }
 
+// The largest cluster of up to `most` CTAs that the current device, or the part of it that this process has, holds of a kernel.
+template <typename K>
+static int lin_cluster(K kern, int threads, int smem, int most) {
+  for (int c = most; c > 1; c /= 2) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)c;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)c);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess && n > 0) return c;
+    (void)cudaGetLastError();
+  }
+  return 1;
+}
+
 template <bool PAIR, int ACT>
 static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void* w8, void* out, const LinearParams& prm, int sms,
                                cudaStream_t st) {
   static DeviceOnce once;
+  static int cluster[64];
   auto kern = linear_kernel<PAIR, ACT>;
   using S = lin::Shape<PAIR>;
   constexpr int SIDE = S::SIDE, CTAS = PAIR ? 2 : 1, SMEM = S::SMEM;
-  int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) == cudaSuccess; });
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SVA_ERR_CUDA;
+  int rc = once.run([&] {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return false;
+    cluster[dev] = lin_cluster(kern, S::THREADS, SMEM, CTAS);
+    return true;
+  });
   if (rc) return rc;
+  if (PAIR && (cluster[dev] < CTAS || prm.debug & 64)) return launch_linear_tiles<false, ACT>(p, x8, w8, out, prm, sms, st);
   CUtensorMap tx, tw, to, tr;
   if ((rc = lin_map(&tx, x8, p->K, p->M, p->x8_stride, 1, 128))) return rc;
   if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, PAIR ? 64 : 128))) return rc;
@@ -815,18 +844,25 @@ template <int T>
 static int launch_linear_few(const sva_linear_t* p, const void* x8, const void* w8, const LinearParams& prm, int sms, cudaStream_t st) {
   using S = few::Shape<T>;
   static DeviceOnce once;
+  static int cluster[64];
   auto kern = linear_few_kernel<T>;
-  int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) == cudaSuccess; });
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SVA_ERR_CUDA;
+  int rc = once.run([&] {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return false;
+    cluster[dev] = lin_cluster(kern, few::THREADS, S::SMEM, 8);
+    return true;
+  });
   if (rc) return rc;
   CUtensorMap tx, tw;
   if ((rc = lin_map(&tx, x8, p->K, p->M, p->x8_stride, 1, T))) return rc;
   if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, 128))) return rc;
-  const long long rows = (p->N + 127) / 128, tokens = (p->M + T - 1) / T;
+  const int rows = (p->N + 127) / 128;
   // The inputs are split while all CTAs still run at once: the HBM then has the most in flight, and all end together.
+  const int most = prm.debug & 64 ? 1 : cluster[dev];     // (test aid: as on a device that holds no clusters)
   int split = 1;
-  while (split < 8 && 2 * split <= prm.Kb && rows * tokens * split * 2 <= (long long)sms * S::PER_SM) split *= 2;
-  if (rows * split > 0x7fffffffLL || tokens > 65535) return SVA_ERR_UNSUPPORTED;
-  return launch_dep_cluster(split, kern, dim3((unsigned)(rows * split), (unsigned)tokens), few::THREADS, S::SMEM, st, tx, tw, prm, split, p->act);
+  while (split < most && 2 * split <= prm.Kb && (long long)rows * split * 2 <= (long long)sms * S::PER_SM) split *= 2;
+  return launch_dep_cluster(split, kern, dim3((unsigned)(rows * split)), few::THREADS, S::SMEM, st, tx, tw, prm, split, p->act);
 }
 
 int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, const void* w8, const float* w_scale, void* out,
@@ -843,8 +879,14 @@ int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, c
   if (p->M <= 16) return launch_linear_few<16>(p, x8, w8, prm, sms, st);
   if (p->M <= 32) return launch_linear_few<32>(p, x8, w8, prm, sms, st);
   if (p->M <= 64) return launch_linear_few<64>(p, x8, w8, prm, sms, st);
-  const long long pairs = (long long)((p->M + 255) / 256) * ((p->N + 255) / 256);
-  return pairs >= sms / 2 ? launch_linear_act<true>(p, x8, w8, out, prm, sms, st) : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
+  // A pair takes some 770 cycles for a group of inputs of its 256 x 256, a CTA by itself 620 for its 128 x 128: whichever needs less for its
+  // rounds over the device.  us, in pairs / without: 1 024 x 2 048 x 2 048 12.8 / 10.7 (one round each), x 4 096 13.8 / 17.3 (one, two),
+  // 300 x 4 096 x 12 288 34.0 / 27.9 (two each), 768 x 4 096 x 4 096 19.9 / 27.0 (one, two).
+  auto rounds = [&](long long side, int places) {
+    return (((p->M + side - 1) / side) * ((p->N + side - 1) / side) + places - 1) / places;
+  };
+  return 5 * rounds(256, sms > 1 ? sms / 2 : 1) <= 4 * rounds(128, sms) ? launch_linear_act<true>(p, x8, w8, out, prm, sms, st)
+                                                          : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
 }
 
 }  // namespace sva

@@ -208,6 +208,18 @@ def test_on_a_side_stream_and_captured():
     np.testing.assert_array_equal(_f64(s["out"]), want)
 
 
+@pytest.mark.parametrize("M,N,K", [(3, 520, 2048), (40, 300, 1000), (1500, 4096, 400)])
+def test_without_clusters(M, N, K):
+    """As on a part of a device that holds none: nothing is split, no pairs."""
+    rng = np.random.default_rng(11)
+    s = _layer(rng, M, N, K, "gelu", True, True)
+    try:
+        B.debug_set_mode(64)
+        _check(s, _product(s))
+    finally:
+        B.debug_set_mode(0)
+
+
 @pytest.mark.parametrize("M,N,K", [(4, 512, 2048), (300, 512, 2048), (1500, 4096, 1024)])
 def test_a_starved_product_gives_up(M, N, K):
     """Inputs after the first 128 are withheld: the waits run out, every role leaves, the call after it is whole."""
