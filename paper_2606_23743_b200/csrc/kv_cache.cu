@@ -4,7 +4,7 @@
 // attention calls take.
 //
 // Both are HBM-bound streaming passes.  d/16 lanes own a row, 16 channels each (one 4-bit scale block), so that a row's maximum is
-// a few shuffles; a thread looks its token's slot up once and then has CACHE_HEADS heads' rows in flight.
+// a few shuffles; a thread looks its token's slot up once and then has some heads' rows in flight.
 #include <cuda_fp4.h>
 
 #include "common.cuh"
@@ -12,7 +12,8 @@
 namespace sva {
 
 static constexpr int CACHE_THREADS = 256;
-static constexpr int CACHE_HEADS = 4;                     // rows in flight per thread
+static constexpr int CACHE_HEADS = 4;                     // rows in flight per thread that is written from, and that is read:
+static constexpr int READ_HEADS = 2;                      // 2 x 47 616 tokens x 32 heads, e4m3, us: one 408, two 374, four 385, eight 433
 
 struct CacheArrays {                                      // one of K, V
   uint8_t* codes;
@@ -143,7 +144,7 @@ cache_write_kernel(const CacheParams prm) {
 }
 
 template <int LANES, bool FP4>
-__global__ void __launch_bounds__(CACHE_THREADS)
+__global__ void __launch_bounds__(CACHE_THREADS, 4)
 cache_read_kernel(const CacheParams prm) {
   const int zero = grid_dep_wait();
   const int which = blockIdx.x & 1, part = (int)((blockIdx.x >> 1) % prm.chunks);
@@ -165,12 +166,12 @@ cache_read_kernel(const CacheParams prm) {
   }
   const int place = n - at * prm.page, hb = part * prm.chunk, he = min(hb + prm.chunk, prm.H);
   uint8_t* dst = (which ? prm.xv : prm.xk) + 2 * (b * s.b + (long long)n * s.n + lane * 16);
-  for (int h0 = hb; h0 < he; h0 += CACHE_HEADS) {
-    uint4 codes[CACHE_HEADS];
-    float scale[CACHE_HEADS];
-    uint32_t sf[CACHE_HEADS];
+  for (int h0 = hb; h0 < he; h0 += READ_HEADS) {
+    uint4 codes[READ_HEADS];
+    float scale[READ_HEADS];
+    uint32_t sf[READ_HEADS];
 #pragma unroll
-    for (int i = 0; i < CACHE_HEADS; ++i) {
+    for (int i = 0; i < READ_HEADS; ++i) {
       codes[i] = make_uint4(0u, 0u, 0u, 0u);
       scale[i] = 0.f;
       sf[i] = 0u;
@@ -187,7 +188,7 @@ cache_read_kernel(const CacheParams prm) {
       }
     }
 #pragma unroll
-    for (int i = 0; i < CACHE_HEADS; ++i) {
+    for (int i = 0; i < READ_HEADS; ++i) {
       if (h0 + i >= he) continue;
       uint32_t o[8];
       const uint32_t w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
@@ -219,7 +220,7 @@ static int launch_cache(bool write, CacheParams& prm, const sva_kv_cache_t* c, c
   const int lanes = c->d / 16;
   const long long tiles = (prm.tokens + CACHE_THREADS / lanes - 1) / (CACHE_THREADS / lanes);
   // Heads per CTA: eight, whose second half's loads find the slots and the table at hand, where the grid comes to sixteen CTAs per SM all the
-  // same.  2 x 47 616 tokens x 32 heads, e4m3, written / read, us: four heads 396 / 427, eight 361 / 391, sixteen 350 / 397.
+  // same.  2 x 47 616 tokens x 32 heads, e4m3, written / read (four rows in flight), us: four heads 396 / 427, eight 361 / 391, sixteen 350 / 397.
   prm.chunk = 2 * CACHE_HEADS;
   if (2 * tiles * ((c->H + prm.chunk - 1) / prm.chunk) < 148 * 16) prm.chunk = CACHE_HEADS;
   prm.chunks = (c->H + prm.chunk - 1) / prm.chunk;
