@@ -566,7 +566,8 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
   const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_free = bar_acc + 8 * BUFS;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x % split, J = blockIdx.x / split;
-  const int per = (prm.Kb + split - 1) / split, ga = min(rank * per, prm.Kb), gb = min(ga + per, prm.Kb);
+  // this CTA's groups of inputs: rank, rank + split, ...: a cluster's CTAs read pieces of the weights rows that lie side by side
+  const int mine_n = rank < prm.Kb ? (prm.Kb - rank + split - 1) / split : 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
     for (int i = 0; i < BUFS; ++i) { mbar_init(bar_acc + 8 * i, 1); mbar_init(bar_free + 8 * i, 4); }
@@ -575,7 +576,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     prefetch_tmap(&tm_x);
     // the weights can be on their way to the L2 while the kernel before this one (the quantiser of the tokens) still runs
-    for (int g = ga; g < min(gb, ga + STAGES); ++g) tma_prefetch_2d(&tm_w, g * 128, J * 128);
+    for (int i = 0; i < min(mine_n, STAGES); ++i) tma_prefetch_2d(&tm_w, (rank + i * split) * 128, J * 128);
   }
   if (warp == 5) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(S::COLUMNS) : "memory");
@@ -591,11 +592,11 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
   for (int t = 0; t < T; ++t) acc[t] = 0.f;
   bool ok = true;
   if (warp == 4) {
-    for (int g = ga; g < gb; ++g) {
-      const int st = (g - ga) % STAGES;
-      ok = lin_wait(bar_empty + 8 * st, (uint32_t)((g - ga) / STAGES + 1) & 1u, abort_flag);
+    for (int i = 0; i < mine_n; ++i) {
+      const int st = i % STAGES, g = rank + i * split;
+      ok = lin_wait(bar_empty + 8 * st, (uint32_t)(i / STAGES + 1) & 1u, abort_flag);
       if (!ok) break;
-      if ((prm.debug & 1024) && g > ga) break;                                 // test aid: the ring runs dry
+      if ((prm.debug & 1024) && i > 0) break;                                 // test aid: the ring runs dry
       if (lane == 0) {
         mbar_expect_tx(bar_full + 8 * st, S::STAGE);
         tma_load_2d(sbase + st * S::STAGE, &tm_w, bar_full + 8 * st, g * 128, J * 128);
@@ -607,8 +608,8 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     constexpr uint32_t IDESC = instr_desc(128, T, 0, false);
     const uint32_t el = elect_one();
     const uint64_t ad0 = smem_desc(sbase, 16, 1024), bd0 = smem_desc(sbase + 128 * 128, 16, 1024);
-    for (int g = ga; g < gb; ++g) {
-      const int i = g - ga, st = i % STAGES, buf = i % BUFS;
+    for (int i = 0; i < mine_n; ++i) {
+      const int st = i % STAGES, buf = i % BUFS;
       ok = lin_wait(bar_free + 8 * buf, (uint32_t)(i / BUFS + 1) & 1u, abort_flag) &&
            lin_wait(bar_full + 8 * st, (uint32_t)(i / STAGES) & 1u, abort_flag);
       if (!ok) break;
@@ -629,19 +630,19 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     const float* ws = prm.ws + J * prm.ws_stride + zero;
     // The scales of AHEAD groups at a time, fetched while those before them are used (one group ahead, a fetch of 800 cycles was what a group took).
     float nx[AHEAD][PER], nw[AHEAD];
-    auto fetch = [&](int g) {
+    auto fetch = [&](int i) {
 #pragma unroll
       for (int q = 0; q < AHEAD; ++q) {
-        const int at = min(g + q, gb - 1);
+        const int at = rank + min(i + q, mine_n - 1) * split;
 #pragma unroll
         for (int j = 0; j < PER; ++j) nx[q][j] = __ldg(xs[j] + at * prm.xs_stride);
         nw[q] = __ldg(ws + at);
       }
     };
-    if (ga < gb) fetch(ga);
+    if (mine_n) fetch(0);
 #pragma unroll 1
-    for (int g = ga; g < gb; ++g) {
-      const int i = g - ga, buf = i % BUFS;
+    for (int i = 0; i < mine_n; ++i) {
+      const int buf = i % BUFS;
       float (*block)[T] = scale_s[i / AHEAD & 1][warp];     // (the other one may still be read by a lane that is behind)
       if (i % AHEAD == 0) {
 #pragma unroll
@@ -649,7 +650,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
 #pragma unroll
           for (int j = 0; j < PER; ++j)
             if (lane < T) block[q][lane + 32 * j] = nx[q][j] * nw[q];
-        if (g + AHEAD < gb) fetch(g + AHEAD);
+        if (i + AHEAD < mine_n) fetch(i + AHEAD);
         __syncwarp();
       }
       const float* s = block[i % AHEAD];
@@ -698,13 +699,29 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
     }
     __syncwarp();
     cluster_sync_all();
-    if (warp < 4 && ok) {
-      for (int t = rank * (T / split); t < (rank + 1) * (T / split); ++t) {
-        if (t >= prm.M) break;
-        float y = 0.f;
-        for (int q = 0; q < split; ++q) y += ld_cluster_f32(mapa(sbase + (uint32_t)(t * 128 + threadIdx.x) * 4u, q));
-        finish(y, t);
+    // sixteen values on their way at a time: a read of another CTA's shared memory takes several hundred cycles
+    auto join = [&](auto split_tag) {
+      constexpr int SPLIT = decltype(split_tag)::value, BATCH = 16 / SPLIT < T / SPLIT ? 16 / SPLIT : T / SPLIT;
+#pragma unroll 1
+      for (int t = rank * (T / SPLIT); t < (rank + 1) * (T / SPLIT) && t < prm.M; t += BATCH) {
+        float v[BATCH][SPLIT];
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e)
+#pragma unroll
+          for (int q = 0; q < SPLIT; ++q) v[e][q] = ld_cluster_f32(mapa(sbase + (uint32_t)((t + e) * 128 + threadIdx.x) * 4u, q));
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+          float y = v[e][0];
+#pragma unroll
+          for (int q = 1; q < SPLIT; ++q) y += v[e][q];
+          finish(y, t + e);
+        }
       }
+    };
+    if (warp < 4 && ok) {
+      if (split == 2) join(std::integral_constant<int, 2>{});
+      else if (split == 4) join(std::integral_constant<int, 4>{});
+      else join(std::integral_constant<int, 8>{});
     }
     __syncwarp();
     cluster_sync_all();                                                         // nobody's sums go before they were read
