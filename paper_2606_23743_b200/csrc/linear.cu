@@ -657,22 +657,28 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
       ok = lin_wait(bar_acc + 8 * buf, (uint32_t)(i / BUFS) & 1u, abort_flag);
       if (!ok) break;
       tc_fence_after();
+      constexpr int C = T < 32 ? T : 32;                    // tokens taken out of the accumulator at a time
 #pragma unroll
-      for (int c = 0; c < T / 16; ++c) {
-        uint32_t v[16];
-        tmem_ld16(taddr + buf * T + c * 16, v);
-        tc_wait_ld16(v);
-        if (c + 1 == T / 16) {
+      for (int c = 0; c < T / C; ++c) {
+        uint32_t v[C];
+        if constexpr (C == 32) tmem_ld32(taddr + buf * T + c * C, v);
+        else tmem_ld16(taddr + buf * T + c * C, v);
+        float4 f[C / 4];                                    // (read while the accumulator is on its way)
+#pragma unroll
+        for (int e = 0; e < C / 4; ++e) f[e] = *reinterpret_cast<const float4*>(s + c * C + 4 * e);
+        if constexpr (C == 32) tc_wait_ld32(v);
+        else tc_wait_ld16(v);
+        if (c + 1 == T / C) {
           tc_fence_before();
           mbar_arrive_if(bar_free + 8 * buf, lane == 0);
         }
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(s + c * 16 + e);
-          acc[c * 16 + e] = fmaf(__uint_as_float(v[e]), f.x, acc[c * 16 + e]);
-          acc[c * 16 + e + 1] = fmaf(__uint_as_float(v[e + 1]), f.y, acc[c * 16 + e + 1]);
-          acc[c * 16 + e + 2] = fmaf(__uint_as_float(v[e + 2]), f.z, acc[c * 16 + e + 2]);
-          acc[c * 16 + e + 3] = fmaf(__uint_as_float(v[e + 3]), f.w, acc[c * 16 + e + 3]);
+        for (int e = 0; e < C; e += 4) {
+          float* a = acc + c * C + e;
+          a[0] = fmaf(__uint_as_float(v[e]), f[e / 4].x, a[0]);
+          a[1] = fmaf(__uint_as_float(v[e + 1]), f[e / 4].y, a[1]);
+          a[2] = fmaf(__uint_as_float(v[e + 2]), f[e / 4].z, a[2]);
+          a[3] = fmaf(__uint_as_float(v[e + 3]), f[e / 4].w, a[3]);
         }
       }
     }

@@ -176,6 +176,9 @@ __device__ __forceinline__ void tc_wait_ld64(uint32_t* v) {
 __device__ __forceinline__ void tc_wait_ld16(uint32_t* v) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : SVA_T8(v, 0), SVA_T8(v, 8)::"memory");
 }
+__device__ __forceinline__ void tc_wait_ld32(uint32_t* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : SVA_T8(v, 0), SVA_T8(v, 8), SVA_T8(v, 16), SVA_T8(v, 24)::"memory");
+}
 #undef SVA_T8
 // The MMA warp runs its loop with all lanes (so addresses and descriptors stay warp-uniform)
 // and only the elected lane executes the tcgen05 instruction itself.
