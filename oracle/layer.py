@@ -77,11 +77,12 @@ def quantize_tiles(w):
 
 
 def activation(y, act):
-    if act == "gelu":
-        return 0.5 * y * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (y + 0.044715 * y ** 3)))
-    if act == "silu":
-        return y / (1.0 + np.exp(-y))
-    return y
+    if act == "none":
+        return y
+    with np.errstate(over="ignore"):                      # (far to the negative side: y / infinity)
+        # 0.5 y (1 + tanh u) = y / (1 + exp(-2u)), without the cancellation of 1 + tanh
+        x = 2.0 * math.sqrt(2.0 / math.pi) * (y + 0.044715 * y ** 3) if act == "gelu" else y
+        return y / (1.0 + np.exp(-x))
 
 
 def linear(x8, x_scale, w8, w_scale, bias=None, act="none", residual=None):

@@ -128,8 +128,8 @@ struct LinearParams {
 };
 
 // GELU (tanh form) 0.5 y (1 + tanh u) = y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3); SiLU y / (1 + exp(-y)).
-// The denominator, with the exponent formed in base 2 and kept below 2^60: far outside of what a bf16 result can show, and the product of
-// two denominators has a reciprocal that is a normal number.
+// The denominator, with the exponent formed in base 2 and kept below 2^60, so that the product of two denominators has a reciprocal that is a
+// normal number; the numerator is kept above -64 (a NaN stays one), so that what is left of values that far out is below 2^-54.
 template <int ACT>
 __device__ __forceinline__ float lin_denominator(float y) {
   constexpr float LOG2E = 1.4426950408889634f, C = -2.f * 0.7978845608028654f * LOG2E;
@@ -140,17 +140,22 @@ __device__ __forceinline__ float lin_rcp(float d) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
   return r;
 }
+__device__ __forceinline__ float lin_numerator(float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(y), "f"(-64.f));
+  return r;
+}
 template <int ACT>
 __device__ __forceinline__ float lin_act(float y) {
-  return ACT == SVA_ACT_NONE ? y : y * lin_rcp(lin_denominator<ACT>(y));
+  return ACT == SVA_ACT_NONE ? y : lin_numerator(y) * lin_rcp(lin_denominator<ACT>(y));
 }
 // two at a time, one reciprocal for both: exponentials and reciprocals leave the SM at 16 a cycle, 4 096 cycles for two of each of 256 x 128 values
 template <int ACT>
 __device__ __forceinline__ void lin_act2(float& a, float& b) {
   if (ACT == SVA_ACT_NONE) return;
   const float da = lin_denominator<ACT>(a), db = lin_denominator<ACT>(b), r = lin_rcp(da * db);
-  a *= r * db;
-  b *= r * da;
+  a = lin_numerator(a) * (r * db);
+  b = lin_numerator(b) * (r * da);
 }
 
 __device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -177,9 +182,8 @@ __device__ __forceinline__ void lin_tile(int i, int mt, int nt, int& m, int& n) 
 //   PAIR   two CTAs make a tile of 256 tokens x 256 weights rows: each stages its 128 tokens and half of the weights rows, the first issues
 //          the MMAs of both (cta_group::2): 32 KB from the L2 per CTA and group where a CTA by itself would need 48 KB for its 128 x 256
 //   else   a CTA makes 128 x 128: problems that are too small to fill the device with pairs
-// Warps: four per 64 columns sum, a thread owning one token's 64 (sixteen warps in a pair's CTA: with eight, 128 columns each,
-// a warp's way through a group -- wait, read, multiply-add -- took 870 cycles, the MMAs 512); then one that loads, one that issues the MMAs, one that
-// brings the scales, one that sees to the staging tiles.
+// Warps: eight sum, a thread owning one token and half of the tile's columns; then one that loads, one that issues the MMAs, one that brings the
+// scales, one that sees to the staging tiles (bias, residual, stores).
 namespace lin {
 constexpr uint32_t A_BYTES = 128 * 128, STAGE = 2 * A_BYTES;
 constexpr uint32_t OUT_BYTES = 128 * 128;                 // staging tile, 128 tokens x 64 columns of bf16
@@ -202,7 +206,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
               const __grid_constant__ CUtensorMap tm_r, const LinearParams prm) {
   using namespace lin;
   using S = Shape<PAIR>;
-  constexpr int STAGES = S::STAGES, SIDE = S::SIDE, BUFS = S::BUFS, SLOTS = S::SLOTS, SLOT = S::SLOT, COLS = S::COLS, UNITS = S::UNITS, LOADER = S::SUM_WARPS;
+  constexpr int STAGES = S::STAGES, SIDE = S::SIDE, BUFS = S::BUFS, SLOTS = S::SLOTS, SLOT = S::SLOT;
+  constexpr int COLS = S::COLS, UNITS = S::UNITS, LOADER = S::SUM_WARPS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS * UNITS + 4];
@@ -212,8 +217,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
   const uint32_t sbase = smem_u32(smem);
-  const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_free = bar_acc + 8 * BUFS * UNITS,
-                 bar_ready = bar_free + 8 * BUFS * UNITS, bar_staged = bar_ready + 16;
+  const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES;
+  const uint32_t bar_free = bar_acc + 8 * BUFS * UNITS, bar_ready = bar_free + 8 * BUFS * UNITS, bar_staged = bar_ready + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, first = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
   const int step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
@@ -394,7 +399,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const int m0 = m * SIDE + rank * 128;
         for (int h = 0; h < 2; ++h) {
           const int n0 = n * SIDE + h * COLS;
-          for (int c = lane; c < COLS; c += 32) bias_s[h][c] = prm.bias && n0 + c < prm.N ? __ldg(prm.bias + n0 + c) : 0.f;
+          for (int c = lane; c < COLS; c += 32) bias_s[h][c] = prm.bias && n0 + c < prm.N ? __ldg(prm.bias + n0 + c + zero) : 0.f;
           __syncwarp();
           if (lane == 0) {
             if (prm.residual) {                              // comes to where the result will be staged
@@ -687,7 +692,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
   const int n = J * 128 + (int)threadIdx.x;
   auto finish = [&](float y, int t) {
     if (t >= prm.M || n >= prm.N) return;
-    if (prm.bias) y += __ldg(prm.bias + n);
+    if (prm.bias) y += __ldg(prm.bias + n + zero);
     y = act == SVA_ACT_GELU ? lin_act<SVA_ACT_GELU>(y) : act == SVA_ACT_SILU ? lin_act<SVA_ACT_SILU>(y) : y;
     if (prm.residual) y += __bfloat162float(prm.residual[(long long)t * prm.res_stride + n]);
     prm.out[(long long)t * prm.out_stride + n] = __float2bfloat16_rn(y);

@@ -29,11 +29,11 @@ struct RopeParams {
 };
 
 struct Turn { float c, s; };
-__device__ __forceinline__ Turn rope_turn(const RopeParams& prm, const int32_t* pos, int pair) {
+__device__ __forceinline__ Turn rope_turn(const RopeParams& prm, const unsigned long long* steps, const int32_t* pos, int pair) {
   Turn t = {1.f, 0.f};                                    // channels that are not rotated
   if (pair < prm.half) {
     const long long p = __ldg(pos + (pair < prm.end0 ? 0 : pair < prm.end1 ? prm.pos_axis : 2 * prm.pos_axis));
-    const unsigned long long phase = (unsigned long long)p * __ldg(prm.steps + pair);
+    const unsigned long long phase = (unsigned long long)p * __ldg(steps + pair);
     float s, c;
     sincospif((float)(int)(phase >> 32) * 4.656612873077393e-10f, &s, &c);       // 2^-31: half turns
     t.c = c * prm.factor;
@@ -97,13 +97,14 @@ rope_kernel(const RopeParams prm, int lanes) {
   load(h0);
   Turn turn[FORM == 0 ? 4 : 8];                           // one per pair, or one per channel
   const int32_t* pos = prm.pos + b * prm.pos_batch + n;
+  const unsigned long long* steps = prm.steps + zero;
 #pragma unroll
   for (int e = 0; e < (FORM == 0 ? 4 : 8); ++e) {
     const int c = c0 + e;
     if (FORM == 0) {
-      turn[e] = mine ? rope_turn(prm, pos, c0 / 2 + e) : Turn{1.f, 0.f};
+      turn[e] = mine ? rope_turn(prm, steps, pos, c0 / 2 + e) : Turn{1.f, 0.f};
     } else {
-      turn[e] = mine && c < 2 * prm.half ? rope_turn(prm, pos, c < prm.half ? c : c - prm.half) : Turn{1.f, 0.f};
+      turn[e] = mine && c < 2 * prm.half ? rope_turn(prm, steps, pos, c < prm.half ? c : c - prm.half) : Turn{1.f, 0.f};
       if (c < prm.half) turn[e].s = -turn[e].s;           // first of a pair: a c - b s; second: b c + a s
     }
   }

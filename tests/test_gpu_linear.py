@@ -185,6 +185,31 @@ def test_a_nan_code_stays_with_its_outputs(M):
     np.testing.assert_array_equal(got[~bad], want[~bad])
 
 
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("M", [2, 200, 2500])
+def test_activations_far_out(M, act):
+    """Sums from the bias alone, far to both sides, infinities and a NaN, which stays alone.  What is left of a value far to the negative side
+    may be 2^-54."""
+    N = 2048
+    b = torch.linspace(-60, 60, N, dtype=torch.float64)
+    b[::16] = torch.tensor([-1e38, -1e30, -1e18, -1e4, -100.0, 0.0, 100.0, 1e4, 1e18, 1e30, 1e38, -0.5, 1e-30, -1e-30, -64.0, -65.0] * (N // 256))
+    b[5], b[700], b[1501] = float("nan"), float("inf"), float("-inf")
+    x8, w8 = torch.zeros(M, 128, dtype=torch.uint8, device="cuda"), torch.zeros(N, 128, dtype=torch.uint8, device="cuda")
+    xs, ws = torch.ones(1, M, device="cuda"), torch.ones(N // 128, 1, device="cuda")
+    out = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    p = B.make_linear(None, x8, xs, w8, ws, out, act, K=128)
+    B.linear_fp8(p, x8, xs, w8, ws, out, b.float().cuda())
+    got = _f64(out)
+    assert (got == got[:1])[:, ~np.isnan(got[0])].all()                 # every row is the same
+    with np.errstate(all="ignore"):
+        ref = L.activation(b.float().double().numpy(), act)
+    ref[1501] = 0.0
+    assert np.isnan(got[:, 5]).all() and np.isnan(got).sum() == M and got[0, 700] == np.inf
+    at = np.isfinite(ref)
+    got, ref = got[0][at], ref[at]
+    assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -18 * np.abs(ref) + 2.0 ** -53).all()
+
+
 def test_on_a_side_stream_and_captured():
     rng = np.random.default_rng(9)
     s = _layer(rng, 37, 520, 512, "silu", True)

@@ -37,6 +37,13 @@ def test_linear_of_exact_codes():
     np.testing.assert_allclose(out, x @ w.T, rtol=1e-12)
 
 
+def test_activations():
+    y = np.array([-50.0, -3.0, -0.5, 0.0, 0.1, 1.0, 4.0, 60.0])
+    np.testing.assert_allclose(L.activation(y, "gelu"), 0.5 * y * (1 + np.tanh(math.sqrt(2 / math.pi) * (y + 0.044715 * y ** 3))), atol=1e-14)
+    np.testing.assert_allclose(L.activation(y, "silu"), y / (1 + np.exp(-y)), rtol=1e-14)
+    assert (L.activation(y, "none") == y).all()
+
+
 def test_zero_rows_have_scale_one():
     codes, scale = L.quantize_rows(np.zeros((2, 130)))
     assert (codes == 0).all() and (scale == 1.0).all() and scale.shape == (2, 2)
