@@ -6,6 +6,7 @@ for device memory and streams.  There is no CPU fallback: a missing library rais
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -170,22 +171,25 @@ def _ptr(t):
 # torch.cuda.current_stream() builds a Stream object, 2 us of the 14 us that the two calls of a small clip spend in Python; the
 # shorter way is not part of torch's public interface, and a torch without it gets the public one.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream():
     """The current stream of the current device, as a pointer."""
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(_raw_device())
 
 
-_Strides = C.c_int64 * 3
+@functools.lru_cache(maxsize=1024)
+def _stride_array(s):
+    assert len(s) == 4 and s[3] == 1, "tensors are [B,H,N,d] with d contiguous"
+    return (C.c_int64 * 3)(*s[:3])
 
 
 def _strides(t):
-    s = t.stride()
-    assert len(s) == 4 and s[3] == 1, "tensors are [B,H,N,d] with d contiguous"
-    return _Strides(s[0], s[1], s[2])
+    """b, h, n strides as the C ABI takes them (read only: tensors of equal strides share the array)."""
+    return _stride_array(t.stride())
 
 
 def make_problem(q, k, v, o, N: int, block: int, scale: float = 0.0, fp8: bool = False) -> Problem:
@@ -448,8 +452,8 @@ def make_linear(x=None, x8=None, x_scale=None, w8=None, w_scale=None, out=None, 
 
 def quantize_rows_fp8(p: Linear, x, x8, x_scale) -> None:
     """Activations to e4m3 codes, a scale per token and 128 inputs."""
-    rc = lib().sva_quantize_rows_fp8(C.byref(p), _ptr(x), _ptr(x8), _ptr(x_scale), _stream())
-    if rc != SVA_OK:
+    rc = (_lib or lib()).sva_quantize_rows_fp8(p, x.data_ptr(), x8.data_ptr(), x_scale.data_ptr(), _stream())
+    if rc:
         raise SvaError(rc, "sva_quantize_rows_fp8")
 
 
@@ -463,9 +467,10 @@ def quantize_tiles_fp8(p: Linear, w, w8, w_scale) -> None:
 def linear_fp8(p: Linear, x8, x_scale, w8, w_scale, out, bias=None, residual=None, status=None) -> None:
     """out = bf16(act(x w^T + bias) + residual) from codes and scales."""
     assert bias is None or bias.dtype is torch.float32 and bias.numel() == p.N and bias.stride(-1) == 1, "bias is [N] fp32"
-    rc = lib().sva_linear_fp8(C.byref(p), _ptr(x8), _ptr(x_scale), _ptr(w8), _ptr(w_scale), _ptr(out), _ptr(bias), _ptr(residual),
-                              _ptr(status), _stream())
-    if rc != SVA_OK:
+    rc = (_lib or lib()).sva_linear_fp8(p, x8.data_ptr(), x_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), out.data_ptr(),
+                                        None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(),
+                                        None if status is None else status.data_ptr(), _stream())
+    if rc:
         raise SvaError(rc, "sva_linear_fp8")
 
 
@@ -503,8 +508,9 @@ def make_rope(q, k, q_out, k_out, positions, rotary_dim: int, layout: str = "int
 
 def rope(p: Rope, q, k, steps, positions, q_out, k_out) -> None:
     """Rotary positions of q and k (k None: q alone)."""
-    rc = lib().sva_rope(C.byref(p), _ptr(q), _ptr(k), _ptr(steps), _ptr(positions), _ptr(q_out), _ptr(k_out), _stream())
-    if rc != SVA_OK:
+    rc = (_lib or lib()).sva_rope(p, q.data_ptr(), None if k is None else k.data_ptr(), steps.data_ptr(), positions.data_ptr(),
+                                  q_out.data_ptr(), None if k_out is None else k_out.data_ptr(), _stream())
+    if rc:
         raise SvaError(rc, "sva_rope")
 
 
@@ -530,20 +536,23 @@ def make_kv_cache(k, v, format: str = "e4m3") -> KvCache:
 def kv_cache_write(c: KvCache, k, v, slots, status=None) -> None:
     """k, v [B,H,T,d] bf16 into the slots [B,T] int32 (negative: left out)."""
     shape = Bq, H, T, d = k.shape
-    assert H == c.H and d == c.d and v.shape == shape and k.dtype is torch.bfloat16 and v.dtype is torch.bfloat16, "k, v are [B,H,T,d] bf16"
+    assert H == c.H and d == c.d and v.shape == shape and k.dtype is v.dtype is torch.bfloat16, "k, v are [B,H,T,d] bf16"
     assert slots.shape == (Bq, T) and slots.dtype is torch.int32 and slots.is_contiguous(), "slots are [B,T] int32"
-    rc = lib().sva_kv_cache_write(C.byref(c), _ptr(k), _ptr(v), _strides(k), _strides(v), Bq, T, _ptr(slots), _ptr(status), _stream())
-    if rc != SVA_OK:
+    rc = (_lib or lib()).sva_kv_cache_write(c, k.data_ptr(), v.data_ptr(), _strides(k), _strides(v), Bq, T, slots.data_ptr(),
+                                            None if status is None else status.data_ptr(), _stream())
+    if rc:
         raise SvaError(rc, "sva_kv_cache_write")
 
 
 def kv_cache_read(c: KvCache, page_table, lengths, k, v, status=None) -> None:
     """Each sequence's first rows, from its pages, into k, v [B,H,N,d] bf16; rows from lengths[b] on become zeros."""
-    Bq, H, N, d = k.shape
-    assert H == c.H and d == c.d and v.shape == k.shape and k.dtype == v.dtype == torch.bfloat16
-    assert page_table.shape[0] == Bq and page_table.dtype == torch.int32 and page_table.stride(1) == 1, "page_table is [B,pages] int32"
-    assert lengths.shape == (Bq,) and lengths.dtype == torch.int32 and lengths.is_contiguous(), "lengths is [B] int32"
-    rc = lib().sva_kv_cache_read(C.byref(c), _ptr(page_table), page_table.stride(0), page_table.shape[1], _ptr(lengths), Bq, N, _ptr(k),
-                                 _ptr(v), _strides(k), _strides(v), _ptr(status), _stream())
-    if rc != SVA_OK:
+    shape = Bq, H, N, d = k.shape
+    assert H == c.H and d == c.d and v.shape == shape and k.dtype is v.dtype is torch.bfloat16, "k, v are [B,H,N,d] bf16"
+    rows, most = page_table.shape
+    stride, inner = page_table.stride()
+    assert rows == Bq and page_table.dtype is torch.int32 and inner == 1, "page_table is [B,pages] int32"
+    assert lengths.shape == (Bq,) and lengths.dtype is torch.int32 and lengths.is_contiguous(), "lengths is [B] int32"
+    rc = (_lib or lib()).sva_kv_cache_read(c, page_table.data_ptr(), stride, most, lengths.data_ptr(), Bq, N, k.data_ptr(), v.data_ptr(),
+                                           _strides(k), _strides(v), None if status is None else status.data_ptr(), _stream())
+    if rc:
         raise SvaError(rc, "sva_kv_cache_read")
