@@ -182,6 +182,8 @@ __device__ __forceinline__ void lin_tile(int i, int mt, int nt, int& m, int& n) 
 //   PAIR   two CTAs make a tile of 256 tokens x 256 weights rows: each stages its 128 tokens and half of the weights rows, the first issues
 //          the MMAs of both (cta_group::2): 32 KB from the L2 per CTA and group where a CTA by itself would need 48 KB for its 128 x 256
 //   else   a CTA makes 128 x 128: problems that are too small to fill the device with pairs
+//   SPLIT  the CTAs of a cluster take every split-th group of a 128 x 128 tile each and join their sums through distributed shared memory, in
+//          the order of the CTAs: few tiles with many inputs
 // Warps: eight sum, a thread owning one token and half of the tile's columns; then one that loads, one that issues the MMAs, one that brings the
 // scales, one that sees to the staging tiles (bias, residual, stores).
 namespace lin {
@@ -200,10 +202,10 @@ template <bool PAIR> struct Shape {                       // (227 KB: the stagin
 };
 }
 
-template <bool PAIR, int ACT>
+template <bool PAIR, int ACT, bool SPLIT>
 __global__ void __launch_bounds__(lin::Shape<PAIR>::THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_o,
-              const __grid_constant__ CUtensorMap tm_r, const LinearParams prm) {
+              const __grid_constant__ CUtensorMap tm_r, const LinearParams prm, int split) {
   using namespace lin;
   using S = Shape<PAIR>;
   constexpr int STAGES = S::STAGES, SIDE = S::SIDE, BUFS = S::BUFS, SLOTS = S::SLOTS, SLOT = S::SLOT;
@@ -220,9 +222,13 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   const uint32_t bar_full = smem_u32(&bars[0]), bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES;
   const uint32_t bar_free = bar_acc + 8 * BUFS * UNITS, bar_ready = bar_free + 8 * BUFS * UNITS, bar_staged = bar_ready + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, first = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
-  const int step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
-  const int mt = (prm.M + SIDE - 1) / SIDE, nt = (prm.N + SIDE - 1) / SIDE, tiles = mt * nt, Kb = prm.Kb;
+  const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, part = SPLIT ? (int)blockIdx.x % split : 0;
+  const int first = PAIR ? (int)(blockIdx.x >> 1) : SPLIT ? (int)blockIdx.x / split : (int)blockIdx.x;
+  const int mt = (prm.M + SIDE - 1) / SIDE, nt = (prm.N + SIDE - 1) / SIDE, tiles = mt * nt;
+  const int step = PAIR ? (int)(gridDim.x >> 1) : SPLIT ? tiles : (int)gridDim.x;
+  // this CTA's groups of inputs: all, or part, part + split, ... of them
+  const int Kb = SPLIT ? (prm.Kb - part + split - 1) / split : prm.Kb;
+  auto group = [&](int g) { return SPLIT ? part + g * split : g; };
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
     for (int i = 0; i < BUFS * UNITS; ++i) {              // full: by the MMAs and the scales; free: by eight warps, a pair's four in each CTA
@@ -279,8 +285,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
               tma_load_2d_pair(dst + A_BYTES + 64 * 128, &tm_w, bar_lead + 8 * st, g * 128, n0 + 128);       // of unit 1
             } else {
               mbar_expect_tx(bar_full + 8 * st, STAGE);
-              tma_load_2d(dst, &tm_x, bar_full + 8 * st, g * 128, m0);
-              tma_load_2d(dst + A_BYTES, &tm_w, bar_full + 8 * st, g * 128, n0);
+              tma_load_2d(dst, &tm_x, bar_full + 8 * st, group(g) * 128, m0);
+              tma_load_2d(dst + A_BYTES, &tm_w, bar_full + 8 * st, group(g) * 128, n0);
             }
           }
           __syncwarp();
@@ -349,7 +355,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         t.n = min(AHEAD, Kb - g);
 #pragma unroll
         for (int q = 0; q < AHEAD; ++q) {
-          const int at = min(g + q, Kb - 1);
+          const int at = group(min(g + q, Kb - 1));
 #pragma unroll
           for (int j = 0; j < 4; ++j) t.x[q][j] = __ldg(xs[j] + at * prm.xs_stride);
 #pragma unroll
@@ -389,7 +395,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         fetch(a);
         if (!hand_over(b)) break;
       }
-    } else if (warp == LOADER + 3) {
+    } else if (warp == LOADER + 3 && !SPLIT) {
       // ---- staging tiles: the bias of their columns, what the result is added to, the stores
       bool ok = true;
       uint32_t ph = 0;
@@ -426,6 +432,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       }
       if (lane == 0) bulk_wait0();
     }
+    __syncwarp();
+    if (SPLIT) cluster_sync_all();                        // (the sum warps' barrier below)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SUM_REGS));
     // ---- sums and epilogue
@@ -482,6 +490,68 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       }
       int m, n;
       lin_tile(i, mt, nt, m, n);
+      if (SPLIT) {
+        // the sums of the cluster's CTAs: everybody's into its own ring (which the MMAs are done with), then each finishes a part of the columns
+        float* mine = reinterpret_cast<float*>(smem);
+        if (ok) {
+#pragma unroll
+          for (int c = 0; c < COLS / 2; ++c) {
+            float lo, hi;
+            unpack2(acc[c], lo, hi);
+            mine[(wg * COLS + 2 * c) * 128 + row] = lo;
+            mine[(wg * COLS + 2 * c + 1) * 128 + row] = hi;
+          }
+        }
+        __syncwarp();
+        cluster_sync_all();
+        if (!ok) break;
+        auto join = [&](auto split_tag) {
+          constexpr int Q = decltype(split_tag)::value, W = COLS / Q;          // columns of a thread
+          const int c0 = part * 2 * W + wg * W;
+          float v[Q][W];
+#pragma unroll
+          for (int q = 0; q < Q; ++q) {
+            const uint32_t from = mapa(sbase + (uint32_t)(c0 * 128 + row) * 4u, q);
+#pragma unroll
+            for (int c = 0; c < W; ++c) v[q][c] = ld_cluster_f32(from + c * 512);
+          }
+          const int tok = m * SIDE + row;
+#pragma unroll
+          for (int c = 0; c < W; c += 8) {
+            float y[8];
+            const int col = n * SIDE + c0 + c;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              y[e] = v[0][c + e];
+#pragma unroll
+              for (int q = 1; q < Q; ++q) y[e] += v[q][c + e];
+              if (prm.bias && col + e < prm.N) y[e] += __ldg(prm.bias + col + e + zero);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) lin_act2<ACT>(y[e], y[e + 1]);
+            if (tok >= prm.M || col >= prm.N) continue;
+            __nv_bfloat16* to = prm.out + (long long)tok * prm.out_stride + col;
+            const __nv_bfloat16* add = prm.residual + (long long)tok * prm.res_stride + col;
+            if (col + 8 <= prm.N) {
+              if (prm.residual) {
+                const uint4 u = *reinterpret_cast<const uint4*>(add);
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { y[2 * e] += bf16lo(w[e]); y[2 * e + 1] += bf16hi(w[e]); }
+              }
+              *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+            } else {
+#pragma unroll
+              for (int e = 0; e < 7; ++e)
+                if (col + e < prm.N) to[e] = __float2bfloat16_rn(y[e] + (prm.residual ? __bfloat162float(add[e]) : 0.f));
+            }
+          }
+        };
+        if (split == 2) join(std::integral_constant<int, 2>{});
+        else if (split == 4) join(std::integral_constant<int, 4>{});
+        else join(std::integral_constant<int, 8>{});
+        break;
+      }
       const int m1 = m * SIDE + rank * 128, n1 = n * SIDE + wg * COLS;
       ok = ok && lin_wait(bar_ready + 8 * wg, rph, abort_flag);
       if (!ok) break;
@@ -528,7 +598,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   if (*abort_flag) lin_settle();
   tc_fence_before();
   __syncthreads();
-  if (PAIR) cluster_sync_all();                           // nothing arrives at a CTA that has gone
+  if (PAIR || SPLIT) cluster_sync_all();                  // nothing arrives at, and nobody reads from, a CTA that has gone
   if (threadIdx.x == 0 && *abort_flag && prm.status) atomicOr(prm.status, SVA_DEV_TIMEOUT);
   if (warp == LOADER + 1) {
     tc_fence_after();
@@ -810,44 +880,53 @@ int launch_quantize_tiles(const sva_linear_t* p, const void* w, void* w8, float*
                     (long long)p->w8_stride, w_scale, (long long)p->w_scale_stride);
 }
 
-// The largest cluster of up to `most` CTAs that the current device, or the part of it that this process has, holds of a kernel.
+// How many clusters of `ctas` CTAs of a kernel the current device, or the part of it that this process has, holds at once.
 template <typename K>
-static int lin_cluster(K kern, int threads, int smem, int most) {
-  for (int c = most; c > 1; c /= 2) {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)c;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)c);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess && n > 0) return c;
-    (void)cudaGetLastError();
-  }
-  return 1;
+static int lin_clusters(K kern, int threads, int smem, int ctas) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)ctas;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess) return n;
+  (void)cudaGetLastError();
+  return 0;
 }
 
-template <bool PAIR, int ACT>
+// split: CTAs that share the inputs of a tile (SPLIT only)
+template <bool PAIR, int ACT, bool SPLIT = false>
 static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void* w8, void* out, const LinearParams& prm, int sms,
                                cudaStream_t st) {
   static DeviceOnce once;
-  static int cluster[64];
-  auto kern = linear_kernel<PAIR, ACT>;
+  static int held[64][4];                                   // clusters of 1, 2, 4, 8 CTAs
+  auto kern = linear_kernel<PAIR, ACT, SPLIT>;
   using S = lin::Shape<PAIR>;
   constexpr int SIDE = S::SIDE, CTAS = PAIR ? 2 : 1, SMEM = S::SMEM;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SVA_ERR_CUDA;
   int rc = once.run([&] {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return false;
-    cluster[dev] = lin_cluster(kern, S::THREADS, SMEM, CTAS);
+    for (int j = 1; j < (SPLIT ? 4 : PAIR ? 2 : 1); ++j) held[dev][j] = lin_clusters(kern, S::THREADS, SMEM, 1 << j);
     return true;
   });
   if (rc) return rc;
-  if (PAIR && (cluster[dev] < CTAS || prm.debug & 64)) return launch_linear_tiles<false, ACT>(p, x8, w8, out, prm, sms, st);
+  if (PAIR && (held[dev][1] == 0 || prm.debug & 64)) return launch_linear_tiles<false, ACT>(p, x8, w8, out, prm, sms, st);
+  const long long tiles = (long long)((p->M + SIDE - 1) / SIDE) * ((p->N + SIDE - 1) / SIDE);
+  int split = 1;
+  if (SPLIT) {
+    // As many as all tiles' clusters run at once with, if that saves more than the joining of the sums takes, some nine groups' time.
+    // us, without / split: 128 x 2 048 x 2 048 9.5 / 8.6, 65 x 4 096 x 4 096 14.9 / 10.2, 100 x 8 192 x 512 24.2 / 9.9, but 300 x 1 024 x 1 024
+    // (eight groups) 7.0 / 8.0.
+    for (int j = 1; j < 4 && !(prm.debug & 64) && tiles <= held[dev][j]; ++j)
+      if (prm.Kb > (prm.Kb + (1 << j) - 1) / (1 << j) + 9) split = 1 << j;
+    if (split == 1) return launch_linear_tiles<false, ACT>(p, x8, w8, out, prm, sms, st);
+  }
   CUtensorMap tx, tw, to, tr;
   if ((rc = lin_map(&tx, x8, p->K, p->M, p->x8_stride, 1, 128))) return rc;
   if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, PAIR ? 64 : 128))) return rc;
@@ -855,30 +934,32 @@ static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void
   if ((rc = lin_map(&to, out, p->N < 8 ? 8 : p->N & ~7, p->M, 2 * p->out_stride, 2, 128))) return rc;
   tr = to;
   if (prm.residual && (rc = lin_map(&tr, prm.residual, p->N, p->M, 2 * p->residual_stride, 2, 128))) return rc;
-  const long long tiles = (long long)((p->M + SIDE - 1) / SIDE) * ((p->N + SIDE - 1) / SIDE);
   if (tiles > 0x7fffffffLL - sms) return SVA_ERR_UNSUPPORTED;
   const long long most = sms / CTAS;
-  return launch_dep_cluster(CTAS, kern, dim3((unsigned)(CTAS * (tiles < most ? tiles : most))), S::THREADS, SMEM, st, tx, tw, to, tr, prm);
+  const int per = SPLIT ? split : CTAS;
+  return launch_dep_cluster(per, kern, dim3((unsigned)(per * (SPLIT || tiles < most ? tiles : most))), S::THREADS, SMEM, st, tx, tw, to, tr, prm,
+                            split);
 }
 
-template <bool PAIR>
+template <bool PAIR, bool SPLIT = false>
 static int launch_linear_act(const sva_linear_t* p, const void* x8, const void* w8, void* out, const LinearParams& prm, int sms, cudaStream_t st) {
-  return p->act == SVA_ACT_GELU ? launch_linear_tiles<PAIR, SVA_ACT_GELU>(p, x8, w8, out, prm, sms, st)
-       : p->act == SVA_ACT_SILU ? launch_linear_tiles<PAIR, SVA_ACT_SILU>(p, x8, w8, out, prm, sms, st)
-                                : launch_linear_tiles<PAIR, SVA_ACT_NONE>(p, x8, w8, out, prm, sms, st);
+  return p->act == SVA_ACT_GELU ? launch_linear_tiles<PAIR, SVA_ACT_GELU, SPLIT>(p, x8, w8, out, prm, sms, st)
+       : p->act == SVA_ACT_SILU ? launch_linear_tiles<PAIR, SVA_ACT_SILU, SPLIT>(p, x8, w8, out, prm, sms, st)
+                                : launch_linear_tiles<PAIR, SVA_ACT_NONE, SPLIT>(p, x8, w8, out, prm, sms, st);
 }
 
 template <int T>
 static int launch_linear_few(const sva_linear_t* p, const void* x8, const void* w8, const LinearParams& prm, int sms, cudaStream_t st) {
   using S = few::Shape<T>;
   static DeviceOnce once;
-  static int cluster[64];
+  static int largest[64];                                   // CTAs in a cluster
   auto kern = linear_few_kernel<T>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SVA_ERR_CUDA;
   int rc = once.run([&] {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return false;
-    cluster[dev] = lin_cluster(kern, few::THREADS, S::SMEM, 8);
+    largest[dev] = 1;
+    for (int c = 2; c <= 8 && lin_clusters(kern, few::THREADS, S::SMEM, c) > 0; c *= 2) largest[dev] = c;
     return true;
   });
   if (rc) return rc;
@@ -887,7 +968,7 @@ static int launch_linear_few(const sva_linear_t* p, const void* x8, const void* 
   if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, 128))) return rc;
   const int rows = (p->N + 127) / 128;
   // The inputs are split while all CTAs still run at once: the HBM then has the most in flight, and all end together.
-  const int most = prm.debug & 64 ? 1 : cluster[dev];     // (test aid: as on a device that holds no clusters)
+  const int most = prm.debug & 64 ? 1 : largest[dev];     // (test aid: as on a device that holds no clusters)
   int split = 1;
   while (split < most && 2 * split <= prm.Kb && (long long)rows * split * 2 <= (long long)sms * S::PER_SM) split *= 2;
   return launch_dep_cluster(split, kern, dim3((unsigned)(rows * split)), few::THREADS, S::SMEM, st, tx, tw, prm, split, p->act);
@@ -913,8 +994,8 @@ int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, c
   auto rounds = [&](long long side, int places) {
     return (((p->M + side - 1) / side) * ((p->N + side - 1) / side) + places - 1) / places;
   };
-  return 5 * rounds(256, sms > 1 ? sms / 2 : 1) <= 4 * rounds(128, sms) ? launch_linear_act<true>(p, x8, w8, out, prm, sms, st)
-                                                          : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
+  if (5 * rounds(256, sms > 1 ? sms / 2 : 1) <= 4 * rounds(128, sms)) return launch_linear_act<true>(p, x8, w8, out, prm, sms, st);
+  return 2 * rounds(128, 1) <= sms ? launch_linear_act<false, true>(p, x8, w8, out, prm, sms, st) : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
 }
 
 }  // namespace sva

@@ -111,7 +111,8 @@ def test_quantisers_at_the_ends_of_the_range():
 
 SIZES = [(1, 8, 16), (1, 2048, 2048), (2, 1000, 4096), (3, 128, 128), (16, 136, 640), (17, 2056, 1000), (31, 384, 8192), (33, 520, 136), (64, 1024, 513),
          (65, 264, 2048), (100, 24, 100), (128, 128, 1), (129, 1000, 127), (200, 4100, 384), (333, 2051, 1031), (512, 512, 512), (1000, 1544, 904),
-         (2050, 2304, 256), (1, 24576, 256), (5, 40, 16384), (9473, 520, 264), (1024, 5000, 1160)]
+         (2050, 2304, 256), (1, 24576, 256), (5, 40, 16384), (9473, 520, 264), (1024, 5000, 1160), (200, 1000, 2048), (257, 515, 1500),
+         (400, 1544, 4096), (65, 8, 16384)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -126,7 +127,7 @@ def test_products(M, N, K):
 
 @pytest.mark.parametrize("act", ["none", "gelu", "silu"])
 @pytest.mark.parametrize("bias,residual", [(True, False), (False, True), (True, True)])
-@pytest.mark.parametrize("M,N,K,extra", [(2, 333, 300, 1), (40, 260, 520, 0), (300, 1155, 384, 3), (1111, 2500, 200, 0), (5003, 1155, 384, 3)])
+@pytest.mark.parametrize("M,N,K,extra", [(2, 333, 300, 1), (40, 260, 520, 0), (300, 1155, 384, 3), (1111, 2500, 200, 0), (5003, 1155, 384, 3), (130, 523, 2100, 1), (70, 1031, 900, 0)])
 def test_epilogues(M, N, K, extra, bias, residual, act):
     rng = np.random.default_rng(M + N)
     s = _layer(rng, M, N, K, act, bias, residual, extra)
@@ -135,7 +136,7 @@ def test_epilogues(M, N, K, extra, bias, residual, act):
         assert (s["obuf"][:, N:] == 5.0).all()
 
 
-@pytest.mark.parametrize("M,N,K", [(7, 256, 512), (300, 640, 512), (2500, 2048, 256)])
+@pytest.mark.parametrize("M,N,K", [(7, 256, 512), (300, 640, 512), (300, 640, 2500), (2500, 2048, 256)])
 def test_residual_in_place_and_repeatable(M, N, K):
     rng = np.random.default_rng(5)
     s = _layer(rng, M, N, K, "none", True, True)
@@ -233,7 +234,7 @@ def test_on_a_side_stream_and_captured():
     np.testing.assert_array_equal(_f64(s["out"]), want)
 
 
-@pytest.mark.parametrize("M,N,K", [(3, 520, 2048), (40, 300, 1000), (1500, 4096, 400)])
+@pytest.mark.parametrize("M,N,K", [(3, 520, 2048), (40, 300, 1000), (1500, 4096, 400), (200, 300, 2048)])
 def test_without_clusters(M, N, K):
     """As on a part of a device that holds none: nothing is split, no pairs."""
     rng = np.random.default_rng(11)
