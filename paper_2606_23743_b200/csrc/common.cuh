@@ -207,6 +207,38 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
+// div_fast of two values: neg_s2 = -s twice, y2 = RN(1/s) twice.  The residual x - q0*s is exact, so that its rounding, downwards, chooses no more
+// than the sign of a zero: -0 from a zero x of either sign, which leaves q0 its own.
+__device__ __forceinline__ uint64_t div_fast2(uint64_t x2, uint64_t neg_s2, uint64_t y2) {
+  const uint64_t q0 = fma2(x2, y2, pack2(-0.f, -0.f));
+  uint64_t t;
+  asm("fma.rm.f32x2 %0, %1, %2, %3;" : "=l"(t) : "l"(q0), "l"(neg_s2), "l"(x2));
+  return fma2(t, y2, q0);
+}
+// amax / D, correctly rounded (D = 448, 2 688, 6); the general division outside of div_fast's range
+__device__ __noinline__ static float div_any(float a, float b) { return __fdiv_rn(a, b); }
+template <int D>
+__device__ __forceinline__ float div_by(float a) {
+  return a >= 8.077935669463161e-28f && a <= 3.4e38f ? div_fast(a, (float)D, 1.0f / D) : div_any(a, (float)D);      // (2^-90)
+}
+// four values to e4m3, eight to e2m1 (round to nearest even, saturating), the first in the lowest bits
+__device__ __forceinline__ uint32_t e4m3x4(uint64_t a, uint64_t b) {
+  uint32_t r;
+  asm("{\n\t.reg .f32 f0, f1, f2, f3;\n\t.reg .b16 h0, h1;\n\t"
+      "mov.b64 {f0, f1}, %1;\n\tmov.b64 {f2, f3}, %2;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 h0, f1, f0;\n\tcvt.rn.satfinite.e4m3x2.f32 h1, f3, f2;\n\t"
+      "mov.b32 %0, {h0, h1};\n\t}" : "=r"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t e2m1x8(uint64_t a, uint64_t b, uint64_t c, uint64_t d) {
+  uint32_t r;
+  asm("{\n\t.reg .f32 f0, f1, f2, f3, f4, f5, f6, f7;\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "mov.b64 {f0, f1}, %1;\n\tmov.b64 {f2, f3}, %2;\n\tmov.b64 {f4, f5}, %3;\n\tmov.b64 {f6, f7}, %4;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, f1, f0;\n\tcvt.rn.satfinite.e2m1x2.f32 b1, f3, f2;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, f5, f4;\n\tcvt.rn.satfinite.e2m1x2.f32 b3, f7, f6;\n\t"
+      "mov.b32 %0, {b0, b1, b2, b3};\n\t}" : "=r"(r) : "l"(a), "l"(b), "l"(c), "l"(d));
+  return r;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));

@@ -32,8 +32,6 @@ struct CacheParams {
   int32_t* status;
 };
 
-__device__ __noinline__ float cache_div_slow(float a, float b) { return __fdiv_rn(a, b); }
-
 // row of (page, head, place) among all rows
 __device__ __forceinline__ long long cache_row(const CacheParams& prm, long long page, int h, int place) {
   return (page * prm.H + h) * prm.page + place;
@@ -90,48 +88,46 @@ cache_write_kernel(const CacheParams prm) {
       if (!there || h0 + i >= he) continue;
       const long long row = cache_row(prm, page, h0 + i, place);
       const uint32_t w[8] = {in[i][0].x, in[i][0].y, in[i][0].z, in[i][0].w, in[i][1].x, in[i][1].y, in[i][1].z, in[i][1].w};
-      const float scale = amax == 0.f ? 1.0f : __fdiv_rn(amax, FP4 ? 2688.0f : 448.0f);
+      const float scale = amax == 0.f ? 1.0f : div_by<FP4 ? 2688 : 448>(amax);
       if (lane == 0) out.scale[row] = scale;
       if (!FP4) {
         uint32_t c[4];
         if (div_fast_ok(scale)) {
           const float rcp = __frcp_rn(scale);
+          const uint64_t neg2 = pack2(-scale, -scale), r2 = pack2(rcp, rcp);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            c[e] = __byte_perm(e4m3x2(div_fast(bf16lo(w[2 * e]), scale, rcp), div_fast(bf16hi(w[2 * e]), scale, rcp)),
-                               e4m3x2(div_fast(bf16lo(w[2 * e + 1]), scale, rcp), div_fast(bf16hi(w[2 * e + 1]), scale, rcp)), 0x5410);
+          for (int e = 0; e < 4; ++e) {
+            c[e] = e4m3x4(div_fast2(pack2(bf16lo(w[2 * e]), bf16hi(w[2 * e])), neg2, r2),
+                          div_fast2(pack2(bf16lo(w[2 * e + 1]), bf16hi(w[2 * e + 1])), neg2, r2));
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            c[e] = __byte_perm(e4m3x2(cache_div_slow(bf16lo(w[2 * e]), scale), cache_div_slow(bf16hi(w[2 * e]), scale)),
-                               e4m3x2(cache_div_slow(bf16lo(w[2 * e + 1]), scale), cache_div_slow(bf16hi(w[2 * e + 1]), scale)), 0x5410);
+            c[e] = __byte_perm(e4m3x2(div_any(bf16lo(w[2 * e]), scale), div_any(bf16hi(w[2 * e]), scale)),
+                               e4m3x2(div_any(bf16lo(w[2 * e + 1]), scale), div_any(bf16hi(w[2 * e + 1]), scale)), 0x5410);
         }
         *reinterpret_cast<uint4*>(out.codes + (row * LANES + lane) * 16) = make_uint4(c[0], c[1], c[2], c[3]);
       } else {
         // (own / 6) / scale, both quotients rounded: from reciprocals where that gives the rounded quotient (div_fast)
-        const bool quick = div_fast_ok(scale) && (own == 0.f || own >= 8.077935669463161e-28f);      // 2^-90
-        const float in6 = quick ? div_fast(own, 6.0f, 0.16666667163372039795f) : cache_div_slow(own, 6.0f);
-        const uint32_t sf = (uint32_t)__nv_cvt_float_to_fp8(quick ? div_fast(in6, scale, __frcp_rn(scale)) : cache_div_slow(in6, scale),
+        const float in6 = div_by<6>(own);
+        const uint32_t sf = (uint32_t)__nv_cvt_float_to_fp8(div_fast_ok(scale) && (own == 0.f || own >= 8.077935669463161e-28f)
+                                                                ? div_fast(in6, scale, __frcp_rn(scale)) : div_any(in6, scale),
                                                             __NV_SATFINITE, __NV_E4M3);
         const float unit = __fmul_rn(e4m3_to_float(sf), scale);
         uint32_t c[2] = {0u, 0u};
         if (unit > 0.f) {
           if (div_fast_ok(unit)) {                            // the same two values at a time
             const float rcp = __frcp_rn(unit);
-            const uint64_t u2 = pack2(unit, unit), r2 = pack2(rcp, rcp), nr2 = pack2(-rcp, -rcp), nz = pack2(-0.f, -0.f);
+            const uint64_t neg2 = pack2(-unit, -unit), r2 = pack2(rcp, rcp);
+            uint64_t y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const uint32_t neg = w[e] ^ 0x80008000u;
-              const uint64_t q0 = fma2(pack2(bf16lo(w[e]), bf16hi(w[e])), r2, nz);
-              const uint64_t res = fma2(q0, u2, pack2(bf16lo(neg), bf16hi(neg)));
-              float2 y;
-              unpack2(fma2(res, nr2, q0), y.x, y.y);
-              c[e >> 2] |= ((uint32_t)__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest) & 0xffu) << (8 * (e & 3));
-            }
+            for (int e = 0; e < 8; ++e) y[e] = div_fast2(pack2(bf16lo(w[e]), bf16hi(w[e])), neg2, r2);
+            c[0] = e2m1x8(y[0], y[1], y[2], y[3]);
+            c[1] = e2m1x8(y[4], y[5], y[6], y[7]);
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float2 y = make_float2(cache_div_slow(bf16lo(w[e]), unit), cache_div_slow(bf16hi(w[e]), unit));
+              const float2 y = make_float2(div_any(bf16lo(w[e]), unit), div_any(bf16hi(w[e]), unit));
               c[e >> 2] |= ((uint32_t)__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest) & 0xffu) << (8 * (e & 3));
             }
           }

@@ -11,8 +11,6 @@
 namespace sva {
 
 // ------------------------------------------------------------------ quantisers
-__device__ __noinline__ float lin_div_slow(float a, float b) { return __fdiv_rn(a, b); }
-
 // 16 consecutive values of a row of K from channel c (zeros beyond K); the row is 16-byte aligned and c a multiple of 16
 __device__ __forceinline__ void lin_load16(const __nv_bfloat16* row, int c, int K, uint4 (&u)[2]) {
   u[0] = u[1] = make_uint4(0u, 0u, 0u, 0u);
@@ -38,22 +36,23 @@ __device__ __forceinline__ float lin_amax(const uint4 (&u)[2]) {
   for (int e = 0; e < 8; ++e) asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(w[e] & 0x7fff7fffu));
   return __uint_as_float(max(m << 16, m & 0xffff0000u));
 }
-__device__ __forceinline__ float lin_scale(float amax) { return amax == 0.f ? 1.0f : __fdiv_rn(amax, 448.0f); }
+__device__ __forceinline__ float lin_scale(float amax) { return amax == 0.f ? 1.0f : div_by<448>(amax); }
 // the codes of 16 values: the correctly rounded fp32 quotients, rounded to e4m3
 __device__ __forceinline__ uint4 lin_codes(const uint4 (&u)[2], float s) {
   const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
   uint32_t c[4];
   if (div_fast_ok(s)) {
     const float r = __frcp_rn(s);
+    const uint64_t neg2 = pack2(-s, -s), r2 = pack2(r, r);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      c[e] = __byte_perm(e4m3x2(div_fast(bf16lo(w[2 * e]), s, r), div_fast(bf16hi(w[2 * e]), s, r)),
-                         e4m3x2(div_fast(bf16lo(w[2 * e + 1]), s, r), div_fast(bf16hi(w[2 * e + 1]), s, r)), 0x5410);
+      c[e] = e4m3x4(div_fast2(pack2(bf16lo(w[2 * e]), bf16hi(w[2 * e])), neg2, r2),
+                    div_fast2(pack2(bf16lo(w[2 * e + 1]), bf16hi(w[2 * e + 1])), neg2, r2));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      c[e] = __byte_perm(e4m3x2(lin_div_slow(bf16lo(w[2 * e]), s), lin_div_slow(bf16hi(w[2 * e]), s)),
-                         e4m3x2(lin_div_slow(bf16lo(w[2 * e + 1]), s), lin_div_slow(bf16hi(w[2 * e + 1]), s)), 0x5410);
+      c[e] = __byte_perm(e4m3x2(div_any(bf16lo(w[2 * e]), s), div_any(bf16hi(w[2 * e]), s)),
+                         e4m3x2(div_any(bf16lo(w[2 * e + 1]), s), div_any(bf16hi(w[2 * e + 1]), s)), 0x5410);
   }
   return make_uint4(c[0], c[1], c[2], c[3]);
 }
