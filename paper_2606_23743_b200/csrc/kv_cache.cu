@@ -3,7 +3,7 @@
 // (page id * page + place in the page); writing quantises into slots, reading collects a sequence's pages into the [B,H,N,d] tensors that the
 // attention calls take.
 //
-// Both are HBM-bound streaming passes.  d/16 lanes own a row, 16 channels each (one 4-bit scale block), so that a row's maximum is
+// Both are HBM-bound streaming passes (the 4-bit cast is bound by its instructions).  d/16 lanes own a row, 16 channels each (one 4-bit scale block), so that a row's maximum is
 // a few shuffles; a thread looks its token's slot up once and then has some heads' rows in flight.
 #include <cuda_fp4.h>
 
@@ -12,8 +12,7 @@
 namespace sva {
 
 static constexpr int CACHE_THREADS = 256;
-static constexpr int CACHE_HEADS = 4;                     // rows in flight per thread that is written from, and that is read:
-static constexpr int READ_HEADS = 2;                      // 2 x 47 616 tokens x 32 heads, e4m3, us: one 408, two 374, four 385, eight 433
+static constexpr int CACHE_HEADS = 4;                     // rows in flight per thread
 
 struct CacheArrays {                                      // one of K, V
   uint8_t* codes;
@@ -30,6 +29,7 @@ struct CacheParams {
   long long slot_count;
   int H, T, page, pages, max_pages, chunk, chunks;        // chunk: heads per CTA, chunks: CTAs per token tile and tensor
   int32_t* status;
+  bool wide;                                              // 32-byte stores into the bf16 tensors
 };
 
 // row of (page, head, place) among all rows
@@ -140,7 +140,7 @@ cache_write_kernel(const CacheParams prm) {
 }
 
 template <int LANES, bool FP4>
-__global__ void __launch_bounds__(CACHE_THREADS, 4)
+__global__ void __launch_bounds__(CACHE_THREADS, 5)
 cache_read_kernel(const CacheParams prm) {
   const int zero = grid_dep_wait();
   const int which = blockIdx.x & 1, part = (int)((blockIdx.x >> 1) % prm.chunks);
@@ -162,12 +162,12 @@ cache_read_kernel(const CacheParams prm) {
   }
   const int place = n - at * prm.page, hb = part * prm.chunk, he = min(hb + prm.chunk, prm.H);
   uint8_t* dst = (which ? prm.xv : prm.xk) + 2 * (b * s.b + (long long)n * s.n + lane * 16);
-  for (int h0 = hb; h0 < he; h0 += READ_HEADS) {
-    uint4 codes[READ_HEADS];
-    float scale[READ_HEADS];
-    uint32_t sf[READ_HEADS];
+  for (int h0 = hb; h0 < he; h0 += CACHE_HEADS) {
+    uint4 codes[CACHE_HEADS];
+    float scale[CACHE_HEADS];
+    uint32_t sf[CACHE_HEADS];
 #pragma unroll
-    for (int i = 0; i < READ_HEADS; ++i) {
+    for (int i = 0; i < CACHE_HEADS; ++i) {
       codes[i] = make_uint4(0u, 0u, 0u, 0u);
       scale[i] = 0.f;
       sf[i] = 0u;
@@ -184,7 +184,7 @@ cache_read_kernel(const CacheParams prm) {
       }
     }
 #pragma unroll
-    for (int i = 0; i < READ_HEADS; ++i) {
+    for (int i = 0; i < CACHE_HEADS; ++i) {
       if (h0 + i >= he) continue;
       uint32_t o[8];
       const uint32_t w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
@@ -203,20 +203,34 @@ cache_read_kernel(const CacheParams prm) {
         o[e] = *reinterpret_cast<const uint32_t*>(&v);
       }
       uint4* row = reinterpret_cast<uint4*>(dst + 2 * (h0 + i) * s.h);
-      row[0] = make_uint4(o[0], o[1], o[2], o[3]);
-      row[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
+      // 2 x 47 616 tokens x 32 heads, e4m3: 373 us in stores of 16 bytes, which touch every sector twice, 360 in stores of 32; (loads of 32 in the
+      // other kernel: 354 us, of 16, the L1 having the other half, 347)
+      if (prm.wide) {
+        stg32(row, lo, hi);
+      } else {
+        row[0] = lo;
+        row[1] = hi;
+      }
     }
   }
+}
+
+// whether every row of a tensor begins on 32 bytes
+static bool rows_on_32(const void* x, const Strides& s) {
+  return (reinterpret_cast<uintptr_t>(x) & 31u) == 0 && ((s.b | s.h | s.n) & 15) == 0;
 }
 
 static int launch_cache(bool write, CacheParams& prm, const sva_kv_cache_t* c, cudaStream_t st) {
   prm.k = CacheArrays{(uint8_t*)c->k_codes, c->k_scale, (uint8_t*)c->k_sf};
   prm.v = CacheArrays{(uint8_t*)c->v_codes, c->v_scale, (uint8_t*)c->v_sf};
   prm.H = c->H; prm.page = c->page; prm.pages = c->pages;
+  prm.wide = rows_on_32(prm.xk, prm.sk) && rows_on_32(prm.xv, prm.sv);
   const int lanes = c->d / 16;
   const long long tiles = (prm.tokens + CACHE_THREADS / lanes - 1) / (CACHE_THREADS / lanes);
   // Heads per CTA: eight, whose second half's loads find the slots and the table at hand, where the grid comes to sixteen CTAs per SM all the
-  // same.  2 x 47 616 tokens x 32 heads, e4m3, written / read (four rows in flight), us: four heads 396 / 427, eight 361 / 391, sixteen 350 / 397.
+  // same.  2 x 47 616 tokens x 32 heads, e4m3, written / read, us: four heads 375 / 358, eight 347 / 360, sixteen 350 / 362;
+  // 24 x 32 760 tokens, 4-bit: 114 / 88, 106 / 86, 108 / 88.
   prm.chunk = 2 * CACHE_HEADS;
   if (2 * tiles * ((c->H + prm.chunk - 1) / prm.chunk) < 148 * 16) prm.chunk = CACHE_HEADS;
   prm.chunks = (c->H + prm.chunk - 1) / prm.chunk;

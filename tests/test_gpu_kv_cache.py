@@ -189,3 +189,25 @@ def test_captured():
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(kg, ko) and torch.equal(vg, ko) and torch.equal(vo, ko)
+
+
+@pytest.mark.parametrize("form", ["e4m3", "fp4"])
+@pytest.mark.parametrize("d,pad,shift", [(64, 0, 8), (128, 8, 0), (64, 24, 8)])
+def test_read_into_rows_on_16_bytes(form, d, pad, shift):
+    """Rows that begin on 16 bytes but not on 32: the same values as in whole tensors, and nothing beside them."""
+    Bq, H, N, page = 2, 5, 21, 8
+    pages = Bq * 3
+    ka, va = _arrays(form, pages, H, page, d), _arrays(form, pages, H, page, d)
+    for t in ka + va:
+        t.copy_(torch.rand(t.shape, device="cuda") if t.dtype == torch.float32 else torch.randint(0, 100, t.shape, device="cuda"))
+    c = B.make_kv_cache(ka, va, form)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(Bq, 3)
+    lengths = torch.tensor([N, 9], dtype=torch.int32, device="cuda")
+    whole = [torch.empty(Bq, H, N, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    B.kv_cache_read(c, table, lengths, *whole)
+    row = d + pad
+    held = [torch.full((shift + Bq * H * N * row,), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    parts = [h[shift:].view(Bq, H, N, row) for h in held]
+    B.kv_cache_read(c, table, lengths, *[p[..., :d] for p in parts])
+    for w, p, h in zip(whole, parts, held):
+        assert torch.equal(w, p[..., :d]) and bool((p[..., d:] == 7.0).all()) and bool((h[:shift] == 7.0).all())
