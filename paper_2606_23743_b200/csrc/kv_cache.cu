@@ -37,13 +37,62 @@ __device__ __forceinline__ long long cache_row(const CacheParams& prm, long long
   return (page * prm.H + h) * prm.page + place;
 }
 
-// the largest magnitude of 16 bf16 values, as fp32
-__device__ __forceinline__ float cache_amax(const uint4& a, const uint4& b) {
+// The casts of a lane's 16 values by general divisions: rows whose scale is far out (zero, infinite, 1e-12 and less) or has a significand of ones.
+struct Cast { uint4 codes; float scale; uint32_t sf; };
+template <bool FP4>
+__device__ __noinline__ Cast cache_cast_any(uint4 a, uint4 b, float amax, float own) {
   const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  uint32_t m = 0u;
+  Cast o;
+  o.codes = make_uint4(0u, 0u, 0u, 0u);
+  o.sf = 0u;
+  uint32_t c[4] = {0u, 0u, 0u, 0u};
+  o.scale = amax == 0.f ? 1.0f : __fdiv_rn(amax, FP4 ? 2688.0f : 448.0f);
+  float unit = o.scale;
+  if (FP4) {
+    o.sf = (uint32_t)__nv_cvt_float_to_fp8(__fdiv_rn(__fdiv_rn(own, 6.0f), o.scale), __NV_SATFINITE, __NV_E4M3);
+    unit = __fmul_rn(e4m3_to_float(o.sf), o.scale);
+    if (!(unit > 0.f)) {
+      o.sf = 0u;
+      return o;
+    }
+  }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(w[e] & 0x7fff7fffu));
-  return __uint_as_float(max(m << 16, m & 0xffff0000u));
+  for (int e = 0; e < 8; ++e) {
+    const float lo = __fdiv_rn(bf16lo(w[e]), unit), hi = __fdiv_rn(bf16hi(w[e]), unit);
+    if (FP4) c[e >> 2] |= ((uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(lo, hi), __NV_E2M1, cudaRoundNearest) & 0xffu) << (8 * (e & 3));
+    else c[e >> 1] |= e4m3x2(lo, hi) << (16 * (e & 1));
+  }
+  o.codes = make_uint4(c[0], c[1], c[2], c[3]);
+  return o;
+}
+
+// The same with quotients from reciprocals (div_fast).  In a row whose amax is in [2^-38, 2^60] every divisor is in div_fast's range, and a 4-bit
+// block's maximum that is too small for it gives a scale of zero in any case.
+template <bool FP4>
+__device__ __forceinline__ Cast cache_cast(const uint4& a, const uint4& b, float amax, float own) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  Cast o;
+  o.scale = div_fast(amax, FP4 ? 2688.0f : 448.0f, FP4 ? 1.0f / 2688.0f : 1.0f / 448.0f);
+  o.sf = 0u;
+  float unit = o.scale, rcp = __frcp_rn(o.scale);
+  bool ones = (__float_as_uint(o.scale) & 0x7fffffu) == 0x7fffffu;
+  if (FP4) {
+    o.sf = (uint32_t)__nv_cvt_float_to_fp8(div_fast(div_fast(own, 6.0f, 1.0f / 6.0f), o.scale, rcp), __NV_SATFINITE, __NV_E4M3);
+    unit = __fmul_rn(e4m3_to_float(o.sf), o.scale);
+    rcp = __frcp_rn(unit);
+    ones |= (__float_as_uint(unit) & 0x7fffffu) == 0x7fffffu;
+  }
+  if (!(amax >= 3.637978807091713e-12f && amax <= 1.152921504606847e18f) || ones) return cache_cast_any<FP4>(a, b, amax, own);
+  const uint64_t neg2 = pack2(-unit, -unit), r2 = pack2(rcp, rcp);
+  uint64_t y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = div_fast2(pack2(bf16lo(w[e]), bf16hi(w[e])), neg2, r2);
+  if (FP4) {
+    o.codes = make_uint4(o.sf ? e2m1x8(y[0], y[1], y[2], y[3]) : 0u, o.sf ? e2m1x8(y[4], y[5], y[6], y[7]) : 0u, 0u, 0u);
+  } else {
+    o.codes = make_uint4(e4m3x4(y[0], y[1]), e4m3x4(y[2], y[3]), e4m3x4(y[4], y[5]), e4m3x4(y[6], y[7]));
+  }
+  return o;
 }
 
 template <int LANES, bool FP4>
@@ -66,75 +115,42 @@ cache_write_kernel(const CacheParams prm) {
   const long long b = there ? t / prm.T : 0, n = there ? t - b * prm.T : 0;
   const long long page = there ? slot / prm.page : 0;
   const int place = there ? (int)(slot - page * prm.page) : 0;
-  const int hb = part * prm.chunk, he = min(hb + prm.chunk, prm.H);
-  const uint8_t* src = (which ? prm.xv : prm.xk) + 2 * (b * s.b + n * s.n + lane * 16);
-  for (int h0 = hb; h0 < he; h0 += CACHE_HEADS) {
+  const int hb = part * prm.chunk, he = there ? min(hb + prm.chunk, prm.H) : 0;
+  const uint8_t* src = (which ? prm.xv : prm.xk) + 2 * (b * s.b + n * s.n + hb * s.h + lane * 16);
+  const long long row = cache_row(prm, page, hb, place);
+  constexpr int BYTES = FP4 ? 8 : 16;
+  uint8_t *codes = out.codes + (row * LANES + lane) * BYTES, *sf = FP4 ? out.sf + row * LANES + lane : nullptr;
+  float* scale = out.scale + row;
+  for (int h0 = hb; h0 < hb + prm.chunk; h0 += CACHE_HEADS) {
     uint4 in[CACHE_HEADS][2];
 #pragma unroll
     for (int i = 0; i < CACHE_HEADS; ++i) {
       in[i][0] = in[i][1] = make_uint4(0u, 0u, 0u, 0u);
-      if (there && h0 + i < he) {
-        const uint4* row = reinterpret_cast<const uint4*>(src + 2 * (h0 + i) * s.h);
-        in[i][0] = __ldg(row);
-        in[i][1] = __ldg(row + 1);
+      if (h0 + i < he) {
+        in[i][0] = __ldg(reinterpret_cast<const uint4*>(src));
+        in[i][1] = __ldg(reinterpret_cast<const uint4*>(src) + 1);
       }
+      src += 2 * s.h;
     }
 #pragma unroll
     for (int i = 0; i < CACHE_HEADS; ++i) {
-      const float own = cache_amax(in[i][0], in[i][1]);
+      const float own = bf16_amax(in[i][0], in[i][1]);
       float amax = own;
 #pragma unroll
       for (int o = LANES / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      if (!there || h0 + i >= he) continue;
-      const long long row = cache_row(prm, page, h0 + i, place);
-      const uint32_t w[8] = {in[i][0].x, in[i][0].y, in[i][0].z, in[i][0].w, in[i][1].x, in[i][1].y, in[i][1].z, in[i][1].w};
-      const float scale = amax == 0.f ? 1.0f : div_by<FP4 ? 2688 : 448>(amax);
-      if (lane == 0) out.scale[row] = scale;
-      if (!FP4) {
-        uint32_t c[4];
-        if (div_fast_ok(scale)) {
-          const float rcp = __frcp_rn(scale);
-          const uint64_t neg2 = pack2(-scale, -scale), r2 = pack2(rcp, rcp);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            c[e] = e4m3x4(div_fast2(pack2(bf16lo(w[2 * e]), bf16hi(w[2 * e])), neg2, r2),
-                          div_fast2(pack2(bf16lo(w[2 * e + 1]), bf16hi(w[2 * e + 1])), neg2, r2));
-          }
+      if (h0 + i < he) {
+        const Cast x = cache_cast<FP4>(in[i][0], in[i][1], amax, own);
+        if (lane == 0) *scale = x.scale;
+        if (FP4) {
+          *sf = (uint8_t)x.sf;
+          *reinterpret_cast<uint2*>(codes) = make_uint2(x.codes.x, x.codes.y);
         } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            c[e] = __byte_perm(e4m3x2(div_any(bf16lo(w[2 * e]), scale), div_any(bf16hi(w[2 * e]), scale)),
-                               e4m3x2(div_any(bf16lo(w[2 * e + 1]), scale), div_any(bf16hi(w[2 * e + 1]), scale)), 0x5410);
+          *reinterpret_cast<uint4*>(codes) = x.codes;
         }
-        *reinterpret_cast<uint4*>(out.codes + (row * LANES + lane) * 16) = make_uint4(c[0], c[1], c[2], c[3]);
-      } else {
-        // (own / 6) / scale, both quotients rounded: from reciprocals where that gives the rounded quotient (div_fast)
-        const float in6 = div_by<6>(own);
-        const uint32_t sf = (uint32_t)__nv_cvt_float_to_fp8(div_fast_ok(scale) && (own == 0.f || own >= 8.077935669463161e-28f)
-                                                                ? div_fast(in6, scale, __frcp_rn(scale)) : div_any(in6, scale),
-                                                            __NV_SATFINITE, __NV_E4M3);
-        const float unit = __fmul_rn(e4m3_to_float(sf), scale);
-        uint32_t c[2] = {0u, 0u};
-        if (unit > 0.f) {
-          if (div_fast_ok(unit)) {                            // the same two values at a time
-            const float rcp = __frcp_rn(unit);
-            const uint64_t neg2 = pack2(-unit, -unit), r2 = pack2(rcp, rcp);
-            uint64_t y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = div_fast2(pack2(bf16lo(w[e]), bf16hi(w[e])), neg2, r2);
-            c[0] = e2m1x8(y[0], y[1], y[2], y[3]);
-            c[1] = e2m1x8(y[4], y[5], y[6], y[7]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 y = make_float2(div_any(bf16lo(w[e]), unit), div_any(bf16hi(w[e]), unit));
-              c[e >> 2] |= ((uint32_t)__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest) & 0xffu) << (8 * (e & 3));
-            }
-          }
-        }
-        out.sf[row * LANES + lane] = unit > 0.f ? (uint8_t)sf : (uint8_t)0;
-        *reinterpret_cast<uint2*>(out.codes + (row * LANES + lane) * 8) = make_uint2(c[0], c[1]);
       }
+      codes += (long long)prm.page * LANES * BYTES;
+      if (FP4) sf += (long long)prm.page * LANES;
+      scale += prm.page;
     }
   }
 }

@@ -29,13 +29,6 @@ __device__ __forceinline__ void lin_load16(const __nv_bfloat16* row, int c, int 
     u[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
-__device__ __forceinline__ float lin_amax(const uint4 (&u)[2]) {
-  const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
-  uint32_t m = 0u;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(w[e] & 0x7fff7fffu));
-  return __uint_as_float(max(m << 16, m & 0xffff0000u));
-}
 __device__ __forceinline__ float lin_scale(float amax) { return amax == 0.f ? 1.0f : div_by<448>(amax); }
 // the codes of 16 values: the correctly rounded fp32 quotients, rounded to e4m3
 __device__ __forceinline__ uint4 lin_codes(const uint4 (&u)[2], float s) {
@@ -75,7 +68,7 @@ quantize_rows_kernel(const __nv_bfloat16* __restrict__ x, int M, int K, long lon
   for (int i = 0; i < GROUPS; ++i) lin_load16(row, (g0 + i) * 128 + lane * 16, there ? K : 0, u[i]);
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) {
-    float amax = lin_amax(u[i]);
+    float amax = bf16_amax(u[i][0], u[i][1]);
 #pragma unroll
     for (int o = 4; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     const int c = (g0 + i) * 128 + lane * 16;
@@ -99,7 +92,7 @@ quantize_tiles_kernel(const __nv_bfloat16* __restrict__ w, int N, int K, long lo
   for (int i = 0; i < 4; ++i) {
     const int n = J * 128 + i * 32 + (threadIdx.x >> 3);
     lin_load16(w + (long long)(n < N ? n : 0) * ws, c, n < N ? K : 0, u[i]);
-    amax = fmaxf(amax, lin_amax(u[i]));
+    amax = fmaxf(amax, bf16_amax(u[i][0], u[i][1]));
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
