@@ -64,11 +64,14 @@ __device__ __forceinline__ uint4 rope_store8(const float (&x)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A thread owns 8 channels (a 16-byte vector), the lanes of a token lie in one warp.
-// FORM 0: interleaved, 4 pairs.
-// FORM 1: half layout whose halves are whole vectors: 8 pairs, whose other halves a lane of the same token holds: they come by shuffles.
-// FORM 2: half layout otherwise: the partners lie at no fixed place of a vector: they come through shared memory.
-// In forms 1 and 2 all lanes of a token have read a row before any of them writes it, so in place is safe.
+// A thread owns 8 channels, the lanes of a token lie in one warp.
+// FORM 0: interleaved: a 16-byte vector, 4 pairs.
+// FORM 1: half layout whose halves are whole 8-byte pieces: 4 pairs again, from one piece of each half; behind the rotated channels 16 bytes.
+// FORM 2: half layout otherwise: a 16-byte vector, whose partners lie at no fixed place of another: they come through shared memory.  All
+// lanes of a token have read a row before any of them writes it, so in place is safe (in the other forms a thread writes what it read).
+// Form 1 with 16-byte vectors and the partners by shuffles, twice the phases and half the loads: 2 x 8 191 tokens, 32 + 8 heads of 64 rotated
+// channels of 128 61.4 us, so 56.7; 16 + 16 heads of 128, 8 190 tokens, 29.6, so 24.1; one token of
+// 8 x (32 + 8) heads 3.9, so 2.7.
 template <int FORM>
 __global__ void __launch_bounds__(ROPE_THREADS, FORM == 2 ? 3 : 4)
 rope_kernel(const RopeParams prm, int lanes) {
@@ -76,9 +79,11 @@ rope_kernel(const RopeParams prm, int lanes) {
   const int zero = grid_dep_wait();
   const int tile_chunk = blockIdx.x % prm.chunks;
   const long long tile = blockIdx.x / prm.chunks;
-  const int u = threadIdx.x % lanes, c0 = u * 8;
+  const int u = threadIdx.x % lanes;
+  const bool split = FORM == 1 && u < prm.half / 4;       // the thread's channels lie in two places
+  const int c0 = split ? u * 4 : u * 8, c1 = split ? c0 + prm.half : c0 + 4;          // its first channel, its fifth
   const long long t = tile * (ROPE_THREADS / lanes) + threadIdx.x / lanes + zero;
-  const bool mine = t < prm.tokens && c0 < prm.d;
+  const bool mine = t < prm.tokens && u * 8 < prm.d;
   const long long b = mine ? t / prm.N : 0, n = mine ? t - b * prm.N : 0;
   const bool is_k = tile_chunk >= prm.q_chunks;
   const int h0 = (is_k ? tile_chunk - prm.q_chunks : tile_chunk) * prm.chunk, h1 = min(h0 + prm.chunk, is_k ? prm.Hk : prm.Hq);
@@ -86,32 +91,38 @@ rope_kernel(const RopeParams prm, int lanes) {
   const uint8_t* src = (is_k ? prm.k : prm.q) + 2 * (b * si.b + n * si.n + c0);
   uint8_t* dst = (is_k ? prm.ko : prm.qo) + 2 * (b * so.b + n * so.n + c0);
 
+  const int far = 2 * (c1 - c0);                          // bytes
+
   uint4 in[ROPE_HEADS];
   auto load = [&](int h) {
 #pragma unroll
     for (int i = 0; i < ROPE_HEADS; ++i) {
       in[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (mine && h + i < h1) in[i] = *reinterpret_cast<const uint4*>(src + 2 * (h + i) * si.h);
+      if (!mine || h + i >= h1) continue;
+      const uint8_t* row = src + 2 * (h + i) * si.h;
+      if (FORM == 1) {
+        const uint2 a = *reinterpret_cast<const uint2*>(row), b = *reinterpret_cast<const uint2*>(row + far);
+        in[i] = make_uint4(a.x, a.y, b.x, b.y);
+      } else {
+        in[i] = *reinterpret_cast<const uint4*>(row);
+      }
     }
   };
   load(h0);
-  Turn turn[FORM == 0 ? 4 : 8];                           // one per pair, or one per channel
+  Turn turn[FORM == 2 ? 8 : 4];                           // one per pair, or one per channel
   const int32_t* pos = prm.pos + b * prm.pos_batch + n;
   const unsigned long long* steps = prm.steps + zero;
 #pragma unroll
-  for (int e = 0; e < (FORM == 0 ? 4 : 8); ++e) {
-    const int c = c0 + e;
-    if (FORM == 0) {
-      turn[e] = mine ? rope_turn(prm, steps, pos, c0 / 2 + e) : Turn{1.f, 0.f};
-    } else {
+  for (int e = 0; e < (FORM == 2 ? 8 : 4); ++e) {
+    if (FORM == 2) {
+      const int c = c0 + e;
       turn[e] = mine && c < 2 * prm.half ? rope_turn(prm, steps, pos, c < prm.half ? c : c - prm.half) : Turn{1.f, 0.f};
       if (c < prm.half) turn[e].s = -turn[e].s;           // first of a pair: a c - b s; second: b c + a s
+    } else {
+      turn[e] = mine ? rope_turn(prm, steps, pos, 4 * u + e) : Turn{1.f, 0.f};
     }
   }
-  const int words = prm.half - c0 / 2;                    // 4-byte words of the vector that are rotated, if fewer than 4
-  // the lane that has the other halves (form 1)
-  const int other = c0 < prm.half ? u + prm.half / 8 : c0 < 2 * prm.half ? u - prm.half / 8 : u;
-  const int from = (threadIdx.x & 31) - u + other;
+  const int words = FORM == 1 ? (split ? 4 : 0) : prm.half - c0 / 2;          // 4-byte words of the thread that are rotated, if fewer than 4
   for (int h = h0; h < h1; h += ROPE_HEADS) {
     if (h > h0) load(h);
     if (FORM == 2) {
@@ -127,15 +138,8 @@ rope_kernel(const RopeParams prm, int lanes) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) rope_pair(x[2 * e], x[2 * e + 1], turn[e]);
       } else if (FORM == 1) {
-        uint4 w;
-        w.x = __shfl_sync(0xffffffffu, in[i].x, from);
-        w.y = __shfl_sync(0xffffffffu, in[i].y, from);
-        w.z = __shfl_sync(0xffffffffu, in[i].z, from);
-        w.w = __shfl_sync(0xffffffffu, in[i].w, from);
-        float y[8];
-        rope_load8(w, y);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * turn[e].c + y[e] * turn[e].s;
+        for (int e = 0; e < 4; ++e) rope_pair(x[e], x[e + 4], turn[e]);
       } else {
         // the token's row begins at its first lane's vector
         const __nv_bfloat16* held = reinterpret_cast<const __nv_bfloat16*>(stage + (i * ROPE_THREADS + threadIdx.x - u) * 16);
@@ -152,7 +156,14 @@ rope_kernel(const RopeParams prm, int lanes) {
         if (words < 3) o.z = in[i].z;
         o.w = in[i].w;
       }
-      if (mine && h + i < h1) *reinterpret_cast<uint4*>(dst + 2 * (h + i) * so.h) = o;
+      if (!mine || h + i >= h1) continue;
+      uint8_t* row = dst + 2 * (h + i) * so.h;
+      if (FORM == 1) {
+        *reinterpret_cast<uint2*>(row) = make_uint2(o.x, o.y);
+        *reinterpret_cast<uint2*>(row + far) = make_uint2(o.z, o.w);
+      } else {
+        *reinterpret_cast<uint4*>(row) = o;
+      }
     }
     if (FORM == 2) __syncwarp();
   }
@@ -174,16 +185,17 @@ int launch_rope(const sva_rope_t* p, const void* q, const void* k, const void* s
   prm.factor = p->factor;
   prm.sin_factor = p->inverse ? -p->factor : p->factor;
 
-  const int form = p->layout == SVA_ROPE_INTERLEAVED ? 0 : prm.half % 8 == 0 ? 1 : 2;
+  const int form = p->layout == SVA_ROPE_INTERLEAVED ? 0 : prm.half % 4 == 0 ? 1 : 2;
   int lanes = 1;
   while (lanes < prm.d / 8) lanes *= 2;
   const long long tiles = (prm.tokens + ROPE_THREADS / lanes - 1) / (ROPE_THREADS / lanes);
-  // Heads per CTA: they share the phases, but the grid should come to eight CTAs per SM; fewer than a thread has in flight gain nothing.
-  // 2 x 8 191 tokens, 32 + 8 heads: up to 32 heads 56.8 us, up to 16 53.4, but 8 192 tokens x 16 + 16 heads then 28.6 instead of 23.8;
-  // 1 024 tokens x 8 + 8: one head per CTA 10.7, four 4.6.
-  prm.chunk = 8 * ROPE_HEADS;
+  // Heads per CTA, which share the phases: sixteen, or fewer while there are not two CTAs per SM; fewer than a thread has in flight gain nothing.
+  // us, up to 32 / 16 / 8 / 4: 2 x 8 191 tokens of 32 + 8 heads 56.9 / 53.1 / 52.7 / 64.4, 32 760 of 24 + 24 124.7 / 123.6 / 126.1 / 152.5, 4 096 of
+  // 40 + 8 18.9 / 17.5 / 17.5 / 21.8, 64 of 32 + 8 7.0 / 4.7 / 3.5 / 2.9.  Where 16 leave less than two CTAs per SM, them / the rule: 1 000 of
+  // 32 + 8 6.4 / 5.7, 700 of 64 + 8 6.3 / 5.7, but 1 024 of 16 + 16 4.5 / 5.3.
+  prm.chunk = 4 * ROPE_HEADS;
   auto ctas = [&](int chunk) { return tiles * ((prm.Hq + chunk - 1) / chunk + (prm.Hk + chunk - 1) / chunk); };
-  while (prm.chunk > ROPE_HEADS && ctas(prm.chunk) < 148 * 8) prm.chunk /= 2;
+  while (prm.chunk > ROPE_HEADS && ctas(prm.chunk) < 148 * 2) prm.chunk /= 2;
   prm.q_chunks = (prm.Hq + prm.chunk - 1) / prm.chunk;
   prm.chunks = prm.q_chunks + (prm.Hk + prm.chunk - 1) / prm.chunk;
   if (tiles * prm.chunks > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;

@@ -181,3 +181,20 @@ def test_captured():
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("d,R", [(64, 8), (64, 24), (128, 40), (72, 72), (8, 8), (256, 200)])
+@pytest.mark.parametrize("N", [1, 33])
+def test_halves_of_whole_pieces_of_four(d, R, N):
+    """Half layout, halves of four channels times an odd number, and even ones; heads beyond those that a CTA takes; what is behind keeps its bits."""
+    rng = np.random.default_rng(d + R + N)
+    q, k = _tensor(rng, (2, 18, N, d), True), _tensor(rng, (2, 5, N, d), False)
+    q[0, 1, 0, R:] = float("nan")
+    pos = np.broadcast_to(np.arange(N) + 1000, (1, 2, N))
+    steps, _ = B.rope_steps(R, device="cuda")
+    positions = torch.from_numpy(np.ascontiguousarray(pos).astype(np.int32)).cuda()
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    B.rope(B.make_rope(q, k, qo, ko, positions, R, "half"), q, k, steps, positions, qo, ko)
+    assert torch.equal(qo[..., R:].contiguous().view(torch.int16), q[..., R:].contiguous().view(torch.int16))
+    for x, y in ((q[..., :R], qo[..., :R]), (k, ko)):
+        _check(_f64(y), _f64(x), L.frequencies([R // 2]), pos, [R // 2], R, "half")
