@@ -189,13 +189,16 @@ int launch_rope(const sva_rope_t* p, const void* q, const void* k, const void* s
   int lanes = 1;
   while (lanes < prm.d / 8) lanes *= 2;
   const long long tiles = (prm.tokens + ROPE_THREADS / lanes - 1) / (ROPE_THREADS / lanes);
-  // Heads per CTA, which share the phases: sixteen, or fewer while there are not two CTAs per SM; fewer than a thread has in flight gain nothing.
-  // us, up to 32 / 16 / 8 / 4: 2 x 8 191 tokens of 32 + 8 heads 56.9 / 53.1 / 52.7 / 64.4, 32 760 of 24 + 24 124.7 / 123.6 / 126.1 / 152.5, 4 096 of
-  // 40 + 8 18.9 / 17.5 / 17.5 / 21.8, 64 of 32 + 8 7.0 / 4.7 / 3.5 / 2.9.  Where 16 leave less than two CTAs per SM, them / the rule: 1 000 of
-  // 32 + 8 6.4 / 5.7, 700 of 64 + 8 6.3 / 5.7, but 1 024 of 16 + 16 4.5 / 5.3.
-  prm.chunk = 4 * ROPE_HEADS;
+  // Heads per CTA, which share the phases: equal shares of the heads, of up to 24, or fewer while there are not two CTAs per SM; fewer than a
+  // thread has in flight gain nothing.
+  // us, up to 32 / 16 / 8 / 4: 2 x 8 191 tokens of 32 + 8 heads 56.9 / 53.1 / 52.7 / 64.4, 4 096 of 40 + 8 18.9 / 17.5 / 17.5 / 21.8, 64 of 32 + 8
+  // 7.0 / 4.7 / 3.5 / 2.9; 32 760 of 24 + 24, 24 heads 126.2, 16 128.4, 12 128.0.  Where 16 leave less than two CTAs per SM, them / the rule: 1 000 of
+  // 32 + 8 6.4 / 5.7, 2 048 of 24 + 24 10.4 / 8.7, but 1 024 of 16 + 16 4.5 / 5.3.
+  const int most = prm.Hq > prm.Hk ? prm.Hq : prm.Hk, shares = most / 24 + (most % 24 != 0);
+  auto whole = [](int heads) { return (heads + ROPE_HEADS - 1) / ROPE_HEADS * ROPE_HEADS; };
+  prm.chunk = whole(most / shares + (most % shares != 0));
   auto ctas = [&](int chunk) { return tiles * ((prm.Hq + chunk - 1) / chunk + (prm.Hk + chunk - 1) / chunk); };
-  while (prm.chunk > ROPE_HEADS && ctas(prm.chunk) < 148 * 2) prm.chunk /= 2;
+  while (prm.chunk > ROPE_HEADS && ctas(prm.chunk) < 148 * 2) prm.chunk = whole(prm.chunk / 2);
   prm.q_chunks = (prm.Hq + prm.chunk - 1) / prm.chunk;
   prm.chunks = prm.q_chunks + (prm.Hk + prm.chunk - 1) / prm.chunk;
   if (tiles * prm.chunks > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
