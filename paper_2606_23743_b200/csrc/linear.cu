@@ -179,18 +179,21 @@ __device__ __forceinline__ void lin_tile(int i, int mt, int nt, int& m, int& n) 
 // Warps: eight sum, a thread owning one token and half of the tile's columns; then one that loads, one that issues the MMAs, one that brings the
 // scales, one that sees to the staging tiles (bias, residual, stores).
 namespace lin {
-constexpr uint32_t A_BYTES = 128 * 128, STAGE = 2 * A_BYTES;
+constexpr uint32_t A_BYTES = 128 * 128, GROUP = 2 * A_BYTES;
 constexpr uint32_t OUT_BYTES = 128 * 128;                 // staging tile, 128 tokens x 64 columns of bf16
-template <bool PAIR> struct Shape {                       // (227 KB: the staging tiles of all columns, the rest is ring)
-  static constexpr int SIDE = PAIR ? 256 : 128, BUFS = 512 / SIDE, COLS = SIDE / 2, SUM_WARPS = 8;      // columns of a sum warp,
-  static constexpr int UNITS = SIDE / 128;                // an accumulator is one or two units of 128 columns with barriers of their own
-  static constexpr int THREADS = 32 * (SUM_WARPS + 4), SLOTS = 2 * BUFS, SLOT = SIDE;      // scale slots, floats of one
-  static constexpr int STAGES = PAIR ? 4 : 5, AHEAD = PAIR ? 2 : 4;      // (a group of a single CTA takes a third of a pair's)
-  static constexpr uint32_t OUT = STAGES * STAGE;
-  static constexpr int SMEM = 1024 + OUT + SIDE / 64 * OUT_BYTES;
+constexpr int BUFS = 2, ACC = 256, SLOTS = 2 * BUFS;      // accumulators and their columns; scale slots, a float per column quarter and token
+template <bool PAIR> struct Shape {
+  static constexpr int SIDE = PAIR ? 256 : 128, COLS = SIDE / 2, SUM_WARPS = 8;      // columns of a sum warp
+  static constexpr int TURN = PAIR ? 1 : 2;                 // groups of inputs per stage and accumulator
+  static constexpr int UNITS = SIDE / 128;                  // an accumulator is one or two units with barriers of their own
+  static constexpr int THREADS = 32 * (SUM_WARPS + 4);
+  static constexpr int STAGES = PAIR ? 4 : 3, AHEAD = PAIR ? 2 : 4;      // groups whose scales are fetched together
+  static constexpr uint32_t STAGE = TURN * GROUP, OUT = STAGES * STAGE;
+  static constexpr int SMEM = 1024 + OUT + (PAIR ? SIDE / 64 * OUT_BYTES : 0);
   // registers of a thread that sums and of the others; the launch has 168 for each
   static constexpr int SUM_REGS = 216, HELPER_REGS = 72;
   static_assert(32 * SUM_WARPS * SUM_REGS + 128 * HELPER_REGS <= THREADS * 168, "setmaxnreg draws on the registers of the launch");
+  static_assert(PAIR || SIDE * SIDE * 4 <= OUT, "the ring takes the sums that are exchanged");
 };
 }
 
@@ -200,13 +203,13 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
               const __grid_constant__ CUtensorMap tm_r, const LinearParams prm, int split) {
   using namespace lin;
   using S = Shape<PAIR>;
-  constexpr int STAGES = S::STAGES, SIDE = S::SIDE, BUFS = S::BUFS, SLOTS = S::SLOTS, SLOT = S::SLOT;
-  constexpr int COLS = S::COLS, UNITS = S::UNITS, LOADER = S::SUM_WARPS;
+  constexpr int STAGES = S::STAGES, SIDE = S::SIDE, COLS = S::COLS, UNITS = S::UNITS, TURN = S::TURN, LOADER = S::SUM_WARPS;
+  constexpr uint32_t STAGE = S::STAGE;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ __align__(8) unsigned long long bars[2 * STAGES + 2 * BUFS * UNITS + 4];
   __shared__ __align__(16) float bias_s[2][COLS];
-  __shared__ float scale_s[SLOTS][SLOT];                   // x_scale * w_scale of a group: [weights block of 128][token]
+  __shared__ float scale_s[SLOTS][256];                    // x_scale * w_scale: [weights block of 128, or group][token]
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_s;
   volatile int* abort_flag = &abort_s;
@@ -222,7 +225,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
   const int Kb = SPLIT ? (prm.Kb - part + split - 1) / split : prm.Kb;
   auto group = [&](int g) { return SPLIT ? part + g * split : g; };
   if (threadIdx.x == 0) {
-    for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+    for (int i = 0; i < STAGES; ++i) { mbar_init(bar_full + 8 * i, PAIR ? 1 : 2); mbar_init(bar_empty + 8 * i, 1); }
     for (int i = 0; i < BUFS * UNITS; ++i) {              // full: by the MMAs and the scales; free: by eight warps, a pair's four in each CTA
       mbar_init(bar_acc + 8 * i, 2);
       mbar_init(bar_free + 8 * i, 8);
@@ -233,8 +236,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     prefetch_tmap(&tm_x);
     prefetch_tmap(&tm_w);
-    prefetch_tmap(&tm_o);
-    if (prm.residual) prefetch_tmap(&tm_r);
+    if (PAIR) prefetch_tmap(&tm_o);
+    if (PAIR && prm.residual) prefetch_tmap(&tm_r);
   }
   if (warp == LOADER + 1) {
     if (PAIR) {
@@ -254,9 +257,10 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 
   if (warp >= LOADER) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::HELPER_REGS));
-    if (warp == LOADER) {
-      // ---- loads; in a pair, the first CTA's barrier waits for the bytes of both
+    if (warp == LOADER || (!PAIR && warp == LOADER + 3)) {
+      // ---- loads; in a pair, the first CTA's barrier waits for the bytes of both; else a warp loads x, another w
       const uint32_t bar_lead = PAIR ? mapa(bar_full, 0) : bar_full;
+      const bool loads_w = warp != LOADER;
       bool ok = true;
       int st = 0;
       uint32_t ph = 0;
@@ -264,7 +268,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         int m, n;
         lin_tile(i, mt, nt, m, n);
         const int m0 = m * SIDE + rank * 128, n0 = n * SIDE + rank * 64;
-        for (int g = 0; g < Kb; ++g) {
+        for (int g = 0; g < Kb; g += TURN) {
           ok = lin_wait(bar_empty + 8 * st, ph ^ 1u, abort_flag);
           if (!ok) break;
           if ((prm.debug & 1024) && g > 0) break;                              // test aid: the ring runs dry
@@ -276,9 +280,12 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
               tma_load_2d_pair(dst + A_BYTES, &tm_w, bar_lead + 8 * st, g * 128, n0);               // this CTA's half of unit 0,
               tma_load_2d_pair(dst + A_BYTES + 64 * 128, &tm_w, bar_lead + 8 * st, g * 128, n0 + 128);       // of unit 1
             } else {
-              mbar_expect_tx(bar_full + 8 * st, STAGE);
-              tma_load_2d(dst, &tm_x, bar_full + 8 * st, group(g) * 128, m0);
-              tma_load_2d(dst + A_BYTES, &tm_w, bar_full + 8 * st, group(g) * 128, n0);
+              const CUtensorMap* tm = loads_w ? &tm_w : &tm_x;
+              const uint32_t to = dst + (loads_w ? A_BYTES : 0u);
+              const int row = loads_w ? n0 : m0;
+              mbar_expect_tx(bar_full + 8 * st, (g + 1 < Kb ? 2 : 1) * A_BYTES);
+              tma_load_2d(to, tm, bar_full + 8 * st, group(g) * 128, row);
+              if (g + 1 < Kb && !(prm.debug & 1024)) tma_load_2d(to + GROUP, tm, bar_full + 8 * st, group(g + 1) * 128, row);
             }
           }
           __syncwarp();
@@ -300,7 +307,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       int st = 0, buf = 0;
       uint32_t ph = 0, bph = 0;
       for (int i = first; i < tiles && ok; i += step) {
-        for (int g = 0; g < Kb && ok; ++g) {
+        for (int g = 0; g < Kb && ok; g += TURN) {
           ok = lin_wait(bar_full + 8 * st, ph, abort_flag);
           const uint64_t ad = ad0 + (uint64_t)(st * (STAGE >> 4)), bd = bd0 + (uint64_t)(st * (STAGE >> 4));
 #pragma unroll
@@ -309,13 +316,21 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             ok = ok && lin_wait(bar_free + 8 * at, bph ^ 1u, abort_flag);
             if (!ok) break;
             tc_fence_after();
+            if (PAIR) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              const uint64_t bu = bd + u * (64 * 128 >> 4) + 2 * kk;
-              if (PAIR) tc_mma_ss_f8_pair(tmem + at * 128, ad + 2 * kk, bu, IDESC, kk > 0 ? 1u : 0u, el);
-              else tc_mma_ss_f8(tmem + at * 128, ad + 2 * kk, bu, IDESC, kk > 0 ? 1u : 0u, el);
+              for (int kk = 0; kk < 4; ++kk)
+                tc_mma_ss_f8_pair(tmem + at * 128, ad + 2 * kk, bd + u * (64 * 128 >> 4) + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
+              tc_commit_pair(bar_acc + 8 * at, el);
+            } else {
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk) tc_mma_ss_f8(tmem + buf * ACC, ad + 2 * kk, bd + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
+              if (g + 1 < Kb) {
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                  tc_mma_ss_f8(tmem + buf * ACC + 128, ad + (GROUP >> 4) + 2 * kk, bd + (GROUP >> 4) + 2 * kk, IDESC, kk > 0 ? 1u : 0u, el);
+              }
+              tc_commit(bar_acc + 8 * at, el);
             }
-            if (PAIR) tc_commit_pair(bar_acc + 8 * at, el); else tc_commit(bar_acc + 8 * at, el);
           }
           if (!ok) break;
           if (PAIR) tc_commit_pair(bar_empty + 8 * st, el); else tc_commit(bar_empty + 8 * st, el);
@@ -325,10 +340,10 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       }
     } else if (warp == LOADER + 2) {
       // ---- scales: a lane has four tokens'; AHEAD groups' values are on their way while as many are handed over
-      // A slot is free when the accumulator of BUFS groups ago is full: its MMAs began when the sum warps had given back the one of 2 BUFS
-      // groups ago, whose scales were in the slot.
+      // A slot is free when the accumulator of BUFS turns ago is full: its MMAs began when the sum warps had given back the one of 2 BUFS
+      // turns ago, whose scales were in the slot.
       constexpr int BLOCKS = SIDE / 128, AHEAD = S::AHEAD;
-      int i = first, g = 0, c = 0;                           // next group to fetch, groups handed over
+      int i = first, g = 0, c = 0;                           // next group to fetch, turns handed over
       const float *xs[4], *ws[BLOCKS];
       auto place = [&]() {
         int m, n;
@@ -362,7 +377,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       };
       auto hand_over = [&](const Some& t) {
 #pragma unroll
-        for (int q = 0; q < AHEAD; ++q) {
+        for (int q = 0; q < AHEAD; q += TURN) {
           if (q >= t.n) break;
           if (c >= BUFS) {
 #pragma unroll
@@ -373,6 +388,10 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
           for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int j = 0; j < 4; ++j) scale_s[c % SLOTS][b * 128 + 32 * j + lane] = t.x[q][j] * t.w[q][b];
+          if (TURN == 2) {                                   // (a group that does not exist: any scale will do)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) scale_s[c % SLOTS][128 + 32 * j + lane] = t.x[q + TURN - 1][j] * t.w[q + TURN - 1][0];
+          }
           __syncwarp();
           if (lane < UNITS) mbar_arrive(bar_acc + 8 * (UNITS * (c % BUFS) + lane));
           ++c;
@@ -387,7 +406,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         fetch(a);
         if (!hand_over(b)) break;
       }
-    } else if (warp == LOADER + 3 && !SPLIT) {
+    } else if (PAIR && warp == LOADER + 3) {
       // ---- staging tiles: the bias of their columns, what the result is added to, the stores
       bool ok = true;
       uint32_t ph = 0;
@@ -432,7 +451,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
     // (a pair's CTA: each group of four warps has a unit of its own, the other's half a group's time later; else half of the unit)
     const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * COLS;
-    const float* scale = &scale_s[0][wg * (SLOT - 128) + row];
+    const float* scale = &scale_s[0][(PAIR ? wg * 128 : 0) + row];
     uint8_t* stage = smem + S::OUT + wg * (COLS / 64) * OUT_BYTES;
     const uint32_t free_lead = PAIR ? mapa(bar_free, 0) : bar_free;
     bool ok = true;
@@ -451,37 +470,80 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 #pragma unroll
       for (int c = 0; c < COLS / 2; ++c) acc[c] = 0ull;
 #pragma unroll 1
-      for (int g = 0; g < Kb; ++g) {
+      for (int g = 0; g < Kb; g += TURN) {
         const int at = PAIR ? buf * UNITS + wg : buf;
         if (!__all_sync(0xffffffffu, there)) ok = lin_wait(bar_acc + 8 * at, bph, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        float s = 0.f;
-        uint64_t s2 = 0ull;
+        auto give_back = [&]() {
+          tc_fence_before();
+          if (PAIR) mbar_arrive_cluster_if(free_lead + 8 * at, first_lane);
+          else mbar_arrive_if(bar_free + 8 * at, first_lane);
+          const bool wraps = buf + 1 == BUFS;
+          there = mbar_test(bar_acc + 8 * (wraps ? at - buf * UNITS : at + UNITS), wraps ? bph ^ 1u : bph);
+        };
+        auto add = [&](const uint32_t (&v)[64], float s, uint64_t* to) {
+          const uint64_t s2 = pack2(s, s);
 #pragma unroll
-        for (int u = 0; u < COLS / 64; ++u) {
-          uint32_t v[64];
-          tmem_ld32(taddr + buf * SIDE + u * 64, v);
-          tmem_ld32(taddr + buf * SIDE + u * 64 + 32, v + 32);
-          if (u == 0) s = scale[slot * SLOT];
+          for (int e = 0; e < 32; ++e) to[e] = fma2(pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), s2, to[e]);
+        };
+        const uint32_t from = taddr + buf * ACC;
+        uint32_t v[64];
+        tmem_ld32(from, v);
+        tmem_ld32(from + 32, v + 32);
+        const float s = scale[slot * 256];
+        tc_wait_ld64(v);
+        if (PAIR) {
+          add(v, s, acc);
+          tmem_ld32(from + 64, v);
+          tmem_ld32(from + 96, v + 32);
           tc_wait_ld64(v);
-          if (u + 1 == COLS / 64) {
-            tc_fence_before();
-            if (PAIR) mbar_arrive_cluster_if(free_lead + 8 * at, first_lane);
-            else mbar_arrive_if(bar_free + 8 * at, first_lane);
-            const bool wraps = buf + 1 == BUFS;
-            there = mbar_test(bar_acc + 8 * (wraps ? at - buf * UNITS : at + UNITS), wraps ? bph ^ 1u : bph);
-          }
-          if (u == 0) s2 = pack2(s, s);
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            acc[u * 32 + e] = fma2(pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), s2, acc[u * 32 + e]);
+          give_back();
+          add(v, s, acc + 32);
+        } else if (g + 1 < Kb) {
+          uint32_t w[64];                                    // the second group comes out while the first is added
+          tmem_ld32(from + 128, w);
+          tmem_ld32(from + 160, w + 32);
+          const float s1 = scale[slot * 256 + 128];
+          add(v, s, acc);
+          tc_wait_ld64(w);
+          give_back();
+          add(w, s1, acc);
+        } else {
+          give_back();
+          add(v, s, acc);
         }
         if (++buf == BUFS) { buf = 0; bph ^= 1u; }
         if (++slot == SLOTS) slot = 0;
       }
       int m, n;
       lin_tile(i, mt, nt, m, n);
+      // eight columns of a token, straight to where they belong
+      auto finish8 = [&](float (&y)[8], int tok, int col) {
+        if (prm.bias) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (col + e < prm.N) y[e] += __ldg(prm.bias + col + e + zero);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) lin_act2<ACT>(y[e], y[e + 1]);
+        if (tok >= prm.M || col >= prm.N) return;
+        __nv_bfloat16* to = prm.out + (long long)tok * prm.out_stride + col;
+        const __nv_bfloat16* add = prm.residual + (long long)tok * prm.res_stride + col;
+        if (col + 8 <= prm.N) {
+          if (prm.residual) {
+            const uint4 u = *reinterpret_cast<const uint4*>(add);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { y[2 * e] += bf16lo(w[e]); y[2 * e + 1] += bf16hi(w[e]); }
+          }
+          *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 7; ++e)
+            if (col + e < prm.N) to[e] = __float2bfloat16_rn(y[e] + (prm.residual ? __bfloat162float(add[e]) : 0.f));
+        }
+      };
       if (SPLIT) {
         // the sums of the cluster's CTAs: everybody's into its own ring (which the MMAs are done with), then each finishes a part of the columns
         float* mine = reinterpret_cast<float*>(smem);
@@ -507,42 +569,33 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 #pragma unroll
             for (int c = 0; c < W; ++c) v[q][c] = ld_cluster_f32(from + c * 512);
           }
-          const int tok = m * SIDE + row;
 #pragma unroll
           for (int c = 0; c < W; c += 8) {
             float y[8];
-            const int col = n * SIDE + c0 + c;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               y[e] = v[0][c + e];
 #pragma unroll
               for (int q = 1; q < Q; ++q) y[e] += v[q][c + e];
-              if (prm.bias && col + e < prm.N) y[e] += __ldg(prm.bias + col + e + zero);
             }
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) lin_act2<ACT>(y[e], y[e + 1]);
-            if (tok >= prm.M || col >= prm.N) continue;
-            __nv_bfloat16* to = prm.out + (long long)tok * prm.out_stride + col;
-            const __nv_bfloat16* add = prm.residual + (long long)tok * prm.res_stride + col;
-            if (col + 8 <= prm.N) {
-              if (prm.residual) {
-                const uint4 u = *reinterpret_cast<const uint4*>(add);
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { y[2 * e] += bf16lo(w[e]); y[2 * e + 1] += bf16hi(w[e]); }
-              }
-              *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-            } else {
-#pragma unroll
-              for (int e = 0; e < 7; ++e)
-                if (col + e < prm.N) to[e] = __float2bfloat16_rn(y[e] + (prm.residual ? __bfloat162float(add[e]) : 0.f));
-            }
+            finish8(y, m * SIDE + row, n * SIDE + c0 + c);
           }
         };
         if (split == 2) join(std::integral_constant<int, 2>{});
         else if (split == 4) join(std::integral_constant<int, 4>{});
         else join(std::integral_constant<int, 8>{});
         break;
+      }
+      if (!PAIR) {
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < COLS; c += 8) {
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) unpack2(acc[c / 2 + e], y[2 * e], y[2 * e + 1]);
+          finish8(y, m * SIDE + row, n * SIDE + wg * COLS + c);
+        }
+        continue;
       }
       const int m1 = m * SIDE + rank * 128, n1 = n * SIDE + wg * COLS;
       ok = ok && lin_wait(bar_ready + 8 * wg, rph, abort_flag);
@@ -923,9 +976,9 @@ static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void
   if ((rc = lin_map(&tx, x8, p->K, p->M, p->x8_stride, 1, 128))) return rc;
   if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, PAIR ? 64 : 128))) return rc;
   // (a tile store writes whole 16-byte pieces, also beyond an inner extent that ends within one: it gets the whole pieces only)
-  if ((rc = lin_map(&to, out, p->N < 8 ? 8 : p->N & ~7, p->M, 2 * p->out_stride, 2, 128))) return rc;
-  tr = to;
-  if (prm.residual && (rc = lin_map(&tr, prm.residual, p->N, p->M, 2 * p->residual_stride, 2, 128))) return rc;
+  to = tr = tx;
+  if (PAIR && (rc = lin_map(&to, out, p->N < 8 ? 8 : p->N & ~7, p->M, 2 * p->out_stride, 2, 128))) return rc;
+  if (PAIR && prm.residual && (rc = lin_map(&tr, prm.residual, p->N, p->M, 2 * p->residual_stride, 2, 128))) return rc;
   if (tiles > 0x7fffffffLL - sms) return SVA_ERR_UNSUPPORTED;
   const long long most = sms / CTAS;
   const int per = SPLIT ? split : CTAS;
