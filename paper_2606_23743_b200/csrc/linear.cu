@@ -117,6 +117,7 @@ struct LinearParams {
   long long xs_stride, ws_stride, out_stride, res_stride;
   int M, N, Kb, debug;
   int32_t* status;
+  bool wide;                                              // rows of out begin on 32 bytes
 };
 
 // GELU (tanh form) 0.5 y (1 + tanh u) = y / (1 + exp(-2u)), u = sqrt(2/pi) (y + 0.044715 y^3); SiLU y / (1 + exp(-y)).
@@ -588,12 +589,54 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       }
       if (!PAIR) {
         if (!ok) break;
+        const int tok = m * SIDE + row, col = n * SIDE + wg * COLS;
+        // straight code where all columns are there (what is optional in its midst ran at the pace of instruction fetches)
+        auto straight = [&](auto bias_tag, auto res_tag) {
+          constexpr bool BIAS = decltype(bias_tag)::value, RES = decltype(res_tag)::value;
+          const bool there = tok < prm.M;
+          const uint4* add = reinterpret_cast<const uint4*>(prm.residual + (RES ? (long long)(there ? tok : 0) * prm.res_stride + col : 0));
+          uint4 r[COLS / 8], o[COLS / 8];
 #pragma unroll
-        for (int c = 0; c < COLS; c += 8) {
-          float y[8];
+          for (int q = 0; q < COLS / 8; ++q) r[q] = RES ? add[q] : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) unpack2(acc[c / 2 + e], y[2 * e], y[2 * e + 1]);
-          finish8(y, m * SIDE + row, n * SIDE + wg * COLS + c);
+          for (int q = 0; q < COLS / 8; ++q) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) unpack2(acc[q * 4 + e], y[2 * e], y[2 * e + 1]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (BIAS) y[e] += __ldg(prm.bias + col + q * 8 + e + zero);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) lin_act2<ACT>(y[e], y[e + 1]);
+            const uint32_t w[4] = {r[q].x, r[q].y, r[q].z, r[q].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (RES) { y[2 * e] += bf16lo(w[e]); y[2 * e + 1] += bf16hi(w[e]); }
+            o[q] = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+          }
+          uint4* to = reinterpret_cast<uint4*>(prm.out + (long long)tok * prm.out_stride + col);
+          if (!there) return;
+          if (prm.wide) {
+#pragma unroll
+            for (int q = 0; q < COLS / 8; q += 2) stg32(to + q, o[q], o[q + 1]);
+          } else {
+#pragma unroll
+            for (int q = 0; q < COLS / 8; ++q) to[q] = o[q];
+          }
+        };
+        if (col + COLS <= prm.N) {
+          if (prm.bias && prm.residual) straight(std::true_type{}, std::true_type{});
+          else if (prm.bias) straight(std::true_type{}, std::false_type{});
+          else if (prm.residual) straight(std::false_type{}, std::true_type{});
+          else straight(std::false_type{}, std::false_type{});
+        } else {
+#pragma unroll
+          for (int c = 0; c < COLS; c += 8) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) unpack2(acc[c / 2 + e], y[2 * e], y[2 * e + 1]);
+            finish8(y, tok, col + c);
+          }
         }
         continue;
       }
@@ -1030,6 +1073,7 @@ int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, c
   prm.M = p->M; prm.N = p->N; prm.Kb = (p->K + 127) / 128;
   prm.debug = g_debug_lin;
   prm.status = status;
+  prm.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0 && (p->out_stride & 15) == 0;
   if (p->M <= 16) return launch_linear_few<16>(p, x8, w8, prm, sms, st);
   if (p->M <= 32) return launch_linear_few<32>(p, x8, w8, prm, sms, st);
   if (p->M <= 64) return launch_linear_few<64>(p, x8, w8, prm, sms, st);
