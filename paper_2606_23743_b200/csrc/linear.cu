@@ -1008,11 +1008,11 @@ static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void
   const long long tiles = (long long)((p->M + SIDE - 1) / SIDE) * ((p->N + SIDE - 1) / SIDE);
   int split = 1;
   if (SPLIT) {
-    // As many as all tiles' clusters run at once with, if that saves more than the joining of the sums takes, some nine groups' time.
-    // us, without / split: 128 x 2 048 x 2 048 9.5 / 8.6, 65 x 4 096 x 4 096 14.9 / 10.2, 100 x 8 192 x 512 24.2 / 9.9, but 300 x 1 024 x 1 024
-    // (eight groups) 7.0 / 8.0.
+    // As many as all tiles' clusters run at once with, if that saves more than the joining of the sums takes, some fourteen groups' time, and
+    // leaves a CTA two turns.  us, without / split in 2, 4, 8: 65 x 4 096 x 4 096 11.2 / 10.1, 9.5, 9.6, 512 x 4 096 x 2 048 12.3 / 10.8, but
+    // 65 x 2 048 x 1 024 (sixteen groups) 7.5 / 8.0, 7.7, 8.5, 100 x 1 024 x 512 6.1 / 7.0, 7.4, 8.1.
     for (int j = 1; j < 4 && !(prm.debug & 64) && tiles <= held[dev][j]; ++j)
-      if (prm.Kb > (prm.Kb + (1 << j) - 1) / (1 << j) + 9) split = 1 << j;
+      if (prm.Kb > (prm.Kb + (1 << j) - 1) / (1 << j) + 14 && prm.Kb >= 4 << j) split = 1 << j;
     if (split == 1) return launch_linear_tiles<false, ACT>(p, x8, w8, out, prm, sms, st);
   }
   CUtensorMap tx, tw, to, tr;
@@ -1077,13 +1077,13 @@ int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, c
   if (p->M <= 16) return launch_linear_few<16>(p, x8, w8, prm, sms, st);
   if (p->M <= 32) return launch_linear_few<32>(p, x8, w8, prm, sms, st);
   if (p->M <= 64) return launch_linear_few<64>(p, x8, w8, prm, sms, st);
-  // A pair takes some 770 cycles for a group of inputs of its 256 x 256, a CTA by itself 620 for its 128 x 128: whichever needs less for its
-  // rounds over the device.  us, in pairs / without: 1 024 x 2 048 x 2 048 12.8 / 10.7 (one round each), x 4 096 13.8 / 17.3 (one, two),
-  // 300 x 4 096 x 12 288 34.0 / 27.9 (two each), 768 x 4 096 x 4 096 19.9 / 27.0 (one, two).
+  // A pair takes some 770 cycles for a group of inputs of its 256 x 256, a CTA by itself 470 for its 128 x 128: whichever needs less for its
+  // rounds over the device.  us, in pairs / without: 1 024 x 2 048 x 4 096 13.8 / 14.8 (one round, two), 768 x 4 096 x 4 096 20.1 / 22.1 (one, two),
+  // 1 024 x 2 048 x 6 144 21.7 / 20.6 (two, three), 2 048 x 4 096 x 4 096 35.6 / 41.3 (two, four), 512 x 2 048 x 2 048 12.3 / 8.5 (one each).
   auto rounds = [&](long long side, int places) {
     return (((p->M + side - 1) / side) * ((p->N + side - 1) / side) + places - 1) / places;
   };
-  if (5 * rounds(256, sms > 1 ? sms / 2 : 1) <= 4 * rounds(128, sms)) return launch_linear_act<true>(p, x8, w8, out, prm, sms, st);
+  if (5 * rounds(256, sms > 1 ? sms / 2 : 1) <= 3 * rounds(128, sms)) return launch_linear_act<true>(p, x8, w8, out, prm, sms, st);
   return 2 * rounds(128, 1) <= sms ? launch_linear_act<false, true>(p, x8, w8, out, prm, sms, st) : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
 }
 
