@@ -521,6 +521,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
       lin_tile(i, mt, nt, m, n);
       // eight columns of a token, straight to where they belong
       auto finish8 = [&](float (&y)[8], int tok, int col) {
+        if (col >= prm.N) return;
         if (prm.bias) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -528,7 +529,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         }
 #pragma unroll
         for (int e = 0; e < 8; e += 2) lin_act2<ACT>(y[e], y[e + 1]);
-        if (tok >= prm.M || col >= prm.N) return;
+        if (tok >= prm.M) return;
         __nv_bfloat16* to = prm.out + (long long)tok * prm.out_stride + col;
         const __nv_bfloat16* add = prm.residual + (long long)tok * prm.res_stride + col;
         if (col + 8 <= prm.N) {
