@@ -3,8 +3,8 @@
 // (page id * page + place in the page); writing quantises into slots, reading collects a sequence's pages into the [B,H,N,d] tensors that the
 // attention calls take.
 //
-// Both are HBM-bound streaming passes (the 4-bit cast is bound by its instructions).  d/16 lanes own a row, 16 channels each (one 4-bit scale block), so that a row's maximum is
-// a few shuffles; a thread looks its token's slot up once and then has some heads' rows in flight.
+// Both are HBM-bound streaming passes, the 4-bit cast also by its instructions.  d/16 lanes own a row, 16 channels each (one 4-bit scale block),
+// so that a row's maximum is a few shuffles; a thread looks its token's slot up once and then has some heads' rows in flight.
 #include <cuda_fp4.h>
 
 #include "common.cuh"

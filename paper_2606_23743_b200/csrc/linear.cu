@@ -178,7 +178,12 @@ __device__ __forceinline__ void lin_tile(int i, int mt, int nt, int& m, int& n) 
 //   SPLIT  the CTAs of a cluster take every split-th group of a 128 x 128 tile each and join their sums through distributed shared memory, in
 //          the order of the CTAs: few tiles with many inputs
 // Warps: eight sum, a thread owning one token and half of the tile's columns; then one that loads, one that issues the MMAs, one that brings the
-// scales, one that sees to the staging tiles (bias, residual, stores).
+// scales, and in a pair one that sees to the staging tiles (bias, residual, stores), else one that loads too: x and w have a warp each.
+// A turn of any of these roles takes some 600 cycles of its own (barriers asked, instructions with their operands issued, barriers told), also
+// where it waits for nothing: a pair's MMAs for one group of inputs take 512, those of a 128 x 128 tile 256.  So a turn of a CTA by itself is two
+// groups, in loads, MMAs, scales and sums alike: 640 -> 470 cycles per group (1 024 x 16 384 x 2 048: 48.4 -> 37.2 us); two groups in the MMAs
+// alone, the barriers asked a turn ahead or loads left out had changed nothing.  Its results go straight from the registers: there is no room
+// for staging tiles beside three stages of two groups.
 namespace lin {
 constexpr uint32_t A_BYTES = 128 * 128, GROUP = 2 * A_BYTES;
 constexpr uint32_t OUT_BYTES = 128 * 128;                 // staging tile, 128 tokens x 64 columns of bf16
@@ -450,7 +455,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SUM_REGS));
     // ---- sums and epilogue
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
-    // (a pair's CTA: each group of four warps has a unit of its own, the other's half a group's time later; else half of the unit)
+    // (a pair's CTA: each group of four warps has a unit of its own, the other's half a group's time later; else half of the columns)
     const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * COLS;
     const float* scale = &scale_s[0][(PAIR ? wg * 128 : 0) + row];
     uint8_t* stage = smem + S::OUT + wg * (COLS / 64) * OUT_BYTES;
@@ -1085,7 +1090,8 @@ int launch_linear(const sva_linear_t* p, const void* x8, const float* x_scale, c
     return (((p->M + side - 1) / side) * ((p->N + side - 1) / side) + places - 1) / places;
   };
   if (5 * rounds(256, sms > 1 ? sms / 2 : 1) <= 3 * rounds(128, sms)) return launch_linear_act<true>(p, x8, w8, out, prm, sms, st);
-  return 2 * rounds(128, 1) <= sms ? launch_linear_act<false, true>(p, x8, w8, out, prm, sms, st) : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
+  return 2 * rounds(128, 1) <= sms ? launch_linear_act<false, true>(p, x8, w8, out, prm, sms, st)
+                                   : launch_linear_act<false>(p, x8, w8, out, prm, sms, st);
 }
 
 }  // namespace sva
