@@ -192,8 +192,8 @@ int launch_rope(const sva_rope_t* p, const void* q, const void* k, const void* s
   // Heads per CTA, which share the phases: equal shares of the heads, of up to 24, or fewer while there are not two CTAs per SM; fewer than a
   // thread has in flight gain nothing.
   // us, up to 32 / 16 / 8 / 4: 2 x 8 191 tokens of 32 + 8 heads 56.9 / 53.1 / 52.7 / 64.4, 4 096 of 40 + 8 18.9 / 17.5 / 17.5 / 21.8, 64 of
-  // 32 + 8 7.0 / 4.7 / 3.5 / 2.9; 32 760 of 24 + 24, 24 heads 126.2, 16 128.4, 12 128.0.  Where 16 leave less than two CTAs per SM, them / the rule: 1 000 of
-  // 32 + 8 6.4 / 5.7, 2 048 of 24 + 24 10.4 / 8.7, but 1 024 of 16 + 16 4.5 / 5.3.
+  // 32 + 8 7.0 / 4.7 / 3.5 / 2.9; 32 760 of 24 + 24, 24 heads 126.2, 16 128.4, 12 128.0.  Where 16 leave less than two CTAs per SM, them / the
+  // rule: 1 000 of 32 + 8 6.4 / 5.7, 2 048 of 24 + 24 10.4 / 8.7, but 1 024 of 16 + 16 4.5 / 5.3.
   const int most = prm.Hq > prm.Hk ? prm.Hq : prm.Hk, shares = most / 24 + (most % 24 != 0);
   auto whole = [](int heads) { return (heads + ROPE_HEADS - 1) / ROPE_HEADS * ROPE_HEADS; };
   prm.chunk = whole(most / shares + (most % shares != 0));
