@@ -437,7 +437,7 @@ typedef struct {
 } sva_rope_t;
 
 /* q_out / k_out may be q / k themselves (same strides), otherwise they must not overlap them.  k and k_out may both be NULL.
- * Errors: INVALID_ARG, ALIGNMENT (16 bytes; steps 8, positions 4), UNSUPPORTED (d). */
+ * Errors: INVALID_ARG, ALIGNMENT (16 bytes; steps 8, positions 4), UNSUPPORTED (d, more than 2^24 heads). */
 int sva_rope(const sva_rope_t* p, const void* q, const void* k, const uint64_t* steps, const int32_t* positions, void* q_out,
              void* k_out, void* stream);
 
@@ -484,7 +484,7 @@ typedef struct {
  * read  : row n < min(N, lengths[b]) of k, v [B,H,N,d] comes from place n % page of page page_table[b][n / page] (int32, max_pages per
  *         row, table_stride between rows); rows from lengths[b] on become zeros.  A page id outside [0, pages), or a page beyond max_pages, is
  *         reported and its rows become zeros.
- * T and N may be 0 (nothing is done).  Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (d, cache size).
+ * T and N may be 0 (nothing is done).  Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (d, cache size, more than 2^24 heads).
  */
 int sva_kv_cache_write(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t k_stride[3], const int64_t v_stride[3],
                        int32_t B, int32_t T, const int32_t* slots, int32_t* device_status, void* stream);

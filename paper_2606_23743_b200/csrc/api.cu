@@ -391,6 +391,8 @@ static int check_floats(const void* ptr, int64_t stride, int64_t row) {
 }
 // (sizes whose tiles of 128 can be counted, and whose last tile's end can be formed, in 32 bits)
 static constexpr int32_t LINEAR_MAX = 0x7fffffff - 1024;
+// (heads whose shares can be rounded up in 32 bits)
+static constexpr int32_t HEADS_MAX = 1 << 24;
 
 int sva_quantize_rows_fp8(const sva_linear_t* p, const void* x_bf16, void* x8, float* x_scale, void* stream) {
   if (!p || p->M < 0 || p->K < 1) return SVA_ERR_INVALID_ARG;
@@ -435,7 +437,7 @@ int sva_rope(const sva_rope_t* p, const void* q, const void* k, const uint64_t* 
   for (int a = 0; a < 3; ++a)
     if (p->axis_pairs[a] < 0 || p->axis_pairs[a] > p->rotary_dim / 2) return SVA_ERR_INVALID_ARG;
   if (p->axis_pairs[0] + p->axis_pairs[1] + p->axis_pairs[2] != p->rotary_dim / 2) return SVA_ERR_INVALID_ARG;
-  if (p->d % 8 != 0 || p->d > 256) return SVA_ERR_UNSUPPORTED;
+  if (p->d % 8 != 0 || p->d > 256 || p->Hq > HEADS_MAX || (k && p->Hk > HEADS_MAX)) return SVA_ERR_UNSUPPORTED;
   if (p->pos_stride[0] < 0 || p->pos_stride[1] < 0) return SVA_ERR_INVALID_ARG;
   if (p->N == 0) return SVA_OK;
   if (!q || !q_out || !steps || !positions) return SVA_ERR_INVALID_ARG;
@@ -484,7 +486,7 @@ int sva_rope_steps(int32_t rotary_dim, const int32_t axis_pairs[3], double base,
 static int validate_cache(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t ks[3], const int64_t vs[3], int B, int T) {
   if (!c || !ks || !vs || B < 1 || T < 0 || c->H < 1 || c->d < 1 || c->page < 1 || c->pages < 1) return SVA_ERR_INVALID_ARG;
   if (c->format != SVA_CACHE_E4M3 && c->format != SVA_CACHE_FP4) return SVA_ERR_INVALID_ARG;
-  if (c->d != 64 && c->d != 128) return SVA_ERR_UNSUPPORTED;
+  if ((c->d != 64 && c->d != 128) || c->H > HEADS_MAX) return SVA_ERR_UNSUPPORTED;
   if ((long long)c->page * c->pages > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
   if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return SVA_ERR_INVALID_ARG;
   if (c->format == SVA_CACHE_FP4 && (!c->k_sf || !c->v_sf)) return SVA_ERR_INVALID_ARG;

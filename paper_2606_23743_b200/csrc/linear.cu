@@ -469,8 +469,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     // read 650, with the sums 768.  The MMA warp finds its barriers passed in nine turns of ten: what is left is the pace of the MMAs, which warps
     // that multiply and add without having anything to do with the product slow down as much (660 -> 890), and which goes with the power drawn:
     // 122 us = 2.25 PFLOP/s in a run of 20, 138 in one of 2 000, 107 with codes of zeros.  128 columns read between sums 32 at a time, no units:
-    // 870; sixteen sum
-    // warps of 64 columns: 1 000.
+    // 870; sixteen sum warps of 64 columns: 1 000.
     const uint32_t first_lane = lane == 0;
     uint32_t there = 0u;
     for (int i = first; i < tiles; i += step) {

@@ -152,3 +152,12 @@ def test_the_binding_refuses_tensors_that_do_not_match(lib):
         B.make_kv_cache([codes, scale[:2]], [codes, scale])
     with pytest.raises(AssertionError):
         B.kv_cache_write(c, q, q, torch.zeros(2, 5, dtype=torch.int32))
+
+
+def test_more_heads_than_can_be_shared_out_are_refused(lib):
+    st = (C.c_int64 * 3)(0, 0, 128)
+    for n in (2 ** 24 + 1, 2 ** 31 - 1):
+        for p in (_rope(Hq=n), _rope(Hk=n)):
+            assert lib.sva_rope(C.byref(p), ONE, ONE, ONE, ONE, ONE, ONE, None) == UNSUPPORTED
+        assert lib.sva_kv_cache_write(C.byref(_cache(H=n)), ONE, ONE, st, st, 1, 1, ONE, None, None) == UNSUPPORTED
+        assert lib.sva_kv_cache_read(C.byref(_cache(H=n)), ONE, 1, 1, ONE, 1, 1, ONE, ONE, st, st, None, None) == UNSUPPORTED
