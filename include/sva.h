@@ -461,7 +461,9 @@ int sva_rope_steps(int32_t rotary_dim, const int32_t axis_pairs[3], double base,
  *   SVA_CACHE_E4M3  scale = amax / 448 (1 if amax = 0), code = e4m3(x / scale);                   x ~= bf16(value(code) * scale)
  *   SVA_CACHE_FP4   scale = amax / (6 * 448) (1 if amax = 0), per 16 channels sf = e4m3((amax16 / 6) / scale),
  *                   code = e2m1(x / (value(sf) * scale)) (0 where sf = 0);                        x ~= bf16(value(code) * value(sf) * scale)
- * round-to-nearest-even and saturating.  Arrays (contiguous, device):
+ * round-to-nearest-even and saturating.  A NaN: in E4M3 amax leaves it out and its code is a NaN, so that it comes back alone; 4-bit codes have
+ * none, so the row's scale becomes NaN (codes and sf 0) and the row comes back as NaNs.  An infinity: the row's scale is infinite, and the
+ * row comes back as NaNs in both.  Arrays (contiguous, device):
  *   codes  [pages][H][page][d] bytes, or [pages][H][page][d/2], two codes per byte (even channel in the low half); 16-byte aligned
  *   scale  [pages][H][page] fp32
  *   sf     [pages][H][page][d/16] bytes (SVA_CACHE_FP4 only)

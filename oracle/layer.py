@@ -39,13 +39,17 @@ def encode(y, table):
 
 
 def e4m3_bytes(y):
-    return (encode(y, E4M3) + 128 * np.signbit(y)).astype(np.uint8)
+    return np.where(np.isnan(y), 127, encode(y, E4M3) + 128 * np.signbit(y)).astype(np.uint8)
 
 
 def e4m3_values(b):
     b = np.asarray(b)
-    assert not np.any((b & 127) == 127), "NaN code"
-    return E4M3[b & 127] * np.where(b >= 128, -1.0, 1.0)
+    return np.append(E4M3, np.nan)[b & 127] * np.where(b >= 128, -1.0, 1.0)
+
+
+def amax_of_numbers(x, axis=None):
+    """Largest magnitude, NaNs left out (0 of nothing)."""
+    return np.where(np.isnan(x), 0.0, np.abs(x)).max(axis)
 
 
 def scale8(amax):
@@ -59,8 +63,9 @@ def quantize_rows(x):
     codes, scale = np.zeros((M, K), np.uint8), np.zeros((G, M))
     for g in range(G):
         part = x[:, 128 * g:128 * g + 128]
-        scale[g] = scale8(np.abs(part).max(1))
-        codes[:, 128 * g:128 * g + 128] = e4m3_bytes(f32(part / scale[g][:, None]))
+        scale[g] = scale8(amax_of_numbers(part, 1))
+        with np.errstate(invalid="ignore"):               # (infinity / infinity: a NaN)
+            codes[:, 128 * g:128 * g + 128] = e4m3_bytes(f32(part / scale[g][:, None]))
     return codes, scale
 
 
@@ -71,8 +76,9 @@ def quantize_tiles(w):
     for J in range(scale.shape[0]):
         for g in range(scale.shape[1]):
             at = np.s_[128 * J:128 * J + 128, 128 * g:128 * g + 128]
-            scale[J, g] = scale8(np.abs(w[at]).max())
-            codes[at] = e4m3_bytes(f32(w[at] / scale[J, g]))
+            scale[J, g] = scale8(amax_of_numbers(w[at]))
+            with np.errstate(invalid="ignore"):
+                codes[at] = e4m3_bytes(f32(w[at] / scale[J, g]))
     return codes, scale
 
 
@@ -135,21 +141,25 @@ def rope(x, theta, positions, axis_pairs, rotary_dim, layout, factor=1.0, invers
 
 
 def cache_row(x, form):
-    """One row [d] -> (code bytes, scale, sf bytes or None, values in fp64 before their rounding to bf16)."""
-    amax = np.abs(x).max()
-    if form == "e4m3":
-        scale = float(scale8(amax))
-        codes = e4m3_bytes(f32(x / scale))
-        return codes, scale, None, f32(e4m3_values(codes) * scale)
-    scale = 1.0 if amax == 0 else float(f32(amax / 2688.0))
-    codes, sf = np.zeros(x.size, np.int64), np.zeros(x.size // 16, np.uint8)
-    values = np.zeros(x.size)
-    for i in range(sf.size):
-        at = np.s_[16 * i:16 * i + 16]
-        sf[i] = e4m3_bytes(f32(f32(np.abs(x[at]).max() / 6.0) / scale))
-        unit = float(f32(e4m3_values(sf[i]) * scale))
-        if unit > 0:
-            y = f32(x[at] / unit)
-            codes[at] = encode(y, E2M1) + 8 * np.signbit(y)
-        values[at] = f32(E2M1[codes[at] & 7] * np.where(codes[at] >= 8, -1.0, 1.0) * e4m3_values(sf[i]) * scale)
+    """One row [d] -> (code bytes, scale, sf bytes or None, values in fp64 before their rounding to bf16).  4-bit codes have no NaN: a row that
+    holds one gets the scale NaN, codes and sf 0."""
+    with np.errstate(invalid="ignore"):
+        if form == "e4m3":
+            scale = float(scale8(amax_of_numbers(x)))
+            codes = e4m3_bytes(f32(x / scale))
+            return codes, scale, None, f32(e4m3_values(codes) * scale)
+        amax = np.abs(x).max()                            # (NaN if there is one)
+        scale = 1.0 if amax == 0 else float(f32(amax / 2688.0))
+        codes, sf = np.zeros(x.size, np.int64), np.zeros(x.size // 16, np.uint8)
+        values = np.zeros(x.size)
+        for i in range(sf.size):
+            at = np.s_[16 * i:16 * i + 16]
+            sf[i] = e4m3_bytes(f32(f32(np.abs(x[at]).max() / 6.0) / scale))
+            unit = float(f32(e4m3_values(sf[i]) * scale))
+            if unit > 0:
+                y = f32(x[at] / unit)
+                codes[at] = encode(y, E2M1) + 8 * np.signbit(y)
+            elif np.isnan(unit):                          # (NaN, or infinite scales)
+                sf[i] = 0
+            values[at] = f32(E2M1[codes[at] & 7] * np.where(codes[at] >= 8, -1.0, 1.0) * e4m3_values(sf[i]) * scale)
     return (codes[0::2] + 16 * codes[1::2]).astype(np.uint8), scale, sf, values

@@ -227,14 +227,18 @@ template <int D>
 __device__ __forceinline__ float div_by(float a) {
   return a >= 8.077935669463161e-28f && a <= 3.4e38f ? div_fast(a, (float)D, 1.0f / D) : div_any(a, (float)D);      // (2^-90)
 }
-// the largest magnitude of 16 bf16 values, NaNs left out, as fp32
+// the largest magnitude of 16 bf16 values as fp32; a NaN among them is the result, or (NANS false) is left out
+template <bool NANS = false>
 __device__ __forceinline__ float bf16_amax(const uint4& a, const uint4& b) {
   const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
   uint32_t m = 0u;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(w[e]));
+  for (int e = 0; e < 8; ++e) {
+    if (NANS) asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(w[e]));
+    else asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(w[e]));
+  }
   m &= 0x7fff7fffu;
-  return __uint_as_float(max(m << 16, m & 0xffff0000u));
+  return __uint_as_float(max(m << 16, m & 0xffff0000u));      // (magnitudes are ordered as their bits are, NaN above infinity)
 }
 // four values to e4m3, eight to e2m1 (round to nearest even, saturating), the first in the lowest bits
 __device__ __forceinline__ uint32_t e4m3x4(uint64_t a, uint64_t b) {

@@ -38,7 +38,7 @@ __device__ __forceinline__ long long cache_row(const CacheParams& prm, long long
   return (page * prm.H + h) * prm.page + place;
 }
 
-// The casts of a lane's 16 values by general divisions: rows whose scale is far out (zero, infinite, 1e-12 and less) or has a significand of ones.
+// The casts of a lane's 16 values by general divisions: rows whose scale is far out (zero, infinite, NaN, 1e-12 and less) or has a significand of ones.
 struct Cast { uint4 codes; float scale; uint32_t sf; };
 template <bool FP4>
 __device__ __noinline__ Cast cache_cast_any(uint4 a, uint4 b, float amax, float own) {
@@ -135,12 +135,13 @@ cache_write_kernel(const CacheParams prm) {
     }
 #pragma unroll
     for (int i = 0; i < CACHE_HEADS; ++i) {
-      const float own = bf16_amax(in[i][0], in[i][1]);
-      float amax = own;
+      // (4-bit codes have no NaN: one that is there becomes the row's scale; as bits, since a maximum of floats would lose it)
+      const float own = bf16_amax<FP4>(in[i][0], in[i][1]);
+      uint32_t amax = __float_as_uint(own);
 #pragma unroll
-      for (int o = LANES / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+      for (int o = LANES / 2; o; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
       if (h0 + i < he) {
-        const Cast x = cache_cast<FP4>(in[i][0], in[i][1], amax, own);
+        const Cast x = cache_cast<FP4>(in[i][0], in[i][1], __uint_as_float(amax), own);
         if (lane == 0) *scale = x.scale;
         if (FP4) {
           *sf = (uint8_t)x.sf;

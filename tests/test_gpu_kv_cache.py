@@ -211,3 +211,24 @@ def test_read_into_rows_on_16_bytes(form, d, pad, shift):
     B.kv_cache_read(c, table, lengths, *[p[..., :d] for p in parts])
     for w, p, h in zip(whole, parts, held):
         assert torch.equal(w, p[..., :d]) and bool((p[..., d:] == 7.0).all()) and bool((h[:shift] == 7.0).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("form", ["e4m3", "fp4"])
+def test_rows_with_nan_and_infinities(form, d):
+    """A NaN stays alone in e4m3 and makes its row NaN in 4 bits, an infinity makes its row NaN; no other row changes."""
+    rng = np.random.default_rng(d)
+    x = _rows(rng, (1, 3, 9, d), False)
+    clean = x.clone()
+    x[0, 0, 0, 5], x[0, 0, 1, d - 1], x[0, 1, 2] = float("nan"), -float("nan"), float("nan")
+    x[0, 2, 3, 20], x[0, 0, 4, 40], x[0, 1, 5, 0:2] = float("inf"), -float("inf"), torch.tensor([float("inf"), float("nan")])
+    x[0, 2, 6], x[0, 2, 6, 63] = 0.0, float("nan")
+    ka, va = _arrays(form, 1, 3, 9, d), _arrays(form, 1, 3, 9, d)
+    c = B.make_kv_cache(ka, va, form)
+    B.kv_cache_write(c, x, clean, torch.arange(9, dtype=torch.int32, device="cuda")[None])
+    out, whole = torch.empty_like(x), torch.empty_like(x)
+    B.kv_cache_read(c, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([9], dtype=torch.int32, device="cuda"), out, whole)
+    for got, given, arrays in ((out, x, ka), (whole, clean, va)):
+        _, scale, _, values = _expect(given, form)
+        np.testing.assert_array_equal(arrays[1].cpu().numpy()[0], scale[0, :, :, 0])
+        np.testing.assert_array_equal(_f64(got), torch.from_numpy(values).float().to(torch.bfloat16).float().numpy())
