@@ -423,10 +423,18 @@ def _row_stride(t, what):
     return t.stride(0)
 
 
+def _holds_whole_pieces(codes, K: int) -> bool:
+    """Whether a matrix of codes has room for rows of whole 16-byte pieces, as the quantisers write them.  (Of several rows the C side sees the
+    stride; a single one may carry any.)"""
+    row, rows, stride = -(-K // 16) * 16, codes.shape[0], codes.stride(0)
+    end = codes.storage_offset() + (rows - 1) * stride + row
+    return rows == 0 or (rows > 1 or codes.shape[1] >= row or stride >= row) and end <= codes.untyped_storage().nbytes()
+
+
 def make_linear(x=None, x8=None, x_scale=None, w8=None, w_scale=None, out=None, act: str = "none", residual=None, w=None, K: int = 0) -> Linear:
     """A linear layer y = x w^T: x [M,K] bf16, x8 [M,>=K] codes, x_scale [ceil(K/128),M] fp32, w [N,K] bf16, w8 [N,>=K] codes,
     w_scale [ceil(N/128),ceil(K/128)] fp32, out and residual [M,N] bf16.  What a call does not use may be left out; K is taken from x or
-    w, or given."""
+    w, or given.  Codes that are written (x8 beside x, w8 beside w) have room for rows of whole 16-byte pieces."""
     p = Linear()
     rows = x if x is not None else x8
     p.M = rows.shape[0] if rows is not None else 0
@@ -444,6 +452,8 @@ def make_linear(x=None, x8=None, x_scale=None, w8=None, w_scale=None, out=None, 
         assert t is None or tuple(t.shape) == shape and t.dtype == torch.bfloat16, "bf16 matrices of matching sizes"
     for t, n in ((x8, p.M), (w8, p.N)):
         assert t is None or t.shape[0] == n and t.shape[1] >= p.K and t.element_size() == 1, "codes are bytes, a row for each row"
+    for given, codes in ((x, x8), (w, w8)):
+        assert given is None or codes is None or _holds_whole_pieces(codes, p.K), "codes that are written are rows of whole 16-byte pieces"
     groups = -(-p.K // 128)
     for t, shape in ((x_scale, (groups, p.M)), (w_scale, (-(-p.N // 128), groups))):
         assert t is None or t.dtype == torch.float32 and t.shape[0] == shape[0] and t.shape[1] >= shape[1], "fp32 scales, one per block of 128"

@@ -161,3 +161,21 @@ def test_more_heads_than_can_be_shared_out_are_refused(lib):
             assert lib.sva_rope(C.byref(p), ONE, ONE, ONE, ONE, ONE, ONE, None) == UNSUPPORTED
         assert lib.sva_kv_cache_write(C.byref(_cache(H=n)), ONE, ONE, st, st, 1, 1, ONE, None, None) == UNSUPPORTED
         assert lib.sva_kv_cache_read(C.byref(_cache(H=n)), ONE, 1, 1, ONE, 1, 1, ONE, ONE, st, st, None, None) == UNSUPPORTED
+
+
+def test_codes_that_end_within_a_piece_are_refused(lib):
+    """The quantisers write whole pieces of 16 bytes: a row of codes has room for them, also where it is the only one or the last."""
+    x = torch.zeros(3, 100, dtype=torch.bfloat16)
+    s = torch.zeros(1, 3)
+    padded, big = torch.zeros(3, 112, dtype=torch.uint8), torch.zeros(1000, dtype=torch.uint8)
+    B.make_linear(x, x8=padded, x_scale=s)
+    assert B.make_linear(x, x8=padded[:, :100], x_scale=s).x8_stride == 112          # (what is behind a row is its own)
+    assert B.make_linear(x[:1], x8=padded[:1, :100], x_scale=s[:, :1]).x8_stride == 112
+    for codes in (torch.zeros(1, 100, dtype=torch.uint8), big[:100][None], big[16:116].expand(1, 100)):
+        with pytest.raises(AssertionError):
+            B.make_linear(x[:1], x8=codes, x_scale=s[:, :1])
+        with pytest.raises(AssertionError):
+            B.make_linear(w=x[:1], w8=codes, w_scale=s[:, :1])
+        B.make_linear(x8=codes, x_scale=s[:, :1], w8=codes, K=100)                   # (read only)
+    with pytest.raises(AssertionError):
+        B.make_linear(x, x8=torch.zeros(324, dtype=torch.uint8).as_strided((3, 100), (112, 1)), x_scale=s)
