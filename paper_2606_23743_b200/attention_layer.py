@@ -65,24 +65,32 @@ class AttentionLayer:
         self.cache = sva.make_kv_cache(*arrays, format=cache)
         self.table = torch.arange(pages, dtype=torch.int32, device=dev).view(batch, per)
         self.slots = (torch.arange(batch, device=dev)[:, None] * (per * page) + n).to(torch.int32).contiguous()      # [B, N]
+        # the same by token index, between two places for indices that name no token: those have no slot
+        self.positions_of = torch.nn.functional.pad(self.positions[:, 0], (1, 1))
+        self.slots_of = torch.nn.functional.pad(self.slots, (1, 1), value=-1)
         self.lengths = torch.full((batch,), self.N, dtype=torch.int32, device=dev)
         # Q of the whole clip; tokens that a call leaves out keep theirs, so that routing sees whole blocks
         self.q, self.k, self.v, self.o = (torch.zeros(batch, self.N, heads, self.d, dtype=torch.bfloat16, device=dev).transpose(1, 2)
                                           for _ in range(4))
 
     def __call__(self, x, token_idx=None):
-        """x [B, M, C] bf16, the tokens token_idx [B, M] (int32, ascending; None: all N): x + attention's projection, for them."""
+        """x [B, M, C] bf16, the tokens token_idx [B, M] (integers, ascending; None: all N): x + attention's projection, for them.  An index
+        that names no token is reported in `status`; its token stays out of the cache, and its row of the result means nothing."""
         B, M, C = x.shape
         H, d = self.H, self.d
-        assert B == self.B and (token_idx is not None or M == self.N), "x holds the call's tokens of every batch item"
+        assert B == self.B and (token_idx is None and M == self.N or token_idx is not None and tuple(token_idx.shape) == (B, M)), \
+            "x holds the call's tokens of every batch item"
+        if M == 0:
+            return torch.empty_like(x)
         x = x.reshape(B * M, C)
         qkv = self.qkv(x, torch.empty(B * M, 3 * H * d, dtype=torch.bfloat16, device=x.device), self.status).view(B, M, 3, H, d)
         q, k, v = (qkv[:, :, i].transpose(1, 2) for i in range(3))
         if token_idx is None:
             positions, slots = self.positions, self.slots
         else:
-            at = token_idx.long()
-            positions, slots = self.positions[:, 0][:, at].contiguous(), torch.gather(self.slots, 1, at).contiguous()
+            token_idx = token_idx.clamp(-1, self.N).int().contiguous()
+            at = token_idx.long() + 1
+            positions, slots = self.positions_of[:, at].contiguous(), torch.gather(self.slots_of, 1, at).contiguous()
         sva.rope(sva.make_rope(q, k, q, k, positions, d, "interleaved", self.pairs), q, k, self.steps, positions, q, k)
         sva.kv_cache_write(self.cache, k, v, slots, self.status)
         sva.kv_cache_read(self.cache, self.table, self.lengths, self.k, self.v, self.status)

@@ -297,8 +297,10 @@ def block_sparse_attn_fwd_prepared(p: Problem, q, k, row_ptr, col_idx, o, lse=No
 
 def _token_move(name, src, token_idx, dst, status):
     Bq, Hq, n_src, d = src.shape
+    assert token_idx.dim() == 2 and token_idx.shape[0] == Bq and token_idx.dtype is torch.int32 and token_idx.is_contiguous(), "token_idx is [B,M] int32"
     M = token_idx.shape[1]
-    n_full = dst.shape[2] if name == "sva_scatter_tokens" else n_src
+    n_full, n_part = (dst.shape[2], n_src) if name == "sva_scatter_tokens" else (n_src, dst.shape[2])
+    assert n_part >= M and dst.shape[:2] == (Bq, Hq) and dst.shape[3] == d and src.dtype is dst.dtype, "src, dst are [B,H,*,d] of one type"
     rc = getattr(lib(), name)(_ptr(src), _strides(src), _ptr(token_idx), Bq, Hq, M, n_full, d, src.element_size(),
                               _ptr(dst), _strides(dst), _ptr(status), _stream())
     if rc != SVA_OK:

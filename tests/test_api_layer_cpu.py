@@ -179,3 +179,16 @@ def test_codes_that_end_within_a_piece_are_refused(lib):
         B.make_linear(x8=codes, x_scale=s[:, :1], w8=codes, K=100)                   # (read only)
     with pytest.raises(AssertionError):
         B.make_linear(x, x8=torch.zeros(324, dtype=torch.uint8).as_strided((3, 100), (112, 1)), x_scale=s)
+
+
+def test_token_indices_that_do_not_match_are_refused(lib):
+    """Indices are read as B x M int32 side by side: a shared row that is spread over the batch, or 64 bits, would be read past its end."""
+    x, part = torch.zeros(2, 3, 50, 16, dtype=torch.bfloat16), torch.zeros(2, 3, 9, 16, dtype=torch.bfloat16)
+    idx = torch.zeros(2, 9, dtype=torch.int32)
+    bad = [(idx.long(), part), (idx[:1].expand(2, 9), part), (idx[:1], part), (torch.zeros(2, 18, dtype=torch.int32)[:, ::2], part), (idx[0], part),
+           (idx, part[:, :, :8]), (idx, part[:1]), (idx, part[:, :2]), (idx, part[..., :8]), (idx, part.float())]
+    for i, p in bad:
+        with pytest.raises(AssertionError):
+            B.gather_tokens(x, i, p)
+        with pytest.raises(AssertionError):
+            B.scatter_tokens(p, i, x)

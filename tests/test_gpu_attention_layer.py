@@ -76,3 +76,28 @@ def test_all_tokens_then_a_subset(form, d):
         rel = np.linalg.norm(got - want) / np.linalg.norm(want)
         # (y = x + .. is rounded to bf16: 2^-9 of x, which is some five times as large as the rest here)
         assert rel <= limit + 2.0 ** -9 * np.linalg.norm(_f64(xs)) / np.linalg.norm(want), rel
+
+
+def test_token_indices_as_they_come():
+    """A row of indices shared by the batch, 64-bit ones, none at all, and some that name no token: those are reported and the others are as without them."""
+    rng = np.random.default_rng(3)
+    Bq, H, d, grid, C = 2, 2, 64, (2, 8, 9), 136
+    N = grid[0] * grid[1] * grid[2]
+    bf = lambda *s: torch.from_numpy(rng.standard_normal(s)).to(torch.bfloat16).cuda()                  # noqa: E731
+    layer = AttentionLayer(bf(3 * H * d, C) / np.sqrt(C), bf(C, H * d), H, grid, B.make_select(0, 1000), Bq)
+    layer(bf(Bq, N, C))
+    idx = torch.from_numpy(np.sort(rng.permutation(N)[:20]).astype(np.int32)).cuda()
+    x = bf(Bq, 20, C)
+    want = layer(x, idx[None].repeat(Bq, 1))
+    assert torch.equal(layer(x, idx[None].expand(Bq, 20)), want)
+    assert torch.equal(layer(x, idx.long()[None].repeat(Bq, 1)), want)
+    assert layer(x[:, :0], idx[None, :0].expand(Bq, 0)).shape == (Bq, 0, C)
+    assert int(layer.status.item()) == 0
+    held = [t.clone() for pair in layer.cache.arrays for t in pair]
+    wide = torch.cat((torch.tensor([-1, -2 ** 31], dtype=torch.int32, device="cuda"), idx, torch.tensor([N, 2 ** 31 - 1], dtype=torch.int32, device="cuda")))
+    got = layer(torch.cat((bf(Bq, 2, C), x, bf(Bq, 2, C)), 1), wide[None].expand(Bq, 24))
+    assert torch.equal(got[:, 2:22], want)
+    assert all(torch.equal(a, b) for a, b in zip(held, (t for pair in layer.cache.arrays for t in pair)))
+    assert int(layer.status.item()) == B.SVA_DEV_BAD_INDEX
+    with pytest.raises(AssertionError):
+        layer(x, idx[None, :19].expand(Bq, 19))
