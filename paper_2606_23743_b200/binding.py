@@ -49,6 +49,9 @@ class Linear(C.Structure):
     _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("act", C.c_int32),
                 ("x_stride", C.c_int64), ("w_stride", C.c_int64), ("out_stride", C.c_int64), ("residual_stride", C.c_int64),
                 ("x8_stride", C.c_int64), ("w8_stride", C.c_int64), ("x_scale_stride", C.c_int64), ("w_scale_stride", C.c_int64)]
+    # bytes of the three calls' tensors (make_linear, if they are on the GPU)
+    rows = tiles = (float("inf"),) * 3
+    product = (float("inf"),) * 7
 
 
 class Rope(C.Structure):
@@ -56,12 +59,14 @@ class Rope(C.Structure):
                 ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("axis_pairs", C.c_int32 * 3), ("inverse", C.c_int32),
                 ("factor", C.c_float), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
                 ("q_out_stride", C.c_int64 * 3), ("k_out_stride", C.c_int64 * 3), ("pos_stride", C.c_int64 * 2)]
+    sizes = (float("inf"),) * 5                            # bytes of the call's tensors (make_rope, if they are on the GPU)
 
 
 class KvCache(C.Structure):
     _fields_ = [("H", C.c_int32), ("d", C.c_int32), ("page", C.c_int32), ("pages", C.c_int32), ("format", C.c_int32),
                 ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("k_sf", C.c_void_p), ("v_sf", C.c_void_p)]
+    arrays, on_gpu = None, False                           # the tensors behind the pointers, and where they are (make_kv_cache)
 
 
 class SvaError(RuntimeError):
@@ -420,6 +425,11 @@ ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
 CACHE_FORMATS = {"e4m3": 0, "fp4": 1}
 
 
+# A call's tensors are those that its plan was made from, or others like them: their sizes are compared, and what the plan has not seen is looked at.
+# (Strides and devices of every tensor again would be a third of what a small call takes in Python.)
+_NOT_THE_PLANS = "tensors on the GPU, no smaller than those that the plan was made for"
+
+
 def _row_stride(t, what):
     assert t.dim() == 2 and t.stride(1) == 1, f"{what} is a matrix with contiguous rows"
     return t.stride(0)
@@ -459,11 +469,18 @@ def make_linear(x=None, x8=None, x_scale=None, w8=None, w_scale=None, out=None, 
     groups = -(-p.K // 128)
     for t, shape in ((x_scale, (groups, p.M)), (w_scale, (-(-p.N // 128), groups))):
         assert t is None or t.dtype == torch.float32 and t.shape[0] == shape[0] and t.shape[1] >= shape[1], "fp32 scales, one per block of 128"
+    given = [t for t in (x, x8, x_scale, w, w8, w_scale, out, residual) if t is not None]
+    if all(t.is_cuda for t in given):
+        size = lambda t: 0 if t is None else t.nbytes                                                                    # noqa: E731
+        p.rows, p.tiles = (size(x), size(x8), size(x_scale)), (size(w), size(w8), size(w_scale))
+        p.product = (*p.rows[1:], *p.tiles[1:], size(out), size(residual), 4 * p.N)
     return p
 
 
 def quantize_rows_fp8(p: Linear, x, x8, x_scale) -> None:
     """Activations to e4m3 codes, a scale per token and 128 inputs."""
+    a, b, c = p.rows
+    assert x.nbytes >= a and x8.nbytes >= b and x_scale.nbytes >= c, _NOT_THE_PLANS
     rc = (_lib or lib()).sva_quantize_rows_fp8(p, x.data_ptr(), x8.data_ptr(), x_scale.data_ptr(), _stream())
     if rc:
         raise SvaError(rc, "sva_quantize_rows_fp8")
@@ -471,6 +488,8 @@ def quantize_rows_fp8(p: Linear, x, x8, x_scale) -> None:
 
 def quantize_tiles_fp8(p: Linear, w, w8, w_scale) -> None:
     """Weights to e4m3 codes, a scale per tile of 128 x 128."""
+    a, b, c = p.tiles
+    assert w.nbytes >= a and w8.nbytes >= b and w_scale.nbytes >= c, _NOT_THE_PLANS
     rc = lib().sva_quantize_tiles_fp8(C.byref(p), _ptr(w), _ptr(w8), _ptr(w_scale), _stream())
     if rc != SVA_OK:
         raise SvaError(rc, "sva_quantize_tiles_fp8")
@@ -478,7 +497,10 @@ def quantize_tiles_fp8(p: Linear, w, w8, w_scale) -> None:
 
 def linear_fp8(p: Linear, x8, x_scale, w8, w_scale, out, bias=None, residual=None, status=None) -> None:
     """out = bf16(act(x w^T + bias) + residual) from codes and scales."""
-    assert bias is None or bias.dtype is torch.float32 and bias.numel() == p.N and bias.stride(-1) == 1, "bias is [N] fp32"
+    a, b, c, d, e, f, g = p.product
+    assert x8.nbytes >= a and x_scale.nbytes >= b and w8.nbytes >= c and w_scale.nbytes >= d and out.nbytes >= e and \
+        (residual is None or residual.nbytes >= f) and (status is None or status.is_cuda), _NOT_THE_PLANS
+    assert bias is None or bias.is_cuda and bias.dtype is torch.float32 and bias.nbytes == g and bias.is_contiguous(), "bias is [N] fp32"
     rc = (_lib or lib()).sva_linear_fp8(p, x8.data_ptr(), x_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), out.data_ptr(),
                                         None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(),
                                         None if status is None else status.data_ptr(), _stream())
@@ -515,11 +537,16 @@ def make_rope(q, k, q_out, k_out, positions, rotary_dim: int, layout: str = "int
     if k is not None:
         assert k.shape == (p.B, p.Hk, p.N, p.d) and k_out.shape == k.shape and k.dtype == k_out.dtype == torch.bfloat16
         p.k_stride, p.k_out_stride = _strides(k), _strides(k_out)
+    if all(t.is_cuda for t in (q, q_out, positions, *((k, k_out) if k is not None else ()))):
+        p.sizes = q.nbytes, 4 * rotary_dim, positions.nbytes, q_out.nbytes, 0 if k is None else k.nbytes
     return p
 
 
 def rope(p: Rope, q, k, steps, positions, q_out, k_out) -> None:
     """Rotary positions of q and k (k None: q alone)."""
+    a, b, c, d, e = p.sizes
+    assert q.nbytes >= a and steps.nbytes >= b and positions.nbytes >= c and q_out.nbytes >= d and steps.is_cuda and \
+        (k is None or k_out is None or k.nbytes >= e and k_out.nbytes >= e), _NOT_THE_PLANS
     rc = (_lib or lib()).sva_rope(p, q.data_ptr(), None if k is None else k.data_ptr(), steps.data_ptr(), positions.data_ptr(),
                                   q_out.data_ptr(), None if k_out is None else k_out.data_ptr(), _stream())
     if rc:
@@ -541,7 +568,7 @@ def make_kv_cache(k, v, format: str = "e4m3") -> KvCache:
     c.k_codes, c.v_codes, c.k_scale, c.v_scale = _ptr(k[0]), _ptr(v[0]), _ptr(k[1]), _ptr(v[1])
     if format == "fp4":
         c.k_sf, c.v_sf = _ptr(k[2]), _ptr(v[2])
-    c.arrays = (tuple(k), tuple(v))
+    c.arrays, c.on_gpu = (tuple(k), tuple(v)), all(t.is_cuda for t in (*k, *v))
     return c
 
 
@@ -550,6 +577,7 @@ def kv_cache_write(c: KvCache, k, v, slots, status=None) -> None:
     shape = Bq, H, T, d = k.shape
     assert H == c.H and d == c.d and v.shape == shape and k.dtype is v.dtype is torch.bfloat16, "k, v are [B,H,T,d] bf16"
     assert slots.shape == (Bq, T) and slots.dtype is torch.int32 and slots.is_contiguous(), "slots are [B,T] int32"
+    assert c.on_gpu and k.is_cuda and v.is_cuda and slots.is_cuda and (status is None or status.is_cuda), "the cache and its tensors are on the GPU"
     rc = (_lib or lib()).sva_kv_cache_write(c, k.data_ptr(), v.data_ptr(), _strides(k), _strides(v), Bq, T, slots.data_ptr(),
                                             None if status is None else status.data_ptr(), _stream())
     if rc:
@@ -564,6 +592,7 @@ def kv_cache_read(c: KvCache, page_table, lengths, k, v, status=None) -> None:
     stride, inner = page_table.stride()
     assert rows == Bq and page_table.dtype is torch.int32 and inner == 1, "page_table is [B,pages] int32"
     assert lengths.shape == (Bq,) and lengths.dtype is torch.int32 and lengths.is_contiguous(), "lengths is [B] int32"
+    assert c.on_gpu and page_table.is_cuda and lengths.is_cuda and k.is_cuda and v.is_cuda and (status is None or status.is_cuda), "the cache and its tensors are on the GPU"
     rc = (_lib or lib()).sva_kv_cache_read(c, page_table.data_ptr(), stride, most, lengths.data_ptr(), Bq, N, k.data_ptr(), v.data_ptr(),
                                            _strides(k), _strides(v), None if status is None else status.data_ptr(), _stream())
     if rc:

@@ -192,3 +192,54 @@ def test_token_indices_that_do_not_match_are_refused(lib):
             B.gather_tokens(x, i, p)
         with pytest.raises(AssertionError):
             B.scatter_tokens(p, i, x)
+
+
+def _refused(call, *args):
+    with pytest.raises(AssertionError):
+        call(*args)
+
+
+def test_calls_refuse_tensors_that_are_not_their_plans(lib):
+    """Sizes below the plan's, and memory that is not the GPU's, end before the C call (which here, without a device, would answer with
+    an error of its own)."""
+    bf, u8 = torch.bfloat16, torch.uint8
+    x, x8, xs, w, w8, ws = (torch.zeros(4, 64, dtype=bf), torch.zeros(4, 64, dtype=u8), torch.zeros(1, 4), torch.zeros(8, 64, dtype=bf),
+                            torch.zeros(8, 64, dtype=u8), torch.zeros(1, 1))
+    out, r, bias = torch.zeros(4, 8, dtype=bf), torch.zeros(4, 8, dtype=bf), torch.zeros(8)
+    p = B.make_linear(x, x8, xs, w8, ws, out, residual=r, w=w)
+    _refused(B.quantize_rows_fp8, p, x, x8, xs)                                      # not on the GPU
+    _refused(B.quantize_tiles_fp8, p, w, w8, ws)
+    _refused(B.linear_fp8, p, x8, xs, w8, ws, out, bias, r)
+    x, x8, xs, w, w8, ws, out, r = (_OnGpu(t) for t in (x, x8, xs, w, w8, ws, out, r))
+    p = B.make_linear(x, x8, xs, w8, ws, out, residual=r, w=w)
+    for call, args in ((B.quantize_rows_fp8, (x, x8, xs)), (B.quantize_tiles_fp8, (w, w8, ws)), (B.linear_fp8, (x8, xs, w8, ws, out, _OnGpu(bias), r))):
+        for i, t in enumerate(args):
+            for other in (t.t[..., :-1], t.t[:0]):
+                _refused(call, p, *args[:i], _OnGpu(other), *args[i + 1:])
+    _refused(B.linear_fp8, p, x8, xs, w8, ws, out, bias, r)
+    _refused(B.linear_fp8, p, x8, xs, w8, ws, out, None, r, torch.zeros(1, dtype=torch.int32))
+    q, pos = torch.zeros(2, 4, 6, 64, dtype=bf), torch.zeros(1, 2, 6, dtype=torch.int32)
+    steps, _ = B.rope_steps(64)                                                      # (on the CPU unless a device is named)
+    _refused(B.rope, B.make_rope(q, q, q, q, pos, 64), q, q, _OnGpu(steps), pos, q, q)
+    q, pos = _OnGpu(q), _OnGpu(pos)
+    p = B.make_rope(q, q, q, q, pos, 64)
+    _refused(B.rope, p, q, q, steps, pos, q, q)
+    args = (q, q, _OnGpu(steps), pos, q, q)
+    for i, t in enumerate(args):
+        for other in (t.t[..., :-1], t.t[:0]):
+            _refused(B.rope, p, *args[:i], _OnGpu(other), *args[i + 1:])
+    codes, scale, q = torch.zeros(3, 4, 16, 64, dtype=u8), torch.zeros(3, 4, 16), q.t
+    c = B.make_kv_cache([codes, scale], [codes, scale])
+    slots, table, lengths = torch.zeros(2, 6, dtype=torch.int32), torch.zeros(2, 1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    _refused(B.kv_cache_write, c, q, q, slots)
+    _refused(B.kv_cache_read, c, table, lengths, q, q)
+
+
+class _OnGpu:
+    """A tensor that says it is on the GPU."""
+
+    def __init__(self, t):
+        self.t, self.is_cuda = t, True
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
