@@ -82,10 +82,10 @@ quantize_rows_kernel(const __nv_bfloat16* __restrict__ x, int M, int K, long lon
 // One CTA per 128 x 128 tile, which stays in registers between the maximum and the cast.
 __global__ void __launch_bounds__(256)
 quantize_tiles_kernel(const __nv_bfloat16* __restrict__ w, int N, int K, long long ws, uint8_t* __restrict__ w8, long long w8s,
-                      float* __restrict__ scale, long long ss) {
+                      float* __restrict__ scale, long long ss, int Kb) {
   __shared__ float part[8];
   const int zero = grid_dep_wait();
-  const int g = blockIdx.x, J = blockIdx.y, c = g * 128 + (threadIdx.x & 7) * 16 + zero;
+  const int g = (int)(blockIdx.x % Kb), J = (int)(blockIdx.x / Kb), c = g * 128 + (threadIdx.x & 7) * 16 + zero;
   uint4 u[4][2];
   float amax = 0.f;
 #pragma unroll
@@ -970,10 +970,11 @@ int launch_quantize_rows(const sva_linear_t* p, const void* x, void* x8, float* 
 }
 
 int launch_quantize_tiles(const sva_linear_t* p, const void* w, void* w8, float* w_scale, cudaStream_t st) {
-  const dim3 grid((p->K + 127) / 128, (p->N + 127) / 128);
-  if (grid.y > 65535) return SVA_ERR_UNSUPPORTED;
-  return launch_dep(quantize_tiles_kernel, grid, 256, 0, st, (const __nv_bfloat16*)w, p->N, p->K, (long long)p->w_stride, (uint8_t*)w8,
-                    (long long)p->w8_stride, w_scale, (long long)p->w_scale_stride);
+  const int Kb = (p->K + 127) / 128;
+  const long long tiles = (long long)Kb * ((p->N + 127) / 128);
+  if (tiles > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  return launch_dep(quantize_tiles_kernel, dim3((unsigned)tiles), 256, 0, st, (const __nv_bfloat16*)w, p->N, p->K, (long long)p->w_stride,
+                    (uint8_t*)w8, (long long)p->w8_stride, w_scale, (long long)p->w_scale_stride, Kb);
 }
 
 // How many clusters of `ctas` CTAs of a kernel the current device, or the part of it that this process has, holds at once.

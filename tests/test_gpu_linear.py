@@ -263,3 +263,18 @@ def test_a_starved_product_gives_up(M, N, K):
     assert int(s["status"].item()) == B.SVA_DEV_TIMEOUT
     s["status"].zero_()
     np.testing.assert_array_equal(_product(s), want)
+
+
+def test_weights_of_very_many_rows():
+    """More than 65 535 tiles of 128 outputs."""
+    rng = np.random.default_rng(12)
+    N, K = 65536 * 128 + 5, 24
+    w, w8 = torch.zeros(N, K, dtype=torch.bfloat16, device="cuda"), torch.full((N, 32), 0x55, dtype=torch.uint8, device="cuda")
+    ws = torch.full((65537, 1), 9.0, device="cuda")
+    w[-133:], w[:128] = _bf16(rng, 133, K).cuda(), _bf16(rng, 128, K).cuda()
+    B.quantize_tiles_fp8(B.make_linear(w8=w8, w_scale=ws, w=w), w, w8, ws)
+    for at, tiles in ((np.s_[:128], np.s_[:1]), (np.s_[-133:], np.s_[-2:])):
+        codes, scale = L.quantize_tiles(_f64(w[at]))
+        np.testing.assert_array_equal(w8[at][:, :K].cpu().numpy(), codes)
+        np.testing.assert_array_equal(_f64(ws[tiles]), scale)
+    assert bool((w8[:, K:] == 0).all()) and bool((w8[128:-133] == 0).all()) and bool((ws[1:-2] == 1.0).all())
