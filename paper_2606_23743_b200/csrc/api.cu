@@ -457,6 +457,7 @@ int sva_rope_steps(int32_t rotary_dim, const int32_t axis_pairs[3], double base,
   if (scaling < SVA_ROPE_PLAIN || scaling > SVA_ROPE_PARTS) return SVA_ERR_INVALID_ARG;
   if (!(base >= 1.0) || !std::isfinite(base) || !(factor >= 1.0) || !std::isfinite(factor)) return SVA_ERR_INVALID_ARG;
   if (scaling == SVA_ROPE_PARTS && !(trained_length > 0.0 && beta_slow >= 0.0 && beta_fast > beta_slow)) return SVA_ERR_INVALID_ARG;
+  if (scaling == SVA_ROPE_PARTS && std::isinf(trained_length) && std::isinf(beta_fast)) return SVA_ERR_INVALID_ARG;      // (their quotient)
   int64_t total = 0;
   for (int a = 0; a < 3; ++a) {
     if (axis_pairs[a] < 0) return SVA_ERR_INVALID_ARG;

@@ -243,3 +243,18 @@ class _OnGpu:
 
     def __getattr__(self, name):
         return getattr(self.t, name)
+
+
+@pytest.mark.parametrize("kw", [dict(trained_length=float("inf"), beta_fast=float("inf")), dict(beta_fast=float("nan")), dict(beta_slow=float("nan")),
+                                dict(trained_length=float("nan"))])
+def test_rope_steps_refuse_what_gives_no_number(lib, kw):
+    with pytest.raises(B.SvaError) as e:
+        B.rope_steps(64, [32], **{"scaling": "parts", "factor": 4.0, "trained_length": 4096.0, **kw})
+    assert e.value.status == INVALID
+
+
+def test_rope_steps_at_the_limits_of_the_rule_by_parts(lib):
+    """Endlessly long training: every pair stays; an endless fast end: every pair is slowed down."""
+    plain, linear = (B.rope_steps(64, [32], scaling=s, factor=4.0)[0] for s in ("none", "linear"))
+    for kw, want in ((dict(trained_length=float("inf")), plain), (dict(trained_length=4096.0, beta_fast=float("inf")), linear)):
+        assert torch.equal(B.rope_steps(64, [32], scaling="parts", factor=4.0, **kw)[0], want)
