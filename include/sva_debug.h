@@ -1,7 +1,7 @@
 /*
  * sva_debug.h -- test and tuning aids exported by libsva.so next to the public calls of sva.h.
  *
- * Unlike everything in sva.h these three calls keep PROCESS-GLOBAL state (host variables and two device
+ * Unlike everything in sva.h these calls keep PROCESS-GLOBAL state (host variables and two device
  * variables per loaded library): a setting stays in force for every later launch of the process
  * until it is set back.  They are meant for single-threaded test and bench programs.  The paper has no
  * counterpart.
@@ -44,6 +44,14 @@ void sva_debug_set_mode(int bits);
  * Returns 0 on success.
  */
 int sva_debug_set_wait_limit(long long cycles);
+
+/*
+ * Test aid: which form the last of these calls chose, so that a test of a form notices when its sizes do not reach it any more.
+ *   sva_linear_fp8: 1 few tokens, 2 single CTAs, 3 inputs split over a cluster, 4 pairs
+ *   sva_quantize_rows_fp8: groups of inputs per thread (1 or 4)
+ *   sva_rope, sva_kv_cache_write, sva_kv_cache_read: heads per CTA
+ */
+int sva_debug_last_choice(void);
 
 #ifdef __cplusplus
 }

@@ -28,7 +28,7 @@ EXPORTS = [
     "sva_quantize_rows_fp8", "sva_quantize_tiles_fp8", "sva_linear_fp8", "sva_rope", "sva_rope_steps", "sva_kv_cache_write",
     "sva_kv_cache_read",
 ]
-DEBUG_EXPORTS = ["sva_debug_set_prof_buffer", "sva_debug_set_mode", "sva_debug_set_wait_limit"]
+DEBUG_EXPORTS = ["sva_debug_set_prof_buffer", "sva_debug_set_mode", "sva_debug_set_wait_limit", "sva_debug_last_choice"]
 NOALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -159,6 +159,8 @@ def lib():
         L.sva_debug_set_mode.argtypes = [C.c_int]
         L.sva_debug_set_wait_limit.restype = C.c_int
         L.sva_debug_set_wait_limit.argtypes = [C.c_longlong]
+        L.sva_debug_last_choice.restype = C.c_int
+        L.sva_debug_last_choice.argtypes = []
         L.sva_status_string.restype = C.c_char_p
         L.sva_status_string.argtypes = [C.c_int]
         _lib = L
@@ -379,6 +381,11 @@ def debug_set_wait_limit(cycles: int) -> None:
     """SM cycles a device-side wait may last before its CTA gives up; <= 0 restores the default."""
     if lib().sva_debug_set_wait_limit(C.c_longlong(int(cycles))) != 0:
         raise RuntimeError("sva_debug_set_wait_limit failed")
+
+
+def debug_last_choice() -> int:
+    """Which form the last linear, rotary or cache call chose (include/sva_debug.h)."""
+    return lib().sva_debug_last_choice()
 
 
 def attn_remainder_workspace_bytes(p: Problem, order: int = 0) -> int:

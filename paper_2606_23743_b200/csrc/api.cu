@@ -14,6 +14,8 @@ int rem_set_wait_limit(long long cycles);
 void lin_set_debug_mode(int v);
 int lin_set_wait_limit(long long cycles);
 
+std::atomic<int> g_last_choice{0};
+
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int validate_problem(const sva_problem_t* p) {
@@ -547,5 +549,7 @@ void sva_debug_set_mode(int v) {
 }
 /* test aid: cycles a device-side wait may last before the CTA gives up (<= 0 restores the default) */
 int sva_debug_set_wait_limit(long long cycles) { return ts_set_wait_limit(cycles) | rem_set_wait_limit(cycles) | lin_set_wait_limit(cycles); }
+/* test aid: the form that the last linear, rotary or cache call chose */
+int sva_debug_last_choice(void) { return g_last_choice.load(std::memory_order_relaxed); }
 
 }  // extern "C"

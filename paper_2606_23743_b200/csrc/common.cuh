@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <mutex>
 
 #include "../../include/sva.h"
@@ -139,6 +140,10 @@ inline int blocks_per_cta(long long blocks, int block_bytes) {
   const int most = (128 << 10) / block_bytes;
   return run < 1 ? 1 : run > most ? most : (int)run;
 }
+
+// what a call chose among its forms, for tests (sva_debug_last_choice)
+extern std::atomic<int> g_last_choice;
+inline void note_choice(int form) { g_last_choice.store(form, std::memory_order_relaxed); }
 
 // host-side argument checks shared by the entry points
 int validate_problem(const sva_problem_t* p);

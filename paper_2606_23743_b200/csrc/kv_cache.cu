@@ -254,6 +254,7 @@ static int launch_cache(bool write, CacheParams& prm, const sva_kv_cache_t* c, c
   prm.chunks = (c->H + prm.chunk - 1) / prm.chunk;
   const long long ctas = 2 * tiles * prm.chunks;
   if (ctas > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  note_choice(prm.chunk);
   const bool fp4 = c->format == SVA_CACHE_FP4;
   auto kern = write ? (lanes == 8 ? (fp4 ? cache_write_kernel<8, true> : cache_write_kernel<8, false>)
                                   : (fp4 ? cache_write_kernel<4, true> : cache_write_kernel<4, false>))

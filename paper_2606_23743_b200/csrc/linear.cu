@@ -965,6 +965,7 @@ int launch_quantize_rows(const sva_linear_t* p, const void* x, void* x8, float* 
   const bool four = rows * ((Kb + 3) / 4) >= 148;
   const int tiles = four ? (Kb + 3) / 4 : Kb;
   if (rows * tiles > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  note_choice(four ? 4 : 1);
   return launch_dep(four ? quantize_rows_kernel<4> : quantize_rows_kernel<1>, dim3((unsigned)(rows * tiles)), 256, 0, st, (const __nv_bfloat16*)x,
                     p->M, p->K, (long long)p->x_stride, (uint8_t*)x8, (long long)p->x8_stride, x_scale, (long long)p->x_scale_stride, tiles);
 }
@@ -1032,6 +1033,7 @@ static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void
   if (PAIR && (rc = lin_map(&to, out, p->N < 8 ? 8 : p->N & ~7, p->M, 2 * p->out_stride, 2, 128))) return rc;
   if (PAIR && prm.residual && (rc = lin_map(&tr, prm.residual, p->N, p->M, 2 * p->residual_stride, 2, 128))) return rc;
   if (tiles > 0x7fffffffLL - sms) return SVA_ERR_UNSUPPORTED;
+  note_choice(PAIR ? 4 : SPLIT ? 3 : 2);
   const long long most = sms / CTAS;
   const int per = SPLIT ? split : CTAS;
   return launch_dep_cluster(per, kern, dim3((unsigned)(per * (SPLIT || tiles < most ? tiles : most))), S::THREADS, SMEM, st, tx, tw, to, tr, prm,
@@ -1068,6 +1070,7 @@ static int launch_linear_few(const sva_linear_t* p, const void* x8, const void* 
   const int most = prm.debug & 64 ? 1 : largest[dev];     // (test aid: as on a device that holds no clusters)
   int split = 1;
   while (split < most && 2 * split <= prm.Kb && (long long)rows * split * 2 <= (long long)sms * S::PER_SM) split *= 2;
+  note_choice(1);
   return launch_dep_cluster(split, kern, dim3((unsigned)(rows * split)), few::THREADS, S::SMEM, st, tx, tw, prm, split, p->act);
 }
 

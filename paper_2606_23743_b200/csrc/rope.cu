@@ -202,6 +202,7 @@ int launch_rope(const sva_rope_t* p, const void* q, const void* k, const void* s
   prm.q_chunks = (prm.Hq + prm.chunk - 1) / prm.chunk;
   prm.chunks = prm.q_chunks + (prm.Hk + prm.chunk - 1) / prm.chunk;
   if (tiles * prm.chunks > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  note_choice(prm.chunk);
   auto kern = form == 0 ? rope_kernel<0> : form == 1 ? rope_kernel<1> : rope_kernel<2>;
   return launch_dep(kern, dim3((unsigned)(tiles * prm.chunks)), ROPE_THREADS, 0, st, prm, lanes);
 }

@@ -278,3 +278,130 @@ def test_weights_of_very_many_rows():
         np.testing.assert_array_equal(w8[at][:, :K].cpu().numpy(), codes)
         np.testing.assert_array_equal(_f64(ws[tiles]), scale)
     assert bool((w8[:, K:] == 0).all()) and bool((w8[128:-133] == 0).all()) and bool((ws[1:-2] == 1.0).all())
+
+
+def _chose(form):
+    names = {1: "few tokens", 2: "single CTAs", 3: "split inputs", 4: "pairs"}
+    got = B.debug_last_choice()
+    assert got == form, f"these sizes are for {names[form]}, and {names.get(got, got)} took them"
+
+
+# Sizes that pairs of CTAs take: several tiles per pair, rings and accumulators that come round, one or two groups of inputs, rows and columns that end
+# within a tile, a single row or column of tiles.
+PAIRS = [(5003, 2500, 1160), (2500, 3001, 2309), (130, 33003, 1030), (33000, 130, 264), (1800, 5003, 100), (3000, 3001, 130)]
+
+
+@pytest.mark.parametrize("M,N,K", PAIRS)
+def test_products_in_pairs(M, N, K):
+    rng = np.random.default_rng(M + 7 * N + K)
+    s = _layer(rng, M, N, K, extra=1)
+    got = _product(s)
+    _chose(4)
+    _check(s, got)
+    assert (s["obuf"][:, N:] == 5.0).all()
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+@pytest.mark.parametrize("bias,residual", [(True, False), (False, True), (True, True)])
+def test_epilogues_in_pairs(bias, residual, act):
+    M, N, K = 5003, 2501, 1160
+    rng = np.random.default_rng(13)
+    s = _layer(rng, M, N, K, act, bias, residual, 1)
+    got = _product(s)
+    _chose(4)
+    _check(s, got)
+    assert (s["obuf"][:, N:] == 5.0).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(5003, 2501, 1160), (2500, 3000, 256)])
+def test_residual_in_place_and_repeatable_in_pairs(M, N, K):
+    rng = np.random.default_rng(14)
+    s = _layer(rng, M, N, K, "silu", True, True)
+    first = s["residual"].clone()
+    want = _product(s)
+    s["out"] = s["residual"]
+    got = _product(s)
+    _chose(4)
+    np.testing.assert_array_equal(got, want)
+    s["residual"].copy_(first)
+    np.testing.assert_array_equal(_product(s), want)
+
+
+def test_a_nan_code_stays_with_its_outputs_in_pairs():
+    rng = np.random.default_rng(15)
+    s = _layer(rng, 5003, 2501, 1160)
+    want = _product(s)
+    s["x8"][4999, 7] = s["x8"][300, 1159] = 0x7F
+    s["w8"][2400, 1159] = s["w8"][130, 640] = 0xFF
+    got = _product(s)
+    _chose(4)
+    bad = np.zeros(got.shape, bool)
+    bad[[300, 4999], :], bad[:, [130, 2400]] = True, True
+    assert np.isnan(got[bad]).all()
+    np.testing.assert_array_equal(got[~bad], want[~bad])
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_activations_far_out_in_pairs(act):
+    """Two values share a reciprocal: a NaN or an infinity beside one leaves it alone."""
+    M, N = 2500, 3008
+    b = torch.linspace(-60, 60, N, dtype=torch.float64)
+    b[5], b[700], b[1501] = float("nan"), float("inf"), float("-inf")
+    b[::32], b[1::32] = -1e38, 1e38
+    x8, w8 = torch.zeros(M, 128, dtype=torch.uint8, device="cuda"), torch.zeros(N, 128, dtype=torch.uint8, device="cuda")
+    xs, ws = torch.ones(1, M, device="cuda"), torch.ones(-(-N // 128), 1, device="cuda")
+    out = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    p = B.make_linear(None, x8, xs, w8, ws, out, act, K=128)
+    B.linear_fp8(p, x8, xs, w8, ws, out, b.float().cuda())
+    _chose(4)
+    got = _f64(out)
+    assert (got == got[:1])[:, ~np.isnan(got[0])].all()
+    with np.errstate(all="ignore"):
+        ref = L.activation(b.float().double().numpy(), act)
+    ref[1501] = 0.0
+    assert np.isnan(got[:, 5]).all() and np.isnan(got).sum() == M and got[0, 700] == np.inf
+    at = np.isfinite(ref)
+    got, ref = got[0][at], ref[at]
+    assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -18 * np.abs(ref) + 2.0 ** -53).all()
+
+
+@pytest.mark.parametrize("M,N,K,form", [(2500, 3000, 400, 4), (200, 300, 4000, 3)])
+def test_what_needs_clusters_goes_without(M, N, K, form):
+    rng = np.random.default_rng(16)
+    s = _layer(rng, M, N, K, "gelu", True, True)
+    _product(s)
+    _chose(form)
+    try:
+        B.debug_set_mode(64)
+        got = _product(s)
+        _chose(2)
+    finally:
+        B.debug_set_mode(0)
+    _check(s, got)
+
+
+def test_starved_pairs_give_up():
+    rng = np.random.default_rng(17)
+    s = _layer(rng, 5003, 2500, 1160, "none", True, True)
+    want = _product(s)
+    try:
+        B.debug_set_wait_limit(100_000_000)                        # about 50 ms
+        B.debug_set_mode(1024)
+        B.linear_fp8(s["p"], s["x8"], s["xs"], s["w8"], s["ws"], s["out"], s["bias"], s["residual"], s["status"])
+        torch.cuda.synchronize()
+        _chose(4)
+    finally:
+        B.debug_set_mode(0)
+        B.debug_set_wait_limit(0)
+    assert int(s["status"].item()) == B.SVA_DEV_TIMEOUT
+    s["status"].zero_()
+    np.testing.assert_array_equal(_product(s), want)
+
+
+@pytest.mark.parametrize("M,N,K,form", [(64, 520, 1030, 1), (65, 520, 1030, 2), (1111, 1501, 1030, 2), (65, 4096, 4096, 3)])
+def test_the_other_forms_are_reached(M, N, K, form):
+    rng = np.random.default_rng(18)
+    s = _layer(rng, M, N, K)
+    got = _product(s)
+    _chose(form)
+    _check(s, got)
