@@ -405,3 +405,21 @@ def test_the_other_forms_are_reached(M, N, K, form):
     got = _product(s)
     _chose(form)
     _check(s, got)
+
+
+@pytest.mark.parametrize("K", [129, 330, 650, 1000, 1100])
+def test_codes_and_scales_of_many_rows(K):
+    """Four groups of inputs per thread: 2, 3, 6, 8 and 9 groups, rows and inputs that end within a block."""
+    M = 4801
+    rng = np.random.default_rng(K)
+    x, xbuf = _padded(M, K, torch.bfloat16, 0, 1)
+    x.copy_(_bf16(rng, M, K))
+    xbuf[:, K:] = 7.0                                              # (not inputs)
+    G, row = -(-K // 128), -(-K // 16) * 16
+    x8, xs = torch.full((M, row + 16), 0x55, dtype=torch.uint8, device="cuda"), torch.full((G, M + 3), 9.0, device="cuda")
+    B.quantize_rows_fp8(B.make_linear(x, x8, xs), x, x8, xs)
+    assert B.debug_last_choice() == 4
+    codes, scale = L.quantize_rows(_f64(x))
+    np.testing.assert_array_equal(x8[:, :K].cpu().numpy(), codes)
+    np.testing.assert_array_equal(_f64(xs[:, :M]), scale)
+    assert (x8[:, K:row] == 0).all() and (x8[:, row:] == 0x55).all() and (xs[:, M:] == 9.0).all()
