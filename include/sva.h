@@ -380,7 +380,8 @@ int sva_scatter_tokens(const void* src, const int64_t src_stride[3], const int32
  *                out[m,n] = bf16(act(y + bias[n]) + residual[m,n])
  * Sums are fp32 throughout (a group's products in the tensor core, the groups with their scales in registers), in a fixed order: results
  * are deterministic.  Codes may come from elsewhere (a checkpoint with fp32 scales per 128 x 128 tile of the weights); a code
- * that is NaN makes its outputs NaN.  act: SVA_ACT_GELU is the tanh form.
+ * that is NaN makes its outputs NaN.  A NaN in x or w is left out of amax and gets such a code; an infinity makes s infinite, and with it all outputs of
+ * its token, or of its tile's 128 outputs, NaN.  act: SVA_ACT_GELU is the tanh form.
  */
 typedef enum { SVA_ACT_NONE = 0, SVA_ACT_GELU = 1, SVA_ACT_SILU = 2 } sva_act_t;
 

@@ -423,3 +423,42 @@ def test_codes_and_scales_of_many_rows(K):
     np.testing.assert_array_equal(x8[:, :K].cpu().numpy(), codes)
     np.testing.assert_array_equal(_f64(xs[:, :M]), scale)
     assert (x8[:, K:row] == 0).all() and (x8[:, row:] == 0x55).all() and (xs[:, M:] == 9.0).all()
+
+
+@pytest.mark.parametrize("M", [5, 200, 4801])
+def test_nan_and_infinities_in_the_inputs(M):
+    """A NaN is left out of its scale and stays with its own token or output; an infinity takes its token, or the 128 outputs of its tile, with it.
+    What is left is as if a zero stood there."""
+    N, K = 300, 1000
+    rng = np.random.default_rng(19)
+    s = _layer(rng, M, N, K)
+    s["x"][1, 7] = s["x"][3, 990] = 0.0
+    s["w"][5, 130] = s["w"][290, 999] = 0.0
+    B.quantize_rows_fp8(s["p"], s["x"], s["x8"], s["xs"])
+    B.quantize_tiles_fp8(s["p"], s["w"], s["w8"], s["ws"])
+    want = _product(s)
+    s["x"][1, 7], s["x"][3, 990] = float("nan"), -float("inf")
+    s["w"][5, 130], s["w"][290, 999] = -float("nan"), float("inf")
+    B.quantize_rows_fp8(s["p"], s["x"], s["x8"], s["xs"])
+    assert B.debug_last_choice() == (4 if M == 4801 else 1)
+    B.quantize_tiles_fp8(s["p"], s["w"], s["w8"], s["ws"])
+    for x, x8, xs, (codes, scale) in ((s["x"], s["x8"], s["xs"], L.quantize_rows(_f64(s["x"]))), (s["w"], s["w8"], s["ws"], L.quantize_tiles(_f64(s["w"])))):
+        got, nan = x8[:, :K].cpu().numpy(), codes == 127
+        assert nan.sum() == 2
+        np.testing.assert_array_equal(got[~nan], codes[~nan])
+        assert ((got[nan] & 127) == 127).all()
+        np.testing.assert_array_equal(_f64(xs), scale)
+    got = _product(s)
+    bad = np.zeros(got.shape, bool)
+    bad[[1, 3], :], bad[:, 5], bad[:, 256:] = True, True, True      # (the tile of outputs 256 to 299)
+    assert np.isnan(got[bad]).all()
+    np.testing.assert_array_equal(got[~bad], want[~bad])
+
+
+def test_rows_of_nan_alone():
+    x = torch.full((3, 256), float("nan"), dtype=torch.bfloat16, device="cuda")
+    x[1, :128] = 1.0
+    x8, xs = torch.zeros(3, 256, dtype=torch.uint8, device="cuda"), torch.zeros(2, 3, device="cuda")
+    B.quantize_rows_fp8(B.make_linear(x, x8, xs), x, x8, xs)
+    assert ((x8 & 127) == 127).sum() == 5 * 128 and (x8[1, :128] == 126).all()
+    assert xs.tolist() == [[1.0, pytest.approx(1 / 448), 1.0], [1.0, 1.0, 1.0]]

@@ -94,3 +94,17 @@ def test_cache_rows_come_back_near(form, worst):
         assert np.abs(values - row).max() <= worst * np.abs(row).max()
     codes, scale, sf, values = L.cache_row(np.zeros(64), form)
     assert (codes == 0).all() and scale == 1.0 and (values == 0).all()
+
+
+def test_nan_and_infinities():
+    nan, inf = float("nan"), float("inf")
+    x = np.tile(np.linspace(-1, 1, 128), (4, 1))
+    x[1, 5], x[2, 5], x[3] = nan, inf, nan
+    codes, scale = L.quantize_rows(x)
+    assert (codes[1] == 127).sum() == (codes[2] == 127).sum() == 1 and (codes[3] == 127).all()
+    assert scale[0].tolist() == [float(L.f32(1 / 448)), float(L.f32(1 / 448)), inf, 1.0]
+    assert np.isnan(L.e4m3_values(L.quantize_tiles(x[1:2])[0])).sum() == 1
+    for form in ("e4m3", "fp4"):
+        values = [L.cache_row(row, form)[3] for row in x]
+        assert np.isfinite(values[0]).all() and np.isnan(values[2]).all() and np.isnan(values[3]).all()
+        assert np.isnan(values[1]).sum() == (1 if form == "e4m3" else 128)
