@@ -232,3 +232,45 @@ def test_rows_with_nan_and_infinities(form, d):
         _, scale, _, values = _expect(given, form)
         np.testing.assert_array_equal(arrays[1].cpu().numpy()[0], scale[0, :, :, 0])
         np.testing.assert_array_equal(_f64(got), torch.from_numpy(values).float().to(torch.bfloat16).float().numpy())
+
+
+@pytest.mark.parametrize("d,T", [(128, 19003), (64, 37950)])
+@pytest.mark.parametrize("form", ["e4m3", "fp4"])
+def test_more_heads_than_a_thread_has_in_flight(form, d, T):
+    """Eight heads per CTA, a thread's pass over four twice, 13 heads; against the oracle at some tokens and, everywhere, against calls of so
+    few tokens that a CTA has four heads."""
+    rng = np.random.default_rng(d)
+    H, page = 13, 48
+    pages = -(-T // page)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    k, v = (torch.randn(1, T, H, d, generator=g, device="cuda", dtype=torch.bfloat16).transpose(1, 2) for _ in range(2))
+    ids = torch.from_numpy(rng.permutation(pages).astype(np.int32)).cuda()
+    at = torch.arange(T, device="cuda")
+    slots = (ids[at // page] * page + at % page).to(torch.int32)[None].contiguous()
+    slots[0, 77] = -1
+    a, b = ((_arrays(form, pages, H, page, d), _arrays(form, pages, H, page, d)) for _ in range(2))
+    ca, cb = B.make_kv_cache(*a, form), B.make_kv_cache(*b, form)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.kv_cache_write(ca, k, v, slots, status)
+    assert B.debug_last_choice() == 8
+    for n in range(0, T, 5000):
+        B.kv_cache_write(cb, k[:, :, n:n + 5000], v[:, :, n:n + 5000], slots[:, n:n + 5000].contiguous(), status)
+        assert B.debug_last_choice() == 4
+    for x, y in zip(a[0] + a[1], b[0] + b[1]):
+        assert torch.equal(x, y)
+    some = torch.from_numpy(np.sort(rng.permutation(T)[:60])).cuda()
+    values = [torch.from_numpy(_expect(x[:, :, some], form)[3]).float().to(torch.bfloat16) for x in (k, v)]
+    ko, vo = (torch.full((1, H, T, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.kv_cache_read(ca, ids[None], torch.tensor([T - 2], dtype=torch.int32, device="cuda"), ko, vo, status)
+    assert B.debug_last_choice() == 8
+    there = (some != 77) & (some < T - 2)
+    for got, want in ((ko, values[0]), (vo, values[1])):
+        assert torch.equal(got[:, :, some[there]].cpu(), want[:, :, there.cpu()]) and bool((got[:, :, T - 2:] == 0).all())
+    n = page * 50
+    for i in range(0, T, n):
+        m = min(n, T - i)
+        parts = [torch.full((1, H, m, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        B.kv_cache_read(ca, ids[None, i // page:].contiguous(), torch.tensor([T - 2 - i], dtype=torch.int32, device="cuda"), *parts, status)
+        assert B.debug_last_choice() == 4
+        assert torch.equal(parts[0], ko[:, :, i:i + m]) and torch.equal(parts[1], vo[:, :, i:i + m])
+    assert int(status.item()) == 0

@@ -198,3 +198,25 @@ def test_halves_of_whole_pieces_of_four(d, R, N):
     assert torch.equal(qo[..., R:].contiguous().view(torch.int16), q[..., R:].contiguous().view(torch.int16))
     for x, y in ((q[..., :R], qo[..., :R]), (k, ko)):
         _check(_f64(y), _f64(x), L.frequencies([R // 2]), pos, [R // 2], R, "half")
+
+
+@pytest.mark.parametrize("first", [False, True])
+@pytest.mark.parametrize("layout,d,R,axes", [("interleaved", 128, 128, 3), ("interleaved", 96, 50, 1), ("half", 128, 64, 1), ("half", 128, 74, 1),
+                                             ("half", 64, 64, 1)])
+def test_more_heads_than_a_thread_has_in_flight(layout, d, R, axes, first):
+    """Twenty heads per CTA, 18 and 5 of them there: passes of four, the last one short; out of place and in place."""
+    Bq, Hq, Hk, N = 2, 18, 5, 2500
+    rng = np.random.default_rng(d + R)
+    q, k = _tensor(rng, (Bq, Hq, N, d), first), _tensor(rng, (Bq, Hk, N, d), first)
+    pairs = _pairs(R, axes)
+    pos = rng.integers(0, 5000, (axes, Bq, N))
+    positions = torch.from_numpy(pos.astype(np.int32)).cuda()
+    steps, _ = B.rope_steps(R, pairs, device="cuda")
+    qo, ko = torch.full_like(q, 3.0), torch.full_like(k, 3.0)
+    B.rope(B.make_rope(q, k, qo, ko, positions, R, layout, pairs), q, k, steps, positions, qo, ko)
+    assert B.debug_last_choice() == 20
+    for x, y in ((q, qo), (k, ko)):
+        _check(_f64(y), _f64(x), L.frequencies(pairs), pos, pairs, R, layout)
+    q2, k2 = q.clone(memory_format=torch.preserve_format), k.clone(memory_format=torch.preserve_format)
+    B.rope(B.make_rope(q2, k2, q2, k2, positions, R, layout, pairs), q2, k2, steps, positions, q2, k2)
+    assert B.debug_last_choice() == 20 and torch.equal(q2, qo) and torch.equal(k2, ko)
