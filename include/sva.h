@@ -482,8 +482,8 @@ typedef struct {
 
 /*
  * write : k, v [B,H,T,d] bf16 (element strides of b, h, n; multiples of 8, 16-byte aligned) into the slots [B,T] int32.  A negative slot
- *         leaves its token out (padding); one beyond the cache is reported (SVA_DEV_BAD_INDEX) and left out.  Slots of a
- *         call that are equal make its result order-dependent.
+ *         leaves its token out (padding); one beyond the cache is reported (SVA_DEV_BAD_INDEX) and left out.  Where slots
+ *         of a call are equal, what their row then holds is not defined (codes of one token, the scale of another).
  * read  : row n < min(N, lengths[b]) of k, v [B,H,N,d] comes from place n % page of page page_table[b][n / page] (int32, max_pages per
  *         row, table_stride between rows); rows from lengths[b] on become zeros.  A page id outside [0, pages), or a page beyond max_pages, is
  *         reported and its rows become zeros.

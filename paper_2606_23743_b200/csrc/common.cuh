@@ -226,11 +226,10 @@ __device__ __forceinline__ uint64_t div_fast2(uint64_t x2, uint64_t neg_s2, uint
   asm("fma.rm.f32x2 %0, %1, %2, %3;" : "=l"(t) : "l"(q0), "l"(neg_s2), "l"(x2));
   return fma2(t, y2, q0);
 }
-// amax / D, correctly rounded (D = 448, 2 688, 6); the general division outside of div_fast's range
+// a / 448, correctly rounded, a >= 0; the general division outside of div_fast's range
 __device__ __noinline__ static float div_any(float a, float b) { return __fdiv_rn(a, b); }
-template <int D>
-__device__ __forceinline__ float div_by(float a) {
-  return a >= 8.077935669463161e-28f && a <= 3.4e38f ? div_fast(a, (float)D, 1.0f / D) : div_any(a, (float)D);      // (2^-90)
+__device__ __forceinline__ float div_by_448(float a) {
+  return a >= 8.077935669463161e-28f && a <= 3.4e38f ? div_fast(a, 448.0f, 1.0f / 448.0f) : div_any(a, 448.0f);      // (2^-90)
 }
 // the largest magnitude of 16 bf16 values as fp32; a NaN among them is the result, or (NANS false) is left out
 template <bool NANS = false>

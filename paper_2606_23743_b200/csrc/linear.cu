@@ -29,7 +29,7 @@ __device__ __forceinline__ void lin_load16(const __nv_bfloat16* row, int c, int 
     u[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
-__device__ __forceinline__ float lin_scale(float amax) { return amax == 0.f ? 1.0f : div_by<448>(amax); }
+__device__ __forceinline__ float lin_scale(float amax) { return amax == 0.f ? 1.0f : div_by_448(amax); }
 // the codes of 16 values: the correctly rounded fp32 quotients, rounded to e4m3
 __device__ __forceinline__ uint4 lin_codes(const uint4 (&u)[2], float s) {
   const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
@@ -1028,9 +1028,10 @@ static int launch_linear_tiles(const sva_linear_t* p, const void* x8, const void
   CUtensorMap tx, tw, to, tr;
   if ((rc = lin_map(&tx, x8, p->K, p->M, p->x8_stride, 1, 128))) return rc;
   if ((rc = lin_map(&tw, w8, p->K, p->N, p->w8_stride, 1, PAIR ? 64 : 128))) return rc;
-  // (a tile store writes whole 16-byte pieces, also beyond an inner extent that ends within one: it gets the whole pieces only)
+  // (a tile store writes whole 16-byte pieces, also beyond an inner extent that ends within one: it gets the whole pieces only; there are some,
+  // since pairs never need fewer rounds for up to 128 columns)
   to = tr = tx;
-  if (PAIR && (rc = lin_map(&to, out, p->N < 8 ? 8 : p->N & ~7, p->M, 2 * p->out_stride, 2, 128))) return rc;
+  if (PAIR && (rc = lin_map(&to, out, p->N & ~7, p->M, 2 * p->out_stride, 2, 128))) return rc;
   if (PAIR && prm.residual && (rc = lin_map(&tr, prm.residual, p->N, p->M, 2 * p->residual_stride, 2, 128))) return rc;
   if (tiles > 0x7fffffffLL - sms) return SVA_ERR_UNSUPPORTED;
   note_choice(PAIR ? 4 : SPLIT ? 3 : 2);
