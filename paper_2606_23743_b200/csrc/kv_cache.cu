@@ -5,7 +5,8 @@
 //
 // Both are HBM-bound streaming passes, the 4-bit cast also by its instructions.  d/16 lanes own a row, 16 channels each (one 4-bit scale block),
 // so that a row's maximum is a few shuffles; a thread looks its token's slot up once and then has some heads' rows in flight.
-// 24 heads of 32 760 tokens, us: e4m3 written 92 = 6.6 TB/s, read 96 = 6.3; 4-bit 90 = 5.8 and 86 = 6.0.
+// 24 heads of 32 760 tokens, us, one call after another: e4m3 written 91 = 6.7 TB/s, read 95 = 6.4; 4-bit 86 = 6.1 and 83 = 6.3; heads of 64: e4m3 48.2
+// and 49.9, 4-bit 47.4 and 44.4.
 #include <cuda_fp4.h>
 
 #include "common.cuh"

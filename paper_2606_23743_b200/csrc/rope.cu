@@ -68,7 +68,8 @@ __device__ __forceinline__ uint4 rope_store8(const float (&x)[8]) {
 // FORM 0: interleaved: a 16-byte vector, 4 pairs.
 // FORM 1: half layout whose halves are whole 8-byte pieces: 4 pairs again, from one piece of each half; behind the rotated channels 16 bytes.
 // FORM 2: half layout otherwise: a 16-byte vector, whose partners lie at no fixed place of another: they come through shared memory.  All
-// lanes of a token have read a row before any of them writes it, so in place is safe (in the other forms a thread writes what it read).
+// lanes of a token have read a row before any of them writes it, so in place is safe (in the other forms a thread writes what it read).  Eight
+// phases per thread and the way through shared memory: 24 + 24 heads of 32 760 tokens, 74 of 128 channels 176 us = 4.6 TB/s, 64 channels (form 1) 125.
 // Form 1 with 16-byte vectors and the partners by shuffles, twice the phases and half the loads: 2 x 8 191 tokens, 32 + 8 heads of 64 rotated
 // channels of 128 61.4 us, so 56.7; 16 + 16 heads of 128, 8 190 tokens, 29.6, so 24.1; one token of
 // 8 x (32 + 8) heads 3.9, so 2.7.
