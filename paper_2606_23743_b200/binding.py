@@ -52,6 +52,7 @@ class Linear(C.Structure):
     # bytes of the three calls' tensors (make_linear, if they are on the GPU)
     rows = tiles = (float("inf"),) * 3
     product = (float("inf"),) * 7
+    gaps = {}
 
 
 class Rope(C.Structure):
@@ -60,6 +61,7 @@ class Rope(C.Structure):
                 ("factor", C.c_float), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
                 ("q_out_stride", C.c_int64 * 3), ("k_out_stride", C.c_int64 * 3), ("pos_stride", C.c_int64 * 2)]
     sizes = (float("inf"),) * 5                            # bytes of the call's tensors (make_rope, if they are on the GPU)
+    gaps = {}
 
 
 class KvCache(C.Structure):
@@ -432,9 +434,25 @@ ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
 CACHE_FORMATS = {"e4m3": 0, "fp4": 1}
 
 
-# A call's tensors are those that its plan was made from, or others like them: their sizes are compared, and what the plan has not seen is looked at.
-# (Strides and devices of every tensor again would be a third of what a small call takes in Python.)
+# A call's tensors are those that its plan was made from, or others like them: their sizes are compared, where the plan's have gaps their strides too, and
+# what the plan has not seen is looked at.  (Strides and devices of every tensor again would be a third of what a small call takes in Python.)
 _NOT_THE_PLANS = "tensors on the GPU, no smaller than those that the plan was made for"
+
+
+def _gaps(**tensors):
+    """The strides (of more than one row) of the tensors that reach further than their bytes."""
+    found = {}
+    for name, t in tensors.items():
+        if t is not None and not t.is_contiguous():
+            steps = [(i, s) for i, (n, s) in enumerate(zip(t.shape, t.stride())) if n > 1]
+            if sum((t.shape[i] - 1) * s for i, s in steps) >= t.numel():
+                found[name] = steps
+    return found
+
+
+def _same_gaps(gaps, **tensors):
+    for name, t in tensors.items():
+        assert t is None or all(t.stride(i) == s for i, s in gaps.get(name, ())), f"{name} has other strides than the plan's"
 
 
 def _row_stride(t, what):
@@ -481,6 +499,7 @@ def make_linear(x=None, x8=None, x_scale=None, w8=None, w_scale=None, out=None, 
         size = lambda t: 0 if t is None else t.nbytes                                                                    # noqa: E731
         p.rows, p.tiles = (size(x), size(x8), size(x_scale)), (size(w), size(w8), size(w_scale))
         p.product = (*p.rows[1:], *p.tiles[1:], size(out), size(residual), 4 * p.N)
+    p.gaps = _gaps(x=x, x8=x8, x_scale=x_scale, w=w, w8=w8, w_scale=w_scale, out=out, residual=residual)
     return p
 
 
@@ -488,6 +507,8 @@ def quantize_rows_fp8(p: Linear, x, x8, x_scale) -> None:
     """Activations to e4m3 codes, a scale per token and 128 inputs."""
     a, b, c = p.rows
     assert x.nbytes >= a and x8.nbytes >= b and x_scale.nbytes >= c, _NOT_THE_PLANS
+    if p.gaps:
+        _same_gaps(p.gaps, x=x, x8=x8, x_scale=x_scale)
     rc = (_lib or lib()).sva_quantize_rows_fp8(p, x.data_ptr(), x8.data_ptr(), x_scale.data_ptr(), _stream())
     if rc:
         raise SvaError(rc, "sva_quantize_rows_fp8")
@@ -497,6 +518,8 @@ def quantize_tiles_fp8(p: Linear, w, w8, w_scale) -> None:
     """Weights to e4m3 codes, a scale per tile of 128 x 128."""
     a, b, c = p.tiles
     assert w.nbytes >= a and w8.nbytes >= b and w_scale.nbytes >= c, _NOT_THE_PLANS
+    if p.gaps:
+        _same_gaps(p.gaps, w=w, w8=w8, w_scale=w_scale)
     rc = lib().sva_quantize_tiles_fp8(C.byref(p), _ptr(w), _ptr(w8), _ptr(w_scale), _stream())
     if rc != SVA_OK:
         raise SvaError(rc, "sva_quantize_tiles_fp8")
@@ -508,6 +531,8 @@ def linear_fp8(p: Linear, x8, x_scale, w8, w_scale, out, bias=None, residual=Non
     assert x8.nbytes >= a and x_scale.nbytes >= b and w8.nbytes >= c and w_scale.nbytes >= d and out.nbytes >= e and \
         (residual is None or residual.nbytes >= f) and (status is None or status.is_cuda), _NOT_THE_PLANS
     assert bias is None or bias.is_cuda and bias.dtype is torch.float32 and bias.nbytes == g and bias.is_contiguous(), "bias is [N] fp32"
+    if p.gaps:
+        _same_gaps(p.gaps, x8=x8, x_scale=x_scale, w8=w8, w_scale=w_scale, out=out, residual=residual)
     rc = (_lib or lib()).sva_linear_fp8(p, x8.data_ptr(), x_scale.data_ptr(), w8.data_ptr(), w_scale.data_ptr(), out.data_ptr(),
                                         None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(),
                                         None if status is None else status.data_ptr(), _stream())
@@ -546,6 +571,7 @@ def make_rope(q, k, q_out, k_out, positions, rotary_dim: int, layout: str = "int
         p.k_stride, p.k_out_stride = _strides(k), _strides(k_out)
     if all(t.is_cuda for t in (q, q_out, positions, *((k, k_out) if k is not None else ()))):
         p.sizes = q.nbytes, 4 * rotary_dim, positions.nbytes, q_out.nbytes, 0 if k is None else k.nbytes
+    p.gaps = _gaps(q=q, k=k, positions=positions, q_out=q_out, k_out=k_out)
     return p
 
 
@@ -554,6 +580,8 @@ def rope(p: Rope, q, k, steps, positions, q_out, k_out) -> None:
     a, b, c, d, e = p.sizes
     assert q.nbytes >= a and steps.nbytes >= b and positions.nbytes >= c and q_out.nbytes >= d and steps.is_cuda and \
         (k is None or k_out is None or k.nbytes >= e and k_out.nbytes >= e), _NOT_THE_PLANS
+    if p.gaps:
+        _same_gaps(p.gaps, q=q, k=k, positions=positions, q_out=q_out, k_out=k_out)
     rc = (_lib or lib()).sva_rope(p, q.data_ptr(), None if k is None else k.data_ptr(), steps.data_ptr(), positions.data_ptr(),
                                   q_out.data_ptr(), None if k_out is None else k_out.data_ptr(), _stream())
     if rc:

@@ -258,3 +258,23 @@ def test_rope_steps_at_the_limits_of_the_rule_by_parts(lib):
     plain, linear = (B.rope_steps(64, [32], scaling=s, factor=4.0)[0] for s in ("none", "linear"))
     for kw, want in ((dict(trained_length=float("inf")), plain), (dict(trained_length=4096.0, beta_fast=float("inf")), linear)):
         assert torch.equal(B.rope_steps(64, [32], scaling="parts", factor=4.0, **kw)[0], want)
+
+
+def test_calls_refuse_other_strides_than_those_of_a_plan_with_gaps(lib):
+    """A plan of views that leave something out between their rows reaches further than their bytes."""
+    bf, u8 = torch.bfloat16, torch.uint8
+    x, x8, xs = _OnGpu(torch.zeros(4, 96, dtype=bf)[:, :64]), _OnGpu(torch.zeros(4, 80, dtype=u8)[:, :64]), _OnGpu(torch.zeros(1, 9)[:, :4])
+    w8, ws, out = _OnGpu(torch.zeros(8, 80, dtype=u8)[:, :64]), _OnGpu(torch.zeros(1, 1)), _OnGpu(torch.zeros(4, 16, dtype=bf)[:, :8])
+    r, w = _OnGpu(torch.zeros(4, 24, dtype=bf)[:, :8]), _OnGpu(torch.zeros(8, 72, dtype=bf)[:, :64])
+    p = B.make_linear(x, x8, xs, w8, ws, out, residual=r, w=w)
+    assert set(p.gaps) == {"x", "x8", "w8", "out", "residual", "w"}                  # (one row of scales has no gap)
+    for call, args, of in ((B.quantize_rows_fp8, (x, x8, xs), (0, 1)), (B.quantize_tiles_fp8, (w, w8, ws), (0, 1)),
+                           (B.linear_fp8, (x8, xs, w8, ws, out, None, r), (0, 2, 4, 6))):
+        for i in of:
+            _refused(call, p, *args[:i], _OnGpu(args[i].t.contiguous()), *args[i + 1:])
+    qkv, pos, steps = torch.zeros(2, 6, 3, 4, 64, dtype=bf), _OnGpu(torch.zeros(1, 2, 6, dtype=torch.int32)), _OnGpu(B.rope_steps(64)[0])
+    q, k, o = _OnGpu(qkv[:, :, 0].transpose(1, 2)), _OnGpu(qkv[:, :, 1].transpose(1, 2)), _OnGpu(torch.zeros(2, 6, 4, 64, dtype=bf).transpose(1, 2))
+    p = B.make_rope(q, k, o, o, pos, 64)
+    assert set(p.gaps) == {"q", "k"}                                                 # (a transposed whole has none)
+    _refused(B.rope, p, _OnGpu(q.t.contiguous()), k, steps, pos, o, o)
+    _refused(B.rope, p, q, _OnGpu(k.t.contiguous()), steps, pos, o, o)
