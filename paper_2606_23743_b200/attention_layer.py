@@ -20,7 +20,7 @@ class _Linear8:
     def __init__(self, w, bias=None):
         n, k = w.shape
         row = -(-k // 16) * 16
-        self.n, self.k, self.row, self.bias = n, k, row, bias
+        self.n, self.k, self.row, self.bias, self.plan = n, k, row, bias, (None, None)
         self.w8 = torch.empty(n, row, dtype=torch.uint8, device=w.device)
         self.w_scale = torch.empty(-(-n // 128), -(-k // 128), dtype=torch.float32, device=w.device)
         sva.quantize_tiles_fp8(sva.make_linear(w8=self.w8, w_scale=self.w_scale, w=w), w, self.w8, self.w_scale)
@@ -28,7 +28,11 @@ class _Linear8:
     def __call__(self, x, out, status, residual=None):
         x8 = torch.empty(x.shape[0], self.row, dtype=torch.uint8, device=x.device)
         x_scale = torch.empty(-(-self.k // 128), x.shape[0], dtype=torch.float32, device=x.device)
-        p = sva.make_linear(x, x8, x_scale, self.w8, self.w_scale, out, residual=residual)
+        made_for, p = self.plan                              # (of sizes and strides alone: calls mostly repeat them)
+        key = (x.shape, x.stride(), out.stride(), residual is not None and residual.stride())
+        if made_for != key:
+            p = sva.make_linear(x, x8, x_scale, self.w8, self.w_scale, out, residual=residual)
+            self.plan = key, p
         sva.quantize_rows_fp8(p, x, x8, x_scale)
         sva.linear_fp8(p, x8, x_scale, self.w8, self.w_scale, out, self.bias, residual, status)
         return out
@@ -70,6 +74,7 @@ class AttentionLayer:
         self.slots_of = torch.nn.functional.pad(self.slots, (1, 1), value=-1)
         self.lengths = torch.full((batch,), self.N, dtype=torch.int32, device=dev)
         # Q of the whole clip; tokens that a call leaves out keep theirs, so that routing sees whole blocks
+        self.plan = (None, None)                              # of the rotation
         self.q, self.k, self.v, self.o = (torch.zeros(batch, self.N, heads, self.d, dtype=torch.bfloat16, device=dev).transpose(1, 2)
                                           for _ in range(4))
 
@@ -91,7 +96,11 @@ class AttentionLayer:
             token_idx = token_idx.clamp(-1, self.N).int().contiguous()
             at = token_idx.long() + 1
             positions, slots = self.positions_of[:, at].contiguous(), torch.gather(self.slots_of, 1, at).contiguous()
-        sva.rope(sva.make_rope(q, k, q, k, positions, d, "interleaved", self.pairs), q, k, self.steps, positions, q, k)
+        made_for, p = self.plan
+        if made_for != (M, positions.shape):
+            p = sva.make_rope(q, k, q, k, positions, d, "interleaved", self.pairs)
+            self.plan = (M, positions.shape), p
+        sva.rope(p, q, k, self.steps, positions, q, k)
         sva.kv_cache_write(self.cache, k, v, slots, self.status)
         sva.kv_cache_read(self.cache, self.table, self.lengths, self.k, self.v, self.status)
         if token_idx is None:

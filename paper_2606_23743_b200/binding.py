@@ -443,10 +443,14 @@ def _gaps(**tensors):
     """The strides (of more than one row) of the tensors that reach further than their bytes."""
     found = {}
     for name, t in tensors.items():
-        if t is not None and not t.is_contiguous():
-            steps = [(i, s) for i, (n, s) in enumerate(zip(t.shape, t.stride())) if n > 1]
-            if sum((t.shape[i] - 1) * s for i, s in steps) >= t.numel():
-                found[name] = steps
+        if t is None or t.is_contiguous():
+            continue
+        shape, strides, reach, size = t.shape, t.stride(), 1, 1
+        for n, s in zip(shape, strides):
+            reach += (n - 1) * s
+            size *= n
+        if reach > size > 0:
+            found[name] = [(i, s) for i, (n, s) in enumerate(zip(shape, strides)) if n > 1]
     return found
 
 
@@ -494,11 +498,10 @@ def make_linear(x=None, x8=None, x_scale=None, w8=None, w_scale=None, out=None, 
     groups = -(-p.K // 128)
     for t, shape in ((x_scale, (groups, p.M)), (w_scale, (-(-p.N // 128), groups))):
         assert t is None or t.dtype == torch.float32 and t.shape[0] == shape[0] and t.shape[1] >= shape[1], "fp32 scales, one per block of 128"
-    given = [t for t in (x, x8, x_scale, w, w8, w_scale, out, residual) if t is not None]
-    if all(t.is_cuda for t in given):
-        size = lambda t: 0 if t is None else t.nbytes                                                                    # noqa: E731
-        p.rows, p.tiles = (size(x), size(x8), size(x_scale)), (size(w), size(w8), size(w_scale))
-        p.product = (*p.rows[1:], *p.tiles[1:], size(out), size(residual), 4 * p.N)
+    tensors = (x, x8, x_scale, w, w8, w_scale, out, residual)
+    if all([t is None or t.is_cuda for t in tensors]):
+        a, b, c, d, e, f, g, h = [0 if t is None else t.nbytes for t in tensors]
+        p.rows, p.tiles, p.product = (a, b, c), (d, e, f), (b, c, e, f, g, h, 4 * p.N)
     p.gaps = _gaps(x=x, x8=x8, x_scale=x_scale, w=w, w8=w8, w_scale=w_scale, out=out, residual=residual)
     return p
 
@@ -569,7 +572,7 @@ def make_rope(q, k, q_out, k_out, positions, rotary_dim: int, layout: str = "int
     if k is not None:
         assert k.shape == (p.B, p.Hk, p.N, p.d) and k_out.shape == k.shape and k.dtype == k_out.dtype == torch.bfloat16
         p.k_stride, p.k_out_stride = _strides(k), _strides(k_out)
-    if all(t.is_cuda for t in (q, q_out, positions, *((k, k_out) if k is not None else ()))):
+    if q.is_cuda and q_out.is_cuda and positions.is_cuda and (k is None or k.is_cuda and k_out.is_cuda):
         p.sizes = q.nbytes, 4 * rotary_dim, positions.nbytes, q_out.nbytes, 0 if k is None else k.nbytes
     p.gaps = _gaps(q=q, k=k, positions=positions, q_out=q_out, k_out=k_out)
     return p

@@ -101,3 +101,26 @@ def test_token_indices_as_they_come():
     assert int(layer.status.item()) == B.SVA_DEV_BAD_INDEX
     with pytest.raises(AssertionError):
         layer(x, idx[None, :19].expand(Bq, 19))
+
+
+def test_calls_of_other_sizes_and_strides_in_turn():
+    """A layer's plans are for the call before: calls that take turns, tokens that are views of something larger, give what a layer that has seen nothing
+    else gives."""
+    rng = np.random.default_rng(4)
+    Bq, H, d, grid, C = 1, 2, 64, (2, 8, 9), 136
+    N = grid[0] * grid[1] * grid[2]
+    bf = lambda *s: torch.from_numpy(rng.standard_normal(s)).to(torch.bfloat16).cuda()                  # noqa: E731
+    w_qkv, w_out = bf(3 * H * d, C) / np.sqrt(C), bf(C, H * d)
+    make = lambda: AttentionLayer(w_qkv, w_out, H, grid, B.make_select(0, 1000), Bq)                    # noqa: E731
+    whole, wide = bf(Bq, N, C), bf(Bq, N, C + 24)
+    idx = torch.from_numpy(np.sort(rng.permutation(N)[:30]).astype(np.int32))[None].cuda()
+    every = torch.arange(N, dtype=torch.int32, device="cuda")[None]
+    calls = [(whole, None), (wide[..., :C], None), (whole[:, :30], idx), (wide[:, 5:35, :C], idx), (whole[:, :1], idx[:, 3:4]), (whole, every), (whole, None)]
+    one = make()
+    for i, (x, at) in enumerate(calls):
+        got, fresh = one(x, at), make()
+        for y, b in calls[:i]:
+            fresh.plan = fresh.qkv.plan = fresh.out.plan = (None, None)
+            fresh(y.clone(memory_format=torch.contiguous_format), b)
+        assert torch.equal(got, fresh(x.clone(memory_format=torch.contiguous_format), at))
+    assert int(one.status.item()) == 0
