@@ -73,8 +73,8 @@ class AttentionLayer:
         self.positions_of = torch.nn.functional.pad(self.positions[:, 0], (1, 1))
         self.slots_of = torch.nn.functional.pad(self.slots, (1, 1), value=-1)
         self.lengths = torch.full((batch,), self.N, dtype=torch.int32, device=dev)
-        # Q of the whole clip; tokens that a call leaves out keep theirs, so that routing sees whole blocks
         self.plan = (None, None)                              # of the rotation
+        # Q of the whole clip; tokens that a call leaves out keep theirs, so that routing sees whole blocks
         self.q, self.k, self.v, self.o = (torch.zeros(batch, self.N, heads, self.d, dtype=torch.bfloat16, device=dev).transpose(1, 2)
                                           for _ in range(4))
 
