@@ -66,6 +66,7 @@ typedef enum {
                                 skipped, replaced by block 0 or its row treated as empty, depending on the kernel);
                                 the affected rows' output is not meaningful */
 #define SVA_DEV_TIMEOUT   2  /* a bounded pipeline wait expired; output of that block is undefined */
+#define SVA_DEV_NO_PAGES  4  /* the pool had fewer free pages than a call asked for */
 
 typedef enum { SVA_BF16 = 0, SVA_FP8_E4M3 = 1 } sva_qk_dtype_t;
 
@@ -469,7 +470,8 @@ int sva_rope_steps(int32_t rotary_dim, const int32_t axis_pairs[3], double base,
  *   scale  [pages][H][page] fp32
  *   sf     [pages][H][page][d/16] bytes (SVA_CACHE_FP4 only)
  */
-typedef enum { SVA_CACHE_E4M3 = 0, SVA_CACHE_FP4 = 1 } sva_cache_format_t;
+typedef enum { SVA_CACHE_E4M3 = 0, SVA_CACHE_FP4 = 1,
+               SVA_CACHE_E4M3_PAGE = 8 /* one scale per page and head: sva_kv_cache_append */ } sva_cache_format_t;
 
 typedef struct {
   int32_t H, d;              /* d = 64 or 128                                                                             */
@@ -494,6 +496,108 @@ int sva_kv_cache_write(const sva_kv_cache_t* c, const void* k, const void* v, co
 int sva_kv_cache_read(const sva_kv_cache_t* c, const int32_t* page_table, int64_t table_stride, int32_t max_pages, const int32_t* lengths,
                       int32_t B, int32_t N, void* k, void* v, const int64_t k_stride[3], const int64_t v_stride[3],
                       int32_t* device_status, void* stream);
+
+/*
+ * SVA_CACHE_E4M3_PAGE: the cache that attention reads where it lies (sva_cached_attn_fwd), for clips that are generated in chunks and for
+ * sequences that grow token by token.  Codes as in SVA_CACHE_E4M3, but one scale per page and head: k_scale, v_scale are [pages][H]
+ * fp32, x ~= value(code) * scale.  A page is 16 tokens or a multiple of that.  sva_kv_cache_read serves it; sva_kv_cache_write, which
+ * knows single tokens only, answers UNSUPPORTED.
+ *
+ * append: token i < counts[b] of item b (counts NULL: all T) goes behind the lengths[b] tokens that its sequence holds, to place
+ *         (lengths[b] + i) % page of page page_table[b][(lengths[b] + i) / page].  Per page and head, K and V alike, every scalar step one
+ *         fp32 operation rounded to nearest, with n the new rows and o those that were there (places below lengths[b]):
+ *           s = max(o ? s_old : 0, amax(n) / 448)
+ *           codes of o, if s > s_old:  e4m3(value(code) * (s_old / s));      codes of n:  e4m3(x / s), 0 where s = 0
+ *         The other rows of a page stay as they are; lengths is not changed.  A NaN or an infinity makes s that, and the page's values with
+ *         it NaN.  A sequence's tokens may go behind others' only in pages that no other sequence of the call names (sva_kv_pages_fork sees to
+ *         it).  A page id outside [0, pages), or a page beyond max_pages, is reported (SVA_DEV_BAD_INDEX) and its tokens left out; a length
+ *         below 0 counts as 0, a count outside [0, T] as the nearer end.
+ * T may be 0 (nothing is done).  Errors: as sva_kv_cache_write.
+ */
+int sva_kv_cache_append(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t k_stride[3], const int64_t v_stride[3],
+                        int32_t B, int32_t T, const int32_t* page_table, int64_t table_stride, int32_t max_pages, const int32_t* lengths,
+                        const int32_t* counts, int32_t* device_status, void* stream);
+
+/*
+ * Attention over that cache:
+ *   o_i = sum_j softmax_j(softmax_scale * <q_i, k_j>) v_j,  lse_i = ln sum_j exp(softmax_scale * <q_i, k_j>),  j < lengths[b], in causal form
+ *   j <= lengths[b] - counts[b] + i  (the queries are the last counts[b] of the sequence's lengths[b] tokens; appended before this call)
+ * for the queries i < counts[b] (NULL: all M); the rows of o and lse behind them stay as they are.  Hq is a multiple of the cache's H: query
+ * heads h*Hq/H .. (h+1)*Hq/H - 1 share cached head h.  A row without keys becomes zeros, its lse -inf.
+ * Codes enter the products as they are (exact in fp16), Q as fp16 after a scaling of each row by a power of two, the probabilities as fp16;
+ * scales, softmax and sums are fp32.  Scales of V below 2^-80 are taken for 2^-80, and above 2^80 a row's sum loses its smallest terms.
+ * Keys on pages that are named wrongly (SVA_DEV_BAD_INDEX) are left out.  Codes are finite (append writes no NaN but beside a scale that is one).
+ * M may be 0 (nothing is done).  q, o: 16-byte aligned, strides multiples of 8; o must not overlap q or the cache.
+ * workspace: >= sva_cached_attn_workspace_bytes (0 on bad input and where none is needed), 256-byte aligned, rewritten by every call: calls that
+ * may overlap on the GPU need one each.  Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (format, d, page not a multiple of 16, sizes), WORKSPACE.
+ */
+typedef struct {
+  int32_t B, Hq, M;          /* sequences, query heads, queries per sequence                                              */
+  int32_t max_pages;         /* entries of page_table per sequence                                                        */
+  int32_t causal;            /* 0 or 1                                                                                    */
+  float softmax_scale;       /* <= 0 selects 1/sqrt(d)                                                                    */
+  int64_t table_stride;      /* entries between sequences                                                                 */
+  int64_t q_stride[3];       /* element strides of b, h, n                                                                */
+  int64_t o_stride[3];
+} sva_cached_attn_t;
+
+size_t sva_cached_attn_workspace_bytes(const sva_kv_cache_t* c, const sva_cached_attn_t* p);
+int sva_cached_attn_fwd(const sva_kv_cache_t* c, const sva_cached_attn_t* p, const void* q, const int32_t* page_table, const int32_t* lengths,
+                        const int32_t* counts, void* o, float* lse, int32_t* device_status, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/*
+ * Cross attention: the tokens of a clip attend to an encoder's states (a prompt's), which have a length of their own:
+ *   o_i = sum_j softmax_j(softmax_scale * <q_i, k_j>) v_j,  lse_i as above,  over the keys j < lengths[b] (NULL: S) whose key_mask[b][j] is not 0
+ *   (NULL: all);  q, o [B,Hq,N,d], k, v [B,Hk,S,d] bf16, Hq a multiple of Hk (heads share as above), d = 64 or 128.
+ * Keys that are left out have no influence, whatever they hold.  A row without keys becomes zeros, its lse -inf.  Q K^T and P V are bf16
+ * products with fp32 sums, the probabilities rounded to bf16.  lengths [B] int32; key_mask [B][S] bytes, mask_stride between
+ * items; lse (optional) [B,Hq,N] fp32 contiguous.  N and S may be 0.  Strides of 0 over items or heads (shared states) are fine.
+ * Alignment, workspace and errors as for the call above.
+ */
+typedef struct {
+  int32_t B, Hq, Hk, N, S, d;
+  float softmax_scale;       /* <= 0 selects 1/sqrt(d)                                                                    */
+  int64_t mask_stride;       /* bytes between items of key_mask; 0: shared                                                */
+  int64_t q_stride[3];       /* element strides of b, h, n                                                                */
+  int64_t k_stride[3];
+  int64_t v_stride[3];
+  int64_t o_stride[3];
+} sva_cross_attn_t;
+
+size_t sva_cross_attn_workspace_bytes(const sva_cross_attn_t* p);
+int sva_cross_attn_fwd(const sva_cross_attn_t* p, const void* q, const void* k, const void* v, const int32_t* lengths, const uint8_t* key_mask,
+                       void* o, float* lse, int32_t* device_status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The pages of a cache, of any format, as a pool that sequences share.  refs [pages] int32 counts for each page the table entries that name it, 0: free;
+ * page_table [rows][max_pages] int32 (table_stride between rows), entries without a page -1; lengths [rows] int32 tokens.  All on the device, so
+ * that no call needs the host to know a length.  Whatever takes pages takes the free ones of the lowest ids, in the order given below: results are
+ * the same whichever thread comes first.  Ids and rows out of range are reported (SVA_DEV_BAD_INDEX) and left out.
+ *
+ * copy    page dst[i] becomes page src[i], i < n, K and V with their scales.  A negative id leaves its pair out.  Pages that are written are neither
+ *         read nor written by another pair (else what they hold then is not defined).
+ * take    row b gets pages for the tokens that come behind those it holds: entries ceil(lengths[b] / page) .. ceil((lengths[b] + counts[b]) / page) - 1,
+ *         in the order of rows and then entries, each with refs 1.  lengths stays.  Where the pool runs out, entries become -1 (SVA_DEV_NO_PAGES).
+ * fork    row children[i] becomes a copy of row parents[i]: full pages are shared (refs + 1), of a last page that is partly filled
+ *         the child gets a copy of its own (taken in the order of i), entries behind are -1, lengths equal.  Children hold nothing before (free them
+ *         first), come once, and are no parents of the call.  Where the pool runs out the child keeps the full pages alone, and their length.
+ * free    the pages of row rows[i] from entry ceil(keep[i] / page) on are given back (refs - 1, entry -1); lengths[rows[i]] = min(itself, keep[i]).
+ *         keep NULL: everything.  A page whose refs is 0 already is reported.
+ * compact the L pages with refs > 0 move to the ids below L: the i-th lowest page from L on to the i-th lowest free id below L.  refs and page_table (all
+ *         rows) follow; *live = L (optional).  workspace: >= sva_kv_pages_compact_workspace_bytes, 16-byte aligned.
+ * n and rows may be 0.  Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (more than 2^20 pages of a row), WORKSPACE.
+ */
+int sva_kv_pages_copy(const sva_kv_cache_t* c, const int32_t* src, const int32_t* dst, int32_t n, int32_t* device_status, void* stream);
+int sva_kv_pages_take(const sva_kv_cache_t* c, int32_t* refs, int32_t* page_table, int64_t table_stride, int32_t rows, int32_t max_pages,
+                      const int32_t* lengths, const int32_t* counts, int32_t* device_status, void* stream);
+int sva_kv_pages_fork(const sva_kv_cache_t* c, int32_t* refs, int32_t* page_table, int64_t table_stride, int32_t rows, int32_t max_pages,
+                      int32_t* lengths, const int32_t* parents, const int32_t* children, int32_t n, int32_t* device_status, void* stream);
+int sva_kv_pages_free(const sva_kv_cache_t* c, int32_t* refs, int32_t* page_table, int64_t table_stride, int32_t rows, int32_t max_pages,
+                      int32_t* lengths, const int32_t* which, const int32_t* keep, int32_t n, int32_t* device_status, void* stream);
+size_t sva_kv_pages_compact_workspace_bytes(const sva_kv_cache_t* c);
+int sva_kv_pages_compact(const sva_kv_cache_t* c, int32_t* refs, int32_t* page_table, int64_t table_stride, int32_t rows, int32_t max_pages,
+                         int32_t* live, int32_t* device_status, void* workspace, size_t workspace_bytes, void* stream);
 
 const char* sva_status_string(int status);
 

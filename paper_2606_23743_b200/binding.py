@@ -17,7 +17,7 @@ _lib = None
 
 SVA_OK = 0
 SVA_BF16, SVA_FP8_E4M3 = 0, 1
-SVA_DEV_BAD_INDEX, SVA_DEV_TIMEOUT = 1, 2
+SVA_DEV_BAD_INDEX, SVA_DEV_TIMEOUT, SVA_DEV_NO_PAGES = 1, 2, 4
 
 EXPORTS = [
     "sva_select_max_nnz", "sva_select_workspace_bytes", "sva_block_select",
@@ -26,7 +26,9 @@ EXPORTS = [
     "sva_attn_prepare_v", "sva_block_sparse_attn_fwd_prepared", "sva_gather_tokens", "sva_scatter_tokens",
     "sva_attn_one_call_workspace_bytes", "sva_quantize_qk_fp4", "sva_block_sparse_attn_fwd_fp4", "sva_attn_remainder_workspace_bytes", "sva_block_sparse_attn_remainder_fwd", "sva_smooth_workspace_bytes", "sva_quantize_qk_fp8_smooth_k", "sva_block_select_pooled", "sva_qk_norm_rope_pool", "sva_pool_qk",
     "sva_quantize_rows_fp8", "sva_quantize_tiles_fp8", "sva_linear_fp8", "sva_rope", "sva_rope_steps", "sva_kv_cache_write",
-    "sva_kv_cache_read",
+    "sva_kv_cache_read", "sva_kv_cache_append", "sva_cached_attn_workspace_bytes", "sva_cached_attn_fwd", "sva_cross_attn_workspace_bytes",
+    "sva_cross_attn_fwd", "sva_kv_pages_copy", "sva_kv_pages_take", "sva_kv_pages_fork", "sva_kv_pages_free",
+    "sva_kv_pages_compact_workspace_bytes", "sva_kv_pages_compact",
 ]
 DEBUG_EXPORTS = ["sva_debug_set_prof_buffer", "sva_debug_set_mode", "sva_debug_set_wait_limit", "sva_debug_last_choice"]
 NOALLOC_SCRATCH_BYTES = 16 << 20
@@ -69,6 +71,18 @@ class KvCache(C.Structure):
                 ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("k_sf", C.c_void_p), ("v_sf", C.c_void_p)]
     arrays, on_gpu = None, False                           # the tensors behind the pointers, and where they are (make_kv_cache)
+
+
+class CachedAttn(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("M", C.c_int32), ("max_pages", C.c_int32), ("causal", C.c_int32), ("softmax_scale", C.c_float),
+                ("table_stride", C.c_int64), ("q_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
+    cache = None                                           # the cache that it was made for (make_cached_attn)
+
+
+class CrossAttn(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hk", C.c_int32), ("N", C.c_int32), ("S", C.c_int32), ("d", C.c_int32),
+                ("softmax_scale", C.c_float), ("mask_stride", C.c_int64), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
+                ("v_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
 
 
 class SvaError(RuntimeError):
@@ -154,6 +168,28 @@ def lib():
         L.sva_kv_cache_read.restype = C.c_int
         L.sva_kv_cache_read.argtypes = [C.POINTER(KvCache), vp, C.c_int64, C.c_int32, vp, C.c_int32, C.c_int32, vp, vp, i64p, i64p,
                                         vp, vp]
+        cache, i32, i64 = C.POINTER(KvCache), C.c_int32, C.c_int64
+        L.sva_kv_cache_append.restype = C.c_int
+        L.sva_kv_cache_append.argtypes = [cache, vp, vp, i64p, i64p, i32, i32, vp, i64, i32, vp, vp, vp, vp]
+        L.sva_cached_attn_workspace_bytes.restype = C.c_size_t
+        L.sva_cached_attn_workspace_bytes.argtypes = [cache, C.POINTER(CachedAttn)]
+        L.sva_cached_attn_fwd.restype = C.c_int
+        L.sva_cached_attn_fwd.argtypes = [cache, C.POINTER(CachedAttn)] + [vp] * 8 + [C.c_size_t, vp]
+        L.sva_cross_attn_workspace_bytes.restype = C.c_size_t
+        L.sva_cross_attn_workspace_bytes.argtypes = [C.POINTER(CrossAttn)]
+        L.sva_cross_attn_fwd.restype = C.c_int
+        L.sva_cross_attn_fwd.argtypes = [C.POINTER(CrossAttn)] + [vp] * 9 + [C.c_size_t, vp]
+        L.sva_kv_pages_copy.restype = C.c_int
+        L.sva_kv_pages_copy.argtypes = [cache, vp, vp, i32, vp, vp]
+        L.sva_kv_pages_take.restype = C.c_int
+        L.sva_kv_pages_take.argtypes = [cache, vp, vp, i64, i32, i32, vp, vp, vp, vp]
+        for fn in (L.sva_kv_pages_fork, L.sva_kv_pages_free):
+            fn.restype = C.c_int
+            fn.argtypes = [cache, vp, vp, i64, i32, i32, vp, vp, vp, i32, vp, vp]
+        L.sva_kv_pages_compact_workspace_bytes.restype = C.c_size_t
+        L.sva_kv_pages_compact_workspace_bytes.argtypes = [cache]
+        L.sva_kv_pages_compact.restype = C.c_int
+        L.sva_kv_pages_compact.argtypes = [cache, vp, vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
         # test and tuning aids (include/sva_debug.h): process-global settings
         L.sva_debug_set_prof_buffer.restype = None
         L.sva_debug_set_prof_buffer.argtypes = [vp]
@@ -431,7 +467,7 @@ def attn_one_call_workspace_bytes(p: Problem) -> int:
 ACTIVATIONS = {"none": 0, "gelu": 1, "silu": 2}
 ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
-CACHE_FORMATS = {"e4m3": 0, "fp4": 1}
+CACHE_FORMATS = {"e4m3": 0, "fp4": 1, "e4m3_page": 8}
 
 
 # A call's tensors are those that its plan was made from, or others like them: their sizes are compared, where the plan's have gaps their strides too, and
@@ -592,13 +628,13 @@ def rope(p: Rope, q, k, steps, positions, q_out, k_out) -> None:
 
 
 def make_kv_cache(k, v, format: str = "e4m3") -> KvCache:
-    """A cache over its arrays: k and v are [codes, scale] (e4m3) or [codes, scale, sf] (fp4), codes [pages,H,page,d or d/2] bytes, scale
-    [pages,H,page] fp32, sf [pages,H,page,d/16] bytes, all contiguous.  The arrays are kept alive."""
+    """A cache over its arrays: k and v are [codes, scale] (e4m3, e4m3_page) or [codes, scale, sf] (fp4), codes [pages,H,page,d or d/2] bytes,
+    scale [pages,H,page] fp32 (e4m3_page: [pages,H]), sf [pages,H,page,d/16] bytes, all contiguous.  The arrays are kept alive."""
     c = KvCache()
     c.format = CACHE_FORMATS[format]
     c.pages, c.H, c.page, row = k[0].shape
     c.d = row * 2 if format == "fp4" else row
-    shapes = [(c.pages, c.H, c.page, row), (c.pages, c.H, c.page), (c.pages, c.H, c.page, c.d // 16)]
+    shapes = [(c.pages, c.H, c.page, row), (c.pages, c.H) if format == "e4m3_page" else (c.pages, c.H, c.page), (c.pages, c.H, c.page, c.d // 16)]
     for arrays in (k, v):
         assert len(arrays) == (3 if format == "fp4" else 2)
         for t, shape, size in zip(arrays, shapes, (1, 4, 1)):
@@ -635,3 +671,166 @@ def kv_cache_read(c: KvCache, page_table, lengths, k, v, status=None) -> None:
                                            _strides(k), _strides(v), None if status is None else status.data_ptr(), _stream())
     if rc:
         raise SvaError(rc, "sva_kv_cache_read")
+
+
+_NOT_ON_GPU = "the cache and its tensors are on the GPU"
+
+
+def _table(page_table, rows):
+    """Row stride and entries per row of a page table."""
+    n, most = page_table.shape
+    stride, inner = page_table.stride()
+    assert n == rows and page_table.dtype is torch.int32 and (inner == 1 or most == 1), "page_table is [rows,pages] int32"
+    return stride, most
+
+
+def _int32s(t, n, what):
+    assert t.dim() == 1 and t.shape[0] == n and t.dtype is torch.int32 and t.is_contiguous(), f"{what} are {n} int32, side by side"
+    assert t.is_cuda, _NOT_ON_GPU
+    return t.data_ptr()
+
+
+def kv_cache_append(c: KvCache, k, v, page_table, lengths, counts=None, status=None) -> None:
+    """k, v [B,H,T,d] bf16 behind the lengths [B] tokens that the sequences hold in their pages (the first counts [B] of each; None: all T).
+    The cache's format is e4m3_page; `lengths` stays as it is."""
+    shape = Bq, H, T, d = k.shape
+    assert H == c.H and d == c.d and v.shape == shape and k.dtype is v.dtype is torch.bfloat16, "k, v are [B,H,T,d] bf16"
+    stride, most = _table(page_table, Bq)
+    assert c.on_gpu and k.is_cuda and v.is_cuda and page_table.is_cuda and (status is None or status.is_cuda), _NOT_ON_GPU
+    rc = (_lib or lib()).sva_kv_cache_append(c, k.data_ptr(), v.data_ptr(), _strides(k), _strides(v), Bq, T, page_table.data_ptr(), stride, most,
+                                             _int32s(lengths, Bq, "lengths"), None if counts is None else _int32s(counts, Bq, "counts"),
+                                             None if status is None else status.data_ptr(), _stream())
+    if rc:
+        raise SvaError(rc, "sva_kv_cache_append")
+
+
+def make_cached_attn(c: KvCache, q, o, page_table, causal: bool = False, scale: float = 0.0) -> CachedAttn:
+    """Attention of q [B,Hq,M,d] over the cache (Hq a multiple of its heads), into o; page_table [B,pages] int32."""
+    p = CachedAttn()
+    p.B, p.Hq, p.M, d = q.shape
+    assert d == c.d and p.Hq % c.H == 0, "q is [B,Hq,M,d] with the cache's d and a multiple of its heads"
+    p.table_stride, p.max_pages = _table(page_table, p.B)
+    p.causal, p.softmax_scale, p.cache = int(causal), scale, c
+    _check_attn(p, q, page_table, o)
+    p.q_stride, p.o_stride = _strides(q), _strides(o)
+    return p
+
+
+def _check_attn(p, q, page_table, o):
+    shape = q.shape
+    assert shape == o.shape and q.dtype is o.dtype is torch.bfloat16 and shape[:3] == (p.B, p.Hq, p.M) and shape[3] == p.cache.d, \
+        "q, o are bf16 and of the sizes that the plan was made for"
+    assert page_table.shape == (p.B, p.max_pages) and page_table.dtype is torch.int32, "page_table is the plan's [B,pages] int32"
+
+
+def cached_attn_workspace_bytes(p: CachedAttn) -> int:
+    return int(lib().sva_cached_attn_workspace_bytes(C.byref(p.cache), C.byref(p)))
+
+
+def cached_attn_fwd(p: CachedAttn, q, page_table, lengths, o, counts=None, lse=None, status=None, workspace=None) -> None:
+    """o = attention of each sequence's counts [B] queries (None: all M) over its lengths [B] cached tokens; lse [B,Hq,M] fp32."""
+    _check_attn(p, q, page_table, o)
+    assert tuple(q.stride()) == (*p.q_stride, 1) and tuple(o.stride()) == (*p.o_stride, 1), "q, o have the plan's strides"
+    assert page_table.stride(0) == p.table_stride or p.B == 1, "page_table has the plan's strides"
+    assert lse is None or lse.shape == (p.B, p.Hq, p.M) and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,M] fp32"
+    assert p.cache.on_gpu and q.is_cuda and o.is_cuda and page_table.is_cuda and (status is None or status.is_cuda) and \
+        (workspace is None or workspace.is_cuda), _NOT_ON_GPU
+    rc = (_lib or lib()).sva_cached_attn_fwd(p.cache, p, q.data_ptr(), page_table.data_ptr(), _int32s(lengths, p.B, "lengths"),
+                                             None if counts is None else _int32s(counts, p.B, "counts"), o.data_ptr(), _ptr(lse), _ptr(status),
+                                             _ptr(workspace), _ws_bytes(workspace), _stream())
+    if rc:
+        raise SvaError(rc, "sva_cached_attn_fwd")
+
+
+def make_cross_attn(q, k, v, o, scale: float = 0.0) -> CrossAttn:
+    """Attention of q [B,Hq,N,d] over an encoder's k, v [B,Hk,S,d] (Hq a multiple of Hk), into o; all bf16."""
+    p = CrossAttn()
+    p.B, p.Hq, p.N, p.d = q.shape
+    p.Hk, p.S = k.shape[1], k.shape[2]
+    assert k.shape == v.shape == (p.B, p.Hk, p.S, p.d) and o.shape == q.shape and p.Hk > 0 and p.Hq % p.Hk == 0, \
+        "q, o are [B,Hq,N,d], k, v [B,Hk,S,d], Hq a multiple of Hk"
+    assert q.dtype is k.dtype is v.dtype is o.dtype is torch.bfloat16, "q, k, v, o are bf16"
+    p.softmax_scale = scale
+    p.q_stride, p.k_stride, p.v_stride, p.o_stride = _strides(q), _strides(k), _strides(v), _strides(o)
+    return p
+
+
+def cross_attn_workspace_bytes(p: CrossAttn) -> int:
+    return int(lib().sva_cross_attn_workspace_bytes(C.byref(p)))
+
+
+def cross_attn_fwd(p: CrossAttn, q, k, v, o, lengths=None, key_mask=None, lse=None, status=None, workspace=None) -> None:
+    """o = attention over the first lengths [B] keys (None: all S) that key_mask [B,S] (bool or bytes, None: all) does not leave out."""
+    assert q.shape == o.shape == (p.B, p.Hq, p.N, p.d) and k.shape == v.shape == (p.B, p.Hk, p.S, p.d) and \
+        q.dtype is k.dtype is v.dtype is o.dtype is torch.bfloat16, "q, k, v, o are bf16 and of the sizes that the plan was made for"
+    assert all([tuple(t.stride()) == (*s, 1) for t, s in ((q, p.q_stride), (k, p.k_stride), (v, p.v_stride), (o, p.o_stride))]), \
+        "q, k, v, o have the plan's strides"
+    mask_stride = 0
+    if key_mask is not None:
+        assert key_mask.shape == (p.B, p.S) and key_mask.element_size() == 1 and (p.S <= 1 or key_mask.stride(1) == 1) and key_mask.is_cuda, \
+            "key_mask is [B,S] bytes on the GPU"
+        mask_stride = key_mask.stride(0)
+    p.mask_stride = mask_stride
+    assert lse is None or lse.shape == (p.B, p.Hq, p.N) and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,N] fp32"
+    assert q.is_cuda and k.is_cuda and v.is_cuda and o.is_cuda and (status is None or status.is_cuda) and (workspace is None or workspace.is_cuda), \
+        "tensors are on the GPU"
+    rc = (_lib or lib()).sva_cross_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lengths is None else _int32s(lengths, p.B, "lengths"),
+                                            _ptr(key_mask), o.data_ptr(), _ptr(lse), _ptr(status), _ptr(workspace), _ws_bytes(workspace), _stream())
+    if rc:
+        raise SvaError(rc, "sva_cross_attn_fwd")
+
+
+def kv_pages_copy(c: KvCache, src, dst, status=None) -> None:
+    """Page dst[i] becomes page src[i] (int32; negative: left out)."""
+    n = src.shape[0]
+    assert c.on_gpu and (status is None or status.is_cuda), _NOT_ON_GPU
+    rc = (_lib or lib()).sva_kv_pages_copy(c, _int32s(src, n, "src"), _int32s(dst, n, "dst"), n, _ptr(status), _stream())
+    if rc:
+        raise SvaError(rc, "sva_kv_pages_copy")
+
+
+def _pool(c, refs, page_table, status):
+    rows = page_table.shape[0]
+    stride, most = _table(page_table, rows)
+    assert c.on_gpu and page_table.is_cuda and (status is None or status.is_cuda), _NOT_ON_GPU
+    return _int32s(refs, c.pages, "refs"), page_table.data_ptr(), stride, rows, most
+
+
+def kv_pages_take(c: KvCache, refs, page_table, lengths, counts, status=None) -> None:
+    """Every row of page_table gets the pages for counts [rows] tokens behind its lengths [rows]: the free ones of the lowest ids."""
+    pool = _pool(c, refs, page_table, status)
+    rc = (_lib or lib()).sva_kv_pages_take(c, *pool, _int32s(lengths, pool[3], "lengths"), _int32s(counts, pool[3], "counts"), _ptr(status), _stream())
+    if rc:
+        raise SvaError(rc, "sva_kv_pages_take")
+
+
+def kv_pages_fork(c: KvCache, refs, page_table, lengths, parents, children, status=None) -> None:
+    """Row children[i] becomes a copy of row parents[i]: full pages shared, a partly filled last one copied to a page of its own."""
+    pool, n = _pool(c, refs, page_table, status), parents.shape[0]
+    rc = (_lib or lib()).sva_kv_pages_fork(c, *pool, _int32s(lengths, pool[3], "lengths"), _int32s(parents, n, "parents"),
+                                           _int32s(children, n, "children"), n, _ptr(status), _stream())
+    if rc:
+        raise SvaError(rc, "sva_kv_pages_fork")
+
+
+def kv_pages_free(c: KvCache, refs, page_table, lengths, rows, keep=None, status=None) -> None:
+    """Gives back the pages of these rows behind their first keep [n] tokens (None: all of them)."""
+    pool, n = _pool(c, refs, page_table, status), rows.shape[0]
+    rc = (_lib or lib()).sva_kv_pages_free(c, *pool, _int32s(lengths, pool[3], "lengths"), _int32s(rows, n, "rows"),
+                                           None if keep is None else _int32s(keep, n, "keep"), n, _ptr(status), _stream())
+    if rc:
+        raise SvaError(rc, "sva_kv_pages_free")
+
+
+def kv_pages_compact_workspace_bytes(c: KvCache) -> int:
+    return int(lib().sva_kv_pages_compact_workspace_bytes(C.byref(c)))
+
+
+def kv_pages_compact(c: KvCache, refs, page_table, workspace, live=None, status=None) -> None:
+    """The pages in use move to the lowest ids; refs and page_table follow, live [1] int32 becomes their number."""
+    pool = _pool(c, refs, page_table, status)
+    assert workspace.is_cuda, _NOT_ON_GPU
+    rc = (_lib or lib()).sva_kv_pages_compact(c, *pool, None if live is None else _int32s(live, 1, "live"), _ptr(status), _ptr(workspace),
+                                              _ws_bytes(workspace), _stream())
+    if rc:
+        raise SvaError(rc, "sva_kv_pages_compact")

@@ -486,24 +486,33 @@ int sva_rope_steps(int32_t rotary_dim, const int32_t axis_pairs[3], double base,
   return SVA_OK;
 }
 
-static int validate_cache(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t ks[3], const int64_t vs[3], int B, int T) {
-  if (!c || !ks || !vs || B < 1 || T < 0 || c->H < 1 || c->d < 1 || c->page < 1 || c->pages < 1) return SVA_ERR_INVALID_ARG;
-  if (c->format != SVA_CACHE_E4M3 && c->format != SVA_CACHE_FP4) return SVA_ERR_INVALID_ARG;
+// A cache's own members (whoever calls): sizes, arrays, alignment.
+static int validate_arrays(const sva_kv_cache_t* c) {
+  if (!c || c->H < 1 || c->d < 1 || c->page < 1 || c->pages < 1) return SVA_ERR_INVALID_ARG;
+  if (c->format != SVA_CACHE_E4M3 && c->format != SVA_CACHE_FP4 && c->format != SVA_CACHE_E4M3_PAGE) return SVA_ERR_INVALID_ARG;
   if ((c->d != 64 && c->d != 128) || c->H > HEADS_MAX) return SVA_ERR_UNSUPPORTED;
   if ((long long)c->page * c->pages > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  if (c->format == SVA_CACHE_E4M3_PAGE && c->page % 16 != 0) return SVA_ERR_UNSUPPORTED;
   if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return SVA_ERR_INVALID_ARG;
   if (c->format == SVA_CACHE_FP4 && (!c->k_sf || !c->v_sf)) return SVA_ERR_INVALID_ARG;
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned4(c->k_scale) || !aligned4(c->v_scale)) return SVA_ERR_ALIGNMENT;
-  if (T == 0) return SVA_OK;
+  return SVA_OK;
+}
+
+static int validate_cache(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t ks[3], const int64_t vs[3], int B, int T) {
+  if (!ks || !vs || B < 1 || T < 0) return SVA_ERR_INVALID_ARG;
+  int rc = validate_arrays(c);
+  if (rc || T == 0) return rc;
   if (!k || !v) return SVA_ERR_INVALID_ARG;
   if (!aligned16(k) || !aligned16(v)) return SVA_ERR_ALIGNMENT;
-  const int rc = check_strides(ks, 8);
+  rc = check_strides(ks, 8);
   return rc ? rc : check_strides(vs, 8);
 }
 
 int sva_kv_cache_write(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t k_stride[3], const int64_t v_stride[3],
                        int32_t B, int32_t T, const int32_t* slots, int32_t* device_status, void* stream) {
   const int rc = validate_cache(c, k, v, k_stride, v_stride, B, T);
+  if (!rc && c->format == SVA_CACHE_E4M3_PAGE) return SVA_ERR_UNSUPPORTED;
   if (rc || T == 0) return rc;
   if (!slots) return SVA_ERR_INVALID_ARG;
   if (!aligned4(slots)) return SVA_ERR_ALIGNMENT;
@@ -519,6 +528,136 @@ int sva_kv_cache_read(const sva_kv_cache_t* c, const int32_t* page_table, int64_
   if (!aligned4(page_table) || !aligned4(lengths)) return SVA_ERR_ALIGNMENT;
   return launch_cache_read(c, page_table, table_stride, max_pages, lengths, B, N, k, v, k_stride, v_stride, device_status,
                            (cudaStream_t)stream);
+}
+
+int sva_kv_cache_append(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t k_stride[3], const int64_t v_stride[3],
+                        int32_t B, int32_t T, const int32_t* page_table, int64_t table_stride, int32_t max_pages, const int32_t* lengths,
+                        const int32_t* counts, int32_t* device_status, void* stream) {
+  const int rc = validate_cache(c, k, v, k_stride, v_stride, B, T);
+  if (!rc && c->format != SVA_CACHE_E4M3_PAGE) return SVA_ERR_UNSUPPORTED;
+  if (rc || T == 0) return rc;
+  if (!page_table || !lengths || max_pages < 1 || table_stride < (B > 1 ? max_pages : 0)) return SVA_ERR_INVALID_ARG;
+  if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(counts)) return SVA_ERR_ALIGNMENT;
+  return launch_cache_append(c, k, v, k_stride, v_stride, B, T, page_table, table_stride, max_pages, lengths, counts, device_status,
+                             (cudaStream_t)stream);
+}
+
+// Sizes of the attention calls over keys of their own; M queries, at most `keys` keys per sequence, rows of work in 32 bits.
+static int validate_keys_sizes(int B, int Hq, int Hk, int M) {
+  if (B < 1 || Hq < 1 || Hk < 1 || M < 0 || Hq % Hk != 0) return SVA_ERR_INVALID_ARG;
+  if (Hq > HEADS_MAX || (long long)M * (Hq / Hk) > LINEAR_MAX) return SVA_ERR_UNSUPPORTED;
+  return SVA_OK;
+}
+static int validate_cached_attn(const sva_kv_cache_t* c, const sva_cached_attn_t* p) {
+  if (!p) return SVA_ERR_INVALID_ARG;
+  int rc = validate_arrays(c);
+  if (rc) return rc;
+  if (c->format != SVA_CACHE_E4M3_PAGE) return SVA_ERR_UNSUPPORTED;
+  if (p->max_pages < 1 || (p->causal != 0 && p->causal != 1)) return SVA_ERR_INVALID_ARG;
+  if ((rc = validate_keys_sizes(p->B, p->Hq, c->H, p->M))) return rc;
+  return (long long)p->max_pages * c->page > LINEAR_MAX ? SVA_ERR_UNSUPPORTED : SVA_OK;
+}
+static int validate_cross_attn(const sva_cross_attn_t* p) {
+  if (!p || p->S < 0) return SVA_ERR_INVALID_ARG;
+  const int rc = validate_keys_sizes(p->B, p->Hq, p->Hk, p->N);
+  if (rc) return rc;
+  return (p->d != 64 && p->d != 128) || p->S > LINEAR_MAX ? SVA_ERR_UNSUPPORTED : SVA_OK;
+}
+
+size_t sva_cached_attn_workspace_bytes(const sva_kv_cache_t* c, const sva_cached_attn_t* p) {
+  return validate_cached_attn(c, p) ? 0 : cached_attn_workspace_bytes(c, p);
+}
+
+int sva_cached_attn_fwd(const sva_kv_cache_t* c, const sva_cached_attn_t* p, const void* q, const int32_t* page_table, const int32_t* lengths,
+                        const int32_t* counts, void* o, float* lse, int32_t* device_status, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+  int rc = validate_cached_attn(c, p);
+  if (rc || p->M == 0) return rc;
+  if (!q || !o || !page_table || !lengths || p->table_stride < (p->B > 1 ? p->max_pages : 0)) return SVA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(o) || !aligned4(page_table) || !aligned4(lengths) || !aligned4(counts) || !aligned4(lse)) return SVA_ERR_ALIGNMENT;
+  rc = check_strides(p->q_stride, 8);
+  if (!rc) rc = check_strides(p->o_stride, 8);
+  return rc ? rc : launch_cached_attn(c, p, q, page_table, lengths, counts, o, lse, device_status, workspace, workspace_bytes, (cudaStream_t)stream);
+}
+
+size_t sva_cross_attn_workspace_bytes(const sva_cross_attn_t* p) { return validate_cross_attn(p) ? 0 : cross_attn_workspace_bytes(p); }
+
+int sva_cross_attn_fwd(const sva_cross_attn_t* p, const void* q, const void* k, const void* v, const int32_t* lengths, const uint8_t* key_mask,
+                       void* o, float* lse, int32_t* device_status, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = validate_cross_attn(p);
+  if (rc || p->N == 0) return rc;
+  if (!q || !o || (p->S > 0 && (!k || !v)) || (key_mask && p->mask_stride < 0)) return SVA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned4(lengths) || !aligned4(lse)) return SVA_ERR_ALIGNMENT;
+  rc = check_strides(p->q_stride, 8);
+  if (!rc) rc = check_strides(p->k_stride, 8);
+  if (!rc) rc = check_strides(p->v_stride, 8);
+  if (!rc) rc = check_strides(p->o_stride, 8);
+  return rc ? rc : launch_cross_attn(p, q, k, v, lengths, key_mask, o, lse, device_status, workspace, workspace_bytes, (cudaStream_t)stream);
+}
+
+// (pages of a row, so that 1024 rows' needs are summed in 32 bits)
+static constexpr int32_t ROW_PAGES_MAX = 1 << 20;
+static int validate_pool(const sva_kv_cache_t* c, const int32_t* refs, const int32_t* table, int64_t stride, int rows, int max_pages) {
+  int rc = validate_arrays(c);
+  if (rc) return rc;
+  if (!aligned4(c->k_sf) || !aligned4(c->v_sf)) return SVA_ERR_ALIGNMENT;
+  if (rows < 0) return SVA_ERR_INVALID_ARG;
+  if (!refs || !table || max_pages < 1 || stride < (rows > 1 ? max_pages : 0)) return SVA_ERR_INVALID_ARG;
+  if (max_pages > ROW_PAGES_MAX) return SVA_ERR_UNSUPPORTED;
+  return aligned4(refs) && aligned4(table) ? SVA_OK : SVA_ERR_ALIGNMENT;
+}
+
+int sva_kv_pages_copy(const sva_kv_cache_t* c, const int32_t* src, const int32_t* dst, int32_t n, int32_t* device_status, void* stream) {
+  const int rc = validate_arrays(c);
+  if (rc) return rc;
+  if (!aligned4(c->k_sf) || !aligned4(c->v_sf)) return SVA_ERR_ALIGNMENT;
+  if (n < 0) return SVA_ERR_INVALID_ARG;
+  if (n == 0) return SVA_OK;
+  if (!src || !dst) return SVA_ERR_INVALID_ARG;
+  if (!aligned4(src) || !aligned4(dst)) return SVA_ERR_ALIGNMENT;
+  return launch_pages_copy(c, src, dst, n, device_status, (cudaStream_t)stream);
+}
+
+int sva_kv_pages_take(const sva_kv_cache_t* c, int32_t* refs, int32_t* page_table, int64_t table_stride, int32_t rows, int32_t max_pages,
+                      const int32_t* lengths, const int32_t* counts, int32_t* device_status, void* stream) {
+  const int rc = validate_pool(c, refs, page_table, table_stride, rows, max_pages);
+  if (rc || rows == 0) return rc;
+  if (!lengths || !counts) return SVA_ERR_INVALID_ARG;
+  if (!aligned4(lengths) || !aligned4(counts)) return SVA_ERR_ALIGNMENT;
+  return launch_pages_take(c, refs, page_table, table_stride, rows, max_pages, lengths, counts, device_status, (cudaStream_t)stream);
+}
+
+int sva_kv_pages_fork(const sva_kv_cache_t* c, int32_t* refs, int32_t* page_table, int64_t table_stride, int32_t rows, int32_t max_pages,
+                      int32_t* lengths, const int32_t* parents, const int32_t* children, int32_t n, int32_t* device_status, void* stream) {
+  const int rc = validate_pool(c, refs, page_table, table_stride, rows, max_pages);
+  if (rc) return rc;
+  if (n < 0) return SVA_ERR_INVALID_ARG;
+  if (n == 0) return SVA_OK;
+  if (!lengths || !parents || !children) return SVA_ERR_INVALID_ARG;
+  if (!aligned4(lengths) || !aligned4(parents) || !aligned4(children)) return SVA_ERR_ALIGNMENT;
+  return launch_pages_fork(c, refs, page_table, table_stride, rows, max_pages, lengths, parents, children, n, device_status, (cudaStream_t)stream);
+}
+
+int sva_kv_pages_free(const sva_kv_cache_t* c, int32_t* refs, int32_t* page_table, int64_t table_stride, int32_t rows, int32_t max_pages,
+                      int32_t* lengths, const int32_t* which, const int32_t* keep, int32_t n, int32_t* device_status, void* stream) {
+  const int rc = validate_pool(c, refs, page_table, table_stride, rows, max_pages);
+  if (rc) return rc;
+  if (n < 0) return SVA_ERR_INVALID_ARG;
+  if (n == 0) return SVA_OK;
+  if (!lengths || !which) return SVA_ERR_INVALID_ARG;
+  if (!aligned4(lengths) || !aligned4(which) || !aligned4(keep)) return SVA_ERR_ALIGNMENT;
+  return launch_pages_free(c, refs, page_table, table_stride, rows, max_pages, lengths, which, keep, n, device_status, (cudaStream_t)stream);
+}
+
+size_t sva_kv_pages_compact_workspace_bytes(const sva_kv_cache_t* c) { return validate_arrays(c) ? 0 : pages_compact_workspace_bytes(c); }
+
+int sva_kv_pages_compact(const sva_kv_cache_t* c, int32_t* refs, int32_t* page_table, int64_t table_stride, int32_t rows, int32_t max_pages,
+                         int32_t* live, int32_t* device_status, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = validate_pool(c, refs, page_table, table_stride, rows, max_pages);
+  if (rc) return rc;
+  if (!workspace || workspace_bytes < pages_compact_workspace_bytes(c)) return SVA_ERR_WORKSPACE;
+  if (!aligned16(workspace) || !aligned4(live)) return SVA_ERR_ALIGNMENT;
+  return launch_pages_compact(c, refs, page_table, table_stride, rows, max_pages, live, device_status, workspace, (cudaStream_t)stream);
 }
 
 const char* sva_status_string(int status) {

@@ -1,0 +1,483 @@
+// Attention of few rows over many keys (sva_cached_attn_fwd, sva_cross_attn_fwd): one token or a few per sequence.
+//
+// Bound by the keys' bytes: every key is read once per 16 rows, straight into the registers of the warp that uses it, and enters mma.sync
+// products (m16n8k16) whose 16 rows are tokens times the heads that share the keys.  A warp takes 16 keys at a time, every 8th group of its
+// CTA's range; the next group's loads are in flight while it works.  In which order the products run over channels is free, so each thread takes
+// whole 16-byte pieces of a row and the operand fragments are cut from them; P needs no shuffle, being A of the second product as it leaves the first.
+// The warps' sums meet in shared memory; ranges of a long axis (splits) meet in a second kernel.
+//
+// e4m3 codes are converted to fp16, exactly; Q is scaled by a power of two per row into fp16's range, P = 2^(s + log2 v_scale - m + 10) with the
+// running maximum m of what is in the exponent: weights of up to 2^10, whose products with codes of any pages add up as they are; the row sum
+// takes 1 / v_scale per group.
+#include <cuda_fp16.h>
+
+#include "attn_keys.cuh"
+#include "tc_ptx.cuh"
+
+namespace sva {
+
+static constexpr int FEW_ROWS = 16, FEW_KEYS = 16, FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32;
+static constexpr float P_UP = 10.0f;               // log2 of the largest fp16 probability
+
+__device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// two e4m3 codes (the low 16 bits) -> two fp16 values
+__device__ __forceinline__ uint32_t codes_f16x2(uint32_t pair) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3);
+  return (uint32_t)h.x | (uint32_t)h.y << 16;
+}
+
+template <int D, bool PAGED>
+__global__ void __launch_bounds__(FEW_THREADS, 1)
+keys_few_kernel(const KeysParams prm) {
+  constexpr int KSTEPS = D / 16, NT = D / 8;
+  // 16-byte pieces of a row that a thread holds: of a key (4 threads per row), of a value row (8 threads per row)
+  constexpr int KP = PAGED ? D / 64 : D / 32, VB = PAGED ? D / 8 : D / 4, VP = VB >= 16 ? VB / 16 : 1;      // (VB: bytes)
+  extern __shared__ float smem_f[];                                       // [warps][16][D] then [warps][16] x 2
+  const int zero = grid_dep_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  long long at = (long long)blockIdx.x + zero;
+  const int tile = (int)(at % prm.tiles); at /= prm.tiles;
+  const int split = (int)(at % prm.splits); at /= prm.splits;
+  const int hk = (int)(at % prm.Hk), b = (int)(at / prm.Hk);
+  const int keys = seq_keys(prm, b), queries = seq_queries(prm, b);
+  const long long row_first = (long long)tile * FEW_ROWS, rows = (long long)queries * prm.group;
+  if (row_first >= rows) return;
+  const int last_t = (int)(min(row_first + FEW_ROWS, rows) - 1) / prm.group;
+  const int end = keys_seen(prm, keys, queries, last_t);
+  const int groups = (end + FEW_KEYS - 1) / FEW_KEYS;
+  const int g_lo = (int)((long long)groups * split / prm.splits), g_hi = (int)((long long)groups * (split + 1) / prm.splits);
+
+  // my two rows (g, g + 8): where their queries are, what they see
+  const uint8_t* qrow[2];
+  int seen[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const long long r = min(row_first + g + 8 * i, rows - 1);
+    const int t = (int)(r / prm.group), h = hk * prm.group + (int)(r % prm.group);
+    qrow[i] = prm.q + 2 * (b * prm.sq.b + h * prm.sq.h + (long long)t * prm.sq.n);
+    seen[i] = keys_seen(prm, keys, queries, t);
+  }
+  // Q: A fragments.  Channels of step s, thread c: codes, piece (s / 4) * 4 + c of 16 channels, from (s % 4) * 4 on; bf16, piece (s / 2) * 4 + c of 8, (s % 2) * 4
+  uint32_t qa[KSTEPS][4];
+  float cc[2];                                                            // logits' scale
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) {
+      const int ch = PAGED ? ((s / 4) * 4 + c) * 16 + (s % 4) * 4 : ((s / 2) * 4 + c) * 8 + (s % 2) * 4;
+      const uint2 u = __ldg(reinterpret_cast<const uint2*>(qrow[i] + 2 * ch));
+      qa[s][i] = u.x;
+      qa[s][2 + i] = u.y;
+    }
+    cc[i] = prm.scale_log2;
+    if (PAGED) {
+      uint32_t top = 0u;
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s)
+#pragma unroll
+        for (int e = i; e < 4; e += 2) top = max(top, max(qa[s][e] & 0x7fffu, qa[s][e] >> 16 & 0x7fffu));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // 2^-e with e the exponent of the row's largest value; 1 where there is none (zeros, infinities, NaNs)
+      const uint32_t ex = top >> 7;
+      const float down = ex == 0u || ex > 252u ? 1.f : __uint_as_float((254u - ex) << 23);
+      cc[i] *= ex == 0u || ex > 252u ? 1.f : __uint_as_float(ex << 23);
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s)
+#pragma unroll
+        for (int e = i; e < 4; e += 2) qa[s][e] = pack_f16(bf16lo(qa[s][e]) * down, bf16hi(qa[s][e]) * down);
+    }
+  }
+
+  float acc[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+  struct Group { uint4 k[2][KP], v[4][VP]; float ks, vs; uint32_t there; };
+  const int per_page = PAGED ? prm.page / FEW_KEYS : 1;
+  auto page_of = [&](int gi) -> int {                                     // page id of a group; -1: named wrongly
+    if (!PAGED || gi >= g_hi) return 0;
+    const int e = gi / per_page;
+    int id = e < prm.max_pages ? __ldg(prm.table + b * prm.table_stride + e) : -1;
+    return id >= prm.pages ? -1 : id;
+  };
+  auto load = [&](int gi, int id, Group& x) {
+    x.there = 0u;
+    if (gi >= g_hi) return;
+    const int key0 = gi * FEW_KEYS;
+    x.there = keys - key0 >= FEW_KEYS ? 0xffffu : (1u << (keys - key0)) - 1u;
+    const uint8_t *kp, *vp;
+    long long ks_row, vs_row;
+    if (PAGED) {
+      if (id < 0) {
+        x.there = 0u;
+        if (lane == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
+        return;
+      }
+      const long long head = (long long)id * prm.Hk + hk;
+      const int place = (gi - gi / per_page * per_page) * FEW_KEYS;
+      kp = prm.k + (head * prm.page + place) * D;
+      vp = prm.v + (head * prm.page + place) * D;
+      ks_row = vs_row = D;
+      x.ks = __ldg(prm.k_scale + head);
+      x.vs = __ldg(prm.v_scale + head);
+    } else {
+      kp = prm.k + 2 * (b * prm.sk.b + hk * prm.sk.h + (long long)key0 * prm.sk.n);
+      vp = prm.v + 2 * (b * prm.sv.b + hk * prm.sv.h + (long long)key0 * prm.sv.n);
+      ks_row = 2 * prm.sk.n;
+      vs_row = 2 * prm.sv.n;
+      if (prm.mask) {
+        const bool on = lane < FEW_KEYS && (x.there >> lane & 1u) && __ldg(prm.mask + b * prm.mask_stride + key0 + lane) != 0;
+        x.there = __ballot_sync(0xffffffffu, on);
+      }
+    }
+    // keys g and g + 8; values of keys 2c, 2c + 1, 2c + 8, 2c + 9.  Rows that are not there are not read: zeros, whatever they hold
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < KP; ++e)
+        x.k[n][e] = x.there >> (g + 8 * n) & 1u ? __ldg(reinterpret_cast<const uint4*>(kp + (g + 8 * n) * ks_row + (e * 4 + c) * 16))
+                                                : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int key = 2 * c + (n & 1) + 8 * (n >> 1);
+      const bool on = x.there >> key & 1u;
+#pragma unroll
+      for (int e = 0; e < VP; ++e) {
+        x.v[n][e] = make_uint4(0u, 0u, 0u, 0u);
+        if (on) {
+          if (VB >= 16) {
+            x.v[n][e] = __ldg(reinterpret_cast<const uint4*>(vp + key * vs_row + (PAGED ? g * VP + e : e * 8 + g) * 16));
+          } else {
+            const uint2 u = __ldg(reinterpret_cast<const uint2*>(vp + key * vs_row + g * 8));
+            x.v[n][0].x = u.x; x.v[n][0].y = u.y;
+          }
+        }
+      }
+    }
+  };
+  auto word = [](const uint4& u, int i) -> uint32_t { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; };
+
+  auto step = [&](int gi, const Group& x) {
+    float s[2][4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KSTEPS; ++i) {
+        if (PAGED) {
+          const uint32_t w = word(x.k[n][i / 4], i % 4);
+          mma_f16(s[n], qa[i], codes_f16x2(w & 0xffffu), codes_f16x2(w >> 16));
+        } else {
+          mma_bf16(s[n], qa[i], word(x.k[n][i / 2], 2 * (i % 2)), word(x.k[n][i / 2], 2 * (i % 2) + 1));
+        }
+      }
+    }
+    const int key0 = gi * FEW_KEYS;
+    float inv_vs = 1.f, lv = 0.f;
+    if (PAGED) {
+      const float vs = v_scale_floor(x.vs);
+      lv = log2f(vs);
+      inv_vs = 1.f / vs;
+    }
+    uint32_t p[2][2];                                                     // [n tile][row]
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float f = PAGED ? cc[i] * x.ks : cc[i];
+      float y[4], top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = (e >> 1) * 8 + 2 * c + (e & 1);
+        y[e] = fmaf(s[e >> 1][2 * i + (e & 1)], f, lv);
+        if (!(x.there >> key & 1u) || key0 + key >= seen[i]) y[e] = -INFINITY;
+        top = fmaxf(top, y[e]);
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      if (top > m[i]) {                                                   // (all four threads of the row)
+        const float down = ex2(m[i] - top);                               // (0 where m was -inf)
+        m[i] = top;
+        l[i] *= down;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          acc[t][2 * i] *= down;
+          acc[t][2 * i + 1] *= down;
+        }
+      }
+      const float ref = (m[i] == -INFINITY ? 0.f : m[i]) - (PAGED ? P_UP : 0.f);
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[e] = ex2(y[e] - ref);
+        sum += y[e];
+      }
+      l[i] = fmaf(sum, inv_vs, l[i]);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) p[n][i] = PAGED ? pack_f16(y[2 * n], y[2 * n + 1]) : pack_bf16(y[2 * n], y[2 * n + 1]);
+    }
+    const uint32_t pa[4] = {p[0][0], p[0][1], p[1][0], p[1][1]};
+#pragma unroll
+    for (int t = 0; t < NT; t += 4) {                                     // four channels of each of the four rows
+      if (PAGED) {
+        const uint32_t w0 = word(x.v[0][t / 16], t / 4 % 4), w1 = word(x.v[1][t / 16], t / 4 % 4), w2 = word(x.v[2][t / 16], t / 4 % 4),
+                       w3 = word(x.v[3][t / 16], t / 4 % 4);
+        const uint32_t a0 = __byte_perm(w0, w1, 0x5140), a1 = __byte_perm(w0, w1, 0x7362), b0 = __byte_perm(w2, w3, 0x5140),
+                       b1 = __byte_perm(w2, w3, 0x7362);
+        mma_f16(acc[t], pa, codes_f16x2(a0 & 0xffffu), codes_f16x2(b0 & 0xffffu));
+        mma_f16(acc[t + 1], pa, codes_f16x2(a0 >> 16), codes_f16x2(b0 >> 16));
+        mma_f16(acc[t + 2], pa, codes_f16x2(a1 & 0xffffu), codes_f16x2(b1 & 0xffffu));
+        mma_f16(acc[t + 3], pa, codes_f16x2(a1 >> 16), codes_f16x2(b1 >> 16));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {                                     // two words of two channels
+          const int piece = t / 8, i = (t / 4 % 2) * 2 + e;
+          const uint32_t w0 = word(x.v[0][piece], i), w1 = word(x.v[1][piece], i), w2 = word(x.v[2][piece], i), w3 = word(x.v[3][piece], i);
+          mma_bf16(acc[t + 2 * e], pa, __byte_perm(w0, w1, 0x5410), __byte_perm(w2, w3, 0x5410));
+          mma_bf16(acc[t + 2 * e + 1], pa, __byte_perm(w0, w1, 0x7632), __byte_perm(w2, w3, 0x7632));
+        }
+      }
+    }
+  };
+
+  {
+    // codes: the group after this one is on its way while this one is used, and the page of the one after that is looked up
+    int gi = g_lo + warp;
+    if (PAGED) {
+      Group x, y;
+      load(gi, page_of(gi), x);
+      int id = page_of(gi + FEW_WARPS);
+      while (gi < g_hi) {
+        load(gi + FEW_WARPS, id, y);
+        id = page_of(gi + 2 * FEW_WARPS);
+        step(gi, x);
+        gi += FEW_WARPS;
+        if (gi >= g_hi) break;
+        load(gi + FEW_WARPS, id, x);
+        id = page_of(gi + 2 * FEW_WARPS);
+        step(gi, y);
+        gi += FEW_WARPS;
+      }
+    } else {
+      for (; gi < g_hi; gi += FEW_WARPS) {
+        Group x;
+        load(gi, 0, x);
+        step(gi, x);
+      }
+    }
+  }
+
+  // ---- the warps' sums: each thread's columns n = 2c, 2c + 1 of tile t are channels of its own order
+  float* so = smem_f + warp * FEW_ROWS * D;
+  float* sm = smem_f + FEW_WARPS * FEW_ROWS * D;                          // m [warps][16], l [warps][16]
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+    if (c == 0) {
+      sm[warp * FEW_ROWS + g + 8 * i] = m[i] == -INFINITY ? 0.f : m[i];
+      sm[(FEW_WARPS + warp) * FEW_ROWS + g + 8 * i] = l[i];
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int col = 2 * c + n;
+#pragma unroll
+      for (int t = 0; t < NT; t += 4) {
+        const int ch = PAGED ? col * NT + t : (t / 8) * 64 + col * 8 + t % 8;
+        *reinterpret_cast<float4*>(so + (g + 8 * i) * D + ch) =
+            make_float4(acc[t][2 * i + n], acc[t + 1][2 * i + n], acc[t + 2][2 * i + n], acc[t + 3][2 * i + n]);
+      }
+    }
+  }
+  __syncthreads();
+  constexpr int EACH = FEW_ROWS * D / FEW_THREADS;                        // channels per thread: 8 or 4
+  const int row = threadIdx.x / (D / EACH), ch = threadIdx.x % (D / EACH) * EACH;
+  float top = -INFINITY, total = 0.f, out[EACH];
+#pragma unroll
+  for (int w = 0; w < FEW_WARPS; ++w)
+    if (sm[(FEW_WARPS + w) * FEW_ROWS + row] != 0.f) top = fmaxf(top, sm[w * FEW_ROWS + row]);
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) out[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < FEW_WARPS; ++w) {
+    const float lw = sm[(FEW_WARPS + w) * FEW_ROWS + row];
+    if (lw != 0.f) {
+      const float f = ex2(sm[w * FEW_ROWS + row] - top);
+      total = fmaf(lw, f, total);
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) out[e] = fmaf(smem_f[(w * FEW_ROWS + row) * D + ch + e], f, out[e]);
+    }
+  }
+  if (prm.splits > 1) {
+    const long long unit = ((long long)b * prm.Hk + hk) * prm.tiles + tile, all = (long long)prm.B * prm.Hk * prm.tiles * FEW_ROWS;
+    const long long mine = split * all + unit * FEW_ROWS + row;
+#pragma unroll
+    for (int e = 0; e < EACH; e += 4) *reinterpret_cast<float4*>(prm.part_o + mine * D + ch + e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
+    if (ch == 0) prm.part_ml[mine] = make_float2(top, total);
+    return;
+  }
+  const long long r = row_first + row;
+  if (r >= rows) return;
+  const int t = (int)(r / prm.group), h = hk * prm.group + (int)(r % prm.group);
+  const float inv = total != 0.f ? 1.f / total : 0.f;
+  uint32_t w[EACH / 2];
+#pragma unroll
+  for (int e = 0; e < EACH; e += 2) w[e / 2] = pack_bf16(out[e] * inv, out[e + 1] * inv);
+  uint8_t* dst = prm.o + 2 * (b * prm.so.b + h * prm.so.h + (long long)t * prm.so.n + ch);
+  if (EACH == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[EACH / 2 - 2], w[EACH / 2 - 1]);
+  else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+  if (ch == 0 && prm.lse)
+    prm.lse[((long long)b * prm.Hq + h) * prm.M + t] = total != 0.f ? (top - (PAGED ? P_UP : 0.f) + log2f(total)) * 0.6931471805599453f : -INFINITY;
+}
+
+// The splits' sums of a row, one warp each: [splits][rows of all][D].  rows_per: rows of a tile of the kernel that wrote them.
+template <int D>
+__global__ void __launch_bounds__(256)
+keys_join_kernel(const KeysParams prm, int rows_per, float up) {
+  constexpr int EACH = D / 32;
+  const int zero = grid_dep_wait();
+  const int lane = threadIdx.x & 31;
+  const long long per_head = (long long)prm.tiles * rows_per, all = (long long)prm.B * prm.Hk * per_head;
+  const long long mine = (long long)blockIdx.x * 8 + (threadIdx.x >> 5) + zero;
+  if (mine >= all) return;
+  const long long r = mine % per_head, unit = mine / per_head;
+  const int hk = (int)(unit % prm.Hk), b = (int)(unit / prm.Hk);
+  if (r >= (long long)seq_queries(prm, b) * prm.group) return;
+  float top = -INFINITY, total = 0.f, out[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) out[e] = 0.f;
+  for (int s = lane; s < prm.splits; s += 32) {
+    const float2 ml = prm.part_ml[s * all + mine];
+    if (ml.y != 0.f) top = fmaxf(top, ml.x);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  for (int s = 0; s < prm.splits; ++s) {
+    const float2 ml = prm.part_ml[s * all + mine];
+    if (ml.y == 0.f) continue;
+    const float f = ex2(ml.x - top);
+    total = fmaf(ml.y, f, total);
+    const float* x = prm.part_o + (s * all + mine) * D + lane * EACH;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) out[e] = fmaf(x[e], f, out[e]);
+  }
+  const int t = (int)(r / prm.group), h = hk * prm.group + (int)(r % prm.group);
+  const float inv = total != 0.f ? 1.f / total : 0.f;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(prm.o + 2 * (b * prm.so.b + h * prm.so.h + (long long)t * prm.so.n + lane * EACH));
+#pragma unroll
+  for (int e = 0; e < EACH; e += 2) dst[e / 2] = pack_bf16(out[e] * inv, out[e + 1] * inv);
+  if (lane == 0 && prm.lse) prm.lse[((long long)b * prm.Hq + h) * prm.M + t] = total != 0.f ? (top - up + log2f(total)) * 0.6931471805599453f : -INFINITY;
+}
+
+static constexpr size_t few_smem(int d) { return (size_t)FEW_WARPS * FEW_ROWS * (d + 2) * 4; }
+
+template <int D, bool PAGED>
+static int launch_few(const KeysParams& prm, cudaStream_t st) {
+  static DeviceOnce once;
+  auto kern = keys_few_kernel<D, PAGED>;
+  int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_smem(D)) == cudaSuccess; });
+  if (rc) return rc;
+  const long long units = (long long)prm.B * prm.Hk * prm.tiles;
+  if (units * prm.splits > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  rc = launch_dep(kern, dim3((unsigned)(units * prm.splits)), FEW_THREADS, few_smem(D), st, prm);
+  if (rc || prm.splits == 1) return rc;
+  return launch_dep(keys_join_kernel<D>, dim3((unsigned)((units * FEW_ROWS + 7) / 8)), 256, 0, st, prm, FEW_ROWS, PAGED ? P_UP : 0.f);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- plan, workspace
+// How a call is cut: row tiles, and splits of the key axis where there are fewer tiles than the device has room for.
+struct KeysPlan {
+  long long tiles, units, all;              // per key head; of the call; rows of all tiles
+  int splits;
+  size_t o_bytes, total;                    // of the workspace
+};
+static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d) {
+  KeysPlan k = {};
+  k.tiles = ((long long)M * group + FEW_ROWS - 1) / FEW_ROWS;
+  k.units = (long long)B * Hk * k.tiles;
+  k.all = k.units * FEW_ROWS;
+  // at least 256 keys per split
+  long long splits = k.units > 0 ? 148 * 4 / k.units : 1;
+  if (splits > S / 256) splits = S / 256;
+  k.splits = (int)(splits < 1 ? 1 : splits);
+  if (k.splits > 1) {
+    k.o_bytes = (size_t)k.splits * k.all * d * 4;
+    k.total = k.o_bytes + (size_t)k.splits * k.all * 8;
+  }
+  return k;
+}
+
+size_t cached_attn_workspace_bytes(const sva_kv_cache_t* c, const sva_cached_attn_t* p) {
+  return keys_plan(p->B, c->H, p->Hq / c->H, p->M, (long long)p->max_pages * c->page, c->d).total;
+}
+size_t cross_attn_workspace_bytes(const sva_cross_attn_t* p) { return keys_plan(p->B, p->Hk, p->Hq / p->Hk, p->N, p->S, p->d).total; }
+
+static int launch_keys(KeysParams& prm, bool paged, const KeysPlan& plan, void* ws, cudaStream_t st) {
+  if (plan.tiles > 0x7fffffffLL / FEW_ROWS || plan.units > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  prm.tiles = (int)plan.tiles;
+  prm.splits = plan.splits;
+  prm.part_o = static_cast<float*>(ws);
+  prm.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + plan.o_bytes);
+  if (paged) return prm.d == 128 ? launch_few<128, true>(prm, st) : launch_few<64, true>(prm, st);
+  return prm.d == 128 ? launch_few<128, false>(prm, st) : launch_few<64, false>(prm, st);
+}
+
+static int check_space(const KeysPlan& plan, const void* ws, size_t ws_bytes) {
+  if (plan.total == 0) return SVA_OK;
+  if (!ws || ws_bytes < plan.total) return SVA_ERR_WORKSPACE;
+  return reinterpret_cast<uintptr_t>(ws) & 255u ? SVA_ERR_ALIGNMENT : SVA_OK;
+}
+
+int launch_cached_attn(const sva_kv_cache_t* c, const sva_cached_attn_t* p, const void* q, const int32_t* table, const int32_t* lengths,
+                       const int32_t* counts, void* o, float* lse, int32_t* status, void* ws, size_t ws_bytes, cudaStream_t st) {
+  const KeysPlan plan = keys_plan(p->B, c->H, p->Hq / c->H, p->M, (long long)p->max_pages * c->page, c->d);
+  int rc = check_space(plan, ws, ws_bytes);
+  if (rc) return rc;
+  KeysParams prm = {};
+  prm.q = (const uint8_t*)q; prm.o = (uint8_t*)o; prm.lse = lse;
+  prm.sq = make_strides(p->q_stride); prm.so = make_strides(p->o_stride);
+  prm.B = p->B; prm.Hq = p->Hq; prm.Hk = c->H; prm.group = p->Hq / c->H; prm.M = p->M; prm.d = c->d;
+  prm.causal = p->causal;
+  prm.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)c->d)) * 1.4426950408889634f;
+  prm.lengths = lengths; prm.counts = counts;
+  prm.k = (const uint8_t*)c->k_codes; prm.v = (const uint8_t*)c->v_codes;
+  prm.k_scale = c->k_scale; prm.v_scale = c->v_scale;
+  prm.table = table; prm.table_stride = p->table_stride;
+  const long long most = (long long)p->max_pages * c->page;
+  prm.S = (int)(most < 0x7fffff00LL ? most : 0x7fffff00LL);
+  prm.page = c->page; prm.pages = c->pages; prm.max_pages = p->max_pages;
+  prm.status = status;
+  return launch_keys(prm, true, plan, ws, st);
+}
+
+int launch_cross_attn(const sva_cross_attn_t* p, const void* q, const void* k, const void* v, const int32_t* lengths, const uint8_t* mask, void* o,
+                      float* lse, int32_t* status, void* ws, size_t ws_bytes, cudaStream_t st) {
+  const KeysPlan plan = keys_plan(p->B, p->Hk, p->Hq / p->Hk, p->N, p->S, p->d);
+  int rc = check_space(plan, ws, ws_bytes);
+  if (rc) return rc;
+  KeysParams prm = {};
+  prm.q = (const uint8_t*)q; prm.o = (uint8_t*)o; prm.lse = lse;
+  prm.sq = make_strides(p->q_stride); prm.so = make_strides(p->o_stride);
+  prm.sk = make_strides(p->k_stride); prm.sv = make_strides(p->v_stride);
+  prm.B = p->B; prm.Hq = p->Hq; prm.Hk = p->Hk; prm.group = p->Hq / p->Hk; prm.M = p->N; prm.d = p->d;
+  prm.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->d)) * 1.4426950408889634f;
+  prm.lengths = lengths;
+  prm.k = (const uint8_t*)k; prm.v = (const uint8_t*)v;
+  prm.mask = mask; prm.mask_stride = p->mask_stride;
+  prm.S = p->S;
+  prm.status = status;
+  return launch_keys(prm, false, plan, ws, st);
+}
+
+}  // namespace sva

@@ -201,6 +201,25 @@ int launch_cache_write(const sva_kv_cache_t* c, const void* k, const void* v, co
                        const int32_t* slots, int32_t* status, cudaStream_t st);
 int launch_cache_read(const sva_kv_cache_t* c, const int32_t* table, int64_t table_stride, int max_pages, const int32_t* lengths, int B, int N,
                       void* k, void* v, const int64_t ks[3], const int64_t vs[3], int32_t* status, cudaStream_t st);
+int launch_cache_append(const sva_kv_cache_t* c, const void* k, const void* v, const int64_t ks[3], const int64_t vs[3], int B, int T,
+                        const int32_t* table, int64_t table_stride, int max_pages, const int32_t* lengths, const int32_t* counts, int32_t* status,
+                        cudaStream_t st);
+size_t cached_attn_workspace_bytes(const sva_kv_cache_t* c, const sva_cached_attn_t* p);
+int launch_cached_attn(const sva_kv_cache_t* c, const sva_cached_attn_t* p, const void* q, const int32_t* table, const int32_t* lengths,
+                       const int32_t* counts, void* o, float* lse, int32_t* status, void* ws, size_t ws_bytes, cudaStream_t st);
+size_t cross_attn_workspace_bytes(const sva_cross_attn_t* p);
+int launch_cross_attn(const sva_cross_attn_t* p, const void* q, const void* k, const void* v, const int32_t* lengths, const uint8_t* mask, void* o,
+                      float* lse, int32_t* status, void* ws, size_t ws_bytes, cudaStream_t st);
+int launch_pages_copy(const sva_kv_cache_t* c, const int32_t* src, const int32_t* dst, int n, int32_t* status, cudaStream_t st);
+int launch_pages_take(const sva_kv_cache_t* c, int32_t* refs, int32_t* table, int64_t stride, int rows, int max_pages, const int32_t* lengths,
+                      const int32_t* counts, int32_t* status, cudaStream_t st);
+int launch_pages_fork(const sva_kv_cache_t* c, int32_t* refs, int32_t* table, int64_t stride, int rows, int max_pages, int32_t* lengths,
+                      const int32_t* parents, const int32_t* children, int n, int32_t* status, cudaStream_t st);
+int launch_pages_free(const sva_kv_cache_t* c, int32_t* refs, int32_t* table, int64_t stride, int rows, int max_pages, int32_t* lengths,
+                      const int32_t* which, const int32_t* keep, int n, int32_t* status, cudaStream_t st);
+size_t pages_compact_workspace_bytes(const sva_kv_cache_t* c);
+int launch_pages_compact(const sva_kv_cache_t* c, int32_t* refs, int32_t* table, int64_t stride, int rows, int max_pages, int32_t* live,
+                         int32_t* status, void* ws, cudaStream_t st);
 int launch_prepare_v_ts(const Dims& m, const sva_problem_t* p, const void* v, void* ws, size_t ws_bytes,
                         cudaStream_t st);
 

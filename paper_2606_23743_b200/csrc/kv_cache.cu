@@ -32,6 +32,7 @@ struct CacheParams {
   int H, T, page, pages, max_pages, chunk, chunks;        // chunk: heads per CTA, chunks: CTAs per token tile and tensor
   int32_t* status;
   bool wide;                                              // 32-byte stores into the bf16 tensors
+  bool per_page;                                          // (read) one scale per page and head
 };
 
 // row of (page, head, place) among all rows
@@ -192,7 +193,7 @@ cache_read_kernel(const CacheParams prm) {
       sf[i] = 0u;
       if (there && h0 + i < he) {
         const long long row = cache_row(prm, page, h0 + i, place);
-        scale[i] = __ldg(in.scale + row);
+        scale[i] = __ldg(in.scale + (prm.per_page ? page * prm.H + h0 + i : row));
         if (FP4) {
           const uint2 c = __ldg(reinterpret_cast<const uint2*>(in.codes + (row * LANES + lane) * 8));
           codes[i].x = c.x; codes[i].y = c.y;
@@ -244,6 +245,7 @@ static int launch_cache(bool write, CacheParams& prm, const sva_kv_cache_t* c, c
   prm.k = CacheArrays{(uint8_t*)c->k_codes, c->k_scale, (uint8_t*)c->k_sf};
   prm.v = CacheArrays{(uint8_t*)c->v_codes, c->v_scale, (uint8_t*)c->v_sf};
   prm.H = c->H; prm.page = c->page; prm.pages = c->pages;
+  prm.per_page = c->format == SVA_CACHE_E4M3_PAGE;
   prm.wide = rows_on_32(prm.xk, prm.sk) && rows_on_32(prm.xv, prm.sv);
   const int lanes = c->d / 16;
   const long long tiles = (prm.tokens + CACHE_THREADS / lanes - 1) / (CACHE_THREADS / lanes);
