@@ -237,6 +237,15 @@ def _strides(t):
     return _stride_array(t.stride())
 
 
+def _strides_any(t):
+    """The same for a tensor that may hold nothing (torch gives such a one any strides)."""
+    return _strides(t) if t.numel() else _stride_array((0, 0, 0, 1))
+
+
+def _has_strides(t, s):
+    return not t.numel() or tuple(t.stride()) == (*s, 1)
+
+
 def make_problem(q, k, v, o, N: int, block: int, scale: float = 0.0, fp8: bool = False) -> Problem:
     """q,k,v,o: [B,H,n_alloc,d] device tensors (d contiguous); N = valid tokens <= n_alloc."""
     B, H, _, d = q.shape
@@ -697,7 +706,7 @@ def kv_cache_append(c: KvCache, k, v, page_table, lengths, counts=None, status=N
     assert H == c.H and d == c.d and v.shape == shape and k.dtype is v.dtype is torch.bfloat16, "k, v are [B,H,T,d] bf16"
     stride, most = _table(page_table, Bq)
     assert c.on_gpu and k.is_cuda and v.is_cuda and page_table.is_cuda and (status is None or status.is_cuda), _NOT_ON_GPU
-    rc = (_lib or lib()).sva_kv_cache_append(c, k.data_ptr(), v.data_ptr(), _strides(k), _strides(v), Bq, T, page_table.data_ptr(), stride, most,
+    rc = (_lib or lib()).sva_kv_cache_append(c, k.data_ptr(), v.data_ptr(), _strides_any(k), _strides_any(v), Bq, T, page_table.data_ptr(), stride, most,
                                              _int32s(lengths, Bq, "lengths"), None if counts is None else _int32s(counts, Bq, "counts"),
                                              None if status is None else status.data_ptr(), _stream())
     if rc:
@@ -712,7 +721,7 @@ def make_cached_attn(c: KvCache, q, o, page_table, causal: bool = False, scale: 
     p.table_stride, p.max_pages = _table(page_table, p.B)
     p.causal, p.softmax_scale, p.cache = int(causal), scale, c
     _check_attn(p, q, page_table, o)
-    p.q_stride, p.o_stride = _strides(q), _strides(o)
+    p.q_stride, p.o_stride = _strides_any(q), _strides_any(o)
     return p
 
 
@@ -730,7 +739,7 @@ def cached_attn_workspace_bytes(p: CachedAttn) -> int:
 def cached_attn_fwd(p: CachedAttn, q, page_table, lengths, o, counts=None, lse=None, status=None, workspace=None) -> None:
     """o = attention of each sequence's counts [B] queries (None: all M) over its lengths [B] cached tokens; lse [B,Hq,M] fp32."""
     _check_attn(p, q, page_table, o)
-    assert tuple(q.stride()) == (*p.q_stride, 1) and tuple(o.stride()) == (*p.o_stride, 1), "q, o have the plan's strides"
+    assert _has_strides(q, p.q_stride) and _has_strides(o, p.o_stride), "q, o have the plan's strides"
     assert page_table.stride(0) == p.table_stride or p.B == 1, "page_table has the plan's strides"
     assert lse is None or lse.shape == (p.B, p.Hq, p.M) and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,M] fp32"
     assert p.cache.on_gpu and q.is_cuda and o.is_cuda and page_table.is_cuda and (status is None or status.is_cuda) and \
@@ -751,7 +760,7 @@ def make_cross_attn(q, k, v, o, scale: float = 0.0) -> CrossAttn:
         "q, o are [B,Hq,N,d], k, v [B,Hk,S,d], Hq a multiple of Hk"
     assert q.dtype is k.dtype is v.dtype is o.dtype is torch.bfloat16, "q, k, v, o are bf16"
     p.softmax_scale = scale
-    p.q_stride, p.k_stride, p.v_stride, p.o_stride = _strides(q), _strides(k), _strides(v), _strides(o)
+    p.q_stride, p.k_stride, p.v_stride, p.o_stride = _strides_any(q), _strides_any(k), _strides_any(v), _strides_any(o)
     return p
 
 
@@ -763,7 +772,7 @@ def cross_attn_fwd(p: CrossAttn, q, k, v, o, lengths=None, key_mask=None, lse=No
     """o = attention over the first lengths [B] keys (None: all S) that key_mask [B,S] (bool or bytes, None: all) does not leave out."""
     assert q.shape == o.shape == (p.B, p.Hq, p.N, p.d) and k.shape == v.shape == (p.B, p.Hk, p.S, p.d) and \
         q.dtype is k.dtype is v.dtype is o.dtype is torch.bfloat16, "q, k, v, o are bf16 and of the sizes that the plan was made for"
-    assert all([tuple(t.stride()) == (*s, 1) for t, s in ((q, p.q_stride), (k, p.k_stride), (v, p.v_stride), (o, p.o_stride))]), \
+    assert _has_strides(q, p.q_stride) and _has_strides(k, p.k_stride) and _has_strides(v, p.v_stride) and _has_strides(o, p.o_stride), \
         "q, k, v, o have the plan's strides"
     mask_stride = 0
     if key_mask is not None:
