@@ -34,7 +34,8 @@ void sva_debug_set_prof_buffer(void* buf);
  *          (the form that serves more than 1024 key blocks) even where the kept-block bit masks would serve;
  *   bit 8: test aid: the kernel of the first-order term's block covariances withholds a part of its V tile, and
  *   bit 9: the one that adds them up withholds every column tile of a CTA after its first, so that bounded waits run out;
- *   bit 10: test aid: the linear layer's kernels withhold the inputs after the first 128 of every tile, likewise.
+ *   bit 10: test aid: the linear layer's kernels withhold the inputs after the first 128 of every tile, likewise;
+ *   bit 11: test aid: the many-row kernel of sva_cached_attn_fwd and sva_cross_attn_fwd withholds a CTA's key tiles after the first, likewise.
  */
 void sva_debug_set_mode(int bits);
 
@@ -50,6 +51,7 @@ int sva_debug_set_wait_limit(long long cycles);
  *   sva_linear_fp8: 1 few tokens, 2 single CTAs, 3 inputs split over a cluster, 4 pairs
  *   sva_quantize_rows_fp8: groups of inputs per thread (1 or 4)
  *   sva_rope, sva_kv_cache_write, sva_kv_cache_read: heads per CTA
+ *   sva_cached_attn_fwd, sva_cross_attn_fwd: rows per tile (16 or 128)
  */
 int sva_debug_last_choice(void);
 

@@ -7,7 +7,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsva.so")
-SOURCES = ["api.cu", "select.cu", "quant.cu", "quant4.cu", "remainder.cu", "prologue.cu", "gather.cu", "linear.cu", "rope.cu", "kv_cache.cu", "kv_append.cu", "kv_pages.cu", "attn_keys.cu", "attn_simt.cu", "attn_sm100.cu"]
+SOURCES = ["api.cu", "select.cu", "quant.cu", "quant4.cu", "remainder.cu", "prologue.cu", "gather.cu", "linear.cu", "rope.cu", "kv_cache.cu", "kv_append.cu", "kv_pages.cu", "attn_keys.cu", "attn_keys_tc.cu", "attn_simt.cu", "attn_sm100.cu"]
 HEADERS = ["common.cuh", "tc_ptx.cuh", "attn_keys.cuh", os.path.join("..", "..", "include", "sva.h")]
 
 

@@ -13,6 +13,8 @@ int ts_set_wait_limit(long long cycles);
 int rem_set_wait_limit(long long cycles);
 void lin_set_debug_mode(int v);
 int lin_set_wait_limit(long long cycles);
+void keys_set_debug_mode(int v);
+int keys_set_wait_limit(long long cycles);
 
 std::atomic<int> g_last_choice{0};
 
@@ -679,15 +681,16 @@ void sva_debug_set_prof_buffer(void* p) { ts_set_prof_buffer(p); }
 /* bit 4 (test aid) withholds a row's K tiles after the first so that a bounded wait runs out; bit 5 (measurement aid) has the one-call
    forms read a transposed copy of V; bit 6 (test aid) has routing ask for clusters that no device holds; bit 7 (test aid) has the
    remainder look kept blocks up in the CSR; bits 8 and 9 (test aids) withhold loads of the first-order term's kernels; bit 10 (test aid) those of the
-   linear layer's kernels */
+   linear layer's kernels, bit 11 (test aid) those of attention over keys of their own */
 void sva_debug_set_mode(int v) {
   ts_set_debug_mode(v);
   route_set_debug_mode(v);
   rem_set_debug_mode(v);
   lin_set_debug_mode(v);
+  keys_set_debug_mode(v);
 }
 /* test aid: cycles a device-side wait may last before the CTA gives up (<= 0 restores the default) */
-int sva_debug_set_wait_limit(long long cycles) { return ts_set_wait_limit(cycles) | rem_set_wait_limit(cycles) | lin_set_wait_limit(cycles); }
+int sva_debug_set_wait_limit(long long cycles) { return ts_set_wait_limit(cycles) | rem_set_wait_limit(cycles) | lin_set_wait_limit(cycles) | keys_set_wait_limit(cycles); }
 /* test aid: the form that the last linear, rotary or cache call chose */
 int sva_debug_last_choice(void) { return g_last_choice.load(std::memory_order_relaxed); }
 

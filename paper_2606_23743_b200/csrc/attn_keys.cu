@@ -341,18 +341,25 @@ keys_few_kernel(const KeysParams prm) {
     prm.lse[((long long)b * prm.Hq + h) * prm.M + t] = total != 0.f ? (top - (PAGED ? P_UP : 0.f) + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
-// The splits' sums of a row, one warp each: [splits][rows of all][D].  rows_per: rows of a tile of the kernel that wrote them.
+// The splits' sums of a row, one warp each: [splits][rows of all][D].  Tiles have rows_per rows, of which those of `tokens` tokens are used (the kernel
+// for few rows: all, tokens that go over a tile's end among them, tokens 0); up: what the references lie below the exponents.
 template <int D>
 __global__ void __launch_bounds__(256)
-keys_join_kernel(const KeysParams prm, int rows_per, float up) {
+keys_join_kernel(const KeysParams prm, int rows_per, int tokens, float up) {
   constexpr int EACH = D / 32;
   const int zero = grid_dep_wait();
   const int lane = threadIdx.x & 31;
   const long long per_head = (long long)prm.tiles * rows_per, all = (long long)prm.B * prm.Hk * per_head;
   const long long mine = (long long)blockIdx.x * 8 + (threadIdx.x >> 5) + zero;
   if (mine >= all) return;
-  const long long r = mine % per_head, unit = mine / per_head;
+  const long long unit = mine / per_head;
+  long long r = mine % per_head;
   const int hk = (int)(unit % prm.Hk), b = (int)(unit / prm.Hk);
+  if (tokens) {
+    const int in_tile = (int)(r % rows_per);
+    if (in_tile >= tokens * prm.group) return;
+    r = r / rows_per * tokens * prm.group + in_tile;
+  }
   if (r >= (long long)seq_queries(prm, b) * prm.group) return;
   float top = -INFINITY, total = 0.f, out[EACH];
 #pragma unroll
@@ -382,6 +389,12 @@ keys_join_kernel(const KeysParams prm, int rows_per, float up) {
 
 static constexpr size_t few_smem(int d) { return (size_t)FEW_WARPS * FEW_ROWS * (d + 2) * 4; }
 
+template <int D>
+static int launch_join(const KeysParams& prm, int rows_per, int tokens, float up, cudaStream_t st) {
+  const long long rows = (long long)prm.B * prm.Hk * prm.tiles * rows_per;
+  return launch_dep(keys_join_kernel<D>, dim3((unsigned)((rows + 7) / 8)), 256, 0, st, prm, rows_per, tokens, up);
+}
+
 template <int D, bool PAGED>
 static int launch_few(const KeysParams& prm, cudaStream_t st) {
   static DeviceOnce once;
@@ -392,24 +405,45 @@ static int launch_few(const KeysParams& prm, cudaStream_t st) {
   if (units * prm.splits > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
   rc = launch_dep(kern, dim3((unsigned)(units * prm.splits)), FEW_THREADS, few_smem(D), st, prm);
   if (rc || prm.splits == 1) return rc;
-  return launch_dep(keys_join_kernel<D>, dim3((unsigned)((units * FEW_ROWS + 7) / 8)), 256, 0, st, prm, FEW_ROWS, PAGED ? P_UP : 0.f);
+  return launch_join<D>(prm, FEW_ROWS, 0, PAGED ? P_UP : 0.f, st);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- plan, workspace
-// How a call is cut: row tiles, and splits of the key axis where there are fewer tiles than the device has room for.
+// How a call is cut: row tiles of 16 or of 128, and splits of the key axis where there are fewer of them than the device has room for.
 struct KeysPlan {
+  bool tc;                                  // tensor memory, 128 rows
+  int tokens, sms;                          // (tc) tokens of a tile
   long long tiles, units, all;              // per key head; of the call; rows of all tiles
   int splits;
   size_t o_bytes, total;                    // of the workspace
 };
-static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d) {
+static int device_sms() {
+  static std::atomic<int> sms[64];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  if ((n = sms[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) {
+    (void)cudaGetLastError();
+    return 148;
+  }
+  sms[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d, bool maps) {
   KeysPlan k = {};
-  k.tiles = ((long long)M * group + FEW_ROWS - 1) / FEW_ROWS;
+  k.sms = device_sms();
+  const long long rows = (long long)M * group;
+  k.tc = maps && group <= 128 && rows > 32;
+  k.tokens = k.tc ? 128 / group : 0;
+  const int per = k.tc ? 128 : FEW_ROWS;
+  k.tiles = k.tc ? (M + k.tokens - 1) / k.tokens : (rows + per - 1) / per;
   k.units = (long long)B * Hk * k.tiles;
-  k.all = k.units * FEW_ROWS;
-  // at least 256 keys per split
-  long long splits = k.units > 0 ? 148 * 4 / k.units : 1;
-  if (splits > S / 256) splits = S / 256;
+  k.all = k.units * per;
+  // few rows: at least 256 keys per split, CTAs for four rounds; many: at least four key tiles, and no more items than SMs
+  const long long items = k.tc ? (long long)B * Hk * ((k.tiles + 1) / 2) : k.units;
+  long long splits = items > 0 ? (k.tc ? k.sms : k.sms * 4) / items : 1;
+  const long long most = S / (k.tc ? 512 : 256);
+  if (splits > most) splits = most;
   k.splits = (int)(splits < 1 ? 1 : splits);
   if (k.splits > 1) {
     k.o_bytes = (size_t)k.splits * k.all * d * 4;
@@ -417,18 +451,32 @@ static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d) {
   }
   return k;
 }
-
-size_t cached_attn_workspace_bytes(const sva_kv_cache_t* c, const sva_cached_attn_t* p) {
-  return keys_plan(p->B, c->H, p->Hq / c->H, p->M, (long long)p->max_pages * c->page, c->d).total;
+static KeysPlan cached_plan(const sva_kv_cache_t* c, const sva_cached_attn_t* p) {
+  return keys_plan(p->B, c->H, p->Hq / c->H, p->M, (long long)p->max_pages * c->page, c->d, true);
 }
-size_t cross_attn_workspace_bytes(const sva_cross_attn_t* p) { return keys_plan(p->B, p->Hk, p->Hq / p->Hk, p->N, p->S, p->d).total; }
+// (tensor maps know no stride of 0 along tokens, none of 0 along Q's heads and items, and strides below 2^40 bytes)
+static KeysPlan cross_plan(const sva_cross_attn_t* p) {
+  auto fits = [](const int64_t s[3]) { return s[0] < (1LL << 38) && s[1] < (1LL << 38) && s[2] < (1LL << 38); };
+  const bool maps = p->S > 0 && (p->N == 1 || p->q_stride[2] > 0) && (p->Hq == 1 || p->q_stride[1] > 0) && (p->B == 1 || p->q_stride[0] > 0) &&
+                    (p->S == 1 || (p->k_stride[2] > 0 && p->v_stride[2] > 0)) && fits(p->q_stride) && fits(p->k_stride) && fits(p->v_stride);
+  return keys_plan(p->B, p->Hk, p->Hq / p->Hk, p->N, p->S, p->d, maps);
+}
+
+size_t cached_attn_workspace_bytes(const sva_kv_cache_t* c, const sva_cached_attn_t* p) { return cached_plan(c, p).total; }
+size_t cross_attn_workspace_bytes(const sva_cross_attn_t* p) { return cross_plan(p).total; }
 
 static int launch_keys(KeysParams& prm, bool paged, const KeysPlan& plan, void* ws, cudaStream_t st) {
-  if (plan.tiles > 0x7fffffffLL / FEW_ROWS || plan.units > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  if (plan.all > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
   prm.tiles = (int)plan.tiles;
   prm.splits = plan.splits;
   prm.part_o = static_cast<float*>(ws);
   prm.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + plan.o_bytes);
+  note_choice(plan.tc ? 128 : FEW_ROWS);
+  if (plan.tc) {
+    const int rc = launch_keys_tc(prm, paged, plan.sms, st);
+    if (rc || prm.splits == 1) return rc;
+    return prm.d == 128 ? launch_join<128>(prm, 128, plan.tokens, 0.f, st) : launch_join<64>(prm, 128, plan.tokens, 0.f, st);
+  }
   if (paged) return prm.d == 128 ? launch_few<128, true>(prm, st) : launch_few<64, true>(prm, st);
   return prm.d == 128 ? launch_few<128, false>(prm, st) : launch_few<64, false>(prm, st);
 }
@@ -441,7 +489,7 @@ static int check_space(const KeysPlan& plan, const void* ws, size_t ws_bytes) {
 
 int launch_cached_attn(const sva_kv_cache_t* c, const sva_cached_attn_t* p, const void* q, const int32_t* table, const int32_t* lengths,
                        const int32_t* counts, void* o, float* lse, int32_t* status, void* ws, size_t ws_bytes, cudaStream_t st) {
-  const KeysPlan plan = keys_plan(p->B, c->H, p->Hq / c->H, p->M, (long long)p->max_pages * c->page, c->d);
+  const KeysPlan plan = cached_plan(c, p);
   int rc = check_space(plan, ws, ws_bytes);
   if (rc) return rc;
   KeysParams prm = {};
@@ -463,7 +511,7 @@ int launch_cached_attn(const sva_kv_cache_t* c, const sva_cached_attn_t* p, cons
 
 int launch_cross_attn(const sva_cross_attn_t* p, const void* q, const void* k, const void* v, const int32_t* lengths, const uint8_t* mask, void* o,
                       float* lse, int32_t* status, void* ws, size_t ws_bytes, cudaStream_t st) {
-  const KeysPlan plan = keys_plan(p->B, p->Hk, p->Hq / p->Hk, p->N, p->S, p->d);
+  const KeysPlan plan = cross_plan(p);
   int rc = check_space(plan, ws, ws_bytes);
   if (rc) return rc;
   KeysParams prm = {};

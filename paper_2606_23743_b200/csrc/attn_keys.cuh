@@ -45,6 +45,6 @@ __device__ __forceinline__ int keys_seen(const KeysParams& prm, int keys, int qu
 // the pages' scales are; 2^-80 stands for less (a page of zeros has scale 0)
 __device__ __forceinline__ float v_scale_floor(float s) { return s < 8.271806125530277e-25f ? 8.271806125530277e-25f : s; }
 
-int launch_keys_few(const KeysParams& prm, bool paged, cudaStream_t st);
+int launch_keys_tc(const KeysParams& prm, bool paged, int sms, cudaStream_t st);
 
 }  // namespace sva
