@@ -3,10 +3,10 @@
 // A CTA takes items: 256 rows (two tiles of 128) of one key head, and a range of its key tiles of 128.  A row is a query of one of the heads that
 // share the key head; a tile holds the `group` heads of 128 / group tokens.  Both tiles use each key tile, so that it is brought in (and, where it
 // is codes, converted) once for 256 rows.  Roles:
-//   warps 0-3, 4-7   softmax of tile 0 and of tile 1; thread <-> row <-> TMEM lane.  Also the epilogue, and for cached keys the Q tile
-//   warps 8-11       bf16 keys: 8 brings in K and 9 V (TMA), 10 and 11 put zeros into rows of V that are left out
+//   warp  0          issues the MMAs;  warp 1  brings in Q for bf16 keys (TMA)
+//   warps 4-7        bf16 keys: 4 brings in K and 5 V (TMA), 6 and 7 put zeros into rows of V that are left out
 //                    cached keys: all four read codes, convert them to fp16 (exactly) and store them in the layout that TMA would leave
-//   warp  12         issues the MMAs;  warp 13  brings in Q for bf16 keys (TMA)
+//   warps 8-11, 12-15   softmax of tile 0 and of tile 1; thread <-> row <-> TMEM lane.  Also the epilogue, and for cached keys the Q tile
 // Per key tile j and row tile w: S_w = Q_w K^T (A, B from shared memory), P_w over the columns of S_w, O_w += P_w V (A from TMEM, V as an MN-major
 // B operand).  TMEM: S_0 | S_1 | O_0 | O_1, 128 columns each.  The issuing order is P V_0(j), S_0(j+1), P V_1(j), S_1(j+1): while one group computes its
 // exponentials the MMAs of the other run.  S_w(j+1) overwrites P_w(j), which P V_w(j) before it reads: MMAs run in the order of their issue.
@@ -30,23 +30,22 @@ constexpr int PANEL = 128 * 128;                      // 128 rows x 128 bytes (6
 constexpr int STAGES = 2;
 constexpr int SCALE_RING = 4;
 constexpr float LAZY = 7.0f;
+constexpr int POLY = 0b10010010;                      // pairs of eight whose exponentials are polynomials
 constexpr float UP_F16 = 8.0f;                        // log2 of a probability at the reference (fp16: 2^15 at most)
-constexpr int SOFTMAX_REGS = 184, LOADER_REGS = 88, ISSUER_REGS = 56;
-static_assert(256 * SOFTMAX_REGS + 128 * LOADER_REGS + 128 * ISSUER_REGS <= THREADS * 128, "setmaxnreg draws on the registers of the launch");
 // shared memory (bytes from a 1024-byte boundary): Q tiles | K stages | V stages | control
 template <int D> struct Smem {
   static constexpr int TILE = D / 64 * PANEL, K = 2 * TILE, V = K + STAGES * TILE, CTRL = V + STAGES * TILE, BYTES = CTRL + 1024 + 1024;
 };
 // control block: barriers (8 bytes each, pairs), then TMEM base and abort flag, then the scales' ring
 enum { K_FULL = 0, K_EMPTY = 16, V_LAND = 32, V_FULL = 48, V_EMPTY = 64, Q_FULL = 80, Q_EMPTY = 96, S_FULL = 112, P_FULL = 128, O_DONE = 144,
-       O_FREE = 160, TMEM_BASE = 176, ABORT = 180, SCALES = 256 };            // SCALES: [ring][8 chunks of 16 keys]{k scale, log2 v scale, 1 / v scale}
+       O_FREE = 160, P_HALF = 176, TMEM_BASE = 192, ABORT = 196, SCALES = 256 };      // SCALES: [ring][8 chunks of 16 keys]{k scale, log2 v scale, 1 / v scale, -}
 }  // namespace kt
 
 struct KeysTcParams {
   KeysParams k;
   int tokens;                                         // of a row tile: 128 / group
   int pairs;                                          // pairs of row tiles per key head
-  long long items;
+  uint32_t items;
   int k_each_h, k_each_b, v_each_h, v_each_b;         // 0: heads / items share K, V (the maps then have one)
   bool wide;                                          // 32-byte stores into o
   int debug;
@@ -68,9 +67,43 @@ __device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ uint32_t f16_of_codes(uint32_t pair) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(pair & 0xffffu), __NV_E4M3);
-  return (uint32_t)h.x | (uint32_t)h.y << 16;
+// Codes 0, 1 (sel 0x1404) or 2, 3 (0x3424) of four as fp16 values, times 2^-8: a code's exponent and significand are moved to where fp16 has
+// them, which is exact for denormals too.  (The conversion instruction shares its pipe with the exponentials.)
+__device__ __forceinline__ uint32_t f16_of_codes(uint32_t codes, uint32_t sel) {
+  const uint32_t x = __byte_perm(codes, 0u, sel);
+  return (x & 0x80008000u) | (x >> 1 & 0x3f803f80u);
+}
+constexpr float CODE_UNIT = 256.0f;                   // what those values are to be multiplied by
+
+// the larger of three, a NaN if there is one
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+// 2^x of two values on the FMA and integer pipes, x <= 126: 2^floor(x) by the exponent field, the rest by a polynomial with the value 1 at 0 (the
+// smallest relative error on [0, 1) of its degree: 8.3e-8; 1.5e-7 as evaluated).  Below -127 exactly 0.
+__device__ __forceinline__ uint64_t ex2_poly(uint64_t x2) {
+  float x0, x1, t0, t1, p0, p1;
+  unpack2(x2, x0, x1);
+  const uint64_t x = pack2(fmaxf(x0, -127.f), fmaxf(x1, -127.f));
+  const uint64_t magic = pack2(12582912.f, 12582912.f), unmagic = pack2(-12582912.f, -12582912.f), minus = pack2(-1.f, -1.f);
+  uint64_t t;
+  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(t) : "l"(x), "l"(magic));       // floor(x) in the low bits
+  const uint64_t f = fma2(add2(t, unmagic), minus, x);
+  uint64_t p = fma2(f, pack2(0.0018671302823349833f, 0.0018671302823349833f), pack2(0.009017029777169228f, 0.009017029777169228f));
+  p = fma2(f, p, pack2(0.05579991266131401f, 0.05579991266131401f));
+  p = fma2(f, p, pack2(0.24016444385051727f, 0.24016444385051727f));
+  p = fma2(f, p, pack2(0.6931512951850891f, 0.6931512951850891f));
+  p = fma2(f, p, pack2(1.f, 1.f));
+  unpack2(t, t0, t1);
+  unpack2(p, p0, p1);
+  return pack2(__uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23)), __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23)));
 }
 
 // Item i; false where it has no rows.
@@ -91,14 +124,15 @@ __device__ __forceinline__ bool item_at(const KeysTcParams& prm, uint32_t i, Key
   x.j0 = 0;
   x.j1 = tiles;
   if (k.splits > 1) {
-    x.j0 = (int)((long long)tiles * x.split / k.splits);
-    x.j1 = (int)((long long)tiles * (x.split + 1) / k.splits);
+    // (at most 2^24 tiles and as many splits as SMs)
+    x.j0 = (int)((uint32_t)tiles * (uint32_t)x.split / (uint32_t)k.splits);
+    x.j1 = (int)((uint32_t)tiles * (uint32_t)(x.split + 1) / (uint32_t)k.splits);
   }
   return true;
 }
 // The next item at or after i (a CTA's are gridDim.x apart) that has key tiles; false at the end.
 __device__ __forceinline__ bool next_item(const KeysTcParams& prm, uint32_t& i, KeysItem& x) {
-  for (; i < (uint32_t)prm.items; i += gridDim.x)
+  for (; i < prm.items; i += gridDim.x)
     if (item_at(prm, i, x) && x.j0 < x.j1) return true;
   return false;
 }
@@ -118,7 +152,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   const uint32_t sbase = smem_u32(smem), cb = sbase + Smem<D>::CTRL;
   uint8_t* ctrl = smem + Smem<D>::CTRL;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + ABORT);
-  float* scales = reinterpret_cast<float*>(ctrl + SCALES);
+  float4* scales = reinterpret_cast<float4*>(ctrl + SCALES);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -131,6 +165,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       mbar_init(cb + Q_FULL + 8 * w, PAGED ? 128 : 1);
       mbar_init(cb + Q_EMPTY + 8 * w, 1);
       mbar_init(cb + S_FULL + 8 * w, 1);
+      mbar_init(cb + P_HALF + 8 * w, 128);
       mbar_init(cb + P_FULL + 8 * w, 128);
       mbar_init(cb + O_DONE + 8 * w, 1);
       mbar_init(cb + O_FREE + 8 * w, 128);
@@ -139,8 +174,8 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
-  if (!PAGED && warp == 13 && lane == 0) { prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v); }
-  if (warp == 12) {
+  if (!PAGED && warp == 1 && lane == 0) { prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v); }
+  if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(cb + TMEM_BASE), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -152,9 +187,8 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   KeysItem it;
   bool ok = true;
 
-  if (warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ISSUER_REGS));
-    if (warp == 12) {
+  if (warp < 4) {
+    if (warp == 0) {
       // ------------------------------------------------------------------------------------------------ issuer
       const uint32_t el = elect_one();
       const uint64_t qd0 = smem_desc(sbase, 16, 1024), kd0 = smem_desc(sbase + OFF_K, 16, 1024),
@@ -175,14 +209,19 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         return true;
       };
       auto issue_pv = [&](int w, bool first, bool last) -> bool {     // with the V tile in use number vn
-        if (!wait(cb + P_FULL + 8 * w, pn[w]++)) return false;
+        if (!wait(cb + P_HALF + 8 * w, pn[w])) return false;
         if (first && on[w] > 0 && !wait(cb + O_FREE + 8 * w, on[w] - 1u)) return false;
         if (first) ++on[w];
-        tc_fence_after();
         const uint64_t vd = vd0 + (uint64_t)((vn & 1u) * (TILE >> 4));
 #pragma unroll
-        for (int kk = 0; kk < KT / 16; ++kk)                          // 16 keys = 16 rows of 128 bytes
-          tc_mma_ts(tmem + COL_O + 128 * w, tmem + COL_S + 128 * w + 8 * kk, vd + (uint64_t)(kk * 128), IDESC_O, !first || kk > 0 ? 1u : 0u, el);
+        for (int i = 0; i < KT / 16; ++i) {
+          // 16 keys = 16 rows of 128 bytes; in the order in which P is made, 32 keys at a time: quarters 0, 3, 1, 2, each where its S was
+          const int quarter = i < 2 ? 0 : i < 4 ? 3 : i / 2 - 1, kk = 2 * quarter + (i & 1);
+          if (i == KT / 32 && !wait(cb + P_FULL + 8 * w, pn[w]++)) return false;
+          if (i % (KT / 32) == 0) tc_fence_after();
+          tc_mma_ts(tmem + COL_O + 128 * w, tmem + COL_S + 128 * w + 32 * quarter + 8 * (i & 1), vd + (uint64_t)(kk * 128), IDESC_O,
+                    !first || i > 0 ? 1u : 0u, el);
+        }
         if (last) tc_commit(cb + O_DONE + 8 * w, el);
         return true;
       };
@@ -220,7 +259,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         more = next_item(prm, at, it);
         if (more) ok = begin(it);
       }
-    } else if (warp == 13 && !PAGED) {
+    } else if (warp == 1 && !PAGED) {
       // ------------------------------------------------------------------------------------------------ Q (bf16 keys)
       const uint32_t el = elect_one();
       const uint32_t bytes = (uint32_t)(prm.tokens * prm.k.group) * 128 * PANELS;
@@ -238,8 +277,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         }
       }
     }
-  } else if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOADER_REGS));
+  } else if (warp < 8) {
     if (!PAGED) {
       // ------------------------------------------------------------------------------------------------ K, V (bf16)
       uint32_t n = 0;
@@ -247,14 +285,14 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       for (; ok && next_item(prm, at, it); at += gridDim.x) {
         for (int j = it.j0; j < it.j1 && ok; ++j, ++n) {
           const uint32_t s = n & 1u, use = n >> 1;
-          if (warp < 10) {
-            const uint32_t empty = cb + (warp == 8 ? K_EMPTY : V_EMPTY) + 8 * s, full = cb + (warp == 8 ? K_FULL : V_LAND) + 8 * s;
+          if (warp < 6) {
+            const uint32_t empty = cb + (warp == 4 ? K_EMPTY : V_EMPTY) + 8 * s, full = cb + (warp == 4 ? K_FULL : V_LAND) + 8 * s;
             if (use > 0) ok = __all_sync(0xffffffffu, mbar_wait(empty, (use - 1u) & 1u, abort_flag));
             if (!ok || ((prm.debug & 2048) && n >= 1)) { ok = false; break; }     // (test aid: later tiles never come)
             mbar_expect_tx_if(full, TILE, el);
 #pragma unroll
             for (int p = 0; p < PANELS; ++p) {
-              if (warp == 8) tma_load_4d_if(sbase + OFF_K + s * TILE + p * PANEL, &tm_k, full, 64 * p, j * KT, it.hk * prm.k_each_h, it.b * prm.k_each_b, el);
+              if (warp == 4) tma_load_4d_if(sbase + OFF_K + s * TILE + p * PANEL, &tm_k, full, 64 * p, j * KT, it.hk * prm.k_each_h, it.b * prm.k_each_b, el);
               else tma_load_4d_if(sbase + OFF_V + s * TILE + p * PANEL, &tm_v, full, 64 * p, j * KT, it.hk * prm.v_each_h, it.b * prm.v_each_b, el);
             }
           } else {
@@ -264,7 +302,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             if (prm.k.mask || (it.keys < prm.k.S && (j + 1) * KT > it.keys)) {
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                const int row = (warp - 10) * 64 + 32 * i + lane, key = j * KT + row;
+                const int row = (warp - 6) * 64 + 32 * i + lane, key = j * KT + row;
                 bool out = key >= it.keys;
                 if (!out && prm.k.mask) out = __ldg(prm.k.mask + it.b * prm.k.mask_stride + key) == 0;
                 if (out) {
@@ -286,7 +324,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       // ------------------------------------------------------------------------------------------------ K, V (codes)
       // A warp converts 32 keys: chunks 2 wl and 2 wl + 1 of 16.  Four lanes hold 64 bytes of a row, 8 rows at a time: their 16-byte stores meet all banks.
       const KeysParams& k = prm.k;
-      const int wl = warp - 8, piece = lane & 3, sub = lane >> 2;
+      const int wl = warp - 4, piece = lane & 3, sub = lane >> 2;
       uint32_t n = 0;
       auto pages_of = [&](const KeysItem& x, int j, int id[2]) {
 #pragma unroll
@@ -329,68 +367,82 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             const uint4 u = r[i * PANELS + p];
             uint8_t* line = tile + p * PANEL + row * 128;
             *reinterpret_cast<uint4*>(line + (((2 * piece) ^ (row & 7)) << 4)) =
-                make_uint4(f16_of_codes(u.x), f16_of_codes(u.x >> 16), f16_of_codes(u.y), f16_of_codes(u.y >> 16));
+                make_uint4(f16_of_codes(u.x, 0x1404u), f16_of_codes(u.x, 0x3424u), f16_of_codes(u.y, 0x1404u), f16_of_codes(u.y, 0x3424u));
             *reinterpret_cast<uint4*>(line + (((2 * piece + 1) ^ (row & 7)) << 4)) =
-                make_uint4(f16_of_codes(u.z), f16_of_codes(u.z >> 16), f16_of_codes(u.w), f16_of_codes(u.w >> 16));
+                make_uint4(f16_of_codes(u.z, 0x1404u), f16_of_codes(u.z, 0x3424u), f16_of_codes(u.w, 0x1404u), f16_of_codes(u.w, 0x3424u));
           }
         }
       };
       auto wait = [&](uint32_t bar, uint32_t use) { return __all_sync(0xffffffffu, mbar_wait(bar, use & 1u, abort_flag)) != 0; };
+      // one tile ahead in registers, its pages looked up another tile ahead
+      struct Place { KeysItem it; uint32_t at; int j; bool more; int id[2]; };
+      auto look_up = [&](Place& x) { if (x.more) pages_of(x.it, x.j, x.id); };
+      auto step_on = [&](Place& x) {
+        if (++x.j == x.it.j1) {
+          x.at += gridDim.x;
+          x.more = next_item(prm, x.at, x.it);
+          x.j = x.it.j0;
+        }
+      };
       uint4 kr[4 * PANELS], vr[4 * PANELS];
-      bool more = next_item(prm, at, it);
-      int id[2], j = it.j0;
+      float ks = 1.f, vs = 1.f;                                                   // (lanes 0 and 1: of their chunk)
+      bool named = false;
+      auto fetch_scales = [&](const Place& x) {
+        const int id = lane == 0 ? x.id[0] : x.id[1];
+        named = id >= 0;
+        if (lane < 2 && named) {
+          ks = __ldg(k.k_scale + (long long)id * k.Hk + x.it.hk);
+          vs = __ldg(k.v_scale + (long long)id * k.Hk + x.it.hk);
+        }
+      };
+      Place nx;                                                                   // the next tile to be fetched
+      nx.at = at;
+      nx.more = next_item(prm, nx.at, nx.it);
+      nx.j = nx.it.j0;
+      bool more = nx.more;                                                        // ... and whether one has been
+      look_up(nx);
       if (more) {
-        pages_of(it, j, id);
-        load(k.k, it, j, id, kr);
+        load(k.k, nx.it, nx.j, nx.id, kr);
+        load(k.v, nx.it, nx.j, nx.id, vr);
+        fetch_scales(nx);
+        step_on(nx);
+        look_up(nx);
       }
-      while (more && ok) {
-        load(k.v, it, j, id, vr);
+      while (more) {
         const uint32_t s = n & 1u, use = n >> 1;
         if (use > 0) ok = wait(cb + K_EMPTY + 8 * s, use - 1u);
-        if (!ok || ((prm.debug & 2048) && n >= 1)) { ok = false; break; }         // (test aid: later tiles never come)
+        if (!ok || ((prm.debug & 2048) && n >= 1)) break;                         // (test aid: later tiles never come)
         if (lane < 2) {
-          float* sc = scales + ((n & (SCALE_RING - 1)) * 8 + 2 * wl + lane) * 3;
-          const int mine = lane == 0 ? id[0] : id[1];
-          const float vs = mine >= 0 ? v_scale_floor(__ldg(k.v_scale + (long long)mine * k.Hk + it.hk)) : 1.f;
-          const float ks = mine >= 0 ? __ldg(k.k_scale + (long long)mine * k.Hk + it.hk) : 1.f;
-          sc[0] = ks == 0.f ? 1.f : ks;                                           // (zeros alone: any scale will do but one that makes -inf a NaN)
-          sc[1] = mine >= 0 ? log2f(vs) : -INFINITY;                              // (named wrongly: left out)
-          sc[2] = 1.f / vs;
+          // (K of zeros alone, scale 0: any scale will do but one that makes -inf a NaN; pages that are named wrongly: left out)
+          const float v = named ? v_scale_floor(vs) : 1.f;
+          scales[(n & (SCALE_RING - 1)) * 8 + 2 * wl + lane] =
+              make_float4(!named || ks == 0.f ? 1.f : ks * CODE_UNIT, named ? log2f(v) : -INFINITY, 1.f / v, 0.f);
         }
+        more = nx.more;
         store(smem + OFF_K + s * TILE, kr);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(cb + K_FULL + 8 * s);
-        // the next tile's K is on its way while this one's V is converted
-        KeysItem nx = it;
-        uint32_t nat = at;
-        int nj = j + 1;
-        if (nj == it.j1) {
-          nat += gridDim.x;
-          more = next_item(prm, nat, nx);
-          nj = nx.j0;
-        }
-        if (more) {
-          pages_of(nx, nj, id);
-          load(k.k, nx, nj, id, kr);
-        }
+        if (more) load(k.k, nx.it, nx.j, nx.id, kr);
         if (use > 0) ok = wait(cb + V_EMPTY + 8 * s, use - 1u);
         if (!ok) break;
         store(smem + OFF_V + s * TILE, vr);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(cb + V_FULL + 8 * s);
-        it = nx;
-        at = nat;
-        j = nj;
+        if (more) {
+          load(k.v, nx.it, nx.j, nx.id, vr);
+          fetch_scales(nx);
+          step_on(nx);
+          look_up(nx);
+        }
         ++n;
       }
     }
   } else {
     // ------------------------------------------------------------------------------------------------ softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     const KeysParams& k = prm.k;
-    const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+    const int w = (warp >> 2) - 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_tmem = tmem + lane_addr + COL_S + 128 * w, o_tmem = tmem + lane_addr + COL_O + 128 * w;
     uint32_t sn = 0, qn = 0, dn = 0, tn = 0;                                  // S tiles, Q tiles, items, and key tiles of all items so far
@@ -415,7 +467,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     };
     // this group's next item (one that has a tile for it), others on the way: key tiles are counted, rows without keys answered
     auto advance = [&](KeysItem& x) -> bool {
-      for (; at < (uint32_t)prm.items; at += gridDim.x) {
+      for (; at < prm.items; at += gridDim.x) {
         if (!item_at(prm, at, x) || (w == 1 && !x.two && x.j0 >= x.j1)) continue;
         if (x.j0 >= x.j1) { empty_item(x); continue; }
         if (w == 1 && !x.two) { tn += (uint32_t)(x.j1 - x.j0); continue; }
@@ -469,86 +521,136 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         if (!__all_sync(0xffffffffu, mbar_wait(cb + S_FULL + 8 * w, sn & 1u, abort_flag))) { ok = false; break; }
         ++sn;
         tc_fence_after();
-        uint32_t sv[128];
-        tmem_ld32(s_tmem, sv);
-        tmem_ld32(s_tmem + 32, sv + 32);
-        tmem_ld32(s_tmem + 64, sv + 64);
-        tmem_ld32(s_tmem + 96, sv + 96);
-        tc_wait_ld64(sv);
-        tc_wait_ld64(sv + 64);
+        // keys that a row does not see: -inf into S (rare, and short: the tile's own code is what the groups' time goes into)
         const int valid = seen - j * KT;
         const bool masked = !PAGED && k.mask != nullptr;
         if (masked || __any_sync(0xffffffffu, valid < KT)) {
-#pragma unroll
+#pragma unroll 1
           for (int i = 0; i < 4; ++i) {
             const int v = valid - 32 * i;
-            uint32_t bits = v >= 32 ? 0xffffffffu : v <= 0 ? 0u : (1u << v) - 1u;
+            uint32_t bits = v >= 32 ? 0xffffffffu : v <= 0 ? 0u : (1u << v) - 1u, x[32];
             if (masked) {
               const int key = j * KT + 32 * i + lane;
               bits &= __ballot_sync(0xffffffffu, key < it.keys && __ldg(k.mask + it.b * k.mask_stride + key) != 0);
             }
+            tmem_ld32(s_tmem + 32 * i, x);
+            tc_wait_ld32(x);
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (!(bits >> e & 1u)) sv[32 * i + e] = 0xff800000u;
+              if (!(bits >> e & 1u)) x[e] = 0xff800000u;
+            tmem_st32(s_tmem + 32 * i, x);
           }
+          tc_wait_st();
         }
-        const float* sc = scales + (tn & (SCALE_RING - 1)) * 24;
-        float mx = -INFINITY;
+        // P = 2^(S c + a - ref) of 32 keys, put where their S was, and their sum (cached keys: over V's scale).  Of eight pairs POLY's go the way of
+        // ex2_poly: the exponentials' pipe would be busy for as long as the MMAs take with all of them
+        const float4* sc = scales + (tn & (SCALE_RING - 1)) * 8;
+        uint32_t pv[16];
+        auto exps = [&](int h, const uint32_t* x, float ref) -> float {
+          float sum = 0.f;
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          float a = -INFINITY, b = -INFINITY;
-#pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            a = max3(a, __uint_as_float(sv[16 * g + e]), __uint_as_float(sv[16 * g + e + 1]));
-            b = max3(b, __uint_as_float(sv[16 * g + e + 2]), __uint_as_float(sv[16 * g + e + 3]));
-          }
-          a = fmaxf(a, b);
-          mx = fmaxf(mx, PAGED ? fmaf(a, cc * sc[3 * g], sc[3 * g + 1]) : a);
-        }
-        if (!PAGED) mx *= cc;
-        if (j == it.j0) {
-          m = mx;
-        } else if (__any_sync(0xffffffffu, mx > m + LAZY)) {
-          // (P V of the tile before has completed: S of this one came after it)
-          float f = 1.f;
-          if (mx > m + LAZY) {
-            f = ex2(m - mx);
-            m = mx;
-            l *= f;
-          }
-#pragma unroll 1
-          for (int c = 0; c < D; c += 16) {
-            uint32_t ov[16];
-            tmem_ld16(o_tmem + c, ov);
-            tc_wait_ld16(ov);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * f);
-            tmem_st16(o_tmem + c, ov);
-          }
-        }
-        const float ref = (m == -INFINITY ? 0.f : m) - UP;
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          uint32_t pv[16];
-#pragma unroll
-          for (int g = 2 * h; g < 2 * h + 2; ++g) {
-            const float c = PAGED ? cc * sc[3 * g] : cc, nm = PAGED ? sc[3 * g + 1] - ref : -ref;
+          for (int g = 0; g < 2; ++g) {
+            const float4 f = PAGED ? sc[2 * h + g] : make_float4(1.f, 0.f, 1.f, 0.f);
+            const float c = PAGED ? cc * f.x : cc, nm = PAGED ? f.y - ref : -ref;
             const uint64_t c2 = pack2(c, c), nm2 = pack2(nm, nm);
             uint64_t sum2 = pack2(0.f, 0.f);
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-              float x0, x1;
-              unpack2(fma2(pack2(__uint_as_float(sv[16 * g + e]), __uint_as_float(sv[16 * g + e + 1])), c2, nm2), x0, x1);
-              const float p0 = ex2(x0), p1 = ex2(x1);
-              sum2 = add2(sum2, pack2(p0, p1));
-              pv[8 * (g - 2 * h) + e / 2] = PAGED ? f16_pair(p0, p1) : pack_bf16(p0, p1);
+              uint64_t p2 = fma2(pack2(__uint_as_float(x[16 * g + e]), __uint_as_float(x[16 * g + e + 1])), c2, nm2);
+              float p0, p1;
+              if (POLY >> (e / 2) & 1) {
+                p2 = ex2_poly(p2);
+                unpack2(p2, p0, p1);
+              } else {
+                unpack2(p2, p0, p1);
+                p0 = ex2(p0);
+                p1 = ex2(p1);
+                p2 = pack2(p0, p1);
+              }
+              sum2 = add2(sum2, p2);
+              pv[8 * g + e / 2] = PAGED ? f16_pair(p0, p1) : pack_bf16(p0, p1);
             }
             float s0, s1;
             unpack2(sum2, s0, s1);
-            l = PAGED ? fmaf(s0 + s1, sc[3 * g + 2], l) : l + (s0 + s1);
+            sum = PAGED ? fmaf(s0 + s1, f.z, sum) : sum + (s0 + s1);
           }
-          tmem_st16(s_tmem + 16 * h, pv);
+          return sum;
+        };
+        auto maximum = [&](int h, const uint32_t* x, float mx) -> float {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            float a = __uint_as_float(x[16 * g]), b = __uint_as_float(x[16 * g + 1]);
+#pragma unroll
+            for (int e = 2; e < 14; e += 4) {
+              a = max3_nan(a, __uint_as_float(x[16 * g + e]), __uint_as_float(x[16 * g + e + 1]));
+              b = max3_nan(b, __uint_as_float(x[16 * g + e + 2]), __uint_as_float(x[16 * g + e + 3]));
+            }
+            a = max3_nan(a, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
+            if (PAGED) {
+              const float4 f = sc[2 * h + g];
+              mx = max_nan(mx, fmaf(max_nan(a, b), cc * f.x, f.y));
+            } else {
+              mx = max3_nan(mx, a, b);
+            }
+          }
+          return mx;
+        };
+        auto reference = [&]() -> float { return (m == -INFINITY ? 0.f : m) - UP; };
+        // Quarters of 32 keys.  The maximum of all four is taken beside the first one's exponentials (of an item's first tile: before them), which
+        // are done again where it has outgrown the reference.  The second and third are read twice for that: the whole tile would take 128 registers.
+        uint32_t x[32], y[32];
+        tmem_ld32(s_tmem, x);
+        tmem_ld32(s_tmem + 32, y);
+        tc_wait_ld32(x);
+        tc_wait_ld32(y);
+        float mx = maximum(1, y, maximum(0, x, -INFINITY)), sum = 0.f;
+        const bool first = j == it.j0;
+        tmem_ld32(s_tmem + 64, y);
+        if (!first) sum = exps(0, x, reference());
+        tc_wait_ld32(y);
+        mx = maximum(2, y, mx);
+        tmem_ld32(s_tmem + 96, y);
+        tc_wait_ld32(y);
+        mx = maximum(3, y, mx);
+        if (!PAGED) mx *= cc;
+        if (first) m = mx;
+        else if (mx != mx) l = mx;                                            // (a NaN: the row's sum, and with it the row, becomes one)
+        if (first || __any_sync(0xffffffffu, mx > m + LAZY)) {
+          // (P V of the tile before has completed: S of this one came after it)
+          if (!first) {
+            float f = 1.f;
+            if (mx > m + LAZY) {
+              f = ex2(m - mx);
+              m = mx;
+              l *= f;
+            }
+#pragma unroll 1
+            for (int c = 0; c < D; c += 16) {
+              tmem_ld16(o_tmem + c, pv);
+              tc_wait_ld16(pv);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) pv[e] = __float_as_uint(__uint_as_float(pv[e]) * f);
+              tmem_st16(o_tmem + c, pv);
+            }
+          }
+          sum = exps(0, x, reference());
         }
+        const float ref = reference();
+        tmem_st16(s_tmem, pv);
+        tmem_ld32(s_tmem + 32, x);
+        sum += exps(3, y, ref);
+        tmem_st16(s_tmem + 96, pv);
+        tc_wait_st();
+        tc_wait_ld32(x);
+        tc_fence_before();
+        mbar_arrive(cb + P_HALF + 8 * w);
+        tmem_ld32(s_tmem + 64, y);
+        sum += exps(1, x, ref);
+        tmem_st16(s_tmem + 32, pv);
+        tc_wait_ld32(y);
+        sum += exps(2, y, ref);
+        tmem_st16(s_tmem + 64, pv);
+        l += sum;
         tc_wait_st();
         tc_fence_before();
         mbar_arrive(cb + P_FULL + 8 * w);
@@ -562,9 +664,11 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       if (!__all_sync(0xffffffffu, mbar_wait(cb + O_DONE + 8 * w, dn & 1u, abort_flag))) { ok = false; break; }
       ++dn;
       tc_fence_after();
-      const float inv = l != 0.f ? 1.0f / l : 0.f;
+      constexpr float UNIT = PAGED ? CODE_UNIT : 1.f;
+      const float inv = l != 0.f ? UNIT / l : 0.f;
       if (k.splits > 1) {
         const long long pr = mine ? part_row(done) : 0;
+        auto scaled = [](uint32_t x) -> uint32_t { return __float_as_uint(__uint_as_float(x) * UNIT); };
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t ov[32];
@@ -573,7 +677,8 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           if (mine) {
             float* dst = k.part_o + pr * D + c;
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(dst + e) = make_uint4(ov[e], ov[e + 1], ov[e + 2], ov[e + 3]);
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(dst + e) = 
+                  make_uint4(scaled(ov[e]), scaled(ov[e + 1]), scaled(ov[e + 2]), scaled(ov[e + 3]));
           }
         }
         tc_fence_before();
@@ -617,7 +722,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 12) {
+  if (warp == 0) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
@@ -658,7 +763,7 @@ static int launch_tc(const KeysTcParams& prm, const CUtensorMap& tq, const CUten
   auto kern = keys_tc_kernel<D, PAGED>;
   const int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kt::Smem<D>::BYTES) == cudaSuccess; });
   if (rc) return rc;
-  const unsigned grid = prm.items < sms ? (unsigned)prm.items : (unsigned)sms;
+  const unsigned grid = prm.items < (unsigned)sms ? prm.items : (unsigned)sms;
   return launch_dep(kern, dim3(grid), kt::THREADS, kt::Smem<D>::BYTES, st, tq, tk, tv, prm);
 }
 
@@ -667,8 +772,9 @@ int launch_keys_tc(const KeysParams& k, bool paged, int sms, cudaStream_t st) {
   prm.k = k;
   prm.tokens = 128 / k.group;
   prm.pairs = (k.tiles + 1) / 2;
-  prm.items = (long long)k.B * k.Hk * prm.pairs * k.splits;
-  if (prm.items > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  const long long items = (long long)k.B * k.Hk * prm.pairs * k.splits;
+  if (items > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  prm.items = (uint32_t)items;
   prm.wide = (reinterpret_cast<uintptr_t>(k.o) & 31u) == 0 && ((k.so.b | k.so.h | k.so.n) & 15) == 0;
   prm.debug = g_debug_keys;
   CUtensorMap tq = {}, tk = {}, tv = {};
