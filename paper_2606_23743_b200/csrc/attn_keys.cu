@@ -439,12 +439,27 @@ static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d, b
   k.tiles = k.tc ? (M + k.tokens - 1) / k.tokens : (rows + per - 1) / per;
   k.units = (long long)B * Hk * k.tiles;
   k.all = k.units * per;
-  // few rows: at least 256 keys per split, CTAs for four rounds; many: at least four key tiles, and no more items than SMs
-  const long long items = k.tc ? (long long)B * Hk * ((k.tiles + 1) / 2) : k.units;
-  long long splits = items > 0 ? (k.tc ? k.sms : k.sms * 4) / items : 1;
-  const long long most = S / (k.tc ? 512 : 256);
-  if (splits > most) splits = most;
-  k.splits = (int)(splits < 1 ? 1 : splits);
+  if (k.tc) {
+    // The number of splits for which the pairs of SMs are done first: rounds of items, each as long as its key tiles and some 2 tiles more, and for more
+    // than one split the partial sums: 512 KB of HBM traffic per item, 3 / 74 of the 2 us that a pair takes for a tile.  At least four key tiles per split.
+    // (24 heads x 4 680 queries x 32 760 keys, 240 items for 74 pairs: 2 418 us in one split, 2 179 in four.)
+    const long long items = (long long)B * Hk * ((k.tiles + 3) / 4), pairs = k.sms / 2 > 0 ? k.sms / 2 : 1, tiles = (S + 127) / 128;
+    double best = 0.0;
+    k.splits = 1;
+    for (int n = 1; n <= 64 && (n == 1 || tiles / n >= 4); ++n) {
+      const double rounds = (double)((items * n + pairs - 1) / pairs);
+      const double time = rounds * ((double)((tiles + n - 1) / n) + 2.0) + (n > 1 ? 3.0 + 3.0 * n * (double)items / (double)pairs : 0.0);
+      if (n == 1 || time < 0.97 * best) {
+        best = time;
+        k.splits = n;
+      }
+    }
+  } else {
+    // at least 256 keys per split, CTAs for four rounds
+    long long splits = k.units > 0 ? k.sms * 4 / k.units : 1;
+    if (splits > S / 256) splits = S / 256;
+    k.splits = (int)(splits < 1 ? 1 : splits);
+  }
   if (k.splits > 1) {
     k.o_bytes = (size_t)k.splits * k.all * d * 4;
     k.total = k.o_bytes + (size_t)k.splits * k.all * 8;

@@ -1,19 +1,23 @@
 // Attention of many rows over many keys (sva_cached_attn_fwd, sva_cross_attn_fwd) on the tensor cores.
 //
-// A CTA takes items: 256 rows (two tiles of 128) of one key head, and a range of its key tiles of 128.  A row is a query of one of the heads that
-// share the key head; a tile holds the `group` heads of 128 / group tokens.  Both tiles use each key tile, so that it is brought in (and, where it
-// is codes, converted) once for 256 rows.  Roles:
-//   warp  0          issues the MMAs;  warp 1  brings in Q for bf16 keys (TMA)
-//   warps 4-7        bf16 keys: 4 brings in K and 5 V (TMA), 6 and 7 put zeros into rows of V that are left out
-//                    cached keys: all four read codes, convert them to fp16 (exactly) and store them in the layout that TMA would leave
+// A pair of CTAs (cta_group::2) takes items: 512 rows (four tiles of 128) of one key head, and a range of its key tiles of 128.  A row is a query of one
+// of the heads that share the key head; a tile holds the `group` heads of 128 / group tokens.  Each CTA has two of the row tiles, w = 0 and 1, and half of
+// each key tile: 64 keys of K, half of the channels of V.  The MMAs (256 rows, the w-th tiles of both CTAs) read both halves; so a key tile is brought
+// in, and where it is codes converted, once for 512 rows, and of what shared memory can deliver the operands take two thirds (with a CTA by itself:
+// all of it, and the MMAs of Q K^T waited for it).  Roles:
+//   warp  0          (first CTA) issues the MMAs of both
+//   warps 1-7        bf16 keys: 1 brings in K, 2 V and 3 Q (TMA); 3 also puts zeros into rows of V that are left out
+//                    cached keys: all seven read codes, convert them to fp16 (exactly) and store them in the layout that TMA would leave
 //   warps 8-11, 12-15   softmax of tile 0 and of tile 1; thread <-> row <-> TMEM lane.  Also the epilogue, and for cached keys the Q tile
-// Per key tile j and row tile w: S_w = Q_w K^T (A, B from shared memory), P_w over the columns of S_w, O_w += P_w V (A from TMEM, V as an MN-major
-// B operand).  TMEM: S_0 | S_1 | O_0 | O_1, 128 columns each.  The issuing order is P V_0(j), S_0(j+1), P V_1(j), S_1(j+1): while one group computes its
-// exponentials the MMAs of the other run.  S_w(j+1) overwrites P_w(j), which P V_w(j) before it reads: MMAs run in the order of their issue.
+// A key tile is worked on in halves h of 64 keys: S_wh = Q_w K_h^T (A, B from shared memory), P_wh over the columns of S_wh, O_w += P_wh V_h (A from TMEM,
+// V as an MN-major B operand).  TMEM: S_0 | S_1 | O_0 | O_1, 128 columns each.  Once a group has handed over P_wh, the issuer lets P V_wh and the next
+// tile's S_wh follow one another, and the group goes on with the other half, whose S is there by then: its exponentials never wait for an MMA that
+// waits for them (with whole tiles the way from P to the next S took 1 200 to 1 700 cycles of 4 000).  The next S_wh overwrites P_wh, which P V_wh before
+// it reads: MMAs run in the order of their issue.
 //
-// The reference m of a row's exponentials follows its maximum lazily: O is rescaled only when a tile's maximum is more than LAZY powers of two above m
-// (probabilities reach 2^LAZY; sums are fp32).  Cached keys: K's scale is a factor of the logits, log2 of V's an addend (both per 16 keys), see
-// attn_keys.cu; P is fp16 and lies at 2^(UP + LAZY) at most.
+// The reference m of a row's exponentials follows its maximum lazily: a tile's first exponentials are taken with the m so far and its maximum beside
+// them; only when that is more than LAZY powers of two above m are they done again, and O rescaled (probabilities reach 2^LAZY; sums are fp32).
+// Cached keys: K's scale is a factor of the logits, log2 of V's an addend (both per 16 keys), see attn_keys.cu; P is fp16 and at most 2^(UP + LAZY).
 //
 // Every wait is bounded; when one runs out all roles leave, the CTA reports SVA_DEV_TIMEOUT and its rows are not stored.
 #include <cuda_fp16.h>
@@ -25,56 +29,92 @@ namespace sva {
 
 namespace kt {
 constexpr int THREADS = 512;
+constexpr int SOFTMAX_REGS = 168, HELPER_REGS = 88;
+static_assert(256 * SOFTMAX_REGS + 256 * HELPER_REGS <= THREADS * 128, "setmaxnreg draws on the registers of the launch");
 constexpr int KT = 128;                               // keys of a tile
-constexpr int PANEL = 128 * 128;                      // 128 rows x 128 bytes (64 channels)
-constexpr int STAGES = 2;
-constexpr int SCALE_RING = 4;
+constexpr int PANEL = 128 * 128;                      // Q: 128 rows x 128 bytes (64 channels)
+constexpr int STAGES = 4;
+constexpr int SCALE_RING = 8;                         // (one more than the stages is enough)
 constexpr float LAZY = 7.0f;
-constexpr int POLY = 0b10010010;                      // pairs of eight whose exponentials are polynomials
+constexpr int POLY = 0b01000100;                      // pairs of eight whose exponentials are polynomials
 constexpr float UP_F16 = 8.0f;                        // log2 of a probability at the reference (fp16: 2^15 at most)
+constexpr int CONVERTERS = 7;                         // warps (cached keys)
 // shared memory (bytes from a 1024-byte boundary): Q tiles | K stages | V stages | control
 template <int D> struct Smem {
-  static constexpr int TILE = D / 64 * PANEL, K = 2 * TILE, V = K + STAGES * TILE, CTRL = V + STAGES * TILE, BYTES = CTRL + 1024 + 1024;
+  static constexpr int TILE = D / 64 * PANEL, HALF = TILE / 2;      // of Q; of K or V, a CTA's half of a key tile
+  static constexpr int K = 2 * TILE, V = K + STAGES * HALF, CTRL = V + STAGES * HALF, BYTES = CTRL + 2048 + 1024;
 };
-// control block: barriers (8 bytes each, pairs), then TMEM base and abort flag, then the scales' ring
-enum { K_FULL = 0, K_EMPTY = 16, V_LAND = 32, V_FULL = 48, V_EMPTY = 64, Q_FULL = 80, Q_EMPTY = 96, S_FULL = 112, P_FULL = 128, O_DONE = 144,
-       O_FREE = 160, P_HALF = 176, TMEM_BASE = 192, ABORT = 196, SCALES = 256 };      // SCALES: [ring][8 chunks of 16 keys]{k scale, log2 v scale, 1 / v scale, -}
+// control block: barriers (8 bytes each), then TMEM base and abort flag, then the scales' ring
+enum { K_FULL = 0, K_EMPTY = 32, V_LAND = 64, V_FULL = 96, V_EMPTY = 128, Q_FULL = 160, Q_EMPTY = 176, S_FULL = 192, P_FULL = 224, PV_DONE = 256,
+       O_DONE = 272, O_FREE = 288, TMEM_BASE = 304, ABORT = 308, SCALES = 512 };      // (S_FULL, P_FULL: [w][h])
+// SCALES: [ring][8 chunks of 16 keys]{k scale, log2 v scale, 1 / v scale, -}
 }  // namespace kt
 
 struct KeysTcParams {
   KeysParams k;
   int tokens;                                         // of a row tile: 128 / group
-  int pairs;                                          // pairs of row tiles per key head
+  int quads;                                          // fours of row tiles per key head
   uint32_t items;
   int k_each_h, k_each_b, v_each_h, v_each_b;         // 0: heads / items share K, V (the maps then have one)
   bool wide;                                          // 32-byte stores into o
   int debug;
 };
 
-// An item: rows [t0, t0 + 2 * tokens) of (b, hk), key tiles [j0, j1).
+// An item: queries [t0, t0 + 4 * tokens) of (b, hk), key tiles [j0, j1).  Tile w of CTA r begins with query t0 + (2 w + r) tokens.
 struct KeysItem {
-  int b, hk, pair, split, keys, queries, t0, j0, j1;
-  bool two;                                           // the second tile has rows
+  int b, hk, quad, split, keys, queries, t0, j0, j1;
+  bool two;                                           // tiles w = 1 have rows
 };
 
-__device__ __forceinline__ void tc_mma_ss_16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t elected) {
+// D[tmem of both CTAs] (+)= A[each CTA's shared memory: its 128 rows] * B[half of the columns from each], 16-bit operands
+__device__ __forceinline__ void tc_mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t elected) {
   asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
-               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
                ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(elected) : "memory");
+}
+// the same with A in each CTA's tensor memory
+__device__ __forceinline__ void tc_mma_ts_pair(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t elected) {
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
+               "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(elected) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d_pair_if(uint32_t dst, const CUtensorMap* map, uint32_t mapped_bar, int c0, int c1, int c2, int c3, uint32_t elected) {
+  asm volatile(
+      "{\n.reg .pred q;\nsetp.ne.b32 q, %7, 0;\n"
+      "@q cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n}"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(mapped_bar), "r"(elected) : "memory");
 }
 __device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// Codes 0, 1 (sel 0x1404) or 2, 3 (0x3424) of four as fp16 values, times 2^-8: a code's exponent and significand are moved to where fp16 has
-// them, which is exact for denormals too.  (The conversion instruction shares its pipe with the exponentials.)
-__device__ __forceinline__ uint32_t f16_of_codes(uint32_t codes, uint32_t sel) {
-  const uint32_t x = __byte_perm(codes, 0u, sel);
-  return (x & 0x80008000u) | (x >> 1 & 0x3f803f80u);
+// Two codes (the low 16 bits) as fp16 values.  (By way of shifts and masks it would take eight operations for four codes on a pipe of half the rate: 25 codes
+// per cycle and SM, this 57.)
+__device__ __forceinline__ uint32_t f16_of_codes(uint32_t pair) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(pair & 0xffffu), __NV_E4M3);
+  return (uint32_t)h.x | (uint32_t)h.y << 16;
 }
-constexpr float CODE_UNIT = 256.0f;                   // what those values are to be multiplied by
 
+// Bounded wait of a warp, as mbar_wait, but suspended until the phase completes (or for as long as the hardware likes) where it polls: a
+// group's way from its last P to its next S goes through six of them.
+__device__ __forceinline__ uint32_t mbar_suspend(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done;
+}
+__device__ __forceinline__ bool keys_wait_long(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  const uint32_t t0 = (uint32_t)clock();
+  do {
+    if (__all_sync(0xffffffffu, mbar_suspend(bar, parity))) return true;
+  } while (!__any_sync(0xffffffffu, *abort_flag || (uint32_t)clock() - t0 > g_wait_limit));
+  *abort_flag = 1;
+  return false;
+}
+__device__ __forceinline__ bool keys_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_suspend(bar, parity))) return true;
+  return keys_wait_long(bar, parity, abort_flag);
+}
 // the larger of three, a NaN if there is one
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float y;
@@ -109,17 +149,17 @@ __device__ __forceinline__ uint64_t ex2_poly(uint64_t x2) {
 // Item i; false where it has no rows.
 __device__ __forceinline__ bool item_at(const KeysTcParams& prm, uint32_t i, KeysItem& x) {
   const KeysParams& k = prm.k;
-  x.pair = (int)(i % (uint32_t)prm.pairs); i /= (uint32_t)prm.pairs;
+  x.quad = (int)(i % (uint32_t)prm.quads); i /= (uint32_t)prm.quads;
   x.split = 0;
   if (k.splits > 1) { x.split = (int)(i % (uint32_t)k.splits); i /= (uint32_t)k.splits; }
   x.hk = (int)(i % (uint32_t)k.Hk);
   x.b = (int)(i / (uint32_t)k.Hk);
   x.keys = seq_keys(k, x.b);
   x.queries = seq_queries(k, x.b);
-  x.t0 = x.pair * 2 * prm.tokens;
+  x.t0 = x.quad * 4 * prm.tokens;
   if (x.t0 >= x.queries) return false;
-  x.two = x.t0 + prm.tokens < x.queries;
-  const int end = keys_seen(k, x.keys, x.queries, min(x.t0 + (x.two ? 2 : 1) * prm.tokens, x.queries) - 1);
+  x.two = x.t0 + 2 * prm.tokens < x.queries;
+  const int end = keys_seen(k, x.keys, x.queries, min(x.t0 + (x.two ? 4 : 2) * prm.tokens, x.queries) - 1);
   const int tiles = (end + kt::KT - 1) / kt::KT;
   x.j0 = 0;
   x.j1 = tiles;
@@ -130,9 +170,9 @@ __device__ __forceinline__ bool item_at(const KeysTcParams& prm, uint32_t i, Key
   }
   return true;
 }
-// The next item at or after i (a CTA's are gridDim.x apart) that has key tiles; false at the end.
+// The next item at or after i (a pair's are as far apart as there are pairs) that has key tiles; false at the end.
 __device__ __forceinline__ bool next_item(const KeysTcParams& prm, uint32_t& i, KeysItem& x) {
-  for (; i < prm.items; i += gridDim.x)
+  for (; i < prm.items; i += gridDim.x / 2)
     if (item_at(prm, i, x) && x.j0 < x.j1) return true;
   return false;
 }
@@ -142,9 +182,11 @@ __global__ void __launch_bounds__(kt::THREADS, 1)
 keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                const KeysTcParams prm) {
   using namespace kt;
-  constexpr int TILE = Smem<D>::TILE, OFF_K = Smem<D>::K, OFF_V = Smem<D>::V, PANELS = D / 64;
+  constexpr int TILE = Smem<D>::TILE, HALF = Smem<D>::HALF, OFF_K = Smem<D>::K, OFF_V = Smem<D>::V, PANELS = D / 64;
+  constexpr int KPANEL = 64 * 128;                                            // K: 64 rows x 128 bytes
+  constexpr int VROW = D;                                                     // V: bytes of a row, D / 2 channels
   constexpr int FMT = PAGED ? 0 : 1;                                          // fp16 or bf16 operands
-  constexpr uint32_t IDESC_S = instr_desc(128, 128, FMT, false), IDESC_O = instr_desc(128, D, FMT, true);
+  constexpr uint32_t IDESC_S = instr_desc(256, 64, FMT, false), IDESC_O = instr_desc(256, D, FMT, true);
   constexpr float UP = PAGED ? UP_F16 : 0.f;
   constexpr uint32_t COL_S = 0, COL_O = 256;
   extern __shared__ uint8_t smem_raw[];
@@ -153,246 +195,274 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   uint8_t* ctrl = smem + Smem<D>::CTRL;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl + ABORT);
   float4* scales = reinterpret_cast<float4*>(ctrl + SCALES);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)(blockIdx.x & 1);
 
   if (threadIdx.x == 0) {
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(cb + K_FULL + 8 * i, PAGED ? 2 * CONVERTERS : 1);
+      mbar_init(cb + K_EMPTY + 8 * i, 1);
+      mbar_init(cb + V_LAND + 8 * i, 1);
+      mbar_init(cb + V_FULL + 8 * i, PAGED ? 2 * CONVERTERS : 2);
+      mbar_init(cb + V_EMPTY + 8 * i, 1);
+    }
     for (int w = 0; w < 2; ++w) {
-      mbar_init(cb + K_FULL + 8 * w, PAGED ? 4 : 1);
-      mbar_init(cb + K_EMPTY + 8 * w, 1);
-      mbar_init(cb + V_LAND + 8 * w, 1);
-      mbar_init(cb + V_FULL + 8 * w, PAGED ? 4 : 2);
-      mbar_init(cb + V_EMPTY + 8 * w, 1);
-      mbar_init(cb + Q_FULL + 8 * w, PAGED ? 128 : 1);
+      mbar_init(cb + Q_FULL + 8 * w, PAGED ? 8 : 1);                          // (8: the warps of a group, in both CTAs)
       mbar_init(cb + Q_EMPTY + 8 * w, 1);
-      mbar_init(cb + S_FULL + 8 * w, 1);
-      mbar_init(cb + P_HALF + 8 * w, 128);
-      mbar_init(cb + P_FULL + 8 * w, 128);
+      for (int h = 0; h < 2; ++h) {
+        mbar_init(cb + S_FULL + 16 * w + 8 * h, 1);
+        mbar_init(cb + P_FULL + 16 * w + 8 * h, 8);
+      }
+      mbar_init(cb + PV_DONE + 8 * w, 1);
       mbar_init(cb + O_DONE + 8 * w, 1);
-      mbar_init(cb + O_FREE + 8 * w, 128);
+      mbar_init(cb + O_FREE + 8 * w, 8);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
+    if (!PAGED) { prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v); }
   }
-  if (!PAGED && warp == 1 && lane == 0) { prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v); }
   if (warp == 0) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(cb + TMEM_BASE), "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(cb + TMEM_BASE), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
+  cluster_sync_all();                                                         // the other CTA's barriers are there
   tc_fence_after();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(ctrl + TMEM_BASE);
-  uint32_t at = blockIdx.x + (uint32_t)grid_dep_wait();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(ctrl + TMEM_BASE), 0);
+  const uint32_t lead = mapa(cb, 0);                                          // the first CTA's barriers: what both CTAs bring the issuer
+  uint32_t at = (blockIdx.x >> 1) + (uint32_t)grid_dep_wait();
+  const uint32_t pairs = gridDim.x / 2;
   KeysItem it;
   bool ok = true;
+  auto wait = [&](uint32_t bar, uint32_t use) -> bool { return keys_wait(bar, use & 1u, abort_flag); };
 
-  if (warp < 4) {
-    if (warp == 0) {
+  if (warp < 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(HELPER_REGS));
+    if (warp == 0 && rank == 0) {
       // ------------------------------------------------------------------------------------------------ issuer
       const uint32_t el = elect_one();
-      const uint64_t qd0 = smem_desc(sbase, 16, 1024), kd0 = smem_desc(sbase + OFF_K, 16, 1024),
-                     vd0 = smem_desc(sbase + OFF_V, PANEL, 1024);
+      const uint64_t qd0 = smem_desc(sbase, 16, 1024), kd0 = smem_desc(sbase + OFF_K, 16, 1024);
+      const uint64_t vd0 = D == 128 ? smem_desc(sbase + OFF_V, 16, 1024) : smem_desc_sw64(sbase + OFF_V);
       uint32_t kn = 0, vn = 0, qn[2] = {0, 0}, pn[2] = {0, 0}, on[2] = {0, 0};      // uses so far
-      auto wait = [&](uint32_t bar, uint32_t use) { return __all_sync(0xffffffffu, mbar_wait(bar, use & 1u, abort_flag)) != 0; };
-      auto issue_s = [&](int w, bool first, bool last) -> bool {      // from the K tile in use number kn
+      auto issue_s = [&](int w, int h, bool first, bool last) -> bool {      // from the K tile in use number kn
         if (first && !wait(cb + Q_FULL + 8 * w, qn[w]++)) return false;
         tc_fence_after();
-        const uint64_t qd = qd0 + (uint64_t)(w * (TILE >> 4)), kd = kd0 + (uint64_t)((kn & 1u) * (TILE >> 4));
+        const uint64_t qd = qd0 + (uint64_t)(w * (TILE >> 4)), kd = kd0 + (uint64_t)((kn % STAGES) * (HALF >> 4) + h * (32 * 128 >> 4));
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint64_t off = (uint64_t)((kk / 4) * (PANEL >> 4) + (kk % 4) * 2);
-          tc_mma_ss_16(tmem + COL_S + 128 * w, qd + off, kd + off, IDESC_S, kk > 0 ? 1u : 0u, el);
-        }
-        tc_commit(cb + S_FULL + 8 * w, el);
-        if (last) tc_commit(cb + Q_EMPTY + 8 * w, el);
+        for (int kk = 0; kk < D / 16; ++kk)
+          tc_mma_ss_pair(tmem + COL_S + 128 * w + 64 * h, qd + (uint64_t)((kk / 4) * (PANEL >> 4) + (kk % 4) * 2),
+                         kd + (uint64_t)((kk / 4) * (KPANEL >> 4) + (kk % 4) * 2), IDESC_S, kk > 0 ? 1u : 0u, el);
+        tc_commit_pair(cb + S_FULL + 16 * w + 8 * h, el);
+        if (last) tc_commit_pair(cb + Q_EMPTY + 8 * w, el);
         return true;
       };
-      auto issue_pv = [&](int w, bool first, bool last) -> bool {     // with the V tile in use number vn
-        if (!wait(cb + P_HALF + 8 * w, pn[w])) return false;
+      auto issue_pv = [&](int w, int h, bool first, bool last) -> bool {     // with the V tile in use number vn
+        if (!wait(cb + P_FULL + 16 * w + 8 * h, pn[w])) return false;
+        if (h == 1) ++pn[w];
         if (first && on[w] > 0 && !wait(cb + O_FREE + 8 * w, on[w] - 1u)) return false;
         if (first) ++on[w];
-        const uint64_t vd = vd0 + (uint64_t)((vn & 1u) * (TILE >> 4));
+        tc_fence_after();
+        const uint64_t vd = vd0 + (uint64_t)((vn % STAGES) * (HALF >> 4) + h * 4 * VROW);
 #pragma unroll
-        for (int i = 0; i < KT / 16; ++i) {
-          // 16 keys = 16 rows of 128 bytes; in the order in which P is made, 32 keys at a time: quarters 0, 3, 1, 2, each where its S was
-          const int quarter = i < 2 ? 0 : i < 4 ? 3 : i / 2 - 1, kk = 2 * quarter + (i & 1);
-          if (i == KT / 32 && !wait(cb + P_FULL + 8 * w, pn[w]++)) return false;
-          if (i % (KT / 32) == 0) tc_fence_after();
-          tc_mma_ts(tmem + COL_O + 128 * w, tmem + COL_S + 128 * w + 32 * quarter + 8 * (i & 1), vd + (uint64_t)(kk * 128), IDESC_O,
-                    !first || i > 0 ? 1u : 0u, el);
-        }
-        if (last) tc_commit(cb + O_DONE + 8 * w, el);
+        for (int kk = 0; kk < KT / 32; ++kk)                          // 16 keys = 16 rows of V
+          tc_mma_ts_pair(tmem + COL_O + 128 * w, tmem + COL_S + 128 * w + 64 * h + 8 * kk, vd + (uint64_t)(kk * VROW), IDESC_O, !first || kk > 0 ? 1u : 0u, el);
+        tc_commit_pair(cb + PV_DONE + 8 * w, el);
+        if (last) tc_commit_pair(cb + O_DONE + 8 * w, el);
         return true;
       };
-      // S of the first tile of an item, both row tiles
+      // S of the first tile of an item
       auto begin = [&](const KeysItem& x) -> bool {
-        if (!wait(cb + K_FULL + 8 * (kn & 1u), kn >> 1)) return false;
+        if (!wait(cb + K_FULL + 8 * (kn % STAGES), kn / STAGES)) return false;
         const bool last = x.j1 - x.j0 == 1;
-        if (!issue_s(0, true, last) || (x.two && !issue_s(1, true, last))) return false;
-        tc_commit(cb + K_EMPTY + 8 * (kn & 1u), el);
+        if (!issue_s(0, 0, true, false) || !issue_s(0, 1, false, last)) return false;
+        if (x.two && (!issue_s(1, 0, true, false) || !issue_s(1, 1, false, last))) return false;
+        tc_commit_pair(cb + K_EMPTY + 8 * (kn % STAGES), el);
         ++kn;
         return true;
       };
-      bool more = next_item(prm, at, it);
+      // (an item's numbers by way of a shuffle: the compiler then knows them to be the same for the warp, and keeps descriptors in uniform
+      // registers.  Without that an MMA took some 70 cycles to issue, and the issuer was what the pair waited for)
+      auto next = [&]() -> bool {
+        const bool more = next_item(prm, at, it);
+        it.j0 = __shfl_sync(0xffffffffu, it.j0, 0);
+        it.j1 = __shfl_sync(0xffffffffu, it.j1, 0);
+        it.two = __shfl_sync(0xffffffffu, (int)it.two, 0) != 0;
+        return __shfl_sync(0xffffffffu, (int)more, 0) != 0;
+      };
+      bool more = next();
       if (more) ok = begin(it);
       while (more && ok) {
         for (int j = it.j0; j < it.j1 && ok; ++j) {
           const bool first = j == it.j0, last = j + 1 == it.j1;
-          ok = wait(cb + V_FULL + 8 * (vn & 1u), vn >> 1) && issue_pv(0, first, last);
-          if (ok && !last) {
-            ok = wait(cb + K_FULL + 8 * (kn & 1u), kn >> 1) && issue_s(0, false, j + 2 == it.j1);
+          // (both tiles first: they are there long before P is, and between P and S nothing is waited for)
+          ok = wait(cb + V_FULL + 8 * (vn % STAGES), vn / STAGES) && (last || wait(cb + K_FULL + 8 * (kn % STAGES), kn / STAGES));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int h = i >> 1, w = i & 1;
+            if (!ok || (w == 1 && !it.two)) continue;
+            ok = issue_pv(w, h, first && h == 0, last && h == 1) && (last || issue_s(w, h, false, h == 1 && j + 2 == it.j1));
           }
-          if (ok && it.two) ok = issue_pv(1, first, last);
           if (!ok) break;
-          tc_commit(cb + V_EMPTY + 8 * (vn & 1u), el);
+          tc_commit_pair(cb + V_EMPTY + 8 * (vn % STAGES), el);
           ++vn;
           if (!last) {
-            if (it.two) ok = issue_s(1, false, j + 2 == it.j1);
-            if (!ok) break;
-            tc_commit(cb + K_EMPTY + 8 * (kn & 1u), el);
+            tc_commit_pair(cb + K_EMPTY + 8 * (kn % STAGES), el);
             ++kn;
           }
         }
         if (!ok) break;
-        at += gridDim.x;
-        more = next_item(prm, at, it);
+        at += pairs;
+        more = next();
         if (more) ok = begin(it);
       }
-    } else if (warp == 1 && !PAGED) {
-      // ------------------------------------------------------------------------------------------------ Q (bf16 keys)
+    } else if (warp > 0 && warp < 4 && !PAGED) {
       const uint32_t el = elect_one();
-      const uint32_t bytes = (uint32_t)(prm.tokens * prm.k.group) * 128 * PANELS;
-      uint32_t qn[2] = {0, 0};
-      for (; ok && next_item(prm, at, it); at += gridDim.x) {
-        for (int w = 0; w < (it.two ? 2 : 1) && ok; ++w) {
-          if (qn[w] > 0) ok = __all_sync(0xffffffffu, mbar_wait(cb + Q_EMPTY + 8 * w, (qn[w] - 1u) & 1u, abort_flag));
-          if (!ok) break;
-          ++qn[w];
-          const uint32_t bar = cb + Q_FULL + 8 * w;
-          mbar_expect_tx_if(bar, bytes, el);
-#pragma unroll
-          for (int p = 0; p < PANELS; ++p)
-            tma_load_4d_if(sbase + w * TILE + p * PANEL, &tm_q, bar, 64 * p, it.hk * prm.k.group, it.t0 + w * prm.tokens, it.b, el);
-        }
-      }
-    }
-  } else if (warp < 8) {
-    if (!PAGED) {
-      // ------------------------------------------------------------------------------------------------ K, V (bf16)
       uint32_t n = 0;
-      const uint32_t el = elect_one();
-      for (; ok && next_item(prm, at, it); at += gridDim.x) {
-        for (int j = it.j0; j < it.j1 && ok; ++j, ++n) {
-          const uint32_t s = n & 1u, use = n >> 1;
-          if (warp < 6) {
-            const uint32_t empty = cb + (warp == 4 ? K_EMPTY : V_EMPTY) + 8 * s, full = cb + (warp == 4 ? K_FULL : V_LAND) + 8 * s;
-            if (use > 0) ok = __all_sync(0xffffffffu, mbar_wait(empty, (use - 1u) & 1u, abort_flag));
-            if (!ok || ((prm.debug & 2048) && n >= 1)) { ok = false; break; }     // (test aid: later tiles never come)
-            mbar_expect_tx_if(full, TILE, el);
+      if (warp < 3) {
+        // ---------------------------------------------------------------------------------------------- K, V (bf16)
+        const uint32_t empty = cb + (warp == 1 ? K_EMPTY : V_EMPTY);
+        for (; ok && next_item(prm, at, it); at += pairs) {
+          for (int j = it.j0; j < it.j1 && ok; ++j, ++n) {
+            const uint32_t s = n % STAGES, use = n / STAGES;
+            if (use > 0) ok = wait(empty + 8 * s, use - 1u);
+            if (!ok || ((prm.debug & 2048) && n >= 1)) { ok = false; break; }       // (test aid: later tiles never come)
+            if (warp == 1) {
+              if (rank == 0) mbar_expect_tx_if(cb + K_FULL + 8 * s, 2 * HALF, el);
 #pragma unroll
-            for (int p = 0; p < PANELS; ++p) {
-              if (warp == 4) tma_load_4d_if(sbase + OFF_K + s * TILE + p * PANEL, &tm_k, full, 64 * p, j * KT, it.hk * prm.k_each_h, it.b * prm.k_each_b, el);
-              else tma_load_4d_if(sbase + OFF_V + s * TILE + p * PANEL, &tm_v, full, 64 * p, j * KT, it.hk * prm.v_each_h, it.b * prm.v_each_b, el);
+              for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)                             // of each half's 64 keys this CTA's 32
+                  tma_load_4d_pair_if(sbase + OFF_K + s * HALF + p * KPANEL + h * 32 * 128, &tm_k, lead + K_FULL + 8 * s, 64 * p,
+                                      j * KT + 64 * h + 32 * rank, it.hk * prm.k_each_h, it.b * prm.k_each_b, el);
+            } else {
+              mbar_expect_tx_if(cb + V_LAND + 8 * s, HALF, el);
+              tma_load_4d_if(sbase + OFF_V + s * HALF, &tm_v, cb + V_LAND + 8 * s, D / 2 * rank, j * KT, it.hk * prm.v_each_h, it.b * prm.v_each_b, el);
             }
-          } else {
-            // rows of V whose keys are left out: zeros, whatever they hold (their probabilities are 0, and 0 times a NaN is one)
-            ok = __all_sync(0xffffffffu, mbar_wait(cb + V_LAND + 8 * s, use & 1u, abort_flag));
+          }
+        }
+        // (the MMAs' arrivals from the first CTA are all here before this one may go)
+        for (uint32_t i = n > STAGES ? n - STAGES : 0; ok && i < n; ++i) ok = wait(empty + 8 * (i % STAGES), i / STAGES);
+      } else {
+        // ---------------------------------------------------------------------------------------------- Q; rows of V that are left out
+        const uint32_t bytes = (uint32_t)(prm.tokens * prm.k.group) * 128 * PANELS;
+        uint32_t qn[2] = {0, 0};
+        for (; ok && next_item(prm, at, it); at += pairs) {
+          for (int w = 0; w < (it.two ? 2 : 1) && ok; ++w) {
+            if (qn[w] > 0) ok = wait(cb + Q_EMPTY + 8 * w, qn[w] - 1u);
+            if (!ok) break;
+            ++qn[w];
+            if (rank == 0) mbar_expect_tx_if(cb + Q_FULL + 8 * w, 2 * bytes, el);
+#pragma unroll
+            for (int p = 0; p < PANELS; ++p)
+              tma_load_4d_pair_if(sbase + w * TILE + p * PANEL, &tm_q, lead + Q_FULL + 8 * w, 64 * p, it.hk * prm.k.group,
+                                  it.t0 + (2 * w + rank) * prm.tokens, it.b, el);
+          }
+          for (int j = it.j0; j < it.j1 && ok; ++j, ++n) {
+            const uint32_t s = n % STAGES;
+            ok = wait(cb + V_LAND + 8 * s, n / STAGES);
             if (!ok) break;
             if (prm.k.mask || (it.keys < prm.k.S && (j + 1) * KT > it.keys)) {
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int row = (warp - 6) * 64 + 32 * i + lane, key = j * KT + row;
+              // zeros, whatever they hold: their probabilities are 0, and 0 times a NaN is one
+#pragma unroll 1
+              for (int row = lane; row < KT; row += 32) {
+                const int key = j * KT + row;
                 bool out = key >= it.keys;
                 if (!out && prm.k.mask) out = __ldg(prm.k.mask + it.b * prm.k.mask_stride + key) == 0;
                 if (out) {
 #pragma unroll
-                  for (int p = 0; p < PANELS; ++p)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                      *reinterpret_cast<uint4*>(smem + OFF_V + s * TILE + p * PANEL + row * 128 + ((e ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                  for (int e = 0; e < VROW; e += 16) *reinterpret_cast<uint4*>(smem + OFF_V + s * HALF + row * VROW + e) = make_uint4(0u, 0u, 0u, 0u);
                 }
               }
               fence_async_smem();
               __syncwarp();
             }
-            if (lane == 0) mbar_arrive(cb + V_FULL + 8 * s);
+            mbar_arrive_cluster_if(lead + V_FULL + 8 * s, lane == 0);
           }
         }
+        for (int w = 0; w < 2 && ok; ++w)
+          if (qn[w] > 0) ok = wait(cb + Q_EMPTY + 8 * w, qn[w] - 1u);
       }
-    } else {
+    } else if (warp > 0 && PAGED) {
       // ------------------------------------------------------------------------------------------------ K, V (codes)
-      // A warp converts 32 keys: chunks 2 wl and 2 wl + 1 of 16.  Four lanes hold 64 bytes of a row, 8 rows at a time: their 16-byte stores meet all banks.
+      // Units of 512 bytes: K's 64 keys 8 at a time and 64 channels at a time, then V's 128 keys (this CTA's half of the channels) 8 at a time (D = 64: 16).  A
+      // lane has 16 codes of a row; its two 16-byte stores meet all banks with those of its neighbours.  Warp a takes units a, a + 7, ...
+      constexpr int KU = 8 * PANELS, VU = D == 128 ? 16 : 8, UNITS = KU + VU, EACH = (UNITS + CONVERTERS - 1) / CONVERTERS;
       const KeysParams& k = prm.k;
-      const int wl = warp - 4, piece = lane & 3, sub = lane >> 2;
+      const int a = warp - 1;
       uint32_t n = 0;
-      auto pages_of = [&](const KeysItem& x, int j, int id[2]) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int key = j * KT + wl * 32 + c * 16;
-          id[c] = -1;
-          if (key < x.keys) {
-            const int e = key / k.page;
-            id[c] = e < k.max_pages ? __ldg(k.table + x.b * k.table_stride + e) : -1;
-            if (id[c] < 0 || id[c] >= k.pages) {
-              id[c] = -1;
-              if (lane == 0 && k.status) atomicOr(k.status, SVA_DEV_BAD_INDEX);
-            }
+      // lane c < 8 knows chunk c of 16 keys: its page (-1: none, or named wrongly), its first row there, its scales
+      struct Place { KeysItem it; uint32_t at; int j; bool more; int id; long long row; };
+      auto look_up = [&](Place& x) {
+        x.id = -1;
+        x.row = 0;
+        const int key = x.j * KT + lane * 16;
+        if (x.more && lane < 8 && key < x.it.keys) {
+          const int e = key / k.page;
+          x.id = e < k.max_pages ? __ldg(k.table + x.it.b * k.table_stride + e) : -1;
+          if (x.id < 0 || x.id >= k.pages) {
+            x.id = -1;
+            if (k.status) atomicOr(k.status, SVA_DEV_BAD_INDEX);
+          } else {
+            x.row = ((long long)x.id * k.Hk + x.it.hk) * k.page + (key - e * k.page);
           }
         }
       };
-      // raw codes of a tile: [chunk][8 rows][panel]
-      auto load = [&](const uint8_t* codes, const KeysItem& x, int j, const int id[2], uint4 (&r)[4 * PANELS]) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int key = j * KT + wl * 32 + c * 16;
-          const long long row = ((long long)id[c] * k.Hk + x.hk) * k.page + (key - key / k.page * k.page);
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int p = 0; p < PANELS; ++p) {
-              uint4& u = r[(2 * c + h) * PANELS + p];
-              u = make_uint4(0u, 0u, 0u, 0u);
-              if (id[c] >= 0 && key + 8 * h + sub < x.keys)
-                u = __ldg(reinterpret_cast<const uint4*>(codes + (row + 8 * h + sub) * D + 64 * p + 16 * piece));
-            }
-        }
-      };
-      auto store = [&](uint8_t* tile, const uint4 (&r)[4 * PANELS]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = wl * 32 + 8 * i + sub;
-#pragma unroll
-          for (int p = 0; p < PANELS; ++p) {
-            const uint4 u = r[i * PANELS + p];
-            uint8_t* line = tile + p * PANEL + row * 128;
-            *reinterpret_cast<uint4*>(line + (((2 * piece) ^ (row & 7)) << 4)) =
-                make_uint4(f16_of_codes(u.x, 0x1404u), f16_of_codes(u.x, 0x3424u), f16_of_codes(u.y, 0x1404u), f16_of_codes(u.y, 0x3424u));
-            *reinterpret_cast<uint4*>(line + (((2 * piece + 1) ^ (row & 7)) << 4)) =
-                make_uint4(f16_of_codes(u.z, 0x1404u), f16_of_codes(u.z, 0x3424u), f16_of_codes(u.w, 0x1404u), f16_of_codes(u.w, 0x3424u));
-          }
-        }
-      };
-      auto wait = [&](uint32_t bar, uint32_t use) { return __all_sync(0xffffffffu, mbar_wait(bar, use & 1u, abort_flag)) != 0; };
-      // one tile ahead in registers, its pages looked up another tile ahead
-      struct Place { KeysItem it; uint32_t at; int j; bool more; int id[2]; };
-      auto look_up = [&](Place& x) { if (x.more) pages_of(x.it, x.j, x.id); };
       auto step_on = [&](Place& x) {
         if (++x.j == x.it.j1) {
-          x.at += gridDim.x;
+          x.at += pairs;
           x.more = next_item(prm, x.at, x.it);
           x.j = x.it.j0;
         }
       };
-      uint4 kr[4 * PANELS], vr[4 * PANELS];
-      float ks = 1.f, vs = 1.f;                                                   // (lanes 0 and 1: of their chunk)
+      // where a unit's lane finds its codes, and puts the values (from the stage's beginning)
+      auto unit_of = [&](int u, int& key, int& byte, int& to0, int& to1) {
+        if (u < KU) {
+          const int sub = lane >> 2, piece = lane & 3, row = u / PANELS * 8 + sub, p = u % PANELS;
+          key = (row & 32) * 2 + 32 * rank + (row & 31);                     // (of each half's 64 keys this CTA's 32)
+          byte = 64 * p + 16 * piece;
+          const int line = p * KPANEL + row * 128;
+          to0 = line + (((2 * piece) ^ (row & 7)) << 4);
+          to1 = line + (((2 * piece + 1) ^ (row & 7)) << 4);
+        } else if (D == 128) {
+          const int sub = lane >> 2, piece = lane & 3;
+          key = (u - KU) * 8 + sub;
+          byte = 64 * rank + 16 * piece;
+          to0 = key * 128 + (((2 * piece) ^ (key & 7)) << 4);
+          to1 = key * 128 + (((2 * piece + 1) ^ (key & 7)) << 4);
+        } else {
+          const int sub = lane >> 1, piece = lane & 1;
+          key = (u - KU) * 16 + sub;
+          byte = 32 * rank + 16 * piece;
+          to0 = key * 64 + (((2 * piece) ^ (key >> 1 & 3)) << 4);
+          to1 = key * 64 + (((2 * piece + 1) ^ (key >> 1 & 3)) << 4);
+        }
+      };
+      auto load = [&](const Place& x, int u, uint4& r) {
+        int key, byte, to0, to1;
+        unit_of(u, key, byte, to0, to1);
+        const long long row = __shfl_sync(0xffffffffu, x.row, key >> 4);
+        const int id = __shfl_sync(0xffffffffu, x.id, key >> 4);
+        r = make_uint4(0u, 0u, 0u, 0u);
+        if (id >= 0 && x.j * KT + key < x.it.keys)
+          r = __ldg(reinterpret_cast<const uint4*>((u < KU ? k.k : k.v) + (row + (key & 15)) * D + byte));
+      };
+      auto store = [&](uint32_t s, int u, const uint4& r) {
+        int key, byte, to0, to1;
+        unit_of(u, key, byte, to0, to1);
+        uint8_t* stage = smem + (u < KU ? OFF_K : OFF_V) + s * HALF;
+        *reinterpret_cast<uint4*>(stage + to0) = make_uint4(f16_of_codes(r.x), f16_of_codes(r.x >> 16), f16_of_codes(r.y), f16_of_codes(r.y >> 16));
+        *reinterpret_cast<uint4*>(stage + to1) = make_uint4(f16_of_codes(r.z), f16_of_codes(r.z >> 16), f16_of_codes(r.w), f16_of_codes(r.w >> 16));
+      };
+      uint4 r[EACH];                                                              // one tile ahead, its pages looked up another tile ahead
+      float ks = 1.f, vs = 1.f;
       bool named = false;
       auto fetch_scales = [&](const Place& x) {
-        const int id = lane == 0 ? x.id[0] : x.id[1];
-        named = id >= 0;
-        if (lane < 2 && named) {
-          ks = __ldg(k.k_scale + (long long)id * k.Hk + x.it.hk);
-          vs = __ldg(k.v_scale + (long long)id * k.Hk + x.it.hk);
+        named = x.id >= 0;
+        if (named && a == 0) {
+          ks = __ldg(k.k_scale + (long long)x.id * k.Hk + x.it.hk);
+          vs = __ldg(k.v_scale + (long long)x.id * k.Hk + x.it.hk);
         }
       };
       Place nx;                                                                   // the next tile to be fetched
@@ -400,62 +470,74 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       nx.more = next_item(prm, nx.at, nx.it);
       nx.j = nx.it.j0;
       bool more = nx.more;                                                        // ... and whether one has been
-      look_up(nx);
       if (more) {
-        load(k.k, nx.it, nx.j, nx.id, kr);
-        load(k.v, nx.it, nx.j, nx.id, vr);
+        look_up(nx);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+          if (a + CONVERTERS * i < UNITS) load(nx, a + CONVERTERS * i, r[i]);
         fetch_scales(nx);
         step_on(nx);
         look_up(nx);
       }
       while (more) {
-        const uint32_t s = n & 1u, use = n >> 1;
+        const uint32_t s = n % STAGES, use = n / STAGES;
         if (use > 0) ok = wait(cb + K_EMPTY + 8 * s, use - 1u);
-        if (!ok || ((prm.debug & 2048) && n >= 1)) break;                         // (test aid: later tiles never come)
-        if (lane < 2) {
+        if (!ok || ((prm.debug & 2048) && n >= 1)) { ok = false; break; }         // (test aid: later tiles never come)
+        if (a == 0 && lane < 8) {
           // (K of zeros alone, scale 0: any scale will do but one that makes -inf a NaN; pages that are named wrongly: left out)
           const float v = named ? v_scale_floor(vs) : 1.f;
-          scales[(n & (SCALE_RING - 1)) * 8 + 2 * wl + lane] =
-              make_float4(!named || ks == 0.f ? 1.f : ks * CODE_UNIT, named ? log2f(v) : -INFINITY, 1.f / v, 0.f);
+          scales[(n % SCALE_RING) * 8 + lane] = make_float4(!named || ks == 0.f ? 1.f : ks, named ? log2f(v) : -INFINITY, 1.f / v, 0.f);
         }
         more = nx.more;
-        store(smem + OFF_K + s * TILE, kr);
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(cb + K_FULL + 8 * s);
-        if (more) load(k.k, nx.it, nx.j, nx.id, kr);
-        if (use > 0) ok = wait(cb + V_EMPTY + 8 * s, use - 1u);
+        bool k_out = false;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          const int u = a + CONVERTERS * i;
+          if (u >= KU && !k_out) {                                                // (uniform in a warp)
+            k_out = true;
+            fence_async_smem();
+            __syncwarp();
+            mbar_arrive_cluster_if(lead + K_FULL + 8 * s, lane == 0);
+            if (use > 0) ok = ok && wait(cb + V_EMPTY + 8 * s, use - 1u);
+          }
+          if (u < UNITS) {
+            store(s, u, r[i]);
+            if (more) load(nx, u, r[i]);
+          }
+        }
         if (!ok) break;
-        store(smem + OFF_V + s * TILE, vr);
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(cb + V_FULL + 8 * s);
+        mbar_arrive_cluster_if(lead + V_FULL + 8 * s, lane == 0);
         if (more) {
-          load(k.v, nx.it, nx.j, nx.id, vr);
           fetch_scales(nx);
           step_on(nx);
           look_up(nx);
         }
         ++n;
       }
+      // (the MMAs' arrivals from the first CTA are all here before this one may go)
+      for (uint32_t i = n > STAGES ? n - STAGES : 0; ok && i < n; ++i)
+        ok = wait(cb + K_EMPTY + 8 * (i % STAGES), i / STAGES) && wait(cb + V_EMPTY + 8 * (i % STAGES), i / STAGES);
     }
   } else {
     // ------------------------------------------------------------------------------------------------ softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     const KeysParams& k = prm.k;
     const int w = (warp >> 2) - 2, row = (warp & 3) * 32 + lane;
-    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16, sole = lane == 0;
     const uint32_t s_tmem = tmem + lane_addr + COL_S + 128 * w, o_tmem = tmem + lane_addr + COL_O + 128 * w;
-    uint32_t sn = 0, qn = 0, dn = 0, tn = 0;                                  // S tiles, Q tiles, items, and key tiles of all items so far
+    uint32_t fn = 0, hn = 0, qn = 0, dn = 0, tn = 0;                          // halves of S fetched, of P handed over, Q tiles, items, and key tiles of all items so far
     // where a row's output goes
-    const int tok = row / k.group, head = row % k.group;
+    const int tok = row / k.group, head = row % k.group, mine_from = (2 * w + rank) * prm.tokens + tok;
     auto out_row = [&](const KeysItem& x, int t) -> long long { return x.b * k.so.b + (long long)(x.hk * k.group + head) * k.so.h + (long long)t * k.so.n; };
     auto lse_at = [&](const KeysItem& x, int t) -> float* { return k.lse + ((long long)x.b * k.Hq + x.hk * k.group + head) * k.M + t; };
     auto part_row = [&](const KeysItem& x) -> long long {
-      return (x.split * ((long long)k.B * k.Hk * k.tiles) + ((long long)x.b * k.Hk + x.hk) * k.tiles + 2 * x.pair + w) * 128 + row;
+      return (x.split * ((long long)k.B * k.Hk * k.tiles) + ((long long)x.b * k.Hk + x.hk) * k.tiles + 4 * x.quad + 2 * w + rank) * 128 + row;
     };
     // (an item without keys: zeros; a split without: an empty part)
     auto empty_item = [&](const KeysItem& x) {
-      const int t = x.t0 + w * prm.tokens + tok;
+      const int t = x.t0 + mine_from;
       if (tok >= prm.tokens || t >= x.queries) return;
       if (k.splits > 1) {
         k.part_ml[part_row(x)] = make_float2(0.f, 0.f);
@@ -465,9 +547,9 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       for (int e = 0; e < D / 8; ++e) dst[e] = make_uint4(0u, 0u, 0u, 0u);
       if (k.lse) *lse_at(x, t) = -INFINITY;
     };
-    // this group's next item (one that has a tile for it), others on the way: key tiles are counted, rows without keys answered
+    // this group's next item (one that has tiles for it), others on the way: key tiles are counted, rows without keys answered
     auto advance = [&](KeysItem& x) -> bool {
-      for (; at < prm.items; at += gridDim.x) {
+      for (; at < prm.items; at += pairs) {
         if (!item_at(prm, at, x) || (w == 1 && !x.two && x.j0 >= x.j1)) continue;
         if (x.j0 >= x.j1) { empty_item(x); continue; }
         if (w == 1 && !x.two) { tn += (uint32_t)(x.j1 - x.j0); continue; }
@@ -478,7 +560,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     float q_scale = 1.f;                                                      // power of two that Q's row was divided by (cached keys)
     // cached keys: the group's Q rows as fp16 into shared memory
     auto put_q = [&](const KeysItem& x) -> bool {
-      const int t = x.t0 + w * prm.tokens + tok;
+      const int t = x.t0 + mine_from;
       const bool there = tok < prm.tokens && t < x.queries;
       uint32_t q[D / 2];
       const uint8_t* src = k.q + 2 * (x.b * k.sq.b + (long long)(x.hk * k.group + head) * k.sq.h + (long long)t * k.sq.n);
@@ -494,7 +576,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       const bool odd = ex == 0u || ex > 252u;                                 // (zeros; infinities, NaNs)
       const float down = odd ? 1.f : __uint_as_float((254u - ex) << 23);
       q_scale = odd ? 1.f : __uint_as_float(ex << 23);
-      if (qn > 0 && !__all_sync(0xffffffffu, mbar_wait(cb + Q_EMPTY + 8 * w, (qn - 1u) & 1u, abort_flag))) return false;
+      if (qn > 0 && !wait(cb + Q_EMPTY + 8 * w, qn - 1u)) return false;
       uint8_t* line = smem + w * TILE + row * 128;
 #pragma unroll
       for (int e = 0; e < D / 8; ++e) {
@@ -504,7 +586,8 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         *reinterpret_cast<uint4*>(line + (e / 8) * PANEL + (((e & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
       }
       fence_async_smem();
-      mbar_arrive(cb + Q_FULL + 8 * w);
+      __syncwarp();
+      mbar_arrive_cluster_if(lead + Q_FULL + 8 * w, sole);
       ++qn;
       return true;
     };
@@ -512,163 +595,158 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     bool more = advance(it);
     if (PAGED && more) ok = put_q(it);
     while (more && ok) {
-      const int t = it.t0 + w * prm.tokens + tok;
+      const int t = it.t0 + mine_from;
       const bool mine = tok < prm.tokens && t < it.queries;
       const int seen = mine ? keys_seen(k, it.keys, it.queries, t) : it.keys;
       const float cc = k.scale_log2 * q_scale;
       float m = -INFINITY, l = 0.f;
-      for (int j = it.j0; j < it.j1; ++j, ++tn) {
-        if (!__all_sync(0xffffffffu, mbar_wait(cb + S_FULL + 8 * w, sn & 1u, abort_flag))) { ok = false; break; }
-        ++sn;
+      uint32_t sv[64], pv[16];
+      // half number i of the item on its way from tensor memory
+      auto fetch = [&](int i) -> bool {
+        const uint32_t h = fn & 1u, sh = s_tmem + 64 * h;
+        if (!wait(cb + S_FULL + 16 * w + 8 * h, fn >> 1)) return false;
+        ++fn;
         tc_fence_after();
-        // keys that a row does not see: -inf into S (rare, and short: the tile's own code is what the groups' time goes into)
-        const int valid = seen - j * KT;
+        // keys that a row does not see: -inf into S (rare, and short: the half's own code is what the groups' time goes into)
+        const int key0 = it.j0 * KT + 64 * i, valid = seen - key0;
         const bool masked = !PAGED && k.mask != nullptr;
-        if (masked || __any_sync(0xffffffffu, valid < KT)) {
+        if (masked || __any_sync(0xffffffffu, valid < 64)) {
 #pragma unroll 1
-          for (int i = 0; i < 4; ++i) {
-            const int v = valid - 32 * i;
+          for (int e0 = 0; e0 < 64; e0 += 32) {
+            const int v = valid - e0;
             uint32_t bits = v >= 32 ? 0xffffffffu : v <= 0 ? 0u : (1u << v) - 1u, x[32];
             if (masked) {
-              const int key = j * KT + 32 * i + lane;
+              const int key = key0 + e0 + lane;
               bits &= __ballot_sync(0xffffffffu, key < it.keys && __ldg(k.mask + it.b * k.mask_stride + key) != 0);
             }
-            tmem_ld32(s_tmem + 32 * i, x);
+            tmem_ld32(sh + e0, x);
             tc_wait_ld32(x);
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (!(bits >> e & 1u)) x[e] = 0xff800000u;
-            tmem_st32(s_tmem + 32 * i, x);
+            tmem_st32(sh + e0, x);
           }
           tc_wait_st();
         }
-        // P = 2^(S c + a - ref) of 32 keys, put where their S was, and their sum (cached keys: over V's scale).  Of eight pairs POLY's go the way of
-        // ex2_poly: the exponentials' pipe would be busy for as long as the MMAs take with all of them
-        const float4* sc = scales + (tn & (SCALE_RING - 1)) * 8;
-        uint32_t pv[16];
-        auto exps = [&](int h, const uint32_t* x, float ref) -> float {
-          float sum = 0.f;
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float4 f = PAGED ? sc[2 * h + g] : make_float4(1.f, 0.f, 1.f, 0.f);
-            const float c = PAGED ? cc * f.x : cc, nm = PAGED ? f.y - ref : -ref;
-            const uint64_t c2 = pack2(c, c), nm2 = pack2(nm, nm);
-            uint64_t sum2 = pack2(0.f, 0.f);
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-              uint64_t p2 = fma2(pack2(__uint_as_float(x[16 * g + e]), __uint_as_float(x[16 * g + e + 1])), c2, nm2);
-              float p0, p1;
-              if (POLY >> (e / 2) & 1) {
-                p2 = ex2_poly(p2);
-                unpack2(p2, p0, p1);
-              } else {
-                unpack2(p2, p0, p1);
-                p0 = ex2(p0);
-                p1 = ex2(p1);
-                p2 = pack2(p0, p1);
-              }
-              sum2 = add2(sum2, p2);
-              pv[8 * g + e / 2] = PAGED ? f16_pair(p0, p1) : pack_bf16(p0, p1);
-            }
-            float s0, s1;
-            unpack2(sum2, s0, s1);
-            sum = PAGED ? fmaf(s0 + s1, f.z, sum) : sum + (s0 + s1);
-          }
-          return sum;
-        };
-        auto maximum = [&](int h, const uint32_t* x, float mx) -> float {
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            float a = __uint_as_float(x[16 * g]), b = __uint_as_float(x[16 * g + 1]);
-#pragma unroll
-            for (int e = 2; e < 14; e += 4) {
-              a = max3_nan(a, __uint_as_float(x[16 * g + e]), __uint_as_float(x[16 * g + e + 1]));
-              b = max3_nan(b, __uint_as_float(x[16 * g + e + 2]), __uint_as_float(x[16 * g + e + 3]));
-            }
-            a = max3_nan(a, __uint_as_float(x[16 * g + 14]), __uint_as_float(x[16 * g + 15]));
-            if (PAGED) {
-              const float4 f = sc[2 * h + g];
-              mx = max_nan(mx, fmaf(max_nan(a, b), cc * f.x, f.y));
-            } else {
-              mx = max3_nan(mx, a, b);
-            }
-          }
-          return mx;
-        };
-        auto reference = [&]() -> float { return (m == -INFINITY ? 0.f : m) - UP; };
-        // Quarters of 32 keys.  The maximum of all four is taken beside the first one's exponentials (of an item's first tile: before them), which
-        // are done again where it has outgrown the reference.  The second and third are read twice for that: the whole tile would take 128 registers.
-        uint32_t x[32], y[32];
-        tmem_ld32(s_tmem, x);
-        tmem_ld32(s_tmem + 32, y);
-        tc_wait_ld32(x);
-        tc_wait_ld32(y);
-        float mx = maximum(1, y, maximum(0, x, -INFINITY)), sum = 0.f;
-        const bool first = j == it.j0;
-        tmem_ld32(s_tmem + 64, y);
-        if (!first) sum = exps(0, x, reference());
-        tc_wait_ld32(y);
-        mx = maximum(2, y, mx);
-        tmem_ld32(s_tmem + 96, y);
-        tc_wait_ld32(y);
-        mx = maximum(3, y, mx);
-        if (!PAGED) mx *= cc;
-        if (first) m = mx;
-        else if (mx != mx) l = mx;                                            // (a NaN: the row's sum, and with it the row, becomes one)
-        if (first || __any_sync(0xffffffffu, mx > m + LAZY)) {
-          // (P V of the tile before has completed: S of this one came after it)
-          if (!first) {
-            float f = 1.f;
-            if (mx > m + LAZY) {
-              f = ex2(m - mx);
-              m = mx;
-              l *= f;
-            }
+        tmem_ld32(sh, sv);
+        tmem_ld32(sh + 32, sv + 32);
+        return true;
+      };
+      const int halves = 2 * (it.j1 - it.j0);
+      if (!fetch(0)) { ok = false; break; }
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {
-              tmem_ld16(o_tmem + c, pv);
-              tc_wait_ld16(pv);
+      for (int i = 0; i < halves; ++i) {
+        const int h = i & 1;
+        const float4* sc = scales + ((tn + (uint32_t)(i >> 1)) % SCALE_RING) * 8;
+        const uint32_t sh = s_tmem + 64 * h;
+        {
+          tc_wait_ld64(sv);
+          // P = 2^(S c + a - ref) of 32 keys and their sum (cached keys: over V's scale).  Of eight pairs POLY's go the way of ex2_poly: the exponentials' pipe
+          // would be busy for as long as the MMAs take with all of them
+          auto exps = [&](int q, float ref) -> float {
+            float sum = 0.f;
 #pragma unroll
-              for (int e = 0; e < 16; ++e) pv[e] = __float_as_uint(__uint_as_float(pv[e]) * f);
-              tmem_st16(o_tmem + c, pv);
+            for (int g = 2 * q; g < 2 * q + 2; ++g) {
+              const float4 f = PAGED ? sc[4 * h + g] : make_float4(1.f, 0.f, 1.f, 0.f);
+              const float c = PAGED ? cc * f.x : cc, nm = PAGED ? f.y - ref : -ref;
+              const uint64_t c2 = pack2(c, c), nm2 = pack2(nm, nm);
+              uint64_t sum2 = pack2(0.f, 0.f);
+#pragma unroll
+              for (int e = 0; e < 16; e += 2) {
+                uint64_t p2 = fma2(pack2(__uint_as_float(sv[16 * g + e]), __uint_as_float(sv[16 * g + e + 1])), c2, nm2);
+                float p0, p1;
+                if (POLY >> (e / 2) & 1) {
+                  p2 = ex2_poly(p2);
+                  unpack2(p2, p0, p1);
+                } else {
+                  unpack2(p2, p0, p1);
+                  p0 = ex2(p0);
+                  p1 = ex2(p1);
+                  p2 = pack2(p0, p1);
+                }
+                sum2 = add2(sum2, p2);
+                pv[8 * (g - 2 * q) + e / 2] = PAGED ? f16_pair(p0, p1) : pack_bf16(p0, p1);
+              }
+              float s0, s1;
+              unpack2(sum2, s0, s1);
+              sum = PAGED ? fmaf(s0 + s1, f.z, sum) : sum + (s0 + s1);
+            }
+            return sum;
+          };
+          auto maximum = [&]() -> float {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              float a = __uint_as_float(sv[16 * g]), b = __uint_as_float(sv[16 * g + 1]);
+#pragma unroll
+              for (int e = 2; e < 14; e += 4) {
+                a = max3_nan(a, __uint_as_float(sv[16 * g + e]), __uint_as_float(sv[16 * g + e + 1]));
+                b = max3_nan(b, __uint_as_float(sv[16 * g + e + 2]), __uint_as_float(sv[16 * g + e + 3]));
+              }
+              a = max3_nan(a, __uint_as_float(sv[16 * g + 14]), __uint_as_float(sv[16 * g + 15]));
+              if (PAGED) {
+                const float4 f = sc[4 * h + g];
+                mx = max_nan(mx, fmaf(max_nan(a, b), cc * f.x, f.y));
+              } else {
+                mx = max3_nan(mx, a, b);
+              }
+            }
+            return PAGED ? mx : mx * cc;
+          };
+          auto reference = [&]() -> float { return (m == -INFINITY ? 0.f : m) - UP; };
+          const bool first = i == 0;
+          if (first) m = maximum();
+          float ref = reference(), sum = exps(0, ref);
+          if (!first) {
+            const float mx = maximum();
+            if (mx != mx) l = mx;                                             // (a NaN: the row's sum, and with it the row, becomes one)
+            if (__any_sync(0xffffffffu, mx > m + LAZY)) {
+              // (O is at rest once P V of the half before has completed)
+              if (!wait(cb + PV_DONE + 8 * w, hn - 1u)) { ok = false; break; }
+              tc_fence_after();
+              float f = 1.f;
+              if (mx > m + LAZY) {
+                f = ex2(m - mx);
+                m = mx;
+                l *= f;
+              }
+#pragma unroll 1
+              for (int c = 0; c < D; c += 16) {
+                tmem_ld16(o_tmem + c, pv);
+                tc_wait_ld16(pv);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) pv[e] = __float_as_uint(__uint_as_float(pv[e]) * f);
+                tmem_st16(o_tmem + c, pv);
+              }
+              ref = reference();
+              sum = exps(0, ref);
             }
           }
-          sum = exps(0, x, reference());
+          l += sum;
+          tmem_st16(sh, pv);
+          l += exps(1, ref);
+          tmem_st16(sh + 16, pv);
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          mbar_arrive_cluster_if(lead + P_FULL + 16 * w + 8 * h, sole);
+          ++hn;
+          if (i + 1 < halves && !fetch(i + 1)) { ok = false; break; }
         }
-        const float ref = reference();
-        tmem_st16(s_tmem, pv);
-        tmem_ld32(s_tmem + 32, x);
-        sum += exps(3, y, ref);
-        tmem_st16(s_tmem + 96, pv);
-        tc_wait_st();
-        tc_wait_ld32(x);
-        tc_fence_before();
-        mbar_arrive(cb + P_HALF + 8 * w);
-        tmem_ld32(s_tmem + 64, y);
-        sum += exps(1, x, ref);
-        tmem_st16(s_tmem + 32, pv);
-        tc_wait_ld32(y);
-        sum += exps(2, y, ref);
-        tmem_st16(s_tmem + 64, pv);
-        l += sum;
-        tc_wait_st();
-        tc_fence_before();
-        mbar_arrive(cb + P_FULL + 8 * w);
       }
+      tn += (uint32_t)(it.j1 - it.j0);
       if (!ok) break;
       // ---- epilogue; the next item's Q first, so that its S can start
       const KeysItem done = it;
-      at += gridDim.x;
+      at += pairs;
       more = advance(it);
       if (PAGED && more && !put_q(it)) { ok = false; break; }
-      if (!__all_sync(0xffffffffu, mbar_wait(cb + O_DONE + 8 * w, dn & 1u, abort_flag))) { ok = false; break; }
+      if (!wait(cb + O_DONE + 8 * w, dn)) { ok = false; break; }
       ++dn;
       tc_fence_after();
-      constexpr float UNIT = PAGED ? CODE_UNIT : 1.f;
-      const float inv = l != 0.f ? UNIT / l : 0.f;
+      const float inv = l != 0.f ? 1.f / l : 0.f;
       if (k.splits > 1) {
         const long long pr = mine ? part_row(done) : 0;
-        auto scaled = [](uint32_t x) -> uint32_t { return __float_as_uint(__uint_as_float(x) * UNIT); };
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t ov[32];
@@ -677,12 +755,13 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           if (mine) {
             float* dst = k.part_o + pr * D + c;
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(dst + e) = 
-                  make_uint4(scaled(ov[e]), scaled(ov[e + 1]), scaled(ov[e + 2]), scaled(ov[e + 3]));
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<uint4*>(dst + e) = make_uint4(ov[e], ov[e + 1], ov[e + 2], ov[e + 3]);
           }
         }
         tc_fence_before();
-        mbar_arrive(cb + O_FREE + 8 * w);
+        __syncwarp();
+        mbar_arrive_cluster_if(lead + O_FREE + 8 * w, sole);
         if (mine) k.part_ml[pr] = make_float2((m == -INFINITY ? 0.f : m) - UP, l);
       } else {
         uint8_t* dst = k.o + 2 * (mine ? out_row(done, t) : 0);
@@ -708,13 +787,16 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           }
         }
         tc_fence_before();
-        mbar_arrive(cb + O_FREE + 8 * w);
+        __syncwarp();
+        mbar_arrive_cluster_if(lead + O_FREE + 8 * w, sole);
         if (mine && k.lse) *lse_at(done, t) = l != 0.f ? ((m == -INFINITY ? 0.f : m) - UP + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
     }
+    if (PAGED && ok && qn > 0) (void)wait(cb + Q_EMPTY + 8 * w, qn - 1u);     // (as the loaders do)
   }
 
   // ---------------------------------------------------------------- tear-down
+  __syncthreads();
   if (*abort_flag) {
     // copies and MMAs still in flight land before shared memory and TMEM go away
     const long long t0 = clock64();
@@ -722,9 +804,10 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   }
   tc_fence_before();
   __syncthreads();
+  cluster_sync_all();                                                         // nothing arrives at a CTA that has gone
   if (warp == 0) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
   if (threadIdx.x == 0 && *abort_flag && prm.k.status) atomicOr(prm.k.status, SVA_DEV_TIMEOUT);
 }
@@ -741,16 +824,16 @@ static keys_encode_t keys_encode() {
   }();
   return fn;
 }
-// 4-D map of bf16, 64 channels (128 bytes, swizzled) x box of the next two dimensions; sizes and element strides of dimensions 1 to 3
-static int keys_map(CUtensorMap* map, const void* ptr, int d, const long long n[3], const long long s[3], int box1, int box2) {
+// 4-D map of bf16, box of box0 channels (64, or 32: the swizzle's span) and of the next two dimensions; sizes and element strides of dimensions 1 to 3
+static int keys_map(CUtensorMap* map, const void* ptr, int d, const long long n[3], const long long s[3], int box0, int box1, int box2) {
   const keys_encode_t enc = keys_encode();
   if (!enc) return SVA_ERR_CUDA;
   const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)n[0], (cuuint64_t)n[1], (cuuint64_t)n[2]};
   cuuint64_t strides[3];
   for (int i = 0; i < 3; ++i) strides[i] = n[i] > 1 ? 2 * (cuuint64_t)s[i] : 2 * (cuuint64_t)d;      // (a dimension of one may carry any)
-  const cuuint32_t box[4] = {64, (cuuint32_t)box1, (cuuint32_t)box2, 1}, each[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {(cuuint32_t)box0, (cuuint32_t)box1, (cuuint32_t)box2, 1}, each[4] = {1, 1, 1, 1};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? SVA_OK : SVA_ERR_CUDA;
+             box0 == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? SVA_OK : SVA_ERR_CUDA;
 }
 
 static int g_debug_keys = 0;
@@ -763,16 +846,16 @@ static int launch_tc(const KeysTcParams& prm, const CUtensorMap& tq, const CUten
   auto kern = keys_tc_kernel<D, PAGED>;
   const int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kt::Smem<D>::BYTES) == cudaSuccess; });
   if (rc) return rc;
-  const unsigned grid = prm.items < (unsigned)sms ? prm.items : (unsigned)sms;
-  return launch_dep(kern, dim3(grid), kt::THREADS, kt::Smem<D>::BYTES, st, tq, tk, tv, prm);
+  const unsigned pairs = prm.items < (unsigned)(sms / 2) ? prm.items : (unsigned)(sms / 2);
+  return launch_dep_cluster(2, kern, dim3(2 * pairs), kt::THREADS, kt::Smem<D>::BYTES, st, tq, tk, tv, prm);
 }
 
 int launch_keys_tc(const KeysParams& k, bool paged, int sms, cudaStream_t st) {
   KeysTcParams prm = {};
   prm.k = k;
   prm.tokens = 128 / k.group;
-  prm.pairs = (k.tiles + 1) / 2;
-  const long long items = (long long)k.B * k.Hk * prm.pairs * k.splits;
+  prm.quads = (k.tiles + 3) / 4;
+  const long long items = (long long)k.B * k.Hk * prm.quads * k.splits;
   if (items > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
   prm.items = (uint32_t)items;
   prm.wide = (reinterpret_cast<uintptr_t>(k.o) & 31u) == 0 && ((k.so.b | k.so.h | k.so.n) & 15) == 0;
@@ -781,12 +864,12 @@ int launch_keys_tc(const KeysParams& k, bool paged, int sms, cudaStream_t st) {
   if (!paged) {
     // (row tiles: the group's heads of each token side by side)
     const long long qn[3] = {k.Hq, k.M, k.B}, qs[3] = {k.sq.h, k.sq.n, k.sq.b};
-    int rc = keys_map(&tq, k.q, k.d, qn, qs, k.group, prm.tokens);
+    int rc = keys_map(&tq, k.q, k.d, qn, qs, 64, k.group, prm.tokens);
     const int hk = k.sk.h == 0 ? 1 : k.Hk, bk = k.sk.b == 0 ? 1 : k.B, hv = k.sv.h == 0 ? 1 : k.Hk, bv = k.sv.b == 0 ? 1 : k.B;
     prm.k_each_h = hk > 1; prm.k_each_b = bk > 1; prm.v_each_h = hv > 1; prm.v_each_b = bv > 1;
     const long long kn[3] = {k.S, hk, bk}, ks[3] = {k.sk.n, k.sk.h, k.sk.b}, vn[3] = {k.S, hv, bv}, vs[3] = {k.sv.n, k.sv.h, k.sv.b};
-    if (!rc) rc = keys_map(&tk, k.k, k.d, kn, ks, kt::KT, 1);
-    if (!rc) rc = keys_map(&tv, k.v, k.d, vn, vs, kt::KT, 1);
+    if (!rc) rc = keys_map(&tk, k.k, k.d, kn, ks, 64, kt::KT / 4, 1);
+    if (!rc) rc = keys_map(&tv, k.v, k.d, vn, vs, k.d / 2, kt::KT, 1);
     if (rc) return rc;
   }
   if (paged) return k.d == 128 ? launch_tc<128, true>(prm, tq, tk, tv, sms, st) : launch_tc<64, true>(prm, tq, tk, tv, sms, st);
