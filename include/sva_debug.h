@@ -51,7 +51,7 @@ int sva_debug_set_wait_limit(long long cycles);
  *   sva_linear_fp8: 1 few tokens, 2 single CTAs, 3 inputs split over a cluster, 4 pairs
  *   sva_quantize_rows_fp8: groups of inputs per thread (1 or 4)
  *   sva_rope, sva_kv_cache_write, sva_kv_cache_read: heads per CTA
- *   sva_cached_attn_fwd, sva_cross_attn_fwd: rows per tile (16 or 128)
+ *   sva_cached_attn_fwd, sva_cross_attn_fwd: rows per tile (8, 16 or 128)
  */
 int sva_debug_last_choice(void);
 

@@ -1,14 +1,12 @@
 // Attention of few rows over many keys (sva_cached_attn_fwd, sva_cross_attn_fwd): one token or a few per sequence.
 //
-// Bound by the keys' bytes: every key is read once per 16 rows, straight into the registers of the warp that uses it, and enters mma.sync
-// products (m16n8k16) whose 16 rows are tokens times the heads that share the keys.  A warp takes 16 keys at a time, every 8th group of its
-// CTA's range; the next group's loads are in flight while it works.  In which order the products run over channels is free, so each thread takes
-// whole 16-byte pieces of a row and the operand fragments are cut from them; P needs no shuffle, being A of the second product as it leaves the first.
-// The warps' sums meet in shared memory; ranges of a long axis (splits) meet in a second kernel.
+// Bound by the keys' bytes: every key is read once per tile of 16 rows (cached keys: 8), straight into the registers of the warp that uses it, and enters
+// mma.sync products (m16n8k16).  A row of a tile is a token times one of the heads that share the keys.  A warp takes 16 keys at a time, every 8th
+// group of its CTA's range.  In which order the products run over channels is free, so each thread takes whole 16-byte pieces of a row and the
+// operand fragments are cut from them.  The warps' sums meet in shared memory; ranges of a long axis (splits) meet in a second kernel.
 //
-// e4m3 codes are converted to fp16, exactly; Q is scaled by a power of two per row into fp16's range, P = 2^(s + log2 v_scale - m + 10) with the
-// running maximum m of what is in the exponent: weights of up to 2^10, whose products with codes of any pages add up as they are; the row sum
-// takes 1 / v_scale per group.
+// e4m3 codes are converted to fp16, exactly; Q is scaled by a power of two per row into fp16's range, P = 2^(s + log2 v_scale - m + P_UP) with a
+// reference m of what is in the exponent: weights whose products with codes of any pages add up as they are; the row sum takes 1 / v_scale per group.
 #include <cuda_fp16.h>
 
 #include "attn_keys.cuh"
@@ -17,7 +15,9 @@
 namespace sva {
 
 static constexpr int FEW_ROWS = 16, FEW_KEYS = 16, FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32;
-static constexpr float P_UP = 10.0f;               // log2 of the largest fp16 probability
+static constexpr int PAGED_ROWS = 8;
+// fp16 probabilities: log2 of one at the reference, and how far above it they may go
+static constexpr float P_UP = 10.0f, FEW_LAZY = 4.0f;
 
 __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -31,18 +31,261 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// two e4m3 codes (the low 16 bits) -> two fp16 values
-__device__ __forceinline__ uint32_t codes_f16x2(uint32_t pair) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3);
-  return (uint32_t)h.x | (uint32_t)h.y << 16;
+// four e4m3 codes -> two pairs of fp16 values
+__device__ __forceinline__ void codes_f16x4(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(codes));
+}
+// an 8 x 8 matrix of 16-bit values that lies over a warp as MMA fragments do, transposed
+__device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 
-template <int D, bool PAGED>
+// ---- cached keys: up to eight rows per tile
+// The products are taken the other way round, keys (S^T = K Q^T) and channels (O^T = V^T P^T) as the MMA's 16 rows and the queries as its 8 columns: half
+// the MMAs, accumulators and Q of 16 rows, so that two CTAs with the next group's codes in flight share an SM.  P is turned by movmatrix on its way.
+// The reference m follows the maximum lazily: only when a weight is more than FEW_LAZY powers of two above it is the group's maximum taken.
+template <int D>
+__global__ void __launch_bounds__(FEW_THREADS, 2)
+keys_paged_few_kernel(const KeysParams prm) {
+  constexpr int KSTEPS = D / 16, MT = D / 16;
+  constexpr int KP = D / 64, VB = D / 8;                                  // 16-byte pieces of a key row per thread; bytes of a value row
+  extern __shared__ float smem_f[];                                       // [warps][8][D] then [warps][8] x 2
+  const int zero = grid_dep_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  uint32_t at = blockIdx.x + (uint32_t)zero;
+  const int tile = (int)(at % (uint32_t)prm.tiles); at /= (uint32_t)prm.tiles;
+  const int split = (int)(at % (uint32_t)prm.splits); at /= (uint32_t)prm.splits;
+  const int hk = (int)(at % (uint32_t)prm.Hk), b = (int)(at / (uint32_t)prm.Hk);
+  const int keys = seq_keys(prm, b), queries = seq_queries(prm, b);
+  const int row_first = tile * PAGED_ROWS, rows = queries * prm.group;
+  if (row_first >= rows) return;
+  const int end = keys_seen(prm, keys, queries, (min(row_first + PAGED_ROWS, rows) - 1) / prm.group);
+  const int groups = (end + FEW_KEYS - 1) / FEW_KEYS;
+  const int g_lo = (int)((long long)groups * split / prm.splits), g_hi = (int)((long long)groups * (split + 1) / prm.splits);
+
+  struct Group { uint4 k[2][KP], v[4]; float ks, vs; uint32_t there; };
+  const int per_page = prm.page / FEW_KEYS;
+  const int32_t* table = prm.table + b * prm.table_stride;
+  // page id of a group; -1: named wrongly
+  auto page_of = [&](int gi, int& in_page) -> int {
+    if (gi >= g_hi) return 0;
+    const int e = gi / per_page;
+    in_page = gi - e * per_page;
+    const int id = e < prm.max_pages ? __ldg(table + e) : -1;
+    return id >= prm.pages ? -1 : id;
+  };
+  auto load = [&](int gi, int id, int in_page, Group& x) {
+    x.there = 0u;
+    if (gi >= g_hi) return;
+    if (id < 0) {
+      if (lane == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
+      return;
+    }
+    const int left = keys - gi * FEW_KEYS;
+    x.there = left >= FEW_KEYS ? 0xffffu : (1u << left) - 1u;
+    const long long head = (long long)id * prm.Hk + hk, row = head * prm.page + in_page * FEW_KEYS;
+    const uint8_t *kp = prm.k + row * D, *vp = prm.v + row * D;
+    x.ks = __ldg(prm.k_scale + head);
+    x.vs = __ldg(prm.v_scale + head);
+    // keys g and g + 8; values of keys 2c, 2c + 1, 2c + 8, 2c + 9.  Rows that are not there are not read: zeros, whatever they hold
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < KP; ++e)
+        x.k[n][e] = x.there >> (g + 8 * n) & 1u ? __ldg(reinterpret_cast<const uint4*>(kp + (g + 8 * n) * D + (e * 4 + c) * 16))
+                                                : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int key = 2 * c + (n & 1) + 8 * (n >> 1);
+      x.v[n] = make_uint4(0u, 0u, 0u, 0u);
+      if (x.there >> key & 1u) {
+        if (VB >= 16) {
+          x.v[n] = __ldg(reinterpret_cast<const uint4*>(vp + key * D + g * 16));
+        } else {
+          const uint2 u = __ldg(reinterpret_cast<const uint2*>(vp + key * D + g * 8));
+          x.v[n].x = u.x; x.v[n].y = u.y;
+        }
+      }
+    }
+  };
+  auto word = [](const uint4& u, int i) -> uint32_t { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; };
+
+  Group x, y;
+  int gi = g_lo + warp, in_page = 0;
+  {
+    const int id = page_of(gi, in_page);
+    load(gi, id, in_page, x);
+  }
+  int id = page_of(gi + FEW_WARPS, in_page);
+
+  // Q: B fragments of row g.  Channels of step s, thread c: piece (s / 4) * 4 + c of 16, from (s % 4) * 4 on.  Each row times a power of two
+  uint32_t qb[KSTEPS][2];
+  float mine_scale = prm.scale_log2;
+  {
+    const int r = min(row_first + g, rows - 1), t = r / prm.group, h = hk * prm.group + r % prm.group;
+    const uint8_t* q = prm.q + 2 * (b * prm.sq.b + h * prm.sq.h + (long long)t * prm.sq.n);
+    uint32_t top = 0u;
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) {
+      const uint2 u = __ldg(reinterpret_cast<const uint2*>(q + 2 * (((s / 4) * 4 + c) * 16 + (s % 4) * 4)));
+      qb[s][0] = u.x;
+      qb[s][1] = u.y;
+      top = max(max(top, max(u.x & 0x7fffu, u.x >> 16 & 0x7fffu)), max(u.y & 0x7fffu, u.y >> 16 & 0x7fffu));
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const uint32_t ex = top >> 7;
+    const bool odd = ex == 0u || ex > 252u;                               // (zeros; infinities, NaNs)
+    const float down = odd ? 1.f : __uint_as_float((254u - ex) << 23);
+    mine_scale *= odd ? 1.f : __uint_as_float(ex << 23);
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) qb[s][e] = pack_f16(bf16lo(qb[s][e]) * down, bf16hi(qb[s][e]) * down);
+  }
+  // my columns of S^T and O^T are rows 2c and 2c + 1: logits' scale, what they see
+  float cc[2], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  int seen[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    cc[i] = __shfl_sync(0xffffffffu, mine_scale, (2 * c + i) * 4);
+    seen[i] = keys_seen(prm, keys, queries, min(row_first + 2 * c + i, rows - 1) / prm.group);
+  }
+  const int seen_least = keys_seen(prm, keys, queries, row_first / prm.group);
+  float acc[MT][4];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
+
+  auto step = [&](int gi, const Group& x) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};                                    // (key g, rows 2c, 2c + 1), (key g + 8, the same)
+#pragma unroll
+    for (int i = 0; i < KSTEPS; ++i) {
+      uint32_t a[4];
+      codes_f16x4(word(x.k[0][i / 4], i % 4), a[0], a[2]);
+      codes_f16x4(word(x.k[1][i / 4], i % 4), a[1], a[3]);
+      mma_f16(s, a, qb[i][0], qb[i][1]);
+    }
+    const float vs = v_scale_floor(x.vs), lv = __log2f(vs), inv_vs = __frcp_rn(vs);
+    float p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = fmaf(s[e], cc[e & 1] * x.ks, lv);
+    if (x.there != 0xffffu || (gi + 1) * FEW_KEYS > seen_least) {         // (uniform in a warp)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = g + 8 * (e >> 1);
+        if (!(x.there >> key & 1u) || gi * FEW_KEYS + key >= seen[e & 1]) p[e] = -INFINITY;
+      }
+    }
+    const float t0 = fmaxf(p[0], p[2]), t1 = fmaxf(p[1], p[3]);
+    if (__any_sync(0xffffffffu, t0 > m[0] + FEW_LAZY || t1 > m[1] + FEW_LAZY)) {
+      float top[2] = {t0, t1};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+        if (top[i] > m[i]) {
+          const float down = ex2(m[i] - top[i]);                          // (0 where m was -inf)
+          m[i] = top[i];
+          l[i] *= down;
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            acc[t][i] *= down;
+            acc[t][i + 2] *= down;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = ex2(p[e] - ((m[e & 1] == -INFINITY ? 0.f : m[e & 1]) - P_UP));
+    l[0] = fmaf(p[0] + p[2], inv_vs, l[0]);
+    l[1] = fmaf(p[1] + p[3], inv_vs, l[1]);
+    const uint32_t b0 = turn8x8(pack_f16(p[0], p[1])), b1 = turn8x8(pack_f16(p[2], p[3]));
+#pragma unroll
+    for (int t = 0; t < MT; t += 2) {                                     // four channels of each of the four rows: two tiles' rows g and g + 8
+      const uint32_t w0 = word(x.v[0], t / 2), w1 = word(x.v[1], t / 2), w2 = word(x.v[2], t / 2), w3 = word(x.v[3], t / 2);
+      uint32_t a[4], d[4];
+      codes_f16x4(__byte_perm(w0, w1, 0x5140), a[0], a[1]);
+      codes_f16x4(__byte_perm(w2, w3, 0x5140), a[2], a[3]);
+      codes_f16x4(__byte_perm(w0, w1, 0x7362), d[0], d[1]);
+      codes_f16x4(__byte_perm(w2, w3, 0x7362), d[2], d[3]);
+      mma_f16(acc[t], a, b0, b1);
+      mma_f16(acc[t + 1], d, b0, b1);
+    }
+  };
+  // the group after this one is on its way while this one is used, and the page of the one after that is looked up
+  while (gi < g_hi) {
+    load(gi + FEW_WARPS, id, in_page, y);
+    id = page_of(gi + 2 * FEW_WARPS, in_page);
+    step(gi, x);
+    gi += FEW_WARPS;
+    if (gi >= g_hi) break;
+    load(gi + FEW_WARPS, id, in_page, x);
+    id = page_of(gi + 2 * FEW_WARPS, in_page);
+    step(gi, y);
+    gi += FEW_WARPS;
+  }
+
+  // ---- the warps' sums.  Of tile t, row g is channel g * D/8 + 2 t, row g + 8 the next
+  float* so = smem_f + warp * PAGED_ROWS * D;
+  float* sm = smem_f + FEW_WARPS * PAGED_ROWS * D;                        // m [warps][8], l [warps][8]
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+    if (g == 0) {
+      sm[warp * PAGED_ROWS + 2 * c + i] = m[i] == -INFINITY ? 0.f : m[i];
+      sm[(FEW_WARPS + warp) * PAGED_ROWS + 2 * c + i] = l[i];
+    }
+#pragma unroll
+    for (int t = 0; t < MT; t += 2)
+      *reinterpret_cast<float4*>(so + (2 * c + i) * D + g * (D / 8) + 2 * t) = make_float4(acc[t][i], acc[t][i + 2], acc[t + 1][i], acc[t + 1][i + 2]);
+  }
+  __syncthreads();
+  constexpr int EACH = PAGED_ROWS * D / FEW_THREADS;                      // channels per thread: 4 or 2
+  const int row = threadIdx.x / (D / EACH), ch = threadIdx.x % (D / EACH) * EACH;
+  float top = -INFINITY, total = 0.f, out[EACH];
+#pragma unroll
+  for (int w = 0; w < FEW_WARPS; ++w)
+    if (sm[(FEW_WARPS + w) * PAGED_ROWS + row] != 0.f) top = fmaxf(top, sm[w * PAGED_ROWS + row]);
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) out[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < FEW_WARPS; ++w) {
+    const float lw = sm[(FEW_WARPS + w) * PAGED_ROWS + row];
+    if (lw != 0.f) {
+      const float f = ex2(sm[w * PAGED_ROWS + row] - top);
+      total = fmaf(lw, f, total);
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) out[e] = fmaf(smem_f[(w * PAGED_ROWS + row) * D + ch + e], f, out[e]);
+    }
+  }
+  if (prm.splits > 1) {
+    const long long unit = ((long long)b * prm.Hk + hk) * prm.tiles + tile, all = (long long)prm.B * prm.Hk * prm.tiles * PAGED_ROWS;
+    const long long mine = split * all + unit * PAGED_ROWS + row;
+#pragma unroll
+    for (int e = 0; e < EACH; e += 2) *reinterpret_cast<float2*>(prm.part_o + mine * D + ch + e) = make_float2(out[e], out[e + 1]);
+    if (ch == 0) prm.part_ml[mine] = make_float2(top, total);
+    return;
+  }
+  const int r = row_first + row;
+  if (r >= rows) return;
+  const int t = r / prm.group, h = hk * prm.group + r % prm.group;
+  const float inv = total != 0.f ? 1.f / total : 0.f;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(prm.o + 2 * (b * prm.so.b + h * prm.so.h + (long long)t * prm.so.n + ch));
+#pragma unroll
+  for (int e = 0; e < EACH; e += 2) dst[e / 2] = pack_bf16(out[e] * inv, out[e + 1] * inv);
+  if (ch == 0 && prm.lse) prm.lse[((long long)b * prm.Hq + h) * prm.M + t] = total != 0.f ? (top - P_UP + log2f(total)) * 0.6931471805599453f : -INFINITY;
+}
+
+// ---- bf16 keys: sixteen rows per tile; P needs no shuffle, being A of the second product as it leaves the first
+template <int D>
 __global__ void __launch_bounds__(FEW_THREADS, 1)
 keys_few_kernel(const KeysParams prm) {
   constexpr int KSTEPS = D / 16, NT = D / 8;
   // 16-byte pieces of a row that a thread holds: of a key (4 threads per row), of a value row (8 threads per row)
-  constexpr int KP = PAGED ? D / 64 : D / 32, VB = PAGED ? D / 8 : D / 4, VP = VB >= 16 ? VB / 16 : 1;      // (VB: bytes)
+  constexpr int KP = D / 32, VP = D / 64;
   extern __shared__ float smem_f[];                                       // [warps][16][D] then [warps][16] x 2
   const int zero = grid_dep_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -68,80 +311,32 @@ keys_few_kernel(const KeysParams prm) {
     qrow[i] = prm.q + 2 * (b * prm.sq.b + h * prm.sq.h + (long long)t * prm.sq.n);
     seen[i] = keys_seen(prm, keys, queries, t);
   }
-  // Q: A fragments.  Channels of step s, thread c: codes, piece (s / 4) * 4 + c of 16 channels, from (s % 4) * 4 on; bf16, piece (s / 2) * 4 + c of 8, (s % 2) * 4
+  // Q: A fragments.  Channels of step s, thread c: piece (s / 2) * 4 + c of 8, from (s % 2) * 4 on
   uint32_t qa[KSTEPS][4];
-  float cc[2];                                                            // logits' scale
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) {
-      const int ch = PAGED ? ((s / 4) * 4 + c) * 16 + (s % 4) * 4 : ((s / 2) * 4 + c) * 8 + (s % 2) * 4;
-      const uint2 u = __ldg(reinterpret_cast<const uint2*>(qrow[i] + 2 * ch));
+      const uint2 u = __ldg(reinterpret_cast<const uint2*>(qrow[i] + 2 * (((s / 2) * 4 + c) * 8 + (s % 2) * 4)));
       qa[s][i] = u.x;
       qa[s][2 + i] = u.y;
     }
-    cc[i] = prm.scale_log2;
-    if (PAGED) {
-      uint32_t top = 0u;
-#pragma unroll
-      for (int s = 0; s < KSTEPS; ++s)
-#pragma unroll
-        for (int e = i; e < 4; e += 2) top = max(top, max(qa[s][e] & 0x7fffu, qa[s][e] >> 16 & 0x7fffu));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      // 2^-e with e the exponent of the row's largest value; 1 where there is none (zeros, infinities, NaNs)
-      const uint32_t ex = top >> 7;
-      const float down = ex == 0u || ex > 252u ? 1.f : __uint_as_float((254u - ex) << 23);
-      cc[i] *= ex == 0u || ex > 252u ? 1.f : __uint_as_float(ex << 23);
-#pragma unroll
-      for (int s = 0; s < KSTEPS; ++s)
-#pragma unroll
-        for (int e = i; e < 4; e += 2) qa[s][e] = pack_f16(bf16lo(qa[s][e]) * down, bf16hi(qa[s][e]) * down);
-    }
-  }
 
   float acc[NT][4];
 #pragma unroll
   for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
-  struct Group { uint4 k[2][KP], v[4][VP]; float ks, vs; uint32_t there; };
-  const int per_page = PAGED ? prm.page / FEW_KEYS : 1;
-  auto page_of = [&](int gi) -> int {                                     // page id of a group; -1: named wrongly
-    if (!PAGED || gi >= g_hi) return 0;
-    const int e = gi / per_page;
-    int id = e < prm.max_pages ? __ldg(prm.table + b * prm.table_stride + e) : -1;
-    return id >= prm.pages ? -1 : id;
-  };
-  auto load = [&](int gi, int id, Group& x) {
-    x.there = 0u;
-    if (gi >= g_hi) return;
+  struct Group { uint4 k[2][KP], v[4][VP]; uint32_t there; };
+  auto load = [&](int gi, Group& x) {
     const int key0 = gi * FEW_KEYS;
     x.there = keys - key0 >= FEW_KEYS ? 0xffffu : (1u << (keys - key0)) - 1u;
-    const uint8_t *kp, *vp;
-    long long ks_row, vs_row;
-    if (PAGED) {
-      if (id < 0) {
-        x.there = 0u;
-        if (lane == 0 && prm.status) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
-        return;
-      }
-      const long long head = (long long)id * prm.Hk + hk;
-      const int place = (gi - gi / per_page * per_page) * FEW_KEYS;
-      kp = prm.k + (head * prm.page + place) * D;
-      vp = prm.v + (head * prm.page + place) * D;
-      ks_row = vs_row = D;
-      x.ks = __ldg(prm.k_scale + head);
-      x.vs = __ldg(prm.v_scale + head);
-    } else {
-      kp = prm.k + 2 * (b * prm.sk.b + hk * prm.sk.h + (long long)key0 * prm.sk.n);
-      vp = prm.v + 2 * (b * prm.sv.b + hk * prm.sv.h + (long long)key0 * prm.sv.n);
-      ks_row = 2 * prm.sk.n;
-      vs_row = 2 * prm.sv.n;
-      if (prm.mask) {
-        const bool on = lane < FEW_KEYS && (x.there >> lane & 1u) && __ldg(prm.mask + b * prm.mask_stride + key0 + lane) != 0;
-        x.there = __ballot_sync(0xffffffffu, on);
-      }
+    const uint8_t *kp = prm.k + 2 * (b * prm.sk.b + hk * prm.sk.h + (long long)key0 * prm.sk.n),
+                  *vp = prm.v + 2 * (b * prm.sv.b + hk * prm.sv.h + (long long)key0 * prm.sv.n);
+    const long long ks_row = 2 * prm.sk.n, vs_row = 2 * prm.sv.n;
+    if (prm.mask) {
+      const bool on = lane < FEW_KEYS && (x.there >> lane & 1u) && __ldg(prm.mask + b * prm.mask_stride + key0 + lane) != 0;
+      x.there = __ballot_sync(0xffffffffu, on);
     }
     // keys g and g + 8; values of keys 2c, 2c + 1, 2c + 8, 2c + 9.  Rows that are not there are not read: zeros, whatever they hold
 #pragma unroll
@@ -155,17 +350,8 @@ keys_few_kernel(const KeysParams prm) {
       const int key = 2 * c + (n & 1) + 8 * (n >> 1);
       const bool on = x.there >> key & 1u;
 #pragma unroll
-      for (int e = 0; e < VP; ++e) {
-        x.v[n][e] = make_uint4(0u, 0u, 0u, 0u);
-        if (on) {
-          if (VB >= 16) {
-            x.v[n][e] = __ldg(reinterpret_cast<const uint4*>(vp + key * vs_row + (PAGED ? g * VP + e : e * 8 + g) * 16));
-          } else {
-            const uint2 u = __ldg(reinterpret_cast<const uint2*>(vp + key * vs_row + g * 8));
-            x.v[n][0].x = u.x; x.v[n][0].y = u.y;
-          }
-        }
-      }
+      for (int e = 0; e < VP; ++e)
+        x.v[n][e] = on ? __ldg(reinterpret_cast<const uint4*>(vp + key * vs_row + (e * 8 + g) * 16)) : make_uint4(0u, 0u, 0u, 0u);
     }
   };
   auto word = [](const uint4& u, int i) -> uint32_t { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; };
@@ -177,30 +363,18 @@ keys_few_kernel(const KeysParams prm) {
       s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
 #pragma unroll
       for (int i = 0; i < KSTEPS; ++i) {
-        if (PAGED) {
-          const uint32_t w = word(x.k[n][i / 4], i % 4);
-          mma_f16(s[n], qa[i], codes_f16x2(w & 0xffffu), codes_f16x2(w >> 16));
-        } else {
-          mma_bf16(s[n], qa[i], word(x.k[n][i / 2], 2 * (i % 2)), word(x.k[n][i / 2], 2 * (i % 2) + 1));
-        }
+        mma_bf16(s[n], qa[i], word(x.k[n][i / 2], 2 * (i % 2)), word(x.k[n][i / 2], 2 * (i % 2) + 1));
       }
     }
     const int key0 = gi * FEW_KEYS;
-    float inv_vs = 1.f, lv = 0.f;
-    if (PAGED) {
-      const float vs = v_scale_floor(x.vs);
-      lv = log2f(vs);
-      inv_vs = 1.f / vs;
-    }
     uint32_t p[2][2];                                                     // [n tile][row]
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float f = PAGED ? cc[i] * x.ks : cc[i];
       float y[4], top = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int key = (e >> 1) * 8 + 2 * c + (e & 1);
-        y[e] = fmaf(s[e >> 1][2 * i + (e & 1)], f, lv);
+        y[e] = s[e >> 1][2 * i + (e & 1)] * prm.scale_log2;
         if (!(x.there >> key & 1u) || key0 + key >= seen[i]) y[e] = -INFINITY;
         top = fmaxf(top, y[e]);
       }
@@ -216,66 +390,34 @@ keys_few_kernel(const KeysParams prm) {
           acc[t][2 * i + 1] *= down;
         }
       }
-      const float ref = (m[i] == -INFINITY ? 0.f : m[i]) - (PAGED ? P_UP : 0.f);
+      const float ref = m[i] == -INFINITY ? 0.f : m[i];
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         y[e] = ex2(y[e] - ref);
         sum += y[e];
       }
-      l[i] = fmaf(sum, inv_vs, l[i]);
+      l[i] += sum;
 #pragma unroll
-      for (int n = 0; n < 2; ++n) p[n][i] = PAGED ? pack_f16(y[2 * n], y[2 * n + 1]) : pack_bf16(y[2 * n], y[2 * n + 1]);
+      for (int n = 0; n < 2; ++n) p[n][i] = pack_bf16(y[2 * n], y[2 * n + 1]);
     }
     const uint32_t pa[4] = {p[0][0], p[0][1], p[1][0], p[1][1]};
 #pragma unroll
     for (int t = 0; t < NT; t += 4) {                                     // four channels of each of the four rows
-      if (PAGED) {
-        const uint32_t w0 = word(x.v[0][t / 16], t / 4 % 4), w1 = word(x.v[1][t / 16], t / 4 % 4), w2 = word(x.v[2][t / 16], t / 4 % 4),
-                       w3 = word(x.v[3][t / 16], t / 4 % 4);
-        const uint32_t a0 = __byte_perm(w0, w1, 0x5140), a1 = __byte_perm(w0, w1, 0x7362), b0 = __byte_perm(w2, w3, 0x5140),
-                       b1 = __byte_perm(w2, w3, 0x7362);
-        mma_f16(acc[t], pa, codes_f16x2(a0 & 0xffffu), codes_f16x2(b0 & 0xffffu));
-        mma_f16(acc[t + 1], pa, codes_f16x2(a0 >> 16), codes_f16x2(b0 >> 16));
-        mma_f16(acc[t + 2], pa, codes_f16x2(a1 & 0xffffu), codes_f16x2(b1 & 0xffffu));
-        mma_f16(acc[t + 3], pa, codes_f16x2(a1 >> 16), codes_f16x2(b1 >> 16));
-      } else {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {                                     // two words of two channels
-          const int piece = t / 8, i = (t / 4 % 2) * 2 + e;
-          const uint32_t w0 = word(x.v[0][piece], i), w1 = word(x.v[1][piece], i), w2 = word(x.v[2][piece], i), w3 = word(x.v[3][piece], i);
-          mma_bf16(acc[t + 2 * e], pa, __byte_perm(w0, w1, 0x5410), __byte_perm(w2, w3, 0x5410));
-          mma_bf16(acc[t + 2 * e + 1], pa, __byte_perm(w0, w1, 0x7632), __byte_perm(w2, w3, 0x7632));
-        }
+      for (int e = 0; e < 2; ++e) {                                       // two words of two channels
+        const int piece = t / 8, i = (t / 4 % 2) * 2 + e;
+        const uint32_t w0 = word(x.v[0][piece], i), w1 = word(x.v[1][piece], i), w2 = word(x.v[2][piece], i), w3 = word(x.v[3][piece], i);
+        mma_bf16(acc[t + 2 * e], pa, __byte_perm(w0, w1, 0x5410), __byte_perm(w2, w3, 0x5410));
+        mma_bf16(acc[t + 2 * e + 1], pa, __byte_perm(w0, w1, 0x7632), __byte_perm(w2, w3, 0x7632));
       }
     }
   };
 
-  {
-    // codes: the group after this one is on its way while this one is used, and the page of the one after that is looked up
-    int gi = g_lo + warp;
-    if (PAGED) {
-      Group x, y;
-      load(gi, page_of(gi), x);
-      int id = page_of(gi + FEW_WARPS);
-      while (gi < g_hi) {
-        load(gi + FEW_WARPS, id, y);
-        id = page_of(gi + 2 * FEW_WARPS);
-        step(gi, x);
-        gi += FEW_WARPS;
-        if (gi >= g_hi) break;
-        load(gi + FEW_WARPS, id, x);
-        id = page_of(gi + 2 * FEW_WARPS);
-        step(gi, y);
-        gi += FEW_WARPS;
-      }
-    } else {
-      for (; gi < g_hi; gi += FEW_WARPS) {
-        Group x;
-        load(gi, 0, x);
-        step(gi, x);
-      }
-    }
+  for (int gi = g_lo + warp; gi < g_hi; gi += FEW_WARPS) {
+    Group x;
+    load(gi, x);
+    step(gi, x);
   }
 
   // ---- the warps' sums: each thread's columns n = 2c, 2c + 1 of tile t are channels of its own order
@@ -294,7 +436,7 @@ keys_few_kernel(const KeysParams prm) {
       const int col = 2 * c + n;
 #pragma unroll
       for (int t = 0; t < NT; t += 4) {
-        const int ch = PAGED ? col * NT + t : (t / 8) * 64 + col * 8 + t % 8;
+        const int ch = (t / 8) * 64 + col * 8 + t % 8;
         *reinterpret_cast<float4*>(so + (g + 8 * i) * D + ch) =
             make_float4(acc[t][2 * i + n], acc[t + 1][2 * i + n], acc[t + 2][2 * i + n], acc[t + 3][2 * i + n]);
       }
@@ -338,21 +480,25 @@ keys_few_kernel(const KeysParams prm) {
   if (EACH == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[EACH / 2 - 2], w[EACH / 2 - 1]);
   else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
   if (ch == 0 && prm.lse)
-    prm.lse[((long long)b * prm.Hq + h) * prm.M + t] = total != 0.f ? (top - (PAGED ? P_UP : 0.f) + log2f(total)) * 0.6931471805599453f : -INFINITY;
+    prm.lse[((long long)b * prm.Hq + h) * prm.M + t] = total != 0.f ? (top + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
-// The splits' sums of a row, one warp each: [splits][rows of all][D].  Tiles have rows_per rows, of which those of `tokens` tokens are used (the kernel
-// for few rows: all, tokens that go over a tile's end among them, tokens 0); up: what the references lie below the exponents.
-template <int D>
-__global__ void __launch_bounds__(256)
+// The splits' sums of a row: [splits][rows of all][D].  WARPS warps take the splits in turn: one where there are up to
+// eight of them, the four of a CTA for more (rows are then few, and the loads' latency is what they wait for).  Tiles have rows_per rows, of
+// which those of `tokens` tokens are used (the kernels for few rows: all, tokens that go over a tile's end among them, tokens 0); up: what
+// the references lie below the exponents.
+static constexpr int JOIN_THREADS = 128;
+template <int D, int WARPS>
+__global__ void __launch_bounds__(JOIN_THREADS)
 keys_join_kernel(const KeysParams prm, int rows_per, int tokens, float up) {
   constexpr int EACH = D / 32;
+  __shared__ float sums[WARPS][D], tops[WARPS], totals[WARPS];
+  static_assert(WARPS == 1 || WARPS == JOIN_THREADS / 32, "a row's warps meet at the CTA's barrier");
   const int zero = grid_dep_wait();
-  const int lane = threadIdx.x & 31;
+  const int warp = (threadIdx.x >> 5) % WARPS, lane = threadIdx.x & 31;
   const long long per_head = (long long)prm.tiles * rows_per, all = (long long)prm.B * prm.Hk * per_head;
-  const long long mine = (long long)blockIdx.x * 8 + (threadIdx.x >> 5) + zero;
+  const long long mine = (long long)blockIdx.x * (JOIN_THREADS / 32 / WARPS) + (threadIdx.x >> 5) / WARPS + zero, unit = mine / per_head;
   if (mine >= all) return;
-  const long long unit = mine / per_head;
   long long r = mine % per_head;
   const int hk = (int)(unit % prm.Hk), b = (int)(unit / prm.Hk);
   if (tokens) {
@@ -364,21 +510,45 @@ keys_join_kernel(const KeysParams prm, int rows_per, int tokens, float up) {
   float top = -INFINITY, total = 0.f, out[EACH];
 #pragma unroll
   for (int e = 0; e < EACH; ++e) out[e] = 0.f;
-  for (int s = lane; s < prm.splits; s += 32) {
+  // (with a running reference: a split's sums are read while the next one's are on their way)
+#pragma unroll 4
+  for (int s = warp; s < prm.splits; s += WARPS) {
     const float2 ml = prm.part_ml[s * all + mine];
-    if (ml.y != 0.f) top = fmaxf(top, ml.x);
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  for (int s = 0; s < prm.splits; ++s) {
-    const float2 ml = prm.part_ml[s * all + mine];
-    if (ml.y == 0.f) continue;
-    const float f = ex2(ml.x - top);
-    total = fmaf(ml.y, f, total);
     const float* x = prm.part_o + (s * all + mine) * D + lane * EACH;
+    float v[EACH];
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) out[e] = fmaf(x[e], f, out[e]);
+    for (int e = 0; e < EACH; e += 2) {
+      const float2 u = *reinterpret_cast<const float2*>(x + e);
+      v[e] = u.x;
+      v[e + 1] = u.y;
+    }
+    if (ml.y != 0.f) {                                                    // (uniform; of an empty split nothing is written)
+      const float now = fmaxf(top, ml.x), f = ex2(ml.x - now), old = ex2(top - now);
+      top = now;
+      total = fmaf(total, old, ml.y * f);
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) out[e] = fmaf(out[e], old, v[e] * f);
+    }
   }
+  if (WARPS > 1) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) sums[warp][lane * EACH + e] = out[e];
+    if (lane == 0) {
+      tops[warp] = top;
+      totals[warp] = total;
+    }
+    __syncthreads();
+    if (warp != 0) return;
+  }
+#pragma unroll
+  for (int w = 1; w < WARPS; ++w)
+    if (totals[w] != 0.f) {
+      const float now = fmaxf(top, tops[w]), f = ex2(tops[w] - now), old = ex2(top - now);
+      top = now;
+      total = fmaf(total, old, totals[w] * f);
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) out[e] = fmaf(out[e], old, sums[w][lane * EACH + e] * f);
+    }
   const int t = (int)(r / prm.group), h = hk * prm.group + (int)(r % prm.group);
   const float inv = total != 0.f ? 1.f / total : 0.f;
   uint32_t* dst = reinterpret_cast<uint32_t*>(prm.o + 2 * (b * prm.so.b + h * prm.so.h + (long long)t * prm.so.n + lane * EACH));
@@ -387,25 +557,24 @@ keys_join_kernel(const KeysParams prm, int rows_per, int tokens, float up) {
   if (lane == 0 && prm.lse) prm.lse[((long long)b * prm.Hq + h) * prm.M + t] = total != 0.f ? (top - up + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
-static constexpr size_t few_smem(int d) { return (size_t)FEW_WARPS * FEW_ROWS * (d + 2) * 4; }
-
 template <int D>
 static int launch_join(const KeysParams& prm, int rows_per, int tokens, float up, cudaStream_t st) {
   const long long rows = (long long)prm.B * prm.Hk * prm.tiles * rows_per;
-  return launch_dep(keys_join_kernel<D>, dim3((unsigned)((rows + 7) / 8)), 256, 0, st, prm, rows_per, tokens, up);
+  if (prm.splits <= 8) return launch_dep(keys_join_kernel<D, 1>, dim3((unsigned)((rows + 3) / 4)), JOIN_THREADS, 0, st, prm, rows_per, tokens, up);
+  return launch_dep(keys_join_kernel<D, 4>, dim3((unsigned)rows), JOIN_THREADS, 0, st, prm, rows_per, tokens, up);
 }
 
 template <int D, bool PAGED>
 static int launch_few(const KeysParams& prm, cudaStream_t st) {
   static DeviceOnce once;
-  auto kern = keys_few_kernel<D, PAGED>;
-  int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_smem(D)) == cudaSuccess; });
+  constexpr int ROWS = PAGED ? PAGED_ROWS : FEW_ROWS, SMEM = FEW_WARPS * ROWS * (D + 2) * 4;
+  auto kern = PAGED ? keys_paged_few_kernel<D> : keys_few_kernel<D>;
+  int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) == cudaSuccess; });
   if (rc) return rc;
-  const long long units = (long long)prm.B * prm.Hk * prm.tiles;
-  if (units * prm.splits > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
-  rc = launch_dep(kern, dim3((unsigned)(units * prm.splits)), FEW_THREADS, few_smem(D), st, prm);
-  if (rc || prm.splits == 1) return rc;
-  return launch_join<D>(prm, FEW_ROWS, 0, PAGED ? P_UP : 0.f, st);
+  const long long ctas = (long long)prm.B * prm.Hk * prm.tiles * prm.splits;
+  if (ctas > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
+  rc = launch_dep(kern, dim3((unsigned)ctas), FEW_THREADS, SMEM, st, prm);
+  return rc || prm.splits == 1 ? rc : launch_join<D>(prm, ROWS, 0, PAGED ? P_UP : 0.f, st);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- plan, workspace
@@ -429,33 +598,34 @@ static int device_sms() {
   sms[dev].store(n, std::memory_order_relaxed);
   return n;
 }
-static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d, bool maps) {
+static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d, bool paged, bool maps) {
   KeysPlan k = {};
   k.sms = device_sms();
   const long long rows = (long long)M * group;
-  k.tc = maps && group <= 128 && rows > 32;
+  k.tc = maps && group <= 128 && rows > (paged ? 2 * PAGED_ROWS : 2 * FEW_ROWS);
   k.tokens = k.tc ? 128 / group : 0;
-  const int per = k.tc ? 128 : FEW_ROWS;
+  const int per = k.tc ? 128 : paged ? PAGED_ROWS : FEW_ROWS;
   k.tiles = k.tc ? (M + k.tokens - 1) / k.tokens : (rows + per - 1) / per;
   k.units = (long long)B * Hk * k.tiles;
   k.all = k.units * per;
   if (k.tc) {
-    // The number of splits for which the pairs of SMs are done first: rounds of items, each as long as its key tiles and some 2 tiles more, and for more
-    // than one split the partial sums: 512 KB of HBM traffic per item, 3 / 74 of the 2 us that a pair takes for a tile.  At least four key tiles per split.
+    // The number of splits for which the pairs of SMs are done first: a pair's share of the items and one more, for the last round and for items of
+    // unequal length, each as long as its key tiles and some 2 tiles more; and for more than one split the partial sums: 512 KB of HBM traffic per item, 3 / 74 of the 2 us that a pair takes for a tile.  At least four key tiles per split.
     // (24 heads x 4 680 queries x 32 760 keys, 240 items for 74 pairs: 2 418 us in one split, 2 179 in four.)
     const long long items = (long long)B * Hk * ((k.tiles + 3) / 4), pairs = k.sms / 2 > 0 ? k.sms / 2 : 1, tiles = (S + 127) / 128;
     double best = 0.0;
     k.splits = 1;
     for (int n = 1; n <= 64 && (n == 1 || tiles / n >= 4); ++n) {
-      const double rounds = (double)((items * n + pairs - 1) / pairs);
-      const double time = rounds * ((double)((tiles + n - 1) / n) + 2.0) + (n > 1 ? 3.0 + 3.0 * n * (double)items / (double)pairs : 0.0);
-      if (n == 1 || time < 0.97 * best) {
+      const double share = (double)(items * n) / (double)pairs, rounds = share <= 1.0 ? 1.0 : share + 1.0;
+      const double time = rounds * ((double)((tiles + n - 1) / n) + 2.0) + (n > 1 ? 3.0 + 3.0 * d / 128 * n * (double)items / (double)pairs : 0.0);
+      if (n == 1 || time < best) {
         best = time;
         k.splits = n;
       }
     }
   } else {
-    // at least 256 keys per split, CTAs for four rounds
+    // at least 256 keys per split; CTAs for four rounds, with cached keys (two per SM) two.  (Two sequences of 65 536 tokens / eight of up to 131 071, 8 key
+    // heads, us: 1 184 CTAs 100 / 372, 592: 86 / 376, 296: 78 / 486.)
     long long splits = k.units > 0 ? k.sms * 4 / k.units : 1;
     if (splits > S / 256) splits = S / 256;
     k.splits = (int)(splits < 1 ? 1 : splits);
@@ -467,14 +637,14 @@ static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d, b
   return k;
 }
 static KeysPlan cached_plan(const sva_kv_cache_t* c, const sva_cached_attn_t* p) {
-  return keys_plan(p->B, c->H, p->Hq / c->H, p->M, (long long)p->max_pages * c->page, c->d, true);
+  return keys_plan(p->B, c->H, p->Hq / c->H, p->M, (long long)p->max_pages * c->page, c->d, true, true);
 }
 // (tensor maps know no stride of 0 along tokens, none of 0 along Q's heads and items, and strides below 2^40 bytes)
 static KeysPlan cross_plan(const sva_cross_attn_t* p) {
   auto fits = [](const int64_t s[3]) { return s[0] < (1LL << 38) && s[1] < (1LL << 38) && s[2] < (1LL << 38); };
   const bool maps = p->S > 0 && (p->N == 1 || p->q_stride[2] > 0) && (p->Hq == 1 || p->q_stride[1] > 0) && (p->B == 1 || p->q_stride[0] > 0) &&
                     (p->S == 1 || (p->k_stride[2] > 0 && p->v_stride[2] > 0)) && fits(p->q_stride) && fits(p->k_stride) && fits(p->v_stride);
-  return keys_plan(p->B, p->Hk, p->Hq / p->Hk, p->N, p->S, p->d, maps);
+  return keys_plan(p->B, p->Hk, p->Hq / p->Hk, p->N, p->S, p->d, false, maps);
 }
 
 size_t cached_attn_workspace_bytes(const sva_kv_cache_t* c, const sva_cached_attn_t* p) { return cached_plan(c, p).total; }
@@ -486,7 +656,7 @@ static int launch_keys(KeysParams& prm, bool paged, const KeysPlan& plan, void* 
   prm.splits = plan.splits;
   prm.part_o = static_cast<float*>(ws);
   prm.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + plan.o_bytes);
-  note_choice(plan.tc ? 128 : FEW_ROWS);
+  note_choice(plan.tc ? 128 : paged ? PAGED_ROWS : FEW_ROWS);
   if (plan.tc) {
     const int rc = launch_keys_tc(prm, paged, plan.sms, st);
     if (rc || prm.splits == 1) return rc;

@@ -89,11 +89,14 @@ __device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// Two codes (the low 16 bits) as fp16 values.  (By way of shifts and masks it would take eight operations for four codes on a pipe of half the rate: 25 codes
+// Eight codes as fp16 values.  (By way of shifts and masks it would take eight operations for four codes on a pipe of half the rate: 25 codes
 // per cycle and SM, this 57.)
-__device__ __forceinline__ uint32_t f16_of_codes(uint32_t pair) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(pair & 0xffffu), __NV_E4M3);
-  return (uint32_t)h.x | (uint32_t)h.y << 16;
+__device__ __forceinline__ uint4 f16_of_codes(uint32_t x, uint32_t y) {
+  uint4 r;
+  asm("{\n\t.reg .b16 a, b, c, d;\n\tmov.b32 {a, b}, %4;\n\tmov.b32 {c, d}, %5;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\tcvt.rn.f16x2.e4m3x2 %2, c;\n\tcvt.rn.f16x2.e4m3x2 %3, d;\n\t}"
+      : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(x), "r"(y));
+  return r;
 }
 
 // Bounded wait of a warp, as mbar_wait, but suspended until the phase completes (or for as long as the hardware likes) where it polls: a
@@ -452,8 +455,8 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         int key, byte, to0, to1;
         unit_of(u, key, byte, to0, to1);
         uint8_t* stage = smem + (u < KU ? OFF_K : OFF_V) + s * HALF;
-        *reinterpret_cast<uint4*>(stage + to0) = make_uint4(f16_of_codes(r.x), f16_of_codes(r.x >> 16), f16_of_codes(r.y), f16_of_codes(r.y >> 16));
-        *reinterpret_cast<uint4*>(stage + to1) = make_uint4(f16_of_codes(r.z), f16_of_codes(r.z >> 16), f16_of_codes(r.w), f16_of_codes(r.w >> 16));
+        *reinterpret_cast<uint4*>(stage + to0) = f16_of_codes(r.x, r.y);
+        *reinterpret_cast<uint4*>(stage + to1) = f16_of_codes(r.z, r.w);
       };
       uint4 r[EACH];                                                              // one tile ahead, its pages looked up another tile ahead
       float ks = 1.f, vs = 1.f;
