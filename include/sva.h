@@ -583,7 +583,8 @@ int sva_cross_attn_fwd(const sva_cross_attn_t* p, const void* q, const void* k, 
  *         the child gets a copy of its own (taken in the order of i), entries behind are -1, lengths equal.  Children hold nothing before (free them
  *         first), come once, and are no parents of the call.  Where the pool runs out the child keeps the full pages alone, and their length.
  * free    the pages of row rows[i] from entry ceil(keep[i] / page) on are given back (refs - 1, entry -1); lengths[rows[i]] = min(itself, keep[i]).
- *         keep NULL: everything.  A page whose refs is 0 already is reported.
+ *         keep NULL: everything.  A page whose refs is 0 already is reported.  A page that is kept in part stays shared if it was: what is appended to it
+ *         later would change it for all of its sequences, so that such a row is given a copy first (copy, and the entry changed).
  * compact the L pages with refs > 0 move to the ids below L: the i-th lowest page from L on to the i-th lowest free id below L.  refs and page_table (all
  *         rows) follow; *live = L (optional).  workspace: >= sva_kv_pages_compact_workspace_bytes, 16-byte aligned.
  * n and rows may be 0.  Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (more than 2^20 pages of a row), WORKSPACE.

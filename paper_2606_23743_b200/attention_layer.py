@@ -4,6 +4,8 @@ attention, in the order in which a denoising loop makes them.
     x -> e4m3 codes -> QKV product -> rotary positions -> K, V into the quantised cache -> K, V of the whole clip read back
       -> routing and block-sparse attention -> e4m3 codes -> output product + residual
 
+ChunkAttentionLayer is such a layer for clips that are generated in chunks, CrossAttentionLayer attends to a prompt's states.
+
 A call gets the tokens that are computed in this step, all of them or a subset (token pruning): the others keep the K and V that an
 earlier call wrote.  Weights are quantised once, when the layer is made.  Batch items share the weights and the grid.
 """
@@ -124,3 +126,105 @@ class AttentionLayer:
         sva.block_select(p, self.select, self.q, self.k, row_ptr, col_idx, ws)
         aws = torch.empty(max(256, sva.attn_one_call_workspace_bytes(p)), dtype=torch.uint8, device=dev)
         sva.block_sparse_attn_fwd(p, self.q, self.k, self.v, row_ptr, col_idx, self.o, None, self.status, workspace=aws)
+
+
+class ChunkAttentionLayer:
+    """The same for a clip that is generated in chunks, or a sequence that grows token by token: the tokens of a call attend to one another (causal: to
+    those before them) and to all tokens that their sequence has had, whose K and V lie in a cache with a scale per page and head and are read
+    where they lie.
+
+        x -> e4m3 codes -> QKV product -> rotary positions -> pages taken -> K, V appended -> attention over the cache -> output product + residual
+
+    w_qkv [(heads + 2 kv_heads) d, C] (Q rows, K rows, V rows, head by head), w_out [C, heads d]; room for `rows` sequences of up to `tokens`
+    tokens in a pool of `pages` pages that they share.  The layer's state (refs, table, lengths) is on the device: no call waits for it."""
+
+    def __init__(self, w_qkv, w_out, heads: int, tokens: int, rows: int = 1, kv_heads: int = 0, bias_qkv=None, bias_out=None, page: int = 64,
+                 pages: int = 0, causal: bool = False, rope_base: float = 10000.0, status=None):
+        dev = w_qkv.device
+        self.Hq, self.H, self.B, self.causal = heads, kv_heads or heads, rows, causal
+        self.d = w_qkv.shape[0] // (heads + 2 * self.H)
+        self.qkv, self.out = _Linear8(w_qkv, bias_qkv), _Linear8(w_out, bias_out)
+        self.status = status if status is not None else torch.zeros(1, dtype=torch.int32, device=dev)
+        self.steps, _ = sva.rope_steps(self.d, [self.d // 2], rope_base, device=dev)
+        per = -(-tokens // page)
+        pages = pages or rows * per
+        self.cache = sva.make_kv_cache(*([torch.zeros(pages, self.H, page, self.d, dtype=torch.uint8, device=dev), torch.zeros(pages, self.H, device=dev)]
+                                         for _ in range(2)), format="e4m3_page")
+        self.refs = torch.zeros(pages, dtype=torch.int32, device=dev)
+        self.table = torch.full((rows, per), -1, dtype=torch.int32, device=dev)
+        self.lengths = torch.zeros(rows, dtype=torch.int32, device=dev)
+        self.work = torch.empty(sva.kv_pages_compact_workspace_bytes(self.cache), dtype=torch.uint8, device=dev)
+
+    def __call__(self, x, counts=None):
+        """x [rows, M, C] bf16, of each sequence's next counts [rows] tokens (int32; None: M): x + attention's projection, for them.  Rows of x behind
+        its count mean nothing, nor do those of the result."""
+        B, M, C = x.shape
+        Hq, H, d = self.Hq, self.H, self.d
+        assert B == self.B, "x holds tokens of every sequence"
+        if M == 0:
+            return torch.empty_like(x)
+        x = x.reshape(B * M, C)
+        if counts is None:
+            counts = torch.full((B,), M, dtype=torch.int32, device=x.device)
+        qkv = self.qkv(x, torch.empty(B * M, (Hq + 2 * H) * d, dtype=torch.bfloat16, device=x.device), self.status).view(B, M, Hq + 2 * H, d).transpose(1, 2)
+        q, k, v = qkv.split((Hq, H, H), 1)
+        positions = (self.lengths[:, None] + torch.arange(M, dtype=torch.int32, device=x.device))[None].contiguous()
+        sva.rope(sva.make_rope(q, k, q, k, positions, d), q, k, self.steps, positions, q, k)
+        sva.kv_pages_take(self.cache, self.refs, self.table, self.lengths, counts, self.status)
+        sva.kv_cache_append(self.cache, k, v, self.table, self.lengths, counts, self.status)
+        self.lengths += counts
+        o = torch.zeros(B, M, Hq, d, dtype=torch.bfloat16, device=x.device).transpose(1, 2)
+        p = sva.make_cached_attn(self.cache, q, o, self.table, self.causal)
+        space = torch.empty(max(256, sva.cached_attn_workspace_bytes(p)), dtype=torch.uint8, device=x.device)
+        sva.cached_attn_fwd(p, q, self.table, self.lengths, o, counts, None, self.status, space)
+        o = o.transpose(1, 2).reshape(B * M, Hq * d)
+        return self.out(o, torch.empty(B * M, C, dtype=torch.bfloat16, device=x.device), self.status, residual=x).view(B, M, C)
+
+    def fork(self, parents, children):
+        """Sequences children (int32) give up what they hold and go on from where sequences parents are, whose full pages they share."""
+        sva.kv_pages_free(self.cache, self.refs, self.table, self.lengths, children, status=self.status)
+        sva.kv_pages_fork(self.cache, self.refs, self.table, self.lengths, parents, children, self.status)
+
+    def forget(self, which, keep=None):
+        """Sequences `which` (int32) forget their tokens from keep (int32; None: 0) on.  A sequence whose last page is shared may not be cut within it:
+        what it appends there its relatives would see."""
+        sva.kv_pages_free(self.cache, self.refs, self.table, self.lengths, which, keep, self.status)
+
+    def compact(self):
+        """Moves the pages in use to the front of the pool."""
+        sva.kv_pages_compact(self.cache, self.refs, self.table, self.work, status=self.status)
+
+
+class CrossAttentionLayer:
+    """Attention of a clip's tokens to an encoder's states (a prompt's), with its projections.  w_q [heads d, C], w_kv [2 kv_heads d, E] (K rows, V rows),
+    w_out [C, heads d].  K and V of a prompt are the same in every denoising step: states() makes them once."""
+
+    def __init__(self, w_q, w_kv, w_out, heads: int, kv_heads: int = 0, bias_q=None, bias_kv=None, bias_out=None, status=None):
+        self.Hq, self.H, self.d = heads, kv_heads or heads, w_q.shape[0] // heads
+        self.q, self.kv, self.out = _Linear8(w_q, bias_q), _Linear8(w_kv, bias_kv), _Linear8(w_out, bias_out)
+        self.status = status if status is not None else torch.zeros(1, dtype=torch.int32, device=w_q.device)
+
+    def states(self, encoded):
+        """encoded [B, S, E] bf16 -> K, V [B, kv_heads, S, d]."""
+        B, S, E = encoded.shape
+        kv = torch.empty(B * S, 2 * self.H * self.d, dtype=torch.bfloat16, device=encoded.device)
+        if S:
+            self.kv(encoded.reshape(B * S, E), kv, self.status)
+        kv = kv.view(B, S, 2, self.H, self.d)
+        return kv[:, :, 0].transpose(1, 2), kv[:, :, 1].transpose(1, 2)
+
+    def __call__(self, x, states, lengths=None, key_mask=None):
+        """x [B, M, C] bf16: x + the projection of its attention to the states, of which the first lengths [B] (int32) and those that key_mask [B, S] does not
+        leave out are there."""
+        B, M, C = x.shape
+        if M == 0:
+            return torch.empty_like(x)
+        k, v = states
+        x = x.reshape(B * M, C)
+        q = self.q(x, torch.empty(B * M, self.Hq * self.d, dtype=torch.bfloat16, device=x.device), self.status).view(B, M, self.Hq, self.d).transpose(1, 2)
+        o = torch.empty(B, M, self.Hq, self.d, dtype=torch.bfloat16, device=x.device).transpose(1, 2)
+        p = sva.make_cross_attn(q, k, v, o)
+        space = torch.empty(max(256, sva.cross_attn_workspace_bytes(p)), dtype=torch.uint8, device=x.device)
+        sva.cross_attn_fwd(p, q, k, v, o, lengths, key_mask, None, self.status, space)
+        o = o.transpose(1, 2).reshape(B * M, self.Hq * self.d)
+        return self.out(o, torch.empty(B * M, C, dtype=torch.bfloat16, device=x.device), self.status, residual=x).view(B, M, C)

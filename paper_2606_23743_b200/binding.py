@@ -70,19 +70,21 @@ class KvCache(C.Structure):
     _fields_ = [("H", C.c_int32), ("d", C.c_int32), ("page", C.c_int32), ("pages", C.c_int32), ("format", C.c_int32),
                 ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("k_sf", C.c_void_p), ("v_sf", C.c_void_p)]
-    arrays, on_gpu = None, False                           # the tensors behind the pointers, and where they are (make_kv_cache)
+    arrays, on_gpu, heads = None, False, None              # the tensors behind the pointers, where they are, and (H, d) (make_kv_cache)
 
 
 class CachedAttn(C.Structure):
     _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("M", C.c_int32), ("max_pages", C.c_int32), ("causal", C.c_int32), ("softmax_scale", C.c_float),
                 ("table_stride", C.c_int64), ("q_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
-    cache = None                                           # the cache that it was made for (make_cached_attn)
+    # the cache that it was made for, q's shape, q's, o's and the table's strides (make_cached_attn)
+    cache = shape = strides = table = None
 
 
 class CrossAttn(C.Structure):
     _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hk", C.c_int32), ("N", C.c_int32), ("S", C.c_int32), ("d", C.c_int32),
                 ("softmax_scale", C.c_float), ("mask_stride", C.c_int64), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
                 ("v_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
+    shapes = strides = None                                # of q, k, v, o (make_cross_attn)
 
 
 class SvaError(RuntimeError):
@@ -239,11 +241,8 @@ def _strides(t):
 
 def _strides_any(t):
     """The same for a tensor that may hold nothing (torch gives such a one any strides)."""
-    return _strides(t) if t.numel() else _stride_array((0, 0, 0, 1))
-
-
-def _has_strides(t, s):
-    return not t.numel() or tuple(t.stride()) == (*s, 1)
+    s = t.stride()
+    return _stride_array(s) if s[3] == 1 or t.numel() else _stride_array((0, 0, 0, 1))
 
 
 def make_problem(q, k, v, o, N: int, block: int, scale: float = 0.0, fp8: bool = False) -> Problem:
@@ -651,7 +650,7 @@ def make_kv_cache(k, v, format: str = "e4m3") -> KvCache:
     c.k_codes, c.v_codes, c.k_scale, c.v_scale = _ptr(k[0]), _ptr(v[0]), _ptr(k[1]), _ptr(v[1])
     if format == "fp4":
         c.k_sf, c.v_sf = _ptr(k[2]), _ptr(v[2])
-    c.arrays, c.on_gpu = (tuple(k), tuple(v)), all(t.is_cuda for t in (*k, *v))
+    c.arrays, c.on_gpu, c.heads = (tuple(k), tuple(v)), all(t.is_cuda for t in (*k, *v)), (c.H, c.d)
     return c
 
 
@@ -689,13 +688,15 @@ def _table(page_table, rows):
     """Row stride and entries per row of a page table."""
     n, most = page_table.shape
     stride, inner = page_table.stride()
-    assert n == rows and page_table.dtype is torch.int32 and (inner == 1 or most == 1), "page_table is [rows,pages] int32"
+    assert n == rows and page_table.dtype is _I32 and (inner == 1 or most == 1), "page_table is [rows,pages] int32"
     return stride, most
 
 
+_I32, _BF16 = torch.int32, torch.bfloat16
+
+
 def _int32s(t, n, what):
-    assert t.dim() == 1 and t.shape[0] == n and t.dtype is torch.int32 and t.is_contiguous(), f"{what} are {n} int32, side by side"
-    assert t.is_cuda, _NOT_ON_GPU
+    assert t.shape == (n,) and t.dtype is _I32 and t.is_contiguous() and t.is_cuda, f"{what} are {n} int32, side by side, on the GPU"
     return t.data_ptr()
 
 
@@ -703,7 +704,7 @@ def kv_cache_append(c: KvCache, k, v, page_table, lengths, counts=None, status=N
     """k, v [B,H,T,d] bf16 behind the lengths [B] tokens that the sequences hold in their pages (the first counts [B] of each; None: all T).
     The cache's format is e4m3_page; `lengths` stays as it is."""
     shape = Bq, H, T, d = k.shape
-    assert H == c.H and d == c.d and v.shape == shape and k.dtype is v.dtype is torch.bfloat16, "k, v are [B,H,T,d] bf16"
+    assert (H, d) == c.heads and v.shape == shape and k.dtype is v.dtype is _BF16, "k, v are [B,H,T,d] bf16"
     stride, most = _table(page_table, Bq)
     assert c.on_gpu and k.is_cuda and v.is_cuda and page_table.is_cuda and (status is None or status.is_cuda), _NOT_ON_GPU
     rc = (_lib or lib()).sva_kv_cache_append(c, k.data_ptr(), v.data_ptr(), _strides_any(k), _strides_any(v), Bq, T, page_table.data_ptr(), stride, most,
@@ -717,19 +718,13 @@ def make_cached_attn(c: KvCache, q, o, page_table, causal: bool = False, scale: 
     """Attention of q [B,Hq,M,d] over the cache (Hq a multiple of its heads), into o; page_table [B,pages] int32."""
     p = CachedAttn()
     p.B, p.Hq, p.M, d = q.shape
-    assert d == c.d and p.Hq % c.H == 0, "q is [B,Hq,M,d] with the cache's d and a multiple of its heads"
+    assert d == c.d and p.Hq % c.H == 0 and o.shape == q.shape and q.dtype is o.dtype is _BF16, \
+        "q, o are [B,Hq,M,d] bf16 with the cache's d and a multiple of its heads"
     p.table_stride, p.max_pages = _table(page_table, p.B)
     p.causal, p.softmax_scale, p.cache = int(causal), scale, c
-    _check_attn(p, q, page_table, o)
     p.q_stride, p.o_stride = _strides_any(q), _strides_any(o)
+    p.shape, p.strides, p.table = q.shape, (q.stride(), o.stride()), (page_table.shape, page_table.stride())
     return p
-
-
-def _check_attn(p, q, page_table, o):
-    shape = q.shape
-    assert shape == o.shape and q.dtype is o.dtype is torch.bfloat16 and shape[:3] == (p.B, p.Hq, p.M) and shape[3] == p.cache.d, \
-        "q, o are bf16 and of the sizes that the plan was made for"
-    assert page_table.shape == (p.B, p.max_pages) and page_table.dtype is torch.int32, "page_table is the plan's [B,pages] int32"
 
 
 def cached_attn_workspace_bytes(p: CachedAttn) -> int:
@@ -738,15 +733,16 @@ def cached_attn_workspace_bytes(p: CachedAttn) -> int:
 
 def cached_attn_fwd(p: CachedAttn, q, page_table, lengths, o, counts=None, lse=None, status=None, workspace=None) -> None:
     """o = attention of each sequence's counts [B] queries (None: all M) over its lengths [B] cached tokens; lse [B,Hq,M] fp32."""
-    _check_attn(p, q, page_table, o)
-    assert _has_strides(q, p.q_stride) and _has_strides(o, p.o_stride), "q, o have the plan's strides"
-    assert page_table.stride(0) == p.table_stride or p.B == 1, "page_table has the plan's strides"
-    assert lse is None or lse.shape == (p.B, p.Hq, p.M) and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,M] fp32"
+    assert q.shape == p.shape == o.shape and q.dtype is o.dtype is _BF16 and (q.stride(), o.stride()) == p.strides, \
+        "q, o are bf16 and of the sizes and strides that the plan was made for"
+    assert (page_table.shape, page_table.stride()) == p.table and page_table.dtype is _I32, "page_table is int32 and of the plan's sizes and strides"
+    assert lse is None or lse.shape == p.shape[:3] and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,M] fp32"
     assert p.cache.on_gpu and q.is_cuda and o.is_cuda and page_table.is_cuda and (status is None or status.is_cuda) and \
         (workspace is None or workspace.is_cuda), _NOT_ON_GPU
-    rc = (_lib or lib()).sva_cached_attn_fwd(p.cache, p, q.data_ptr(), page_table.data_ptr(), _int32s(lengths, p.B, "lengths"),
-                                             None if counts is None else _int32s(counts, p.B, "counts"), o.data_ptr(), _ptr(lse), _ptr(status),
-                                             _ptr(workspace), _ws_bytes(workspace), _stream())
+    rc = (_lib or lib()).sva_cached_attn_fwd(p.cache, p, q.data_ptr(), page_table.data_ptr(), _int32s(lengths, p.shape[0], "lengths"),
+                                             None if counts is None else _int32s(counts, p.shape[0], "counts"), o.data_ptr(),
+                                             None if lse is None else lse.data_ptr(), None if status is None else status.data_ptr(),
+                                             None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream())
     if rc:
         raise SvaError(rc, "sva_cached_attn_fwd")
 
@@ -761,6 +757,7 @@ def make_cross_attn(q, k, v, o, scale: float = 0.0) -> CrossAttn:
     assert q.dtype is k.dtype is v.dtype is o.dtype is torch.bfloat16, "q, k, v, o are bf16"
     p.softmax_scale = scale
     p.q_stride, p.k_stride, p.v_stride, p.o_stride = _strides_any(q), _strides_any(k), _strides_any(v), _strides_any(o)
+    p.shapes, p.strides = (q.shape, k.shape), (q.stride(), k.stride(), v.stride(), o.stride())
     return p
 
 
@@ -770,21 +767,20 @@ def cross_attn_workspace_bytes(p: CrossAttn) -> int:
 
 def cross_attn_fwd(p: CrossAttn, q, k, v, o, lengths=None, key_mask=None, lse=None, status=None, workspace=None) -> None:
     """o = attention over the first lengths [B] keys (None: all S) that key_mask [B,S] (bool or bytes, None: all) does not leave out."""
-    assert q.shape == o.shape == (p.B, p.Hq, p.N, p.d) and k.shape == v.shape == (p.B, p.Hk, p.S, p.d) and \
-        q.dtype is k.dtype is v.dtype is o.dtype is torch.bfloat16, "q, k, v, o are bf16 and of the sizes that the plan was made for"
-    assert _has_strides(q, p.q_stride) and _has_strides(k, p.k_stride) and _has_strides(v, p.v_stride) and _has_strides(o, p.o_stride), \
-        "q, k, v, o have the plan's strides"
-    mask_stride = 0
+    of_q, of_k = p.shapes
+    assert q.shape == of_q == o.shape and k.shape == of_k == v.shape and q.dtype is k.dtype is v.dtype is o.dtype is _BF16 and \
+        (q.stride(), k.stride(), v.stride(), o.stride()) == p.strides, "q, k, v, o are bf16 and of the sizes and strides that the plan was made for"
     if key_mask is not None:
-        assert key_mask.shape == (p.B, p.S) and key_mask.element_size() == 1 and (p.S <= 1 or key_mask.stride(1) == 1) and key_mask.is_cuda, \
+        assert key_mask.shape == (of_k[0], of_k[2]) and key_mask.element_size() == 1 and (of_k[2] <= 1 or key_mask.stride(1) == 1) and key_mask.is_cuda, \
             "key_mask is [B,S] bytes on the GPU"
-        mask_stride = key_mask.stride(0)
-    p.mask_stride = mask_stride
-    assert lse is None or lse.shape == (p.B, p.Hq, p.N) and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,N] fp32"
+        p.mask_stride = key_mask.stride(0)
+    assert lse is None or lse.shape == of_q[:3] and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,N] fp32"
     assert q.is_cuda and k.is_cuda and v.is_cuda and o.is_cuda and (status is None or status.is_cuda) and (workspace is None or workspace.is_cuda), \
         "tensors are on the GPU"
-    rc = (_lib or lib()).sva_cross_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lengths is None else _int32s(lengths, p.B, "lengths"),
-                                            _ptr(key_mask), o.data_ptr(), _ptr(lse), _ptr(status), _ptr(workspace), _ws_bytes(workspace), _stream())
+    rc = (_lib or lib()).sva_cross_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lengths is None else _int32s(lengths, of_q[0], "lengths"),
+                                            None if key_mask is None else key_mask.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(),
+                                            None if status is None else status.data_ptr(), None if workspace is None else workspace.data_ptr(),
+                                            0 if workspace is None else workspace.nbytes, _stream())
     if rc:
         raise SvaError(rc, "sva_cross_attn_fwd")
 

@@ -120,28 +120,33 @@ __global__ void __launch_bounds__(PLAN_THREADS) pages_take_kernel(const PoolPara
   }
 }
 
-// One array's page, or a slice of it: whole pieces of 16 bytes, or of 4.
-template <typename Piece>
-__device__ __forceinline__ void copy_pieces(uint8_t* base, long long bytes, int src, int dst, int part, int parts) {
-  const Piece* from = reinterpret_cast<const Piece*>(base + src * bytes);
-  Piece* to = reinterpret_cast<Piece*>(base + dst * bytes);
-  const long long pieces = bytes / (long long)sizeof(Piece);
-  const long long lo = pieces * part / parts, hi = pieces * (part + 1) / parts;
-  long long i = lo + threadIdx.x;
-  for (; i + 3 * MOVE_THREADS < hi; i += 4 * MOVE_THREADS) {
-    Piece x[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = from[i + e * MOVE_THREADS];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) to[i + e * MOVE_THREADS] = x[e];
-  }
-  for (; i < hi; i += MOVE_THREADS) to[i] = from[i];
+// A slice of a page: of the codes a step of 32 KB or less, all of whose loads are in flight before the first store; with the first slice go the scales.
+// 24 heads of 64 tokens x 128, 507 pages moved: 88.7 us with slices of 16 KB of K and then of V, four loads in flight; now see below.
+static constexpr int COPY_EACH = 8;                          // 16-byte pieces per thread and step
+__device__ __forceinline__ void copy_words(uint8_t* base, long long bytes, int src, int dst) {
+  const uint32_t* from = reinterpret_cast<const uint32_t*>(base + src * bytes);
+  uint32_t* to = reinterpret_cast<uint32_t*>(base + dst * bytes);
+  for (long long i = threadIdx.x; i < bytes / 4; i += MOVE_THREADS) to[i] = from[i];
 }
+// parts: of K and V together (even ones K's)
 __device__ __forceinline__ void copy_page(const PoolParams& prm, int src, int dst, int part, int parts) {
-  for (int tensor = 0; tensor < 2; ++tensor) {
-    copy_pieces<uint4>(prm.arrays[3 * tensor], prm.bytes[0], src, dst, part, parts);
-    copy_pieces<uint32_t>(prm.arrays[3 * tensor + 1], prm.bytes[1], src, dst, part, parts);
-    if (prm.bytes[2]) copy_pieces<uint32_t>(prm.arrays[3 * tensor + 2], prm.bytes[2], src, dst, part, parts);
+  const int tensor = part & 1, mine = part >> 1, of = parts >> 1;
+  uint8_t* base = prm.arrays[3 * tensor];
+  const uint4* from = reinterpret_cast<const uint4*>(base + src * prm.bytes[0]);
+  uint4* to = reinterpret_cast<uint4*>(base + dst * prm.bytes[0]);
+  const long long pieces = prm.bytes[0] / 16, lo = pieces * mine / of, hi = pieces * (mine + 1) / of;
+  for (long long i = lo + threadIdx.x; i < hi; i += COPY_EACH * MOVE_THREADS) {
+    uint4 x[COPY_EACH];
+#pragma unroll
+    for (int e = 0; e < COPY_EACH; ++e)
+      if (i + e * MOVE_THREADS < hi) x[e] = from[i + e * MOVE_THREADS];
+#pragma unroll
+    for (int e = 0; e < COPY_EACH; ++e)
+      if (i + e * MOVE_THREADS < hi) to[i + e * MOVE_THREADS] = x[e];
+  }
+  if (mine == 0) {
+    copy_words(prm.arrays[3 * tensor + 1], prm.bytes[1], src, dst);
+    if (prm.bytes[2]) copy_words(prm.arrays[3 * tensor + 2], prm.bytes[2], src, dst);
   }
 }
 __device__ __forceinline__ bool page_named(const PoolParams& prm, int id) { return id >= 0 && id < prm.pages; }
@@ -353,17 +358,19 @@ static PoolParams pool_params(const sva_kv_cache_t* c) {
   prm.page = c->page;
   return prm;
 }
-// slices of a page: 16 KB of each of K's and V's codes, one step of copy_pieces
-static int page_parts(const PoolParams& prm) {
-  const long long parts = (prm.bytes[0] + 16383) / 16384;
-  return (int)(parts < 1 ? 1 : parts > 1024 ? 1024 : parts);
+// slices of a page, half of them K's: as many as make few calls fill the device, down to 4 KB, and none larger than a step
+static int page_parts(const PoolParams& prm, long long pages) {
+  long long least = (prm.bytes[0] + COPY_EACH * MOVE_THREADS * 16 - 1) / (COPY_EACH * MOVE_THREADS * 16), most = (prm.bytes[0] + 4095) / 4096;
+  long long of = pages > 0 ? 148 * 4 / pages : 1;
+  of = of < least ? least : of > most ? most : of;
+  return 2 * (int)(of < 1 ? 1 : of > 1024 ? 1024 : of);
 }
 static unsigned grid_rows(int n) { return (unsigned)(n < 65535 ? n : 65535); }
 
 int launch_pages_copy(const sva_kv_cache_t* c, const int32_t* src, const int32_t* dst, int n, int32_t* status, cudaStream_t st) {
   PoolParams prm = pool_params(c);
   prm.from = src; prm.to = dst; prm.n = n; prm.status = status;
-  return launch_dep(pages_copy_kernel, dim3((unsigned)page_parts(prm), grid_rows(n)), MOVE_THREADS, 0, st, prm);
+  return launch_dep(pages_copy_kernel, dim3((unsigned)page_parts(prm, n), grid_rows(n)), MOVE_THREADS, 0, st, prm);
 }
 
 static PoolParams table_params(const sva_kv_cache_t* c, int32_t* refs, int32_t* table, int64_t stride, int rows, int max_pages, int32_t* status) {
@@ -384,7 +391,7 @@ int launch_pages_fork(const sva_kv_cache_t* c, int32_t* refs, int32_t* table, in
   PoolParams prm = table_params(c, refs, table, stride, rows, max_pages, status);
   prm.lengths = lengths; prm.from = parents; prm.to = children; prm.n = n;
   const int rc = launch_dep(pages_fork_plan_kernel, 1, PLAN_THREADS, 0, st, prm);
-  return rc ? rc : launch_dep(pages_fork_kernel, dim3((unsigned)page_parts(prm) + 1, grid_rows(n)), MOVE_THREADS, 0, st, prm);
+  return rc ? rc : launch_dep(pages_fork_kernel, dim3((unsigned)page_parts(prm, n) + 1, grid_rows(n)), MOVE_THREADS, 0, st, prm);
 }
 
 int launch_pages_free(const sva_kv_cache_t* c, int32_t* refs, int32_t* table, int64_t stride, int rows, int max_pages, int32_t* lengths,
@@ -400,7 +407,7 @@ int launch_pages_compact(const sva_kv_cache_t* c, int32_t* refs, int32_t* table,
                          int32_t* status, void* ws, cudaStream_t st) {
   PoolParams prm = table_params(c, refs, table, stride, rows, max_pages, status);
   const int rc = launch_dep(pages_compact_plan_kernel, 1, PLAN_THREADS, 0, st, prm, ws, live);
-  return rc ? rc : launch_dep(pages_compact_kernel, 148 * 8, MOVE_THREADS, 0, st, prm, ws, page_parts(prm));
+  return rc ? rc : launch_dep(pages_compact_kernel, 148 * 4, MOVE_THREADS, 0, st, prm, ws, page_parts(prm, c->pages));
 }
 
 }  // namespace sva

@@ -1,0 +1,103 @@
+"""The layers that run the operators over keys of their own together, against their definitions in 64 bits: a clip in chunks and then token by token,
+forked, cut back and compacted on the way; a clip's tokens over a prompt's states."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import keys as K
+from oracle import layer as L
+from paper_2606_23743_b200.attention_layer import ChunkAttentionLayer, CrossAttentionLayer
+
+pytestmark = pytest.mark.gpu
+
+
+def _f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def _bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).float().to(torch.bfloat16).float().numpy().astype(np.float64)
+
+
+def _linear(x, w, bias):
+    return L.linear(*L.quantize_rows(x), *L.quantize_tiles(_f64(w)), None if bias is None else _f64(bias))[0]
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _close(got, want):
+    """Attention itself is held to less elsewhere; a value that is half a per cent off now and then takes the next e4m3 code, a step of 6 % (1.5 % in
+    the 2-norm), in Q and K, in V, and before the last product."""
+    off = np.linalg.norm(got - want) / np.linalg.norm(want)
+    assert off < 3e-2, off
+
+
+@pytest.mark.parametrize("Hq,H,d,causal", [(2, 2, 128, False), (6, 2, 64, True)])
+def test_a_clip_in_chunks(Hq, H, d, causal):
+    rng = np.random.default_rng(d)
+    bf = lambda *s: torch.from_numpy(rng.standard_normal(s)).to(torch.bfloat16).cuda()                  # noqa: E731
+    C, rows, page = 200, 3, 16
+    w_qkv, w_out = bf((Hq + 2 * H) * d, C) / np.sqrt(C), bf(C, Hq * d) / np.sqrt(Hq * d)
+    b_qkv = torch.from_numpy(0.1 * rng.standard_normal((Hq + 2 * H) * d)).float().cuda()
+    layer = ChunkAttentionLayer(w_qkv, w_out, Hq, 300, rows, H, b_qkv, page=page, pages=50, causal=causal)
+    theta = L.frequencies([d // 2])
+    # each sequence's own pages: codes and scales of K and V
+    blank = lambda: [(np.zeros((20, H, page, d), np.uint8), np.zeros((20, H))) for _ in range(2)]           # noqa: E731
+    held, lengths, own = [blank() for _ in range(rows)], [0] * rows, [list(range(20))]
+
+    def call(M, counts=None):
+        x = bf(rows, M, C)
+        cnt = counts or [M] * rows
+        got = _f64(layer(x, None if counts is None else _i32(counts))) - _f64(x)
+        assert int(layer.status) == 0
+        qkv = _bf16(_linear(_f64(x).reshape(-1, C), w_qkv, b_qkv)).reshape(rows, M, Hq + 2 * H, d).transpose(0, 2, 1, 3)
+        pos = [np.array(lengths)[:, None] + np.arange(M)]
+        q, k = (_bf16(L.rope(t, theta, pos, [d // 2], d, "interleaved")) for t in (qkv[:, :Hq], qkv[:, Hq:Hq + H]))
+        v = qkv[:, Hq + H:]
+        for b in range(rows):
+            o = np.zeros((cnt[b], Hq, d))
+            for arrays, t in zip(held[b], (k, v)):
+                K.append(*arrays, t[b:b + 1], own, [lengths[b]], [cnt[b]], page)
+            lengths[b] += cnt[b]
+            n = lengths[b]
+            kk, vv = (K.gathered(*arrays, own[0], n, page) for arrays in held[b])
+            there = np.arange(n)[None] <= n - cnt[b] + np.arange(cnt[b])[:, None] if causal else np.ones((cnt[b], n), bool)
+            for h in range(Hq):
+                o[:, h] = K.attention(q[b, h, :cnt[b]], kk[h * H // Hq], vv[h * H // Hq], there, d ** -0.5)[0]
+            _close(got[b, :cnt[b]], _linear(_bf16(o.reshape(-1, Hq * d)), w_out, None))
+
+    call(130)
+    call(37, [37, 1, 20])
+    call(1)
+    layer.fork(_i32([0]), _i32([2]))
+    held[2], lengths[2] = [tuple(a.copy() for a in arrays) for arrays in held[0]], lengths[0]
+    call(1)                                                                    # the two go on by themselves
+    layer.forget(_i32([1]), _i32([129]))
+    lengths[1] = 129
+    layer.compact()
+    assert layer.lengths.tolist() == lengths and int(layer.refs.sum()) == int((layer.table >= 0).sum())
+    assert int((layer.refs > 0).sum()) == int(layer.refs.nonzero().max()) + 1
+    call(20, [3, 20, 7])
+
+
+@pytest.mark.parametrize("Hq,H,d,M,masked", [(2, 2, 128, 333, False), (4, 2, 64, 3, True)])
+def test_a_clip_and_its_prompt(Hq, H, d, M, masked):
+    rng = np.random.default_rng(M)
+    bf = lambda *s: torch.from_numpy(rng.standard_normal(s)).to(torch.bfloat16).cuda()                  # noqa: E731
+    Bq, C, E, S = 2, 136, 72, 77
+    w_q, w_kv, w_out = bf(Hq * d, C) / np.sqrt(C), bf(2 * H * d, E) / np.sqrt(E), bf(C, Hq * d) / np.sqrt(Hq * d)
+    layer = CrossAttentionLayer(w_q, w_kv, w_out, Hq, H)
+    encoded, x = bf(Bq, S, E), bf(Bq, M, C)
+    there = rng.random((Bq, S)) < 0.4 if masked else np.arange(S)[None] < np.array([[77], [12]])
+    states = layer.states(encoded)
+    got = layer(x, states, *((None, torch.from_numpy(there).cuda()) if masked else (_i32([77, 12]),)))
+    assert int(layer.status) == 0
+    kv = _bf16(_linear(_f64(encoded).reshape(-1, E), w_kv, None)).reshape(Bq, S, 2, H, d)
+    q = _bf16(_linear(_f64(x).reshape(-1, C), w_q, None)).reshape(Bq, M, Hq, d)
+    o = np.zeros((Bq, M, Hq, d))
+    for b in range(Bq):
+        for h in range(Hq):
+            o[b, :, h] = K.attention(q[b, :, h], kv[b, :, 0, h * H // Hq], kv[b, :, 1, h * H // Hq], there[b], d ** -0.5)[0]
+    _close(_f64(got) - _f64(x), _linear(_bf16(o.reshape(-1, Hq * d)), w_out, None).reshape(Bq, M, C))
