@@ -1,8 +1,8 @@
 // Attention of few rows over many keys (sva_cached_attn_fwd, sva_cross_attn_fwd): one token or a few per sequence.
 //
 // Bound by the keys' bytes: every key is read once per tile of 16 rows (cached keys: 8), straight into the registers of the warp that uses it, and enters
-// mma.sync products (m16n8k16).  A row of a tile is a token times one of the heads that share the keys.  A warp takes 16 keys at a time, every 8th
-// group of its CTA's range.  In which order the products run over channels is free, so each thread takes whole 16-byte pieces of a row and the
+// mma.sync products (m16n8k16).  A row of a tile is a token times one of the heads that share the keys.  A warp takes 16 keys at a time, in turn with
+// the others of its CTA.  In which order the products run over channels is free, so each thread takes whole 16-byte pieces of a row and the
 // operand fragments are cut from them.  The warps' sums meet in shared memory; ranges of a long axis (splits) meet in a second kernel.
 //
 // e4m3 codes are converted to fp16, exactly; Q is scaled by a power of two per row into fp16's range, P = 2^(s + log2 v_scale - m + P_UP) with a
@@ -15,7 +15,7 @@
 namespace sva {
 
 static constexpr int FEW_ROWS = 16, FEW_KEYS = 16, FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32;
-static constexpr int PAGED_ROWS = 8;
+static constexpr int PAGED_ROWS = 8, PAGED_WARPS = 4, PAGED_CTAS = 3;      // (CTAs per SM)
 // fp16 probabilities: log2 of one at the reference, and how far above it they may go
 static constexpr float P_UP = 10.0f, FEW_LAZY = 4.0f;
 
@@ -44,10 +44,12 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
 
 // ---- cached keys: up to eight rows per tile
 // The products are taken the other way round, keys (S^T = K Q^T) and channels (O^T = V^T P^T) as the MMA's 16 rows and the queries as its 8 columns: half
-// the MMAs, accumulators and Q of 16 rows, so that two CTAs with the next group's codes in flight share an SM.  P is turned by movmatrix on its way.
+// the MMAs, accumulators and Q of 16 rows, so that twelve warps with the next group's codes in flight share an SM.  P is turned by movmatrix on its way.
 // The reference m follows the maximum lazily: only when a weight is more than FEW_LAZY powers of two above it is the group's maximum taken.
+// Eight sequences of up to 131 071 tokens, 8 key heads of 128, four query heads each: 320 us = 5.0 TB/s; with 16 rows per tile, eight warps per SM and
+// the maximum in every group 653.  What is left is latency: a group is on its way for as long as the group before it is worked on.
 template <int D>
-__global__ void __launch_bounds__(FEW_THREADS, 2)
+__global__ void __launch_bounds__(PAGED_WARPS * 32, PAGED_CTAS)
 keys_paged_few_kernel(const KeysParams prm) {
   constexpr int KSTEPS = D / 16, MT = D / 16;
   constexpr int KP = D / 64, VB = D / 8;                                  // 16-byte pieces of a key row per thread; bytes of a value row
@@ -118,7 +120,7 @@ keys_paged_few_kernel(const KeysParams prm) {
     const int id = page_of(gi, in_page);
     load(gi, id, in_page, x);
   }
-  int id = page_of(gi + FEW_WARPS, in_page);
+  int id = page_of(gi + PAGED_WARPS, in_page);
 
   // Q: B fragments of row g.  Channels of step s, thread c: piece (s / 4) * 4 + c of 16, from (s % 4) * 4 on.  Each row times a power of two
   uint32_t qb[KSTEPS][2];
@@ -159,6 +161,7 @@ keys_paged_few_kernel(const KeysParams prm) {
   for (int t = 0; t < MT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
 
   auto step = [&](int gi, const Group& x) {
+    if (x.there == 0u) return;                                            // (a page that is named wrongly: nothing was read)
     float s[4] = {0.f, 0.f, 0.f, 0.f};                                    // (key g, rows 2c, 2c + 1), (key g + 8, the same)
 #pragma unroll
     for (int i = 0; i < KSTEPS; ++i) {
@@ -216,44 +219,44 @@ keys_paged_few_kernel(const KeysParams prm) {
   };
   // the group after this one is on its way while this one is used, and the page of the one after that is looked up
   while (gi < g_hi) {
-    load(gi + FEW_WARPS, id, in_page, y);
-    id = page_of(gi + 2 * FEW_WARPS, in_page);
+    load(gi + PAGED_WARPS, id, in_page, y);
+    id = page_of(gi + 2 * PAGED_WARPS, in_page);
     step(gi, x);
-    gi += FEW_WARPS;
+    gi += PAGED_WARPS;
     if (gi >= g_hi) break;
-    load(gi + FEW_WARPS, id, in_page, x);
-    id = page_of(gi + 2 * FEW_WARPS, in_page);
+    load(gi + PAGED_WARPS, id, in_page, x);
+    id = page_of(gi + 2 * PAGED_WARPS, in_page);
     step(gi, y);
-    gi += FEW_WARPS;
+    gi += PAGED_WARPS;
   }
 
   // ---- the warps' sums.  Of tile t, row g is channel g * D/8 + 2 t, row g + 8 the next
   float* so = smem_f + warp * PAGED_ROWS * D;
-  float* sm = smem_f + FEW_WARPS * PAGED_ROWS * D;                        // m [warps][8], l [warps][8]
+  float* sm = smem_f + PAGED_WARPS * PAGED_ROWS * D;                        // m [warps][8], l [warps][8]
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
     if (g == 0) {
       sm[warp * PAGED_ROWS + 2 * c + i] = m[i] == -INFINITY ? 0.f : m[i];
-      sm[(FEW_WARPS + warp) * PAGED_ROWS + 2 * c + i] = l[i];
+      sm[(PAGED_WARPS + warp) * PAGED_ROWS + 2 * c + i] = l[i];
     }
 #pragma unroll
     for (int t = 0; t < MT; t += 2)
       *reinterpret_cast<float4*>(so + (2 * c + i) * D + g * (D / 8) + 2 * t) = make_float4(acc[t][i], acc[t][i + 2], acc[t + 1][i], acc[t + 1][i + 2]);
   }
   __syncthreads();
-  constexpr int EACH = PAGED_ROWS * D / FEW_THREADS;                      // channels per thread: 4 or 2
+  constexpr int EACH = PAGED_ROWS * D / (PAGED_WARPS * 32);                      // channels per thread: 4 or 2
   const int row = threadIdx.x / (D / EACH), ch = threadIdx.x % (D / EACH) * EACH;
   float top = -INFINITY, total = 0.f, out[EACH];
 #pragma unroll
-  for (int w = 0; w < FEW_WARPS; ++w)
-    if (sm[(FEW_WARPS + w) * PAGED_ROWS + row] != 0.f) top = fmaxf(top, sm[w * PAGED_ROWS + row]);
+  for (int w = 0; w < PAGED_WARPS; ++w)
+    if (sm[(PAGED_WARPS + w) * PAGED_ROWS + row] != 0.f) top = fmaxf(top, sm[w * PAGED_ROWS + row]);
 #pragma unroll
   for (int e = 0; e < EACH; ++e) out[e] = 0.f;
 #pragma unroll
-  for (int w = 0; w < FEW_WARPS; ++w) {
-    const float lw = sm[(FEW_WARPS + w) * PAGED_ROWS + row];
+  for (int w = 0; w < PAGED_WARPS; ++w) {
+    const float lw = sm[(PAGED_WARPS + w) * PAGED_ROWS + row];
     if (lw != 0.f) {
       const float f = ex2(sm[w * PAGED_ROWS + row] - top);
       total = fmaf(lw, f, total);
@@ -567,13 +570,13 @@ static int launch_join(const KeysParams& prm, int rows_per, int tokens, float up
 template <int D, bool PAGED>
 static int launch_few(const KeysParams& prm, cudaStream_t st) {
   static DeviceOnce once;
-  constexpr int ROWS = PAGED ? PAGED_ROWS : FEW_ROWS, SMEM = FEW_WARPS * ROWS * (D + 2) * 4;
+  constexpr int ROWS = PAGED ? PAGED_ROWS : FEW_ROWS, WARPS = PAGED ? PAGED_WARPS : FEW_WARPS, SMEM = WARPS * ROWS * (D + 2) * 4;
   auto kern = PAGED ? keys_paged_few_kernel<D> : keys_few_kernel<D>;
   int rc = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) == cudaSuccess; });
   if (rc) return rc;
   const long long ctas = (long long)prm.B * prm.Hk * prm.tiles * prm.splits;
   if (ctas > 0x7fffffffLL) return SVA_ERR_UNSUPPORTED;
-  rc = launch_dep(kern, dim3((unsigned)ctas), FEW_THREADS, SMEM, st, prm);
+  rc = launch_dep(kern, dim3((unsigned)ctas), WARPS * 32, SMEM, st, prm);
   return rc || prm.splits == 1 ? rc : launch_join<D>(prm, ROWS, 0, PAGED ? P_UP : 0.f, st);
 }
 
@@ -624,9 +627,9 @@ static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d, b
       }
     }
   } else {
-    // at least 256 keys per split; CTAs for four rounds, with cached keys (two per SM) two.  (Two sequences of 65 536 tokens / eight of up to 131 071, 8 key
-    // heads, us: 1 184 CTAs 100 / 372, 592: 86 / 376, 296: 78 / 486.)
-    long long splits = k.units > 0 ? k.sms * 4 / k.units : 1;
+    // at least 256 keys per split; CTAs for four rounds, with cached keys (three per SM) two.  (Two sequences of 65 536 tokens / eight of up to 131 071, 8 key
+    // heads, us: 6 CTAs' worth per SM 78 / 320, 7: 94 / 348, 9: 87 / 322, 12: 98 / 312; CTAs of eight warps, two per SM, 4: 86 / 376, 8: 100 / 372.)
+    long long splits = k.units > 0 ? k.sms * (paged ? 2 * PAGED_CTAS : 4) / k.units : 1;
     if (splits > S / 256) splits = S / 256;
     k.splits = (int)(splits < 1 ? 1 : splits);
   }
