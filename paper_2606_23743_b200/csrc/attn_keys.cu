@@ -513,24 +513,36 @@ keys_join_kernel(const KeysParams prm, int rows_per, int tokens, float up) {
   float top = -INFINITY, total = 0.f, out[EACH];
 #pragma unroll
   for (int e = 0; e < EACH; ++e) out[e] = 0.f;
-  // (with a running reference: a split's sums are read while the next one's are on their way)
-#pragma unroll 4
-  for (int s = warp; s < prm.splits; s += WARPS) {
-    const float2 ml = prm.part_ml[s * all + mine];
-    const float* x = prm.part_o + (s * all + mine) * D + lane * EACH;
-    float v[EACH];
+  // 32 of the warp's splits at a time: each lane has the reference and the row sum of one, so that the loop's loads wait for nothing
+#pragma unroll 1
+  for (int base = warp; base < prm.splits; base += 32 * WARPS) {
+    const int s = base + lane * WARPS;
+    const float2 ml = s < prm.splits ? prm.part_ml[s * all + mine] : make_float2(0.f, 0.f);
+    float now = ml.y != 0.f ? ml.x : -INFINITY;
 #pragma unroll
-    for (int e = 0; e < EACH; e += 2) {
-      const float2 u = *reinterpret_cast<const float2*>(x + e);
-      v[e] = u.x;
-      v[e + 1] = u.y;
-    }
-    if (ml.y != 0.f) {                                                    // (uniform; of an empty split nothing is written)
-      const float now = fmaxf(top, ml.x), f = ex2(ml.x - now), old = ex2(top - now);
-      top = now;
-      total = fmaf(total, old, ml.y * f);
+    for (int o = 16; o; o >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, o));
+    now = fmaxf(now, top);
+    if (now == -INFINITY) continue;                                       // (nothing but empty splits so far)
+    const float old = ex2(top - now), factor = ml.y != 0.f ? ex2(ml.x - now) : 0.f;
+    float part = ml.y != 0.f ? ml.y * factor : 0.f;
 #pragma unroll
-      for (int e = 0; e < EACH; ++e) out[e] = fmaf(out[e], old, v[e] * f);
+    for (int o = 16; o; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+    top = now;
+    total = fmaf(total, old, part);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) out[e] *= old;
+    const uint32_t there = __ballot_sync(0xffffffffu, ml.y != 0.f);      // (of an empty split nothing is written)
+    const float* x = prm.part_o + (base * all + mine) * D + lane * EACH;
+    const int n = min(32, (prm.splits - base + WARPS - 1) / WARPS);
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      const float f = __shfl_sync(0xffffffffu, factor, i);
+#pragma unroll
+      for (int e = 0; e < EACH; e += 2) {
+        const float2 u = there >> i & 1u ? *reinterpret_cast<const float2*>(x + (long long)i * WARPS * all * D + e) : make_float2(0.f, 0.f);
+        out[e] = fmaf(u.x, f, out[e]);
+        out[e + 1] = fmaf(u.y, f, out[e + 1]);
+      }
     }
   }
   if (WARPS > 1) {
