@@ -39,10 +39,10 @@ constexpr float LAZY = 7.0f;
 constexpr int POLY = 0b01000100;                      // pairs of eight whose exponentials are polynomials
 constexpr float UP_F16 = 8.0f;                        // log2 of a probability at the reference (fp16: 2^15 at most)
 constexpr int CONVERTERS = 7;                         // warps (cached keys)
-// shared memory (bytes from a 1024-byte boundary): Q tiles | K stages | V stages | control
+// shared memory (bytes from a 1024-byte boundary): Q tiles | K stages | V stages | control | 2 KB per softmax warp on O's way out
 template <int D> struct Smem {
   static constexpr int TILE = D / 64 * PANEL, HALF = TILE / 2;      // of Q; of K or V, a CTA's half of a key tile
-  static constexpr int K = 2 * TILE, V = K + STAGES * HALF, CTRL = V + STAGES * HALF, BYTES = CTRL + 2048 + 1024;
+  static constexpr int K = 2 * TILE, V = K + STAGES * HALF, CTRL = V + STAGES * HALF, OUT = CTRL + 2048, BYTES = OUT + 8 * 2048 + 1024;
 };
 // control block: barriers (8 bytes each), then TMEM base and abort flag, then the scales' ring
 enum { K_FULL = 0, K_EMPTY = 32, V_LAND = 64, V_FULL = 96, V_EMPTY = 128, Q_FULL = 160, Q_EMPTY = 176, S_FULL = 192, P_FULL = 224, PV_DONE = 256,
@@ -565,28 +565,28 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     auto put_q = [&](const KeysItem& x) -> bool {
       const int t = x.t0 + mine_from;
       const bool there = tok < prm.tokens && t < x.queries;
-      uint32_t q[D / 2];
-      const uint8_t* src = k.q + 2 * (x.b * k.sq.b + (long long)(x.hk * k.group + head) * k.sq.h + (long long)t * k.sq.n);
+      const uint4* src = reinterpret_cast<const uint4*>(k.q + 2 * (x.b * k.sq.b + (long long)(x.hk * k.group + head) * k.sq.h + (long long)t * k.sq.n));
+      auto piece = [&](int e) -> uint4 { return there ? __ldg(src + e) : make_uint4(0u, 0u, 0u, 0u); };
       uint32_t top = 0u;
-#pragma unroll
+#pragma unroll 4
       for (int e = 0; e < D / 8; ++e) {
-        const uint4 u = there ? __ldg(reinterpret_cast<const uint4*>(src) + e) : make_uint4(0u, 0u, 0u, 0u);
-        q[4 * e] = u.x; q[4 * e + 1] = u.y; q[4 * e + 2] = u.z; q[4 * e + 3] = u.w;
+        const uint4 u = piece(e);
+        const uint32_t a = max(max(u.x & 0x7fff7fffu, u.x << 16 & 0x7fffffffu), max(u.y & 0x7fff7fffu, u.y << 16 & 0x7fffffffu)),
+                       c = max(max(u.z & 0x7fff7fffu, u.z << 16 & 0x7fffffffu), max(u.w & 0x7fff7fffu, u.w << 16 & 0x7fffffffu));
+        top = max(top, max(a, c));
       }
-#pragma unroll
-      for (int e = 0; e < D / 2; ++e) top = max(top, max(q[e] & 0x7fffu, q[e] >> 16 & 0x7fffu));
-      const uint32_t ex = top >> 7;
+      const uint32_t ex = top >> 23;
       const bool odd = ex == 0u || ex > 252u;                                 // (zeros; infinities, NaNs)
       const float down = odd ? 1.f : __uint_as_float((254u - ex) << 23);
       q_scale = odd ? 1.f : __uint_as_float(ex << 23);
       if (qn > 0 && !wait(cb + Q_EMPTY + 8 * w, qn - 1u)) return false;
       uint8_t* line = smem + w * TILE + row * 128;
-#pragma unroll
+#pragma unroll 2
       for (int e = 0; e < D / 8; ++e) {
-        uint32_t h[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = f16_pair(bf16lo(q[4 * e + i]) * down, bf16hi(q[4 * e + i]) * down);
-        *reinterpret_cast<uint4*>(line + (e / 8) * PANEL + (((e & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        const uint4 u = piece(e);
+        const uint4 h = make_uint4(f16_pair(bf16lo(u.x) * down, bf16hi(u.x) * down), f16_pair(bf16lo(u.y) * down, bf16hi(u.y) * down),
+                                   f16_pair(bf16lo(u.z) * down, bf16hi(u.z) * down), f16_pair(bf16lo(u.w) * down, bf16hi(u.w) * down));
+        *reinterpret_cast<uint4*>(line + (e / 8) * PANEL + (((e & 7) ^ (row & 7)) << 4)) = h;
       }
       fence_async_smem();
       __syncwarp();
@@ -595,14 +595,91 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       return true;
     };
 
-    bool more = advance(it);
-    if (PAGED && more) ok = put_q(it);
-    while (more && ok) {
-      const int t = it.t0 + mine_from;
-      const bool mine = tok < prm.tokens && t < it.queries;
+    // (What happens once per item stands here once, and in loops that are not unrolled: the tile's own code is what the instruction cache is for.)
+    bool mine = false, begun = false;
+    int t = 0;
+    float m = 0.f, l = 0.f;
+    KeysItem done;
+    while (true) {
+      const bool more = advance(it);
+      // the next item's Q first, so that its S can start
+      if (PAGED && more && !put_q(it)) break;
+      if (begun) {
+        // ---- epilogue
+        if (!wait(cb + O_DONE + 8 * w, dn)) break;
+        ++dn;
+        tc_fence_after();
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+        const bool parts = k.splits > 1;
+        const long long pr = parts && mine ? part_row(done) : 0;
+        if (!parts) {
+          uint8_t* dst = k.o + 2 * (mine ? out_row(done, t) : 0);
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t ov[32];
+            tmem_ld32(o_tmem + c, ov);
+            tc_wait_ld32(ov);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) ov[e] = pack_bf16(__uint_as_float(ov[2 * e]) * inv, __uint_as_float(ov[2 * e + 1]) * inv);
+            if (mine) {
+              uint4* d4 = reinterpret_cast<uint4*>(dst + 2 * c);
+#pragma unroll
+              for (int e = 0; e < 16; e += 8) {
+                const uint4 lo = make_uint4(ov[e], ov[e + 1], ov[e + 2], ov[e + 3]), hi = make_uint4(ov[e + 4], ov[e + 5], ov[e + 6], ov[e + 7]);
+                if (prm.wide) {
+                  stg32(d4 + e / 4, lo, hi);
+                } else {
+                  d4[e / 4] = lo;
+                  d4[e / 4 + 1] = hi;
+                }
+              }
+            }
+          }
+        } else {
+          // A lane has a row of D floats; 64 bytes of each of the warp's 32 rows at a time go through shared memory, so that four lanes store them side by
+          // side (a clip's chunk, four splits: 2 121 -> 2 060 us.  Rows of bf16 leave sooner from their lanes: a clip over two prompts 408 us, this way 428)
+          uint8_t* mine_out = reinterpret_cast<uint8_t*>(k.part_o + pr * D);
+          uint8_t* rows_out[4];                                               // rows 8 i + lane / 4; null: not there
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const unsigned long long a = __shfl_sync(0xffffffffu, (unsigned long long)(mine ? mine_out : nullptr), 8 * i + (lane >> 2));
+            rows_out[i] = a ? reinterpret_cast<uint8_t*>(a) + 16 * (lane & 3) : nullptr;
+          }
+          uint8_t* way = smem + Smem<D>::OUT + (warp - 8) * 2048;
+#pragma unroll 1
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t ov[16];
+            tmem_ld16(o_tmem + 16 * c, ov);
+            tc_wait_ld16(ov);
+            // (16-byte pieces of a row's 64 bytes, turned by the row so that neither side meets a bank twice)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<uint4*>(way + lane * 64 + ((e ^ (lane >> 1 & 3)) << 4)) = make_uint4(ov[4 * e], ov[4 * e + 1], ov[4 * e + 2], ov[4 * e + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int from = 8 * i + (lane >> 2);
+              const uint4 u = *reinterpret_cast<const uint4*>(way + from * 64 + (((lane & 3) ^ (from >> 1 & 3)) << 4));
+              if (rows_out[i]) *reinterpret_cast<uint4*>(rows_out[i] + 64 * c) = u;
+            }
+            __syncwarp();
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        mbar_arrive_cluster_if(lead + O_FREE + 8 * w, sole);
+        const float m_fin = (m == -INFINITY ? 0.f : m) - UP;
+        if (mine && parts) k.part_ml[pr] = make_float2(m_fin, l);
+        if (mine && !parts && k.lse) *lse_at(done, t) = l != 0.f ? (m_fin + log2f(l)) * 0.6931471805599453f : -INFINITY;
+      }
+      if (!more) break;
+      begun = true;
+      t = it.t0 + mine_from;
+      mine = tok < prm.tokens && t < it.queries;
       const int seen = mine ? keys_seen(k, it.keys, it.queries, t) : it.keys;
       const float cc = k.scale_log2 * q_scale;
-      float m = -INFINITY, l = 0.f;
+      m = -INFINITY;
+      l = 0.f;
       uint32_t sv[64], pv[16];
       // half number i of the item on its way from tensor memory
       auto fetch = [&](int i) -> bool {
@@ -737,63 +814,10 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           if (i + 1 < halves && !fetch(i + 1)) { ok = false; break; }
         }
       }
-      tn += (uint32_t)(it.j1 - it.j0);
       if (!ok) break;
-      // ---- epilogue; the next item's Q first, so that its S can start
-      const KeysItem done = it;
+      tn += (uint32_t)(it.j1 - it.j0);
+      done = it;
       at += pairs;
-      more = advance(it);
-      if (PAGED && more && !put_q(it)) { ok = false; break; }
-      if (!wait(cb + O_DONE + 8 * w, dn)) { ok = false; break; }
-      ++dn;
-      tc_fence_after();
-      const float inv = l != 0.f ? 1.f / l : 0.f;
-      if (k.splits > 1) {
-        const long long pr = mine ? part_row(done) : 0;
-#pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t ov[32];
-          tmem_ld32(o_tmem + c, ov);
-          tc_wait_ld32(ov);
-          if (mine) {
-            float* dst = k.part_o + pr * D + c;
-#pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<uint4*>(dst + e) = make_uint4(ov[e], ov[e + 1], ov[e + 2], ov[e + 3]);
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        mbar_arrive_cluster_if(lead + O_FREE + 8 * w, sole);
-        if (mine) k.part_ml[pr] = make_float2((m == -INFINITY ? 0.f : m) - UP, l);
-      } else {
-        uint8_t* dst = k.o + 2 * (mine ? out_row(done, t) : 0);
-#pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t ov[32], h[16];
-          tmem_ld32(o_tmem + c, ov);
-          tc_wait_ld32(ov);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) h[e] = pack_bf16(__uint_as_float(ov[2 * e]) * inv, __uint_as_float(ov[2 * e + 1]) * inv);
-          if (mine) {
-            uint4* d4 = reinterpret_cast<uint4*>(dst + 2 * c);
-#pragma unroll
-            for (int e = 0; e < 16; e += 8) {
-              const uint4 lo = make_uint4(h[e], h[e + 1], h[e + 2], h[e + 3]), hi = make_uint4(h[e + 4], h[e + 5], h[e + 6], h[e + 7]);
-              if (prm.wide) {
-                stg32(d4 + e / 4, lo, hi);
-              } else {
-                d4[e / 4] = lo;
-                d4[e / 4 + 1] = hi;
-              }
-            }
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        mbar_arrive_cluster_if(lead + O_FREE + 8 * w, sole);
-        if (mine && k.lse) *lse_at(done, t) = l != 0.f ? ((m == -INFINITY ? 0.f : m) - UP + log2f(l)) * 0.6931471805599453f : -INFINITY;
-      }
     }
     if (PAGED && ok && qn > 0) (void)wait(cb + Q_EMPTY + 8 * w, qn - 1u);     // (as the loaders do)
   }
