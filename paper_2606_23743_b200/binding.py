@@ -70,7 +70,8 @@ class KvCache(C.Structure):
     _fields_ = [("H", C.c_int32), ("d", C.c_int32), ("page", C.c_int32), ("pages", C.c_int32), ("format", C.c_int32),
                 ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("k_sf", C.c_void_p), ("v_sf", C.c_void_p)]
-    arrays, on_gpu, heads = None, False, None              # the tensors behind the pointers, where they are, and (H, d) (make_kv_cache)
+    # the tensors behind the pointers, whether they are on the GPU, on which (-1: none, or on several), and (H, d) (make_kv_cache)
+    arrays, on_gpu, device, heads = None, False, -1, None
 
 
 class CachedAttn(C.Structure):
@@ -651,6 +652,7 @@ def make_kv_cache(k, v, format: str = "e4m3") -> KvCache:
     if format == "fp4":
         c.k_sf, c.v_sf = _ptr(k[2]), _ptr(v[2])
     c.arrays, c.on_gpu, c.heads = (tuple(k), tuple(v)), all(t.is_cuda for t in (*k, *v)), (c.H, c.d)
+    c.device = k[0].get_device() if len({t.get_device() for t in (*k, *v)}) == 1 else -1
     return c
 
 
@@ -681,7 +683,7 @@ def kv_cache_read(c: KvCache, page_table, lengths, k, v, status=None) -> None:
         raise SvaError(rc, "sva_kv_cache_read")
 
 
-_NOT_ON_GPU = "the cache and its tensors are on the GPU"
+_NOT_ON_GPU = "the cache and its tensors are on the current GPU"
 
 
 def _table(page_table, rows):
@@ -695,9 +697,17 @@ def _table(page_table, rows):
 _I32, _BF16 = torch.int32, torch.bfloat16
 
 
-def _int32s(t, n, what):
-    assert t.shape == (n,) and t.dtype is _I32 and t.is_contiguous() and t.is_cuda, f"{what} are {n} int32, side by side, on the GPU"
+def _int32s(t, n, what, device):
+    assert t.shape == (n,) and t.dtype is _I32 and t.is_contiguous() and t.get_device() == device, f"{what} are {n} int32, side by side, on the GPU"
     return t.data_ptr()
+
+
+def _all_on(device, *tensors):
+    """Whether the tensors (or None) are on that GPU, and it is the current one: kernels run there."""
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            return False
+    return device >= 0 and device == _raw_device()
 
 
 def kv_cache_append(c: KvCache, k, v, page_table, lengths, counts=None, status=None) -> None:
@@ -706,9 +716,10 @@ def kv_cache_append(c: KvCache, k, v, page_table, lengths, counts=None, status=N
     shape = Bq, H, T, d = k.shape
     assert (H, d) == c.heads and v.shape == shape and k.dtype is v.dtype is _BF16, "k, v are [B,H,T,d] bf16"
     stride, most = _table(page_table, Bq)
-    assert c.on_gpu and k.is_cuda and v.is_cuda and page_table.is_cuda and (status is None or status.is_cuda), _NOT_ON_GPU
+    dev = c.device
+    assert _all_on(dev, k, v, page_table, status), _NOT_ON_GPU
     rc = (_lib or lib()).sva_kv_cache_append(c, k.data_ptr(), v.data_ptr(), _strides_any(k), _strides_any(v), Bq, T, page_table.data_ptr(), stride, most,
-                                             _int32s(lengths, Bq, "lengths"), None if counts is None else _int32s(counts, Bq, "counts"),
+                                             _int32s(lengths, Bq, "lengths", dev), None if counts is None else _int32s(counts, Bq, "counts", dev),
                                              None if status is None else status.data_ptr(), _stream())
     if rc:
         raise SvaError(rc, "sva_kv_cache_append")
@@ -736,11 +747,11 @@ def cached_attn_fwd(p: CachedAttn, q, page_table, lengths, o, counts=None, lse=N
     assert q.shape == p.shape == o.shape and q.dtype is o.dtype is _BF16 and (q.stride(), o.stride()) == p.strides, \
         "q, o are bf16 and of the sizes and strides that the plan was made for"
     assert (page_table.shape, page_table.stride()) == p.table and page_table.dtype is _I32, "page_table is int32 and of the plan's sizes and strides"
-    assert lse is None or lse.shape == p.shape[:3] and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,M] fp32"
-    assert p.cache.on_gpu and q.is_cuda and o.is_cuda and page_table.is_cuda and (status is None or status.is_cuda) and \
-        (workspace is None or workspace.is_cuda), _NOT_ON_GPU
-    rc = (_lib or lib()).sva_cached_attn_fwd(p.cache, p, q.data_ptr(), page_table.data_ptr(), _int32s(lengths, p.shape[0], "lengths"),
-                                             None if counts is None else _int32s(counts, p.shape[0], "counts"), o.data_ptr(),
+    assert lse is None or lse.shape == p.shape[:3] and lse.dtype is torch.float32 and lse.is_contiguous(), "lse is [B,Hq,M] fp32"
+    dev = p.cache.device
+    assert _all_on(dev, q, o, page_table, lse, status, workspace), _NOT_ON_GPU
+    rc = (_lib or lib()).sva_cached_attn_fwd(p.cache, p, q.data_ptr(), page_table.data_ptr(), _int32s(lengths, p.shape[0], "lengths", dev),
+                                             None if counts is None else _int32s(counts, p.shape[0], "counts", dev), o.data_ptr(),
                                              None if lse is None else lse.data_ptr(), None if status is None else status.data_ptr(),
                                              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream())
     if rc:
@@ -771,13 +782,13 @@ def cross_attn_fwd(p: CrossAttn, q, k, v, o, lengths=None, key_mask=None, lse=No
     assert q.shape == of_q == o.shape and k.shape == of_k == v.shape and q.dtype is k.dtype is v.dtype is o.dtype is _BF16 and \
         (q.stride(), k.stride(), v.stride(), o.stride()) == p.strides, "q, k, v, o are bf16 and of the sizes and strides that the plan was made for"
     if key_mask is not None:
-        assert key_mask.shape == (of_k[0], of_k[2]) and key_mask.element_size() == 1 and (of_k[2] <= 1 or key_mask.stride(1) == 1) and key_mask.is_cuda, \
-            "key_mask is [B,S] bytes on the GPU"
+        assert key_mask.shape == (of_k[0], of_k[2]) and key_mask.element_size() == 1 and (of_k[2] <= 1 or key_mask.stride(1) == 1), \
+            "key_mask is [B,S] bytes"
         p.mask_stride = key_mask.stride(0)
-    assert lse is None or lse.shape == of_q[:3] and lse.dtype is torch.float32 and lse.is_contiguous() and lse.is_cuda, "lse is [B,Hq,N] fp32"
-    assert q.is_cuda and k.is_cuda and v.is_cuda and o.is_cuda and (status is None or status.is_cuda) and (workspace is None or workspace.is_cuda), \
-        "tensors are on the GPU"
-    rc = (_lib or lib()).sva_cross_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lengths is None else _int32s(lengths, of_q[0], "lengths"),
+    assert lse is None or lse.shape == of_q[:3] and lse.dtype is torch.float32 and lse.is_contiguous(), "lse is [B,Hq,N] fp32"
+    dev = q.get_device()
+    assert _all_on(dev, k, v, o, key_mask, lse, status, workspace), "tensors are on the current GPU"
+    rc = (_lib or lib()).sva_cross_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if lengths is None else _int32s(lengths, of_q[0], "lengths", dev),
                                             None if key_mask is None else key_mask.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(),
                                             None if status is None else status.data_ptr(), None if workspace is None else workspace.data_ptr(),
                                             0 if workspace is None else workspace.nbytes, _stream())
@@ -788,8 +799,8 @@ def cross_attn_fwd(p: CrossAttn, q, k, v, o, lengths=None, key_mask=None, lse=No
 def kv_pages_copy(c: KvCache, src, dst, status=None) -> None:
     """Page dst[i] becomes page src[i] (int32; negative: left out)."""
     n = src.shape[0]
-    assert c.on_gpu and (status is None or status.is_cuda), _NOT_ON_GPU
-    rc = (_lib or lib()).sva_kv_pages_copy(c, _int32s(src, n, "src"), _int32s(dst, n, "dst"), n, _ptr(status), _stream())
+    assert _all_on(c.device, status), _NOT_ON_GPU
+    rc = (_lib or lib()).sva_kv_pages_copy(c, _int32s(src, n, "src", c.device), _int32s(dst, n, "dst", c.device), n, _ptr(status), _stream())
     if rc:
         raise SvaError(rc, "sva_kv_pages_copy")
 
@@ -797,14 +808,14 @@ def kv_pages_copy(c: KvCache, src, dst, status=None) -> None:
 def _pool(c, refs, page_table, status):
     rows = page_table.shape[0]
     stride, most = _table(page_table, rows)
-    assert c.on_gpu and page_table.is_cuda and (status is None or status.is_cuda), _NOT_ON_GPU
-    return _int32s(refs, c.pages, "refs"), page_table.data_ptr(), stride, rows, most
+    assert _all_on(c.device, page_table, status), _NOT_ON_GPU
+    return _int32s(refs, c.pages, "refs", c.device), page_table.data_ptr(), stride, rows, most
 
 
 def kv_pages_take(c: KvCache, refs, page_table, lengths, counts, status=None) -> None:
     """Every row of page_table gets the pages for counts [rows] tokens behind its lengths [rows]: the free ones of the lowest ids."""
     pool = _pool(c, refs, page_table, status)
-    rc = (_lib or lib()).sva_kv_pages_take(c, *pool, _int32s(lengths, pool[3], "lengths"), _int32s(counts, pool[3], "counts"), _ptr(status), _stream())
+    rc = (_lib or lib()).sva_kv_pages_take(c, *pool, _int32s(lengths, pool[3], "lengths", c.device), _int32s(counts, pool[3], "counts", c.device), _ptr(status), _stream())
     if rc:
         raise SvaError(rc, "sva_kv_pages_take")
 
@@ -812,8 +823,8 @@ def kv_pages_take(c: KvCache, refs, page_table, lengths, counts, status=None) ->
 def kv_pages_fork(c: KvCache, refs, page_table, lengths, parents, children, status=None) -> None:
     """Row children[i] becomes a copy of row parents[i]: full pages shared, a partly filled last one copied to a page of its own."""
     pool, n = _pool(c, refs, page_table, status), parents.shape[0]
-    rc = (_lib or lib()).sva_kv_pages_fork(c, *pool, _int32s(lengths, pool[3], "lengths"), _int32s(parents, n, "parents"),
-                                           _int32s(children, n, "children"), n, _ptr(status), _stream())
+    rc = (_lib or lib()).sva_kv_pages_fork(c, *pool, _int32s(lengths, pool[3], "lengths", c.device), _int32s(parents, n, "parents", c.device),
+                                           _int32s(children, n, "children", c.device), n, _ptr(status), _stream())
     if rc:
         raise SvaError(rc, "sva_kv_pages_fork")
 
@@ -821,8 +832,8 @@ def kv_pages_fork(c: KvCache, refs, page_table, lengths, parents, children, stat
 def kv_pages_free(c: KvCache, refs, page_table, lengths, rows, keep=None, status=None) -> None:
     """Gives back the pages of these rows behind their first keep [n] tokens (None: all of them)."""
     pool, n = _pool(c, refs, page_table, status), rows.shape[0]
-    rc = (_lib or lib()).sva_kv_pages_free(c, *pool, _int32s(lengths, pool[3], "lengths"), _int32s(rows, n, "rows"),
-                                           None if keep is None else _int32s(keep, n, "keep"), n, _ptr(status), _stream())
+    rc = (_lib or lib()).sva_kv_pages_free(c, *pool, _int32s(lengths, pool[3], "lengths", c.device), _int32s(rows, n, "rows", c.device),
+                                           None if keep is None else _int32s(keep, n, "keep", c.device), n, _ptr(status), _stream())
     if rc:
         raise SvaError(rc, "sva_kv_pages_free")
 
@@ -834,8 +845,8 @@ def kv_pages_compact_workspace_bytes(c: KvCache) -> int:
 def kv_pages_compact(c: KvCache, refs, page_table, workspace, live=None, status=None) -> None:
     """The pages in use move to the lowest ids; refs and page_table follow, live [1] int32 becomes their number."""
     pool = _pool(c, refs, page_table, status)
-    assert workspace.is_cuda, _NOT_ON_GPU
-    rc = (_lib or lib()).sva_kv_pages_compact(c, *pool, None if live is None else _int32s(live, 1, "live"), _ptr(status), _ptr(workspace),
+    assert workspace.get_device() == c.device, _NOT_ON_GPU
+    rc = (_lib or lib()).sva_kv_pages_compact(c, *pool, None if live is None else _int32s(live, 1, "live", c.device), _ptr(status), _ptr(workspace),
                                               _ws_bytes(workspace), _stream())
     if rc:
         raise SvaError(rc, "sva_kv_pages_compact")
