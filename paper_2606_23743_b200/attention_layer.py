@@ -156,16 +156,15 @@ class ChunkAttentionLayer:
         self.work = torch.empty(sva.kv_pages_compact_workspace_bytes(self.cache), dtype=torch.uint8, device=dev)
 
     def __call__(self, x, counts=None):
-        """x [rows, M, C] bf16, of each sequence's next counts [rows] tokens (int32; None: M): x + attention's projection, for them.  Rows of x behind
-        its count mean nothing, nor do those of the result."""
+        """x [rows, M, C] bf16, of each sequence's next counts [rows] tokens (int32, outside [0, M] the nearer end; None: M): x + attention's projection, for
+        them.  Rows of x behind its count mean nothing, nor do those of the result."""
         B, M, C = x.shape
         Hq, H, d = self.Hq, self.H, self.d
         assert B == self.B, "x holds tokens of every sequence"
         if M == 0:
             return torch.empty_like(x)
         x = x.reshape(B * M, C)
-        if counts is None:
-            counts = torch.full((B,), M, dtype=torch.int32, device=x.device)
+        counts = torch.full((B,), M, dtype=torch.int32, device=x.device) if counts is None else counts.clamp(0, M)
         qkv = self.qkv(x, torch.empty(B * M, (Hq + 2 * H) * d, dtype=torch.bfloat16, device=x.device), self.status).view(B, M, Hq + 2 * H, d).transpose(1, 2)
         q, k, v = qkv.split((Hq, H, H), 1)
         positions = (self.lengths[:, None] + torch.arange(M, dtype=torch.int32, device=x.device))[None].contiguous()
@@ -181,7 +180,8 @@ class ChunkAttentionLayer:
         return self.out(o, torch.empty(B * M, C, dtype=torch.bfloat16, device=x.device), self.status, residual=x).view(B, M, C)
 
     def fork(self, parents, children):
-        """Sequences children (int32) give up what they hold and go on from where sequences parents are, whose full pages they share."""
+        """Sequences children (int32) give up what they hold and go on from where sequences parents are, whose full pages they share.  A child comes once
+        and is no parent of the call: a parent that is named among the children has given up its pages by then."""
         sva.kv_pages_free(self.cache, self.refs, self.table, self.lengths, children, status=self.status)
         sva.kv_pages_fork(self.cache, self.refs, self.table, self.lengths, parents, children, self.status)
 

@@ -821,7 +821,8 @@ def kv_pages_take(c: KvCache, refs, page_table, lengths, counts, status=None) ->
 
 
 def kv_pages_fork(c: KvCache, refs, page_table, lengths, parents, children, status=None) -> None:
-    """Row children[i] becomes a copy of row parents[i]: full pages shared, a partly filled last one copied to a page of its own."""
+    """Row children[i] becomes a copy of row parents[i]: full pages shared, a partly filled last one copied to a page of its own.  Children
+    hold nothing before, come once and are no parents of the call."""
     pool, n = _pool(c, refs, page_table, status), parents.shape[0]
     rc = (_lib or lib()).sva_kv_pages_fork(c, *pool, _int32s(lengths, pool[3], "lengths", c.device), _int32s(parents, n, "parents", c.device),
                                            _int32s(children, n, "children", c.device), n, _ptr(status), _stream())

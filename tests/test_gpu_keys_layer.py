@@ -82,6 +82,21 @@ def test_a_clip_in_chunks(Hq, H, d, causal):
     call(20, [3, 20, 7])
 
 
+def test_counts_beyond_the_call():
+    """A count outside [0, M] is the nearer end for pages, lengths and attention alike, as it is for what is appended."""
+    gen = torch.Generator("cuda").manual_seed(5)
+    bf = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)                    # noqa: E731
+    C, d, M = 64, 64, 5
+    w_qkv, w_out, x, y = bf(3 * d, C) / 8, bf(C, d) / 8, bf(3, M, C), bf(3, 1, C)
+    said, meant = (ChunkAttentionLayer(w_qkv, w_out, 1, 64, 3, page=16) for _ in range(2))
+    given = _i32([40, -7, 2])
+    got, want = said(x, given), meant(x, _i32([M, 0, 2]))
+    assert given.tolist() == [40, -7, 2] and said.lengths.tolist() == [M, 0, 2]
+    assert torch.equal(said.table, meant.table) and torch.equal(said.refs, meant.refs)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2, :2], want[2, :2])
+    assert torch.equal(said(y), meant(y)) and int(said.status) == 0
+
+
 @pytest.mark.parametrize("Hq,H,d,M,masked", [(2, 2, 128, 333, False), (4, 2, 64, 3, True)])
 def test_a_clip_and_its_prompt(Hq, H, d, M, masked):
     rng = np.random.default_rng(M)
