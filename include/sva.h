@@ -523,7 +523,8 @@ int sva_kv_cache_append(const sva_kv_cache_t* c, const void* k, const void* v, c
  *   o_i = sum_j softmax_j(softmax_scale * <q_i, k_j>) v_j,  lse_i = ln sum_j exp(softmax_scale * <q_i, k_j>),  j < lengths[b], in causal form
  *   j <= lengths[b] - counts[b] + i  (the queries are the last counts[b] of the sequence's lengths[b] tokens; appended before this call)
  * for the queries i < counts[b] (NULL: all M); the rows of o and lse behind them stay as they are.  Hq is a multiple of the cache's H: query
- * heads h*Hq/H .. (h+1)*Hq/H - 1 share cached head h.  A row without keys becomes zeros, its lse -inf.
+ * heads h*Hq/H .. (h+1)*Hq/H - 1 share cached head h.  A row without keys becomes zeros, its lse -inf.  A logit that is a NaN or +infinity (beyond
+ * fp32) makes its row NaNs, its lse a NaN; a key whose logit is -infinity is as one that is left out.
  * Codes enter the products as they are (exact in fp16), Q as fp16 after a scaling of each row by a power of two, the probabilities as fp16;
  * scales, softmax and sums are fp32.  Scales of V below 2^-80 are taken for 2^-80, and above 2^80 a row's sum loses its smallest terms.
  * Keys on pages that are named wrongly (SVA_DEV_BAD_INDEX) are left out.  Codes are finite (append writes no NaN but beside a scale that is one).
@@ -550,7 +551,7 @@ int sva_cached_attn_fwd(const sva_kv_cache_t* c, const sva_cached_attn_t* p, con
  * Cross attention: the tokens of a clip attend to an encoder's states (a prompt's), which have a length of their own:
  *   o_i = sum_j softmax_j(softmax_scale * <q_i, k_j>) v_j,  lse_i as above,  over the keys j < lengths[b] (NULL: S) whose key_mask[b][j] is not 0
  *   (NULL: all);  q, o [B,Hq,N,d], k, v [B,Hk,S,d] bf16, Hq a multiple of Hk (heads share as above), d = 64 or 128.
- * Keys that are left out have no influence, whatever they hold.  A row without keys becomes zeros, its lse -inf.  Q K^T and P V are bf16
+ * Keys that are left out have no influence, whatever they hold.  A row without keys becomes zeros, its lse -inf; logits that are no numbers as above.  Q K^T and P V are bf16
  * products with fp32 sums, the probabilities rounded to bf16.  lengths [B] int32; key_mask [B][S] bytes, mask_stride between
  * items; lse (optional) [B,Hq,N] fp32 contiguous.  N and S may be 0.  Strides of 0 over items or heads (shared states) are fine.
  * Alignment, workspace and errors as for the call above.

@@ -132,6 +132,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
+// 0, and of a NaN or +infinity a NaN
+__device__ __forceinline__ float nan_if_endless(float x) {
+  x = max_nan(x, -3.402823466e38f);
+  return x - x;
+}
 // 2^x of two values on the FMA and integer pipes, x <= 126: 2^floor(x) by the exponent field, the rest by a polynomial with the value 1 at 0 (the
 // smallest relative error on [0, 1) of its degree: 8.3e-8; 1.5e-7 as evaluated).  Below -127 exactly 0.
 __device__ __forceinline__ uint64_t ex2_poly(uint64_t x2) {
@@ -670,7 +675,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         tc_fence_before();
         __syncwarp();
         mbar_arrive_cluster_if(lead + O_FREE + 8 * w, sole);
-        const float m_fin = (m == -INFINITY ? 0.f : m) - UP;
+        const float m_fin = (m > -INFINITY ? m : 0.f) - UP;                   // (of a NaN 0 too: what splits are joined by is a number)
         if (mine && parts) k.part_ml[pr] = make_float2(m_fin, l);
         if (mine && !parts && k.lse) *lse_at(done, t) = l != 0.f ? (m_fin + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
@@ -775,13 +780,18 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             }
             return PAGED ? mx : mx * cc;
           };
-          auto reference = [&]() -> float { return (m == -INFINITY ? 0.f : m) - UP; };
+          auto reference = [&]() -> float { return (m > -INFINITY ? m : 0.f) - UP; };
           const bool first = i == 0;
-          if (first) m = maximum();
+          // (a logit that is a NaN or +infinity makes the row's sum, and with it the row, a NaN, whatever the exponentials make of it: ex2_poly takes a
+          // NaN for -127)
+          if (first) {
+            m = maximum();
+            l = nan_if_endless(m);
+          }
           float ref = reference(), sum = exps(0, ref);
           if (!first) {
             const float mx = maximum();
-            if (mx != mx) l = mx;                                             // (a NaN: the row's sum, and with it the row, becomes one)
+            l += nan_if_endless(mx);
             if (__any_sync(0xffffffffu, mx > m + LAZY)) {
               // (O is at rest once P V of the half before has completed)
               if (!wait(cb + PV_DONE + 8 * w, hn - 1u)) { ok = false; break; }
