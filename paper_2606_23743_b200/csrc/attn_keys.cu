@@ -160,7 +160,7 @@ keys_paged_few_kernel(const KeysParams prm) {
 #pragma unroll
   for (int t = 0; t < MT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
 
-  auto step = [&](int gi, const Group& x) {
+  auto step = [&](int gi, Group& x) {
     if (x.there == 0u) return;                                            // (a page that is named wrongly: nothing was read)
     float s[4] = {0.f, 0.f, 0.f, 0.f};                                    // (key g, rows 2c, 2c + 1), (key g + 8, the same)
 #pragma unroll
@@ -169,6 +169,13 @@ keys_paged_few_kernel(const KeysParams prm) {
       codes_f16x4(word(x.k[0][i / 4], i % 4), a[0], a[2]);
       codes_f16x4(word(x.k[1][i / 4], i % 4), a[1], a[3]);
       mma_f16(s, a, qb[i][0], qb[i][1]);
+    }
+    // a page with a scale that is a NaN or infinite: logits of NaN for the rows that see it, values of zeros, which spoil no other row
+    if (!(fabsf(x.ks) < INFINITY && fabsf(x.vs) < INFINITY)) {            // (uniform in a warp)
+      s[0] = s[1] = s[2] = s[3] = __int_as_float(0x7fc00000);
+      x.ks = x.vs = 1.f;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) x.v[n] = make_uint4(0u, 0u, 0u, 0u);
     }
     const float vs = v_scale_floor(x.vs), lv = __log2f(vs), inv_vs = __frcp_rn(vs);
     float p[4];

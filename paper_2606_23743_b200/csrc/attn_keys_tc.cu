@@ -470,7 +470,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       bool named = false;
       auto fetch_scales = [&](const Place& x) {
         named = x.id >= 0;
-        if (named && a == 0) {
+        if (named) {
           ks = __ldg(k.k_scale + (long long)x.id * k.Hk + x.it.hk);
           vs = __ldg(k.v_scale + (long long)x.id * k.Hk + x.it.hk);
         }
@@ -493,10 +493,22 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         const uint32_t s = n % STAGES, use = n / STAGES;
         if (use > 0) ok = wait(cb + K_EMPTY + 8 * s, use - 1u);
         if (!ok || ((prm.debug & 2048) && n >= 1)) { ok = false; break; }         // (test aid: later tiles never come)
+        // A chunk on a page with a scale that is a NaN or infinite: its keys become NaNs, which masks take out of S for the rows that do not see them, its
+        // values zeros, which spoil no row
+        const bool good = named && max_nan(fabsf(ks), fabsf(vs)) < INFINITY;
+        if (const uint32_t bad = __ballot_sync(0xffffffffu, named && !good)) {
+#pragma unroll
+          for (int i = 0; i < EACH; ++i) {
+            const int u = a + CONVERTERS * i;
+            int key, byte, to0, to1;
+            unit_of(u, key, byte, to0, to1);
+            if (bad >> (key >> 4 & 7) & 1u) r[i].x = r[i].y = r[i].z = r[i].w = u < KU ? 0x7f7f7f7fu : 0u;
+          }
+        }
         if (a == 0 && lane < 8) {
           // (K of zeros alone, scale 0: any scale will do but one that makes -inf a NaN; pages that are named wrongly: left out)
-          const float v = named ? v_scale_floor(vs) : 1.f;
-          scales[(n % SCALE_RING) * 8 + lane] = make_float4(!named || ks == 0.f ? 1.f : ks, named ? log2f(v) : -INFINITY, 1.f / v, 0.f);
+          const float v = good ? v_scale_floor(vs) : 1.f;
+          scales[(n % SCALE_RING) * 8 + lane] = make_float4(!good || ks == 0.f ? 1.f : ks, named ? log2f(v) : -INFINITY, 1.f / v, 0.f);
         }
         more = nx.more;
         bool k_out = false;

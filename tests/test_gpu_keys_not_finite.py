@@ -48,3 +48,63 @@ def test_not_a_number_in_parts_of_a_split_axis(N, S, what):
     rows = slice(1, 2) if what == "q" else slice(None)
     assert torch.isnan(o[0, 0, rows]).all() and torch.isnan(lse[0, 0, rows]).all()
     assert what != "q" or torch.isfinite(o[0, 0, 2:]).all() and torch.isfinite(o[0, 0, 0]).all()
+
+
+BAD = [("k", float("nan")), ("v", float("nan")), ("k", float("inf")), ("v", float("inf")), ("kv", float("nan"))]
+
+
+@pytest.mark.parametrize("which,value", BAD)
+@pytest.mark.parametrize("Hq,H,M,d,keys", [(1, 1, 3, 64, 194), (4, 2, 3, 128, 194), (2, 1, 20, 128, 194), (2, 2, 140, 64, 194), (2, 2, 140, 128, 258),
+                                           (1, 1, 2, 128, 20001), (2, 1, 64, 128, 6001)])
+def test_a_page_that_is_not_a_number_and_queries_before_it(Hq, H, M, d, keys, which, value):
+    """Causal: the last page of a sequence is spoilt; the queries before it do not see it.  (The last two: split key axes.)"""
+    page = 16
+    rng = np.random.default_rng(M + keys)
+    x = Cached(rng, 1, Hq, H, M, d, page, [keys], True)
+    bad, first = x.ids[0][keys // page], keys // page * page
+    clean = [(c.copy(), s.copy()) for c, s in zip(x.codes, x.scales)]
+    for i, name in enumerate("kv"):
+        if name in which:
+            x.scales[i][bad, H - 1] = value
+            x.codes[i][bad, H - 1] = 0x7f
+    x.run(True, None)
+    sees = keys - M + np.arange(M) >= first
+    assert sees.any() and not sees.all()
+    o, lse = _f64(x.o)[0], _f64(x.lse)[0]
+    k, v = (K.gathered(c, s, x.ids[0].tolist(), keys, page) for c, s in clean)
+    there = np.arange(keys)[None] <= keys - M + np.arange(M)[:, None]
+    for h in range(Hq):
+        rows = ~sees if h // (Hq // H) == H - 1 else np.ones(M, bool)
+        assert np.isnan(o[h, ~rows]).all() and np.isnan(lse[h, ~rows]).all()
+        want = K.attention(_f64(x.q)[0, h, rows], k[h // (Hq // H)], v[h // (Hq // H)], there[rows], d ** -0.5)
+        _compare(o[h, rows], lse[h, rows], want, 2.0 ** -11, d, v[h // (Hq // H)])
+    assert int(x.status) == 0
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("M", [4, 70])
+def test_a_token_that_is_not_a_number(M, bad):
+    """The same as a user meets it: a chunk with a NaN (an infinity) in its last token is appended, and attended to in causal form."""
+    H, d, page, held = 2, 64, 16, 47                       # (the chunk's last token begins a page)
+    n = held + M - (held + M - 1) % page
+    M = n - held
+    rng = np.random.default_rng(M)
+    x = torch.from_numpy(rng.standard_normal((1, n, H, d))).to(torch.bfloat16).cuda().transpose(1, 2)
+    q = torch.from_numpy(rng.standard_normal((1, M, H, d))).to(torch.bfloat16).cuda().transpose(1, 2)
+    pages = -(-n // page)
+    arrays = [[torch.zeros(pages, H, page, d, dtype=torch.uint8, device="cuda"), torch.zeros(pages, H, device="cuda")] for _ in range(2)]
+    c, table, status = B.make_kv_cache(*arrays, format="e4m3_page"), torch.arange(pages, dtype=torch.int32, device="cuda")[None].contiguous(), _i32([0])
+    spoilt = x.clone()
+    spoilt[0, :, n - 1, 3] = bad
+    B.kv_cache_append(c, spoilt[:, :, :held], spoilt[:, :, :held], table, _i32([0]), status=status)
+    B.kv_cache_append(c, spoilt[:, :, held:], spoilt[:, :, held:], table, _i32([held]), status=status)
+    o, lse = torch.empty_like(q), torch.empty(1, H, M, device="cuda")
+    p = B.make_cached_attn(c, q, o, table, True)
+    ws = torch.empty(max(256, B.cached_attn_workspace_bytes(p)), dtype=torch.uint8, device="cuda")
+    B.cached_attn_fwd(p, q, table, _i32([n]), o, None, lse, status, ws)
+    assert torch.isnan(o[0, :, M - 1]).all() and torch.isnan(lse[0, :, M - 1]).all() and int(status) == 0
+    kv = K.gathered(arrays[0][0].cpu().numpy(), arrays[0][1].cpu().numpy().astype(np.float64), table[0].tolist(), n, page)[:, :n - 1]
+    there = np.arange(n - 1)[None] <= held + np.arange(M - 1)[:, None]
+    for h in range(H):
+        want = K.attention(_f64(q)[0, h, :M - 1], kv[h], kv[h], there, d ** -0.5)
+        _compare(_f64(o)[0, h, :M - 1], _f64(lse)[0, h, :M - 1], want, 2.0 ** -11, d, kv[h])
