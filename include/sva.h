@@ -524,7 +524,8 @@ int sva_kv_cache_append(const sva_kv_cache_t* c, const void* k, const void* v, c
  *   j <= lengths[b] - counts[b] + i  (the queries are the last counts[b] of the sequence's lengths[b] tokens; appended before this call)
  * for the queries i < counts[b] (NULL: all M); the rows of o and lse behind them stay as they are.  Hq is a multiple of the cache's H: query
  * heads h*Hq/H .. (h+1)*Hq/H - 1 share cached head h.  A row without keys becomes zeros, its lse -inf.  A logit that is a NaN or +infinity (beyond
- * fp32) makes its row NaNs, its lse a NaN; a key whose logit is -infinity is as one that is left out.
+ * fp32) makes its row NaNs, its lse a NaN; a key whose logit is -infinity is as one that is left out.  (A row's largest |q| * softmax_scale
+ * times a page's scale of K has to lie within fp32.)
  * Codes enter the products as they are (exact in fp16), Q as fp16 after a scaling of each row by a power of two, the probabilities as fp16;
  * scales, softmax and sums are fp32.  Scales of V below 2^-80 are taken for 2^-80, and above 2^80 a row's sum loses its smallest terms.
  * Keys on pages that are named wrongly (SVA_DEV_BAD_INDEX) are left out.  A page whose scale (K's or V's) of a head is a NaN or infinite makes NaNs of the

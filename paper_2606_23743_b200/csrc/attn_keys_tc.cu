@@ -132,6 +132,8 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
+// What a logit of codes is multiplied by, a row's factor times a page's scale of K; not 0, so that a logit of -inf (a key that is left out) stays one.
+__device__ __forceinline__ float logit_factor(float row, float page) { return fmaxf(row * page, 1.17549435e-38f); }
 // 0, and of a NaN or +infinity a NaN
 __device__ __forceinline__ float nan_if_endless(float x) {
   x = max_nan(x, -3.402823466e38f);
@@ -506,9 +508,9 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           }
         }
         if (a == 0 && lane < 8) {
-          // (K of zeros alone, scale 0: any scale will do but one that makes -inf a NaN; pages that are named wrongly: left out)
+          // (pages that are named wrongly: left out)
           const float v = good ? v_scale_floor(vs) : 1.f;
-          scales[(n % SCALE_RING) * 8 + lane] = make_float4(!good || ks == 0.f ? 1.f : ks, named ? log2f(v) : -INFINITY, 1.f / v, 0.f);
+          scales[(n % SCALE_RING) * 8 + lane] = make_float4(good ? ks : 1.f, named ? log2f(v) : -INFINITY, 1.f / v, 0.f);
         }
         more = nx.more;
         bool k_out = false;
@@ -747,7 +749,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 #pragma unroll
             for (int g = 2 * q; g < 2 * q + 2; ++g) {
               const float4 f = PAGED ? sc[4 * h + g] : make_float4(1.f, 0.f, 1.f, 0.f);
-              const float c = PAGED ? cc * f.x : cc, nm = PAGED ? f.y - ref : -ref;
+              const float c = PAGED ? logit_factor(cc, f.x) : cc, nm = PAGED ? f.y - ref : -ref;
               const uint64_t c2 = pack2(c, c), nm2 = pack2(nm, nm);
               uint64_t sum2 = pack2(0.f, 0.f);
 #pragma unroll
@@ -785,7 +787,7 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
               a = max3_nan(a, __uint_as_float(sv[16 * g + 14]), __uint_as_float(sv[16 * g + 15]));
               if (PAGED) {
                 const float4 f = sc[4 * h + g];
-                mx = max_nan(mx, fmaf(max_nan(a, b), cc * f.x, f.y));
+                mx = max_nan(mx, fmaf(max_nan(a, b), logit_factor(cc, f.x), f.y));
               } else {
                 mx = max3_nan(mx, a, b);
               }

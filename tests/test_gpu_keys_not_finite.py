@@ -50,6 +50,31 @@ def test_not_a_number_in_parts_of_a_split_axis(N, S, what):
     assert what != "q" or torch.isfinite(o[0, 0, 2:]).all() and torch.isfinite(o[0, 0, 0]).all()
 
 
+@pytest.mark.parametrize("M", [2, 40, 300])
+@pytest.mark.parametrize("group", [0, 5, 11])
+def test_a_logit_over_cached_keys_that_overflows(group, M):
+    """The same by way of a page's scale."""
+    rng = np.random.default_rng(group + M)
+    d, Bq, n = 128, 16, 200
+    x = Cached(rng, Bq, 1, 1, M, d, 16, [n] * Bq, True)
+    x.codes[0][..., 0] = 0
+    sign = torch.where(torch.arange(M, device="cuda") % 2 == 0, 1.0, -1.0)
+    x.q.zero_()
+    x.q[..., 0] = sign * 2.0 ** 60
+    for b in range(Bq):
+        page = x.ids[b][group]
+        x.scales[0][page] = 2.0 ** 63
+        x.codes[0][page] = 0
+        x.codes[0][page, 0, b, 0] = K.e4m3_bytes(np.array(448.0))
+    x.run(False, None)
+    assert torch.isnan(x.o[:, :, ::2]).all() and torch.isnan(x.lse[:, :, ::2]).all()
+    for b in range(Bq):
+        v = K.gathered(x.codes[1], x.scales[1], x.ids[b].tolist(), n, 16)[0]
+        want = K.attention(np.zeros((M // 2, d)), v * 0, v, np.arange(n) != 16 * group + b, d ** -0.5)
+        _compare(_f64(x.o)[b, 0, 1::2], _f64(x.lse)[b, 0, 1::2], want, 2.0 ** -11, d, v)
+    assert int(x.status) == 0
+
+
 BAD = [("k", float("nan")), ("v", float("nan")), ("k", float("inf")), ("v", float("inf")), ("kv", float("nan"))]
 
 
@@ -108,3 +133,17 @@ def test_a_token_that_is_not_a_number(M, bad):
     for h in range(H):
         want = K.attention(_f64(q)[0, h, :M - 1], kv[h], kv[h], there, d ** -0.5)
         _compare(_f64(o)[0, h, :M - 1], _f64(lse)[0, h, :M - 1], want, 2.0 ** -11, d, kv[h])
+
+
+@pytest.mark.parametrize("M", [1, 3, 140])
+def test_scales_next_to_zero(M):
+    """Keys whose scale times the row's is no number of fp32 but 0, and a length that ends within a tile: logits of 0, not NaNs."""
+    x = Cached(np.random.default_rng(21), 1, 2, 1, M, 64, 16, [203], True)
+    x.scales[0][:] = np.float32(1e-44)
+    x.scales[0][x.ids[0][::3]] = 0.0
+    x.codes[0][x.ids[0][::3]] = 0
+    x.q *= 1e-3
+    x.run(True, None)
+    x.check(True, None)
+    x.run(False, None)
+    x.check(False, None)
