@@ -528,7 +528,8 @@ int sva_kv_cache_append(const sva_kv_cache_t* c, const void* k, const void* v, c
  * times a page's scale of K has to lie within fp32.)
  * Codes enter the products as they are (exact in fp16), Q as fp16 after a scaling of each row by a power of two, the probabilities as fp16;
  * scales, softmax and sums are fp32.  Scales of V below 2^-80 are taken for 2^-80, and above 2^80 a row's sum loses its smallest terms.
- * Keys on pages that are named wrongly (SVA_DEV_BAD_INDEX) are left out.  A page whose scale (K's or V's) of a head is a NaN or infinite makes NaNs of the
+ * Keys on pages that are named wrongly (SVA_DEV_BAD_INDEX) are left out.  A length above max_pages * page is reported too and counts as that, a length below 0
+ * as 0, in causal form as well (where queries then see keys from the wrong place: keep lengths to what append has stored).  A page whose scale (K's or V's) of a head is a NaN or infinite makes NaNs of the
  * rows that see one of its keys, o and lse, and of no others; what its codes are means nothing then.  Beside a finite scale codes are finite (append sees to it).
  * M may be 0 (nothing is done).  q, o: 16-byte aligned, strides multiples of 8; o must not overlap q or the cache.
  * workspace: >= sva_cached_attn_workspace_bytes (0 on bad input and where none is needed), 256-byte aligned, rewritten by every call: calls that

@@ -56,6 +56,7 @@ keys_paged_few_kernel(const KeysParams prm) {
   extern __shared__ float smem_f[];                                       // [warps][8][D] then [warps][8] x 2
   const int zero = grid_dep_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  report_long(prm, zero);
   uint32_t at = blockIdx.x + (uint32_t)zero;
   const int tile = (int)(at % (uint32_t)prm.tiles); at /= (uint32_t)prm.tiles;
   const int split = (int)(at % (uint32_t)prm.splits); at /= (uint32_t)prm.splits;

@@ -37,6 +37,12 @@ __device__ __forceinline__ int seq_keys(const KeysParams& prm, int b) {
 __device__ __forceinline__ int seq_queries(const KeysParams& prm, int b) {
   return prm.counts ? min(max(__ldg(prm.counts + b), 0), prm.M) : prm.M;
 }
+// Cached keys: a sequence that is longer than its table has pages for is reported (by the first CTA; zero: of grid_dep_wait).
+__device__ __forceinline__ void report_long(const KeysParams& prm, int zero) {
+  if (blockIdx.x != 0 || !prm.status) return;
+  for (int b = (int)threadIdx.x + zero; b < prm.B; b += (int)blockDim.x)
+    if (__ldg(prm.lengths + b) > prm.S) atomicOr(prm.status, SVA_DEV_BAD_INDEX);
+}
 // keys that query t of a sequence sees (causal: up to its own position)
 __device__ __forceinline__ int keys_seen(const KeysParams& prm, int keys, int queries, int t) {
   return prm.causal ? min(keys, max(keys - queries + t + 1, 0)) : keys;

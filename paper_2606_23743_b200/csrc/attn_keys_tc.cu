@@ -245,7 +245,9 @@ keys_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(ctrl + TMEM_BASE), 0);
   const uint32_t lead = mapa(cb, 0);                                          // the first CTA's barriers: what both CTAs bring the issuer
-  uint32_t at = (blockIdx.x >> 1) + (uint32_t)grid_dep_wait();
+  const int zero = grid_dep_wait();
+  if (PAGED) report_long(prm.k, zero);
+  uint32_t at = (blockIdx.x >> 1) + (uint32_t)zero;
   const uint32_t pairs = gridDim.x / 2;
   KeysItem it;
   bool ok = true;

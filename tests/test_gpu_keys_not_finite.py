@@ -147,3 +147,14 @@ def test_scales_next_to_zero(M):
     x.check(True, None)
     x.run(False, None)
     x.check(False, None)
+
+
+@pytest.mark.parametrize("M", [1, 140])
+def test_a_sequence_longer_than_its_table_is_reported(M):
+    """It counts as long as its table has pages for; the call says so, as the append does."""
+    x = Cached(np.random.default_rng(17), 2, 1, 1, M, 128, 16, [160, 160], True)
+    c, p, table, ws = x.run(True, None)
+    assert int(x.status) == 0
+    o, lse, status = x.o.clone(), x.lse.clone(), _i32([0])
+    B.cached_attn_fwd(p, x.q, table, _i32([160, 161]), x.o, None, x.lse, status, ws)
+    assert torch.equal(o, x.o) and torch.equal(lse, x.lse) and int(status) == B.SVA_DEV_BAD_INDEX
