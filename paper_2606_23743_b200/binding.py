@@ -766,7 +766,7 @@ def make_cross_attn(q, k, v, o, scale: float = 0.0) -> CrossAttn:
     assert k.shape == v.shape == (p.B, p.Hk, p.S, p.d) and o.shape == q.shape and p.Hk > 0 and p.Hq % p.Hk == 0, \
         "q, o are [B,Hq,N,d], k, v [B,Hk,S,d], Hq a multiple of Hk"
     assert q.dtype is k.dtype is v.dtype is o.dtype is torch.bfloat16, "q, k, v, o are bf16"
-    p.softmax_scale = scale
+    p.softmax_scale, p.mask_stride = scale, p.S
     p.q_stride, p.k_stride, p.v_stride, p.o_stride = _strides_any(q), _strides_any(k), _strides_any(v), _strides_any(o)
     p.shapes, p.strides = (q.shape, k.shape), (q.stride(), k.stride(), v.stride(), o.stride())
     return p
@@ -784,7 +784,9 @@ def cross_attn_fwd(p: CrossAttn, q, k, v, o, lengths=None, key_mask=None, lse=No
     if key_mask is not None:
         assert key_mask.shape == (of_k[0], of_k[2]) and key_mask.element_size() == 1 and (of_k[2] <= 1 or key_mask.stride(1) == 1), \
             "key_mask is [B,S] bytes"
-        p.mask_stride = key_mask.stride(0)
+        if of_k[0] > 1 and key_mask.stride(0) != p.mask_stride:              # (a plan is not changed by its calls: others may share it)
+            p = CrossAttn.from_buffer_copy(p)
+            p.mask_stride = key_mask.stride(0)
     assert lse is None or lse.shape == of_q[:3] and lse.dtype is torch.float32 and lse.is_contiguous(), "lse is [B,Hq,N] fp32"
     dev = q.get_device()
     assert _all_on(dev, k, v, o, key_mask, lse, status, workspace), "tensors are on the current GPU"
