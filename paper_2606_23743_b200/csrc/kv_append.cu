@@ -3,7 +3,7 @@
 // A CTA owns one page of one head of K or V: it reads the page's new rows once, keeps them in registers while their largest magnitude is found, and
 // writes their codes.  Where that outgrows the scale of rows that are there already, the CTA reads their codes and writes them again under the
 // new one: at most d bytes a row, and only in the page that a sequence ended in.  d/16 lanes own a row, 16 channels each; up to APPEND_PASSES
-// rows per lane stay in registers, which is the whole page wherever it has up to 512 tokens (256 for d = 128).
+// rows per lane stay in registers, which is a call's part of the page up to 1 024 tokens (512 for d = 128); rows behind them are read twice.
 // HBM-bound: 2 d bytes of a row are read and d written.
 #include "common.cuh"
 

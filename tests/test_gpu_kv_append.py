@@ -170,3 +170,24 @@ def test_captured_and_on_another_stream():
     for a, t in zip(arrays, x):
         fresh = [torch.full_like(a[0], 0x11), torch.full_like(a[1], 0.5)]
         _same(a, _expect(fresh, t, table.tolist(), [7], [50], page))
+
+
+@pytest.mark.parametrize("d,page,calls", [(64, 2048, [(0, 1500), (1500, 1700)]), (128, 1040, [(0, 1040), (1040, 7), (1047, 1500)]), (64, 1040, [(3, 1037)])])
+def test_pages_beyond_what_the_registers_hold(d, page, calls):
+    """A call's rows of one page beyond those that stay in registers (1 024 of 64 channels, 512 of 128): the page's largest value is one of them."""
+    rng = np.random.default_rng(d + page)
+    H = 2
+    pages = -(-sum(calls[-1]) // page) + 1
+    table = rng.permutation(pages)[None]
+    c, arrays = _cache(pages, H, page, d)
+    status = _i32([0])
+    for at, cnt in calls:
+        x = [_rows(rng, (1, H, cnt, d), True) for _ in range(2)]
+        last = min(page - at % page, cnt) - 1                                  # the call's last row in its first page
+        for n, t in enumerate(x):
+            t[0, n, last, 5] = 3000.0 * (1 + at)
+        want = [_expect(a, t, table.tolist(), [at], [cnt], page) for a, t in zip(arrays, x)]
+        B.kv_cache_append(c, *x, _i32(table), _i32([at]), _i32([cnt]), status)
+        for a, w in zip(arrays, want):
+            _same(a, w)
+    assert int(status) == 0
