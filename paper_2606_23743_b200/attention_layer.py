@@ -157,7 +157,8 @@ class ChunkAttentionLayer:
 
     def __call__(self, x, counts=None):
         """x [rows, M, C] bf16, of each sequence's next counts [rows] tokens (int32, outside [0, M] the nearer end; None: M): x + attention's projection, for
-        them.  Rows of x behind its count mean nothing, nor do those of the result."""
+        them.  Rows of x behind its count mean nothing, nor do those of the result.  Where the pool or a sequence's table has no more pages the status says
+        so, and a sequence goes on by the tokens that it has pages for: `lengths` is what it holds, and the others are as rows behind its count."""
         B, M, C = x.shape
         Hq, H, d = self.Hq, self.H, self.d
         assert B == self.B, "x holds tokens of every sequence"
@@ -170,6 +171,7 @@ class ChunkAttentionLayer:
         positions = (self.lengths[:, None] + torch.arange(M, dtype=torch.int32, device=x.device))[None].contiguous()
         sva.rope(sva.make_rope(q, k, q, k, positions, d), q, k, self.steps, positions, q, k)
         sva.kv_pages_take(self.cache, self.refs, self.table, self.lengths, counts, self.status)
+        counts = torch.minimum(counts, (self.table >= 0).sum(1, dtype=torch.int32) * self.cache.page - self.lengths)
         sva.kv_cache_append(self.cache, k, v, self.table, self.lengths, counts, self.status)
         self.lengths += counts
         o = torch.zeros(B, M, Hq, d, dtype=torch.bfloat16, device=x.device).transpose(1, 2)
