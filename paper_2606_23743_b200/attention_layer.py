@@ -188,9 +188,31 @@ class ChunkAttentionLayer:
         sva.kv_pages_fork(self.cache, self.refs, self.table, self.lengths, parents, children, self.status)
 
     def forget(self, which, keep=None):
-        """Sequences `which` (int32) forget their tokens from keep (int32; None: 0) on.  A sequence whose last page is shared may not be cut within it:
-        what it appends there its relatives would see."""
+        """Sequences `which` (int32) forget their tokens from keep (int32; None: 0) on.  A sequence that is cut within a page which others share gets a copy
+        of it, so that what comes next is its own; where the pool has no page for that the status says so, and its full pages are what is left."""
         sva.kv_pages_free(self.cache, self.refs, self.table, self.lengths, which, keep, self.status)
+        if keep is not None:
+            self._own_last_pages()
+
+    def _own_last_pages(self):
+        """Gives every sequence whose last page is partly filled and shared a copy of it, on a free page of the lowest id, in the order of the rows.  Where nobody
+        but such sequences shares a page the last of them keeps it.  (Nothing here waits for the device.)"""
+        page, pages = self.cache.page, self.cache.pages
+        at = (self.lengths // page).clamp_(max=self.table.shape[1] - 1).long()[:, None]
+        src = self.table.gather(1, at)[:, 0]
+        held = src.clamp(min=0).long()
+        shares = (self.lengths % page != 0) & (src >= 0) & (self.refs[held] > 1)
+        same = (src[:, None] == src) & shares
+        needs = shares & ((same.sum(1) < self.refs[held]) | same.triu(1).any(1))
+        dst = torch.searchsorted((self.refs <= 0).cumsum(0), needs.cumsum(0))       # (pages: there is none)
+        gets = needs & (dst < pages)
+        none = src.new_full((), -1)
+        sva.kv_pages_copy(self.cache, torch.where(gets, src, none), torch.where(gets, dst.int(), none), self.status)
+        self.refs.index_add_(0, held, -needs.int()).index_add_(0, dst.clamp(max=pages - 1), gets.int())
+        self.table.scatter_(1, at, torch.where(needs, torch.where(gets, dst.int(), none), src)[:, None])
+        short = needs & ~gets
+        self.lengths -= torch.where(short, self.lengths % page, 0)
+        self.status |= short.any().int() * sva.SVA_DEV_NO_PAGES
 
     def compact(self):
         """Moves the pages in use to the front of the pool."""

@@ -70,3 +70,73 @@ def test_a_table_that_is_full(causal):
         layer.forget(_i32([0]), _i32([21]))
     assert torch.equal(short(x[3]), wide(x[3])) and int(short.status) == 0 and short.lengths.tolist() == [30]
     _books(short)
+
+
+def test_a_sequence_cut_within_a_page_that_others_share():
+    bf = _maker()
+    shared, apart = _layers(2, tokens=96, rows=3, pages=18)
+    x, y, z = bf(3, 40, C), bf(3, 9, C), bf(3, 1, C)
+    x[1:] = x[:1]
+    shared(x, _i32([40, 0, 0]))
+    shared.fork(_i32([0, 0]), _i32([1, 2]))
+    apart(x)
+    for layer in (shared, apart):
+        layer.forget(_i32([1, 2, 1]), _i32([20, 33, 20]))                      # (row 2: within a page of its own)
+    _books(shared)
+    y[1] *= 100.0                                                              # the page's scale grows, its codes are re-expressed
+    for t, counts in ((y, _i32([0, 9, 9])), (z, None)):
+        got, want = shared(t, counts), apart(t, counts)
+        for b in range(3):
+            n = t.shape[1] if counts is None else int(counts[b])
+            assert torch.equal(got[b, :n], want[b, :n])
+    assert int(shared.status) == 0 and shared.lengths.tolist() == apart.lengths.tolist()
+    _books(shared)
+
+
+def test_a_cut_without_a_page_for_the_copy():
+    bf = _maker()
+    x = bf(2, 32, C)
+    layer, = _layers(1, tokens=64, rows=2, pages=2)
+    layer(x, _i32([32, 0]))
+    layer.fork(_i32([0]), _i32([1]))
+    layer.forget(_i32([1]), _i32([20]))                                        # no page for a copy: its full pages are left
+    assert int(layer.status) == B.SVA_DEV_NO_PAGES and layer.lengths.tolist() == [32, 16] and layer.refs.tolist() == [2, 1]
+    _books(layer)
+    layer, = _layers(1, tokens=64, rows=2, pages=2)
+    layer(x, _i32([32, 0]))
+    layer.fork(_i32([0]), _i32([1]))
+    layer.forget(_i32([0, 1]), _i32([20, 20]))                                 # both are cut: the page stays with one of them
+    assert int(layer.status) == B.SVA_DEV_NO_PAGES and sorted(layer.lengths.tolist()) == [16, 20] and layer.refs.tolist() == [2, 1]
+    _books(layer)
+    layer, = _layers(1, tokens=64, rows=2, pages=3)
+    layer(x, _i32([32, 0]))
+    layer.fork(_i32([0]), _i32([1]))
+    layer.forget(_i32([0, 1]), _i32([20, 20]))                                 # one copy is enough for two
+    assert int(layer.status) == 0 and layer.lengths.tolist() == [20, 20] and layer.refs.tolist() == [2, 1, 1]
+    _books(layer)
+
+
+def test_a_cut_and_a_call_are_captured():
+    bf = _maker()
+    live, seen = _layers(2, tokens=96, rows=2, pages=12)
+    x, y = bf(2, 40, C), bf(2, 3, C)
+    which, keep = _i32([1]), _i32([20])
+    for layer in (live, seen):
+        layer(x, _i32([40, 0]))
+        layer.fork(_i32([0]), _i32([1]))
+        layer(y)
+        layer.forget(which, _i32([41]))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        live.forget(which, keep)
+        got = live(y)
+    for n in (20, 17, 5):
+        keep.fill_(n)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        seen.forget(which, keep)
+        assert torch.equal(got, seen(y)) and torch.equal(live.table, seen.table) and torch.equal(live.refs, seen.refs)
+    _books(live)
