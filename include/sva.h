@@ -555,7 +555,8 @@ int sva_cached_attn_fwd(const sva_kv_cache_t* c, const sva_cached_attn_t* p, con
  *   o_i = sum_j softmax_j(softmax_scale * <q_i, k_j>) v_j,  lse_i as above,  over the keys j < lengths[b] (NULL: S) whose key_mask[b][j] is not 0
  *   (NULL: all);  q, o [B,Hq,N,d], k, v [B,Hk,S,d] bf16, Hq a multiple of Hk (heads share as above), d = 64 or 128.
  * Keys that are left out have no influence, whatever they hold.  A row without keys becomes zeros, its lse -inf; logits that are no numbers as above.  Q K^T and P V are bf16
- * products with fp32 sums, the probabilities rounded to bf16.  lengths [B] int32; key_mask [B][S] bytes, mask_stride between
+ * products with fp32 sums, the probabilities as bf16 (as two bf16 terms, 16 bits, for
+ * up to 32 rows of a key head, a row being a query of one of its heads).  lengths [B] int32; key_mask [B][S] bytes, mask_stride between
  * items; lse (optional) [B,Hq,N] fp32 contiguous.  N and S may be 0.  Strides of 0 over items or heads (shared states) are fine.
  * Alignment, workspace and errors as for the call above.
  */

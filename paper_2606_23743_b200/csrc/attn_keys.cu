@@ -290,7 +290,8 @@ keys_paged_few_kernel(const KeysParams prm) {
   if (ch == 0 && prm.lse) prm.lse[((long long)b * prm.Hq + h) * prm.M + t] = total != 0.f ? (top - P_UP + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
-// ---- bf16 keys: sixteen rows per tile; P needs no shuffle, being A of the second product as it leaves the first
+// ---- bf16 keys: sixteen rows per tile; P needs no shuffle, being A of the second product as it leaves the first.  It enters as two bf16 terms (MMA operands
+// have one type, V's), so that 16 of its bits count: the kernel waits for its loads, and the second product is hidden behind them
 template <int D>
 __global__ void __launch_bounds__(FEW_THREADS, 1)
 keys_few_kernel(const KeysParams prm) {
@@ -378,7 +379,7 @@ keys_few_kernel(const KeysParams prm) {
       }
     }
     const int key0 = gi * FEW_KEYS;
-    uint32_t p[2][2];                                                     // [n tile][row]
+    uint32_t p[2][2], rest[2][2];                                         // [n tile][row]
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       float y[4], top = -INFINITY;
@@ -410,17 +411,24 @@ keys_few_kernel(const KeysParams prm) {
       }
       l[i] += sum;
 #pragma unroll
-      for (int n = 0; n < 2; ++n) p[n][i] = pack_bf16(y[2 * n], y[2 * n + 1]);
+      for (int n = 0; n < 2; ++n) {
+        p[n][i] = pack_bf16(y[2 * n], y[2 * n + 1]);
+        rest[n][i] = pack_bf16(y[2 * n] - bf16lo(p[n][i]), y[2 * n + 1] - bf16hi(p[n][i]));
+      }
     }
-    const uint32_t pa[4] = {p[0][0], p[0][1], p[1][0], p[1][1]};
+    const uint32_t pa[4] = {p[0][0], p[0][1], p[1][0], p[1][1]}, pr[4] = {rest[0][0], rest[0][1], rest[1][0], rest[1][1]};
 #pragma unroll
     for (int t = 0; t < NT; t += 4) {                                     // four channels of each of the four rows
 #pragma unroll
       for (int e = 0; e < 2; ++e) {                                       // two words of two channels
         const int piece = t / 8, i = (t / 4 % 2) * 2 + e;
         const uint32_t w0 = word(x.v[0][piece], i), w1 = word(x.v[1][piece], i), w2 = word(x.v[2][piece], i), w3 = word(x.v[3][piece], i);
-        mma_bf16(acc[t + 2 * e], pa, __byte_perm(w0, w1, 0x5410), __byte_perm(w2, w3, 0x5410));
-        mma_bf16(acc[t + 2 * e + 1], pa, __byte_perm(w0, w1, 0x7632), __byte_perm(w2, w3, 0x7632));
+        const uint32_t lo01 = __byte_perm(w0, w1, 0x5410), lo23 = __byte_perm(w2, w3, 0x5410), hi01 = __byte_perm(w0, w1, 0x7632),
+                       hi23 = __byte_perm(w2, w3, 0x7632);
+        mma_bf16(acc[t + 2 * e], pa, lo01, lo23);
+        mma_bf16(acc[t + 2 * e + 1], pa, hi01, hi23);
+        mma_bf16(acc[t + 2 * e], pr, lo01, lo23);
+        mma_bf16(acc[t + 2 * e + 1], pr, hi01, hi23);
       }
     }
   };

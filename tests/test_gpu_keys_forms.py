@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import keys as K
 from paper_2606_23743_b200 import binding as B
 from test_gpu_keys import Cached, _cross, _cross_check, _heads, _i32
 
@@ -70,3 +71,19 @@ def test_given_keys_that_no_tensor_map_describes(what, d, S):
     B.cross_attn_fwd(p, q2, k2, v, o, _i32([S, S - 5]), None, lse, None, ws)
     assert B.debug_last_choice() == 16
     _cross_check(q2, k2, v, np.arange(S)[None] < np.array([[S], [S - 5]]), o, lse)
+
+
+@pytest.mark.parametrize("d,S", [(64, 77), (128, 512), (128, 3000)])
+def test_probabilities_of_few_rows_over_given_keys(d, S):
+    """They count with 16 bits: what is left of an output's error is its own rounding, 2^-8 of it, and 2^-16 of the weights' mean magnitude of v (with the
+    logits' errors as in test_gpu_keys)."""
+    rng = np.random.default_rng(S)
+    q, k, v = _heads(rng, (2, 4, 4, d), True, 0.5), _heads(rng, (2, 2, S, d), True), _heads(rng, (2, 2, S, d), True)
+    o, lse = _cross(q, k, v, None, None)
+    assert B.debug_last_choice() == 16
+    q, k, v, o = (t.float().cpu().numpy().astype(np.float64) for t in (q, k, v, o))
+    for b in range(2):
+        for h in range(4):
+            want, _, size, top = K.attention(q[b, h], k[b, h // 2], v[b, h // 2], np.ones(S, bool), d ** -0.5)
+            e = (d + 8) * 2.0 ** -23 * top + 2.0 ** -20
+            assert (np.abs(o[b, h] - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -16 + 2 * e) * size).all()
