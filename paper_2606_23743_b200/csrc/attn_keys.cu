@@ -334,9 +334,9 @@ keys_few_kernel(const KeysParams prm) {
       qa[s][2 + i] = u.y;
     }
 
-  float acc[NT][4];
+  float acc[NT][4], more[NT][4];                                          // (more: of P's second term)
 #pragma unroll
-  for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
+  for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = more[t][0] = more[t][1] = more[t][2] = more[t][3] = 0.f;
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
   struct Group { uint4 k[2][KP], v[4][VP]; uint32_t there; };
@@ -400,6 +400,8 @@ keys_few_kernel(const KeysParams prm) {
         for (int t = 0; t < NT; ++t) {
           acc[t][2 * i] *= down;
           acc[t][2 * i + 1] *= down;
+          more[t][2 * i] *= down;
+          more[t][2 * i + 1] *= down;
         }
       }
       const float ref = m[i] == -INFINITY ? 0.f : m[i];
@@ -427,8 +429,8 @@ keys_few_kernel(const KeysParams prm) {
                        hi23 = __byte_perm(w2, w3, 0x7632);
         mma_bf16(acc[t + 2 * e], pa, lo01, lo23);
         mma_bf16(acc[t + 2 * e + 1], pa, hi01, hi23);
-        mma_bf16(acc[t + 2 * e], pr, lo01, lo23);
-        mma_bf16(acc[t + 2 * e + 1], pr, hi01, hi23);
+        mma_bf16(more[t + 2 * e], pr, lo01, lo23);
+        mma_bf16(more[t + 2 * e + 1], pr, hi01, hi23);
       }
     }
   };
@@ -438,6 +440,12 @@ keys_few_kernel(const KeysParams prm) {
     load(gi, x);
     step(gi, x);
   }
+
+  // (the second term's products with an infinite value may have the other sign, or none: the first term's stand for those)
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[t][e] += fabsf(more[t][e]) < INFINITY ? more[t][e] : 0.f;
 
   // ---- the warps' sums: each thread's columns n = 2c, 2c + 1 of tile t are channels of its own order
   float* so = smem_f + warp * FEW_ROWS * D;

@@ -158,3 +158,19 @@ def test_a_sequence_longer_than_its_table_is_reported(M):
     o, lse, status = x.o.clone(), x.lse.clone(), _i32([0])
     B.cached_attn_fwd(p, x.q, table, _i32([160, 161]), x.o, None, x.lse, status, ws)
     assert torch.equal(o, x.o) and torch.equal(lse, x.lse) and int(status) == B.SVA_DEV_BAD_INDEX
+
+
+@pytest.mark.parametrize("N,S", [(2, 77), (2, 3000), (40, 77), (64, 3000)])
+def test_values_that_are_infinite(N, S):
+    """An infinity among the values a row sees is the row's output in its channel, two of unlike sign are a NaN; what is left out has no part in it."""
+    gen = torch.Generator("cuda").manual_seed(N + S)
+    q, k, v = (torch.randn(1, 2, n, 64, generator=gen, device="cuda").to(torch.bfloat16) for n in (N, S, S))
+    lengths = _i32([S - 5])
+    clean, clean_lse = _cross(q, k, v, lengths, None)
+    inf = float("inf")
+    v[0, 0, 20, 3], v[0, 0, 31, 4], v[0, 0, 40, 5], v[0, 0, 50, 5], v[0, 1, S - 2, 6] = inf, -inf, inf, -inf, inf
+    o, lse = _cross(q, k, v, lengths, None)
+    assert (o[0, 0, :, 3] == inf).all() and (o[0, 0, :, 4] == -inf).all() and torch.isnan(o[0, 0, :, 5]).all()
+    same = torch.ones(64, dtype=torch.bool, device="cuda")
+    same[3:6] = False
+    assert torch.equal(o[0, 0][:, same], clean[0, 0][:, same]) and torch.equal(o[0, 1], clean[0, 1]) and torch.equal(lse, clean_lse)
