@@ -533,7 +533,9 @@ int sva_kv_cache_append(const sva_kv_cache_t* c, const void* k, const void* v, c
  * rows that see one of its keys, o and lse, and of no others; what its codes are means nothing then.  Beside a finite scale codes are finite (append sees to it).
  * M may be 0 (nothing is done).  q, o: 16-byte aligned, strides multiples of 8; o must not overlap q or the cache.
  * workspace: >= sva_cached_attn_workspace_bytes (0 on bad input and where none is needed), 256-byte aligned, rewritten by every call: calls that
- * may overlap on the GPU need one each.  Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (format, d, page not a multiple of 16, sizes), WORKSPACE.
+ * may overlap on the GPU need one each.  It holds the partial sums of a split key axis, splits * (rows, in whole tiles) * (4 d + 8) bytes, and follows what the
+ * table has room for (max_pages * page), not the lengths: 4 680 queries of 24 heads of 128 over 32 768 places take four splits, 236 MB.
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (format, d, page not a multiple of 16, sizes), WORKSPACE.
  */
 typedef struct {
   int32_t B, Hq, M;          /* sequences, query heads, queries per sequence                                              */
@@ -554,10 +556,10 @@ int sva_cached_attn_fwd(const sva_kv_cache_t* c, const sva_cached_attn_t* p, con
  * Cross attention: the tokens of a clip attend to an encoder's states (a prompt's), which have a length of their own:
  *   o_i = sum_j softmax_j(softmax_scale * <q_i, k_j>) v_j,  lse_i as above,  over the keys j < lengths[b] (NULL: S) whose key_mask[b][j] is not 0
  *   (NULL: all);  q, o [B,Hq,N,d], k, v [B,Hk,S,d] bf16, Hq a multiple of Hk (heads share as above), d = 64 or 128.
- * Keys that are left out have no influence, whatever they hold.  A row without keys becomes zeros, its lse -inf; logits that are no numbers as above.  Q K^T and P V are bf16
- * products with fp32 sums, the probabilities as bf16 (as two bf16 terms, 16 bits, for
- * up to 32 rows of a key head, a row being a query of one of its heads).  lengths [B] int32; key_mask [B][S] bytes, mask_stride between
- * items; lse (optional) [B,Hq,N] fp32 contiguous.  N and S may be 0.  Strides of 0 over items or heads (shared states) are fine.
+ * Keys that are left out have no influence, whatever they hold.  A row without keys becomes zeros, its lse -inf; logits that are no numbers as above.
+ * Q K^T and P V are bf16 products with fp32 sums, the probabilities as bf16; as two bf16 terms, 16 bits, for up to 32 rows of a key head (a row: a query of
+ * one of its heads).  lengths [B] int32; key_mask [B][S] bytes, mask_stride between items; lse (optional) [B,Hq,N] fp32 contiguous.  N and S may be 0.
+ * Strides of 0 over items or heads (shared states) are fine.
  * Alignment, workspace and errors as for the call above.
  */
 typedef struct {

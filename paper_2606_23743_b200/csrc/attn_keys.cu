@@ -46,8 +46,8 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
 // The products are taken the other way round, keys (S^T = K Q^T) and channels (O^T = V^T P^T) as the MMA's 16 rows and the queries as its 8 columns: half
 // the MMAs, accumulators and Q of 16 rows, so that twelve warps with the next group's codes in flight share an SM.  P is turned by movmatrix on its way.
 // The reference m follows the maximum lazily: only when a weight is more than FEW_LAZY powers of two above it is the group's maximum taken.
-// Eight sequences of up to 131 071 tokens, 8 key heads of 128, four query heads each: 320 us = 5.0 TB/s; with 16 rows per tile, eight warps per SM and
-// the maximum in every group 653.  What is left is latency: a group is on its way for as long as the group before it is worked on.
+// Eight sequences of up to 131 071 tokens (unequal ones), 8 key heads of 128, four query heads each, a pass among others: 376 to 397 us = 4.2 TB/s; the same
+// call by itself over and over, when it was built, 320, and with 16 rows per tile, eight warps per SM and the maximum in every group 653.  What is left is latency: a group is on its way for as long as the group before it is worked on.
 template <int D>
 __global__ void __launch_bounds__(PAGED_WARPS * 32, PAGED_CTAS)
 keys_paged_few_kernel(const KeysParams prm) {
@@ -641,6 +641,11 @@ static KeysPlan keys_plan(int B, int Hk, int group, int M, long long S, int d, b
   KeysPlan k = {};
   k.sms = device_sms();
   const long long rows = (long long)M * group;
+  // Rows of a key head, few-row kernel against many-row kernel, us.  Cached keys, eight sequences of 65 536 tokens, 8 key heads of 128: 8 rows 239 / 1 025, 16:
+  // 470 / 1 024, 20: 676 / 1 025, 32: 898 / 1 025, 48: 1 320 / 1 025; 64 sequences of 2 048: 16 rows 140 / 234, 20: 183 / 236, 32: 228 / 238, 64: 436 / 240; two of
+  // 32 768, 24 heads: 16 rows 170 / 406, 24: 240 / 409, 32: 348 / 406, 64: 662 / 409.  So from 17 to 32 rows the few-row kernel would be the faster one too, by 4 to
+  // 70 %, and neither is near what the codes take (164, 41, 62): such calls lack a kernel of their own.  bf16 keys, 2 x 24 heads x 512 keys: 16 rows
+  // 11.6 / 11.8, 17: 18.9 / 11.8, 32: 19.2 / 11.7; 16 heads x 8 192 keys of 64: 16 rows 23.6 / 33.0, 32: 30.7 / 32.3, 33: 36.6 / 33.1.
   k.tc = maps && group <= 128 && rows > (paged ? 2 * PAGED_ROWS : 2 * FEW_ROWS);
   k.tokens = k.tc ? 128 / group : 0;
   const int per = k.tc ? 128 : paged ? PAGED_ROWS : FEW_ROWS;

@@ -17,12 +17,13 @@
 //
 // The reference m of a row's exponentials follows its maximum lazily: a tile's first exponentials are taken with the m so far and its maximum beside
 // them; only when that is more than LAZY powers of two above m are they done again, and O rescaled (probabilities reach 2^LAZY; sums are fp32).
-// Probabilities have the operands' type, which is V's: bf16 beside bf16 keys (an output's error is then up to twice its own rounding; a second term as in
-// attn_keys.cu would be half as many MMAs again and a third more of the softmax warps' work, which is what bounds the kernel), fp16 beside codes.  Row sums take them unrounded.
+// Probabilities have the operands' type, which is V's: bf16 beside bf16 keys (2^-8 of each weight; a second term as in attn_keys.cu would be half as many
+// MMAs again, and its subtractions and stores the softmax warps', which are what bounds the kernel), fp16 beside codes.  Row sums take them unrounded.
 // Cached keys: K's scale is a factor of the logits, log2 of V's an addend (both per 16 keys), see attn_keys.cu; P is fp16 and at most 2^(UP + LAZY).
 //
-// 24 heads x 4 680 queries x 32 760 cached keys: 2.1 ms = 0.88 PFLOP/s; 2 x 24 heads x 32 760 queries x 512 bf16 keys 480 us.  What bounds it is the softmax warps' own latency: a
-// scheduler has one of each group, and no pipe is more than half busy (tensor 52 %, issue 44 %, exponentials 39 %).
+// 24 heads x 4 680 queries x 32 760 cached keys: 2.2 ms = 0.84 PFLOP/s; 2 x 24 heads x 32 760 queries x 512 bf16 keys 490 us.  What bounds it is the softmax warps' own latency, in
+// this arrangement (attn_sm100.cu has as many warps per scheduler and takes some 1 460 cycles for a 128 x 128 tile and SM, this kernel 2 000): a scheduler has
+// one of each group, and no pipe is more than half busy (tensor 52 %, issue 44 %, exponentials 39 %).
 //
 // Every wait is bounded; when one runs out all roles leave, the CTA reports SVA_DEV_TIMEOUT and its rows are not stored.
 #include <cuda_fp16.h>

@@ -4,7 +4,8 @@
 // writes their codes.  Where that outgrows the scale of rows that are there already, the CTA reads their codes and writes them again under the
 // new one: at most d bytes a row, and only in the page that a sequence ended in.  d/16 lanes own a row, 16 channels each; up to APPEND_PASSES
 // rows per lane stay in registers, which is a call's part of the page up to 1 024 tokens (512 for d = 128); rows behind them are read twice.
-// HBM-bound: 2 d bytes of a row are read and d written.
+// HBM-bound: 2 d bytes of a row are read and d written.  A call is sized by its new rows: one token for each of 64 sequences, 8 heads of 128, takes 2.8 us where
+// no scale grows; where all of them do, one warp re-expresses each page in turns of four rows, 5.7 us with pages of 64 tokens, 17.7 with 256 and 133 with 1 024.
 #include "common.cuh"
 
 namespace sva {
