@@ -153,6 +153,8 @@ class ChunkAttentionLayer:
         self.refs = torch.zeros(pages, dtype=torch.int32, device=dev)
         self.table = torch.full((rows, per), -1, dtype=torch.int32, device=dev)
         self.lengths = torch.zeros(rows, dtype=torch.int32, device=dev)
+        # tokens that each sequence can come to have pages for; None: the pool may run out before
+        self.most = torch.full((rows,), per * page, dtype=torch.int32, device=dev) if pages >= rows * per else None
         self.work = torch.empty(sva.kv_pages_compact_workspace_bytes(self.cache), dtype=torch.uint8, device=dev)
 
     def __call__(self, x, counts=None):
@@ -171,7 +173,8 @@ class ChunkAttentionLayer:
         positions = (self.lengths[:, None] + torch.arange(M, dtype=torch.int32, device=x.device))[None].contiguous()
         sva.rope(sva.make_rope(q, k, q, k, positions, d), q, k, self.steps, positions, q, k)
         sva.kv_pages_take(self.cache, self.refs, self.table, self.lengths, counts, self.status)
-        counts = torch.minimum(counts, (self.table >= 0).sum(1, dtype=torch.int32) * self.cache.page - self.lengths)
+        held = (self.table >= 0).sum(1, dtype=torch.int32) * self.cache.page if self.most is None else self.most
+        counts = torch.minimum(counts, held - self.lengths)
         sva.kv_cache_append(self.cache, k, v, self.table, self.lengths, counts, self.status)
         self.lengths += counts
         o = torch.zeros(B, M, Hq, d, dtype=torch.bfloat16, device=x.device).transpose(1, 2)
